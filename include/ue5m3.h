@@ -288,6 +288,108 @@ UE5M3_API int ue5m3_gemm_stall_selftest(int which, int64_t Mo, int64_t No, int64
                const uint8_t* b_payload, const uint8_t* b_scales, int b_scale_mode, const float* b_decode,
                void* out, int out_dtype, int64_t ldo, int64_t wait_limit_cycles, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * The operators between the quantized linears of a transformer block: layer norm, dropout on the residual stream and
+ * attention, each with its backward pass.  They stay in the activations' own precision (the recipe quantizes the linears
+ * only, Section 5.3).  General rules as above; in addition an empty tensor (zero rows, zero length, zero batch) is not an
+ * error: what depends on nothing is written as zero, and an empty tensor's pointer may be null.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/*
+ * Layer norm of every row of x [rows, cols] (leading dimension ldx, elements):
+ *     mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps),  y = (x - mean) * rstd * weight + bias
+ * in binary32 from centred values (two passes over the row, which is read from memory once for cols <= 16384), rounded
+ * once to y's type.
+ *   dtype          type of x and y: UE5M3_F32 or UE5M3_BF16.    weight_dtype   type of weight and bias, either one.
+ *   weight, bias   device, [cols] contiguous; each may be null (1 and 0).
+ *   mean, rstd     device, [rows] binary32 outputs, each may be null; ue5m3_layer_norm_backward takes them.
+ *   ldx, ldy >= cols.  Pointers are aligned to their element; rows that are 16-byte aligned throughout (pointers, leading
+ *   dimensions and cols * element size) are read with 16-byte loads, others element by element.
+ *   eps >= 0 and finite.
+ */
+UE5M3_API int ue5m3_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx,
+                               const void* weight, const void* bias, int weight_dtype, float eps,
+                               void* y, int64_t ldy, float* mean, float* rstd, void* stream);
+
+/*
+ * Backward pass of ue5m3_layer_norm.  With xh = (x - mean) * rstd and g = dy * weight:
+ *     dx = rstd * (g - sum_c g / cols - xh * sum_c (g * xh) / cols)
+ *     dweight = sum_r dy * xh,   dbias = sum_r dy
+ * One pass over x and dy; the column sums are kept in binary32 per CTA, written to `workspace` and added in a fixed order
+ * by a second kernel, so that the result does not change from call to call.
+ *   dx             device, [rows, cols], leading dimension lddx, type dtype.
+ *   dweight, dbias device, [cols], type weight_dtype; each may be null.  weight may be null (1).
+ *   workspace      device, ue5m3_layer_norm_backward_workspace_bytes(rows, cols) bytes, 16-byte aligned; may be null when
+ *                  dweight and dbias both are.
+ */
+UE5M3_API size_t ue5m3_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+UE5M3_API int ue5m3_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int dtype, int64_t rows, int64_t cols,
+                               int64_t ldx, const void* weight, int weight_dtype, const float* mean, const float* rstd,
+                               void* dx, int64_t lddx, void* dweight, void* dbias, void* workspace, void* stream);
+
+/*
+ * Dropout added to a residual: y = residual + keep * x / (1 - t / 65536), with t = floor(65536 p + 1/2).
+ * Element i = row * cols + col is kept when its 16 random bits are at least t, so that E[y] = residual + x holds exactly
+ * for the probability t / 65536 that is really used.  The bits come from Philox4x32 with 7 rounds, key = (seed low, seed
+ * high) and counter = (low32(i>>3), high32(i>>3), 1, 0): lane j = i & 7 uses half (j & 1) of output word j >> 1 (the third
+ * counter word keeps these draws apart from those of stochastic rounding under the same seed).  No mask is stored: the
+ * backward pass is this call on dy with the same p and seed and no residual; the residual's gradient is dy itself.
+ * A dropped element contributes exactly zero whatever its value (NaN included).
+ *   x, residual, y   device, [rows, cols], leading dimensions ldx, ldr, ldy >= cols, type dtype; residual may be null; y may be
+ *                    x or residual (same pointer and leading dimension).  Pointers aligned to their element; tensors whose
+ *                    groups of eight elements are 16-byte aligned throughout are read with 16-byte loads.
+ *   p                0 <= p <= 1.
+ */
+UE5M3_API int ue5m3_dropout_add(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype, int64_t rows,
+                               int64_t cols, float p, uint64_t seed, void* y, int64_t ldy, void* stream);
+
+/* One tensor [batch, tokens, heads, head_dim] of an attention call: the last dimension is contiguous, the other strides
+ * are in elements (a view into a fused projection is fine). */
+typedef struct {
+    void* data;
+    int64_t batch_stride, token_stride, head_stride;
+} ue5m3_heads;
+
+typedef struct {
+    int64_t batch, q_len, k_len, heads, kv_heads, head_dim;
+    int64_t window_left;     /* keys a query sees before its own position; -1 = all */
+    const int32_t* k_lens;   /* device, [batch] valid keys of each sequence (clamped to 0 .. k_len); null = k_len everywhere */
+    float scale;             /* > 0, finite */
+    int dtype;               /* UE5M3_BF16 */
+    int causal;              /* 0 or 1 */
+} ue5m3_attention_shape;
+
+/*
+ * Attention.  Query i of a sequence stands at key position i + k_len - q_len; it sees the keys j with j < k_lens[b],
+ * j <= position (causal) and j >= position - window_left (window_left >= 0).  Query head h uses key/value head
+ * h / (heads / kv_heads).
+ *     S_ij = scale * q_i . k_j,   lse_i = log sum_j exp S_ij,   o_i = sum_j exp(S_ij - lse_i) v_j      over the keys it sees
+ * A query that sees no key gets o = 0 and lse = -inf.  Keys and values at positions >= k_lens[b] are never used, whatever
+ * they hold (NaN included).  Products of BF16 values are accumulated in binary32; the probabilities are rounded to BF16
+ * for the second product; maximum, sum and lse are binary32.
+ *   q [batch, q_len, heads, head_dim], k and v [batch, k_len, kv_heads, head_dim], o like q; lse device, binary32
+ *   [batch, heads, q_len] contiguous.
+ *   head_dim a multiple of 8 up to 128, heads a multiple of kv_heads (UE5M3_ERR_SHAPE); pointers 16-byte aligned and
+ *   strides multiples of 8 elements, positive where the dimension is larger than 1 (UE5M3_ERR_ALIGN).
+ */
+UE5M3_API int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, const ue5m3_heads* k,
+                              const ue5m3_heads* v, const ue5m3_heads* o, float* lse, void* stream);
+
+/*
+ * Backward pass of ue5m3_attention: nothing of the forward pass but o and lse is kept, the probabilities are recomputed.
+ * With P_ij = exp(S_ij - lse_i) and D_i = dout_i . o_i:
+ *     dv_j = sum_i P_ij dout_i,   dS_ij = P_ij (dout_i . v_j - D_i),   dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i
+ * dk and dv are summed over the query heads that share a key/value head, in binary32 and in a fixed order (no atomics).
+ * Gradients of keys and values that no query sees, and of queries that see no key, are zero.
+ *   dout, o, dq like q; dk, dv like k (each with strides of its own).
+ *   workspace  device, ue5m3_attention_backward_workspace_bytes(shape) bytes, 16-byte aligned.
+ */
+UE5M3_API size_t ue5m3_attention_backward_workspace_bytes(const ue5m3_attention_shape* shape);
+UE5M3_API int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_heads* dout, const ue5m3_heads* q,
+                              const ue5m3_heads* k, const ue5m3_heads* v, const ue5m3_heads* o, const float* lse,
+                              const ue5m3_heads* dq, const ue5m3_heads* dk, const ue5m3_heads* dv, void* workspace,
+                              void* stream);
+
 /*
  * Bytes a scale buffer needs.  rows/cols are those of the SOURCE tensor given to ue5m3_quantize.
  * (Section 3.2: one scale per block of B = 16; Section 3.3: one per 16x16 weight tile.)

@@ -23,11 +23,23 @@ FPROP, DGRAD, WGRAD = 0, 1, 2
 
 SYMBOLS = ("ue5m3_sample_amax", "ue5m3_quantize", "ue5m3_quantize_dual", "ue5m3_quantize_current", "ue5m3_gemm",
            "ue5m3_gemm_probe_matched", "ue5m3_gemm_stall_selftest", "ue5m3_scales_bytes", "ue5m3_unswizzle_scales",
-           "ue5m3_last_device_status", "ue5m3_status_string")
+           "ue5m3_last_device_status", "ue5m3_status_string", "ue5m3_layer_norm", "ue5m3_layer_norm_backward_workspace_bytes",
+           "ue5m3_layer_norm_backward", "ue5m3_dropout_add", "ue5m3_attention", "ue5m3_attention_backward_workspace_bytes",
+           "ue5m3_attention_backward")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libue5m3.so")
 _lib = None
+
+
+class _Heads(C.Structure):                  # ue5m3_heads
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _AttentionShape(C.Structure):         # ue5m3_attention_shape
+    _fields_ = [("batch", C.c_int64), ("q_len", C.c_int64), ("k_len", C.c_int64), ("heads", C.c_int64), ("kv_heads", C.c_int64),
+                ("head_dim", C.c_int64), ("window_left", C.c_int64), ("k_lens", C.c_void_p), ("scale", C.c_float), ("dtype", C.c_int),
+                ("causal", C.c_int)]
 
 
 class Ue5m3Error(RuntimeError):
@@ -77,6 +89,21 @@ def _load() -> C.CDLL:
         L.ue5m3_unswizzle_scales.argtypes = [vp, vp, i64, i64, vp]
         L.ue5m3_last_device_status.restype = ci
         L.ue5m3_last_device_status.argtypes = []
+        L.ue5m3_layer_norm.restype = ci
+        L.ue5m3_layer_norm.argtypes = [vp, ci, i64, i64, i64, vp, vp, ci, f32, vp, i64, vp, vp, vp]
+        L.ue5m3_layer_norm_backward_workspace_bytes.restype = C.c_size_t
+        L.ue5m3_layer_norm_backward_workspace_bytes.argtypes = [i64, i64]
+        L.ue5m3_layer_norm_backward.restype = ci
+        L.ue5m3_layer_norm_backward.argtypes = [vp, i64, vp, ci, i64, i64, i64, vp, ci, vp, vp, vp, i64, vp, vp, vp, vp]
+        L.ue5m3_dropout_add.restype = ci
+        L.ue5m3_dropout_add.argtypes = [vp, i64, vp, i64, ci, i64, i64, f32, u64, vp, i64, vp]
+        shape, heads = C.POINTER(_AttentionShape), C.POINTER(_Heads)
+        L.ue5m3_attention.restype = ci
+        L.ue5m3_attention.argtypes = [shape, heads, heads, heads, heads, vp, vp]
+        L.ue5m3_attention_backward_workspace_bytes.restype = C.c_size_t
+        L.ue5m3_attention_backward_workspace_bytes.argtypes = [shape]
+        L.ue5m3_attention_backward.restype = ci
+        L.ue5m3_attention_backward.argtypes = [shape, heads, heads, heads, heads, heads, vp, heads, heads, heads, vp, vp]
         L.ue5m3_status_string.restype = C.c_char_p
         L.ue5m3_status_string.argtypes = [ci]
         _lib = L
@@ -408,6 +435,142 @@ def gemm_stall_selftest(which: int, a: QuantizedOperand, b: QuantizedOperand, ou
 
 def last_device_status() -> int:
     return int(_load().ue5m3_last_device_status())
+
+
+# ---------------------------------------------------------------------------------------------
+# The operators between the quantized linears.
+def _rows(x: torch.Tensor, like: Optional[torch.Tensor] = None):
+    """(rows, cols, leading dimension) of a 2-D tensor with contiguous rows; `like`: its shape, type and device are required."""
+    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+        raise ValueError("expected a 2-D tensor whose rows are contiguous")
+    if like is not None and (x.shape != like.shape or x.dtype != like.dtype or x.device != like.device):
+        raise ValueError(f"expected a tensor like [{tuple(like.shape)}, {like.dtype}, {like.device}], got [{tuple(x.shape)}, {x.dtype}, {x.device}]")
+    rows, cols = x.shape
+    return rows, cols, x.stride(0) if rows > 1 else cols
+
+
+def _vector(t: Optional[torch.Tensor], n: int, device, dtype=None):
+    if t is not None and (t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.device != device or (dtype is not None and t.dtype != dtype)):
+        raise ValueError(f"expected a contiguous vector of {n} values{'' if dtype is None else f' of {dtype}'} on {device}")
+    return t
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               out: Optional[torch.Tensor] = None) -> tuple:
+    """ue5m3_layer_norm: (y, mean, rstd) of the rows of `x` [rows, cols] (float32 or bfloat16); weight and bias [cols], float32 or
+    bfloat16, may be None.  mean and rstd (float32 [rows]) are what `layer_norm_backward` takes."""
+    rows, cols, ldx = _rows(x)
+    param = weight if weight is not None else bias
+    _vector(weight, cols, x.device)
+    _vector(bias, cols, x.device, None if param is None else param.dtype)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    _, _, ldy = _rows(out, x)
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    with torch.cuda.device(x.device):
+        _check(_load().ue5m3_layer_norm(_dev_ptr(x), _dtype_code(x), rows, cols, ldx, _dev_ptr(weight), _dev_ptr(bias),
+                                        F32 if param is None else _dtype_code(param), eps, _dev_ptr(out), ldy, _dev_ptr(mean),
+                                        _dev_ptr(rstd), _stream(x)), "ue5m3_layer_norm")
+    return out, mean, rstd
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                        want_weight: bool = True, want_bias: bool = True, out: Optional[torch.Tensor] = None) -> tuple:
+    """ue5m3_layer_norm_backward: (dx, dweight, dbias).  dweight is None without a weight or when not wanted, dbias when not
+    wanted; both have the weight's type (x's without a weight)."""
+    rows, cols, ldx = _rows(x)
+    _, _, lddy = _rows(dy, x)
+    _vector(weight, cols, x.device)
+    _vector(mean, rows, x.device, torch.float32)
+    _vector(rstd, rows, x.device, torch.float32)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    _, _, lddx = _rows(out, x)
+    param = weight if weight is not None else x
+    lib = _load()
+    dw = torch.empty(cols, dtype=param.dtype, device=x.device) if want_weight and weight is not None else None
+    db = torch.empty(cols, dtype=param.dtype, device=x.device) if want_bias else None
+    ws = None
+    if dw is not None or db is not None:
+        ws = torch.empty(lib.ue5m3_layer_norm_backward_workspace_bytes(rows, cols), dtype=torch.uint8, device=x.device)
+    with torch.cuda.device(x.device):
+        _check(lib.ue5m3_layer_norm_backward(_dev_ptr(dy), lddy, _dev_ptr(x), _dtype_code(x), rows, cols, ldx, _dev_ptr(weight),
+                                             _dtype_code(param), _dev_ptr(mean), _dev_ptr(rstd), _dev_ptr(out), lddx, _dev_ptr(dw),
+                                             _dev_ptr(db), _dev_ptr(ws), _stream(x)), "ue5m3_layer_norm_backward")
+    return out, dw, db
+
+
+def dropout_add(x: torch.Tensor, p: float, seed: int, residual: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """ue5m3_dropout_add: residual + dropout(x) for `x` [rows, cols]; the draws depend on the seed and the element's index only.
+    The gradient of x is this call on dy with the same p and seed and no residual."""
+    rows, cols, ldx = _rows(x)
+    ldr = 0 if residual is None else _rows(residual, x)[2]
+    if out is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    _, _, ldy = _rows(out, x)
+    with torch.cuda.device(x.device):
+        _check(_load().ue5m3_dropout_add(_dev_ptr(x), ldx, _dev_ptr(residual), ldr, _dtype_code(x), rows, cols, p,
+                                         int(seed) & (2 ** 64 - 1), _dev_ptr(out), ldy, _stream(x)), "ue5m3_dropout_add")
+    return out
+
+
+def _heads(t: torch.Tensor, shape: tuple, like: torch.Tensor) -> _Heads:
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"expected a tensor like [{tuple(shape)}, {like.dtype}, {like.device}], got [{tuple(t.shape)}, {t.dtype}, {t.device}]")
+    if not t.is_cuda:
+        raise ValueError("the library takes device tensors only")
+    if t.stride(3) != 1 and t.shape[3] > 1:
+        raise ValueError("expected tensors [batch, tokens, heads, head_dim] whose last dimension is contiguous")
+    return _Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def _attention_shape(q, k, v, causal, window_left, k_lens, scale) -> _AttentionShape:
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("expected tensors [batch, tokens, heads, head_dim]")
+    B, Lq, H, D = q.shape
+    if k.shape[0] != B or k.shape[3] != D:
+        raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} differ in batch or head dimension")
+    if k_lens is not None and (k_lens.dim() != 1 or k_lens.shape[0] != B or k_lens.dtype != torch.int32 or not k_lens.is_contiguous()
+                               or k_lens.device != q.device):
+        raise ValueError("k_lens must be a contiguous int32 tensor with one length per sequence, on the queries' device")
+    return _AttentionShape(B, Lq, k.shape[1], H, k.shape[2], D, int(window_left), None if k_lens is None else k_lens.data_ptr(),
+                           D ** -0.5 if scale is None else float(scale), _dtype_code(q), 1 if causal else 0)
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, window_left: int = -1,
+              k_lens: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> tuple:
+    """ue5m3_attention: (o, lse) for q [batch, tokens, heads, head_dim] and k, v [batch, keys, kv_heads, head_dim], bfloat16.  Any
+    strides with a contiguous last dimension (views of a fused projection); `window_left` = keys a query sees before its own
+    position (-1: all), `k_lens` int32 [batch] = valid keys of each sequence, `scale` defaults to head_dim ** -0.5."""
+    shape = _attention_shape(q, k, v, causal, window_left, k_lens, scale)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty((shape.batch, shape.heads, shape.q_len), dtype=torch.float32, device=q.device)
+    args = [_heads(q, q.shape, q), _heads(k, k.shape, q), _heads(v, k.shape, q), _heads(out, q.shape, q)]
+    with torch.cuda.device(q.device):
+        _check(_load().ue5m3_attention(shape, *args, _dev_ptr(lse), _stream(q)), "ue5m3_attention")
+    return out, lse
+
+
+def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                       causal: bool = False, window_left: int = -1, k_lens: Optional[torch.Tensor] = None,
+                       scale: Optional[float] = None, out: Optional[tuple] = None) -> tuple:
+    """ue5m3_attention_backward: (dq, dk, dv) from what `attention` returned (o, lse) and the gradient of o; the other arguments as
+    in that call.  `out`: three tensors to write to (any strides with a contiguous last dimension, e.g. views of one fused
+    gradient)."""
+    shape = _attention_shape(q, k, v, causal, window_left, k_lens, scale)
+    if lse.shape != (shape.batch, shape.heads, shape.q_len) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != q.device:
+        raise ValueError("lse must be the contiguous float32 [batch, heads, tokens] tensor that attention returned")
+    if out is None:
+        out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    lib = _load()
+    ws = torch.empty(lib.ue5m3_attention_backward_workspace_bytes(shape), dtype=torch.uint8, device=q.device)
+    ins = [_heads(dout, q.shape, q), _heads(q, q.shape, q), _heads(k, k.shape, q), _heads(v, k.shape, q), _heads(o, q.shape, q)]
+    outs = [_heads(out[0], q.shape, q), _heads(out[1], k.shape, q), _heads(out[2], k.shape, q)]
+    with torch.cuda.device(q.device):
+        _check(lib.ue5m3_attention_backward(shape, *ins, _dev_ptr(lse), *outs, _dev_ptr(ws), _stream(q)), "ue5m3_attention_backward")
+    return tuple(out)
 
 
 # ---------------------------------------------------------------------------------------------

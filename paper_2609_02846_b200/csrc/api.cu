@@ -4,6 +4,7 @@
 #include <cstdint>
 #include <mutex>
 #include "../../include/ue5m3.h"
+#include "block_ops.h"
 #include "launch.h"
 
 namespace ue5m3 {
@@ -344,11 +345,172 @@ int ue5m3_unswizzle_scales(const uint8_t* in, uint8_t* out, int64_t R, int64_t k
     return launch_unswizzle(in, out, R, kblocks, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
+// ---------------------------------------------------------------------------------------------
+// the operators between the linears
+static inline bool known_dtype(int t) { return t == UE5M3_F32 || t == UE5M3_BF16; }
+static inline bool aligned_to(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == UE5M3_F32 ? 3u : 1u)) == 0; }
+
+static int device_ready(int& sms) {
+    const DeviceInfo di = device_info();
+    if (!di.ok) return UE5M3_ERR_CUDA;
+    sms = di.sms;
+    return di.major == 10 ? UE5M3_OK : UE5M3_ERR_UNSUPPORTED;
+}
+
+// Largest matrix these calls take: element offsets stay far inside 63 bits.
+static inline bool too_large(int64_t rows, int64_t cols, int64_t ld) {
+    const int64_t most = (int64_t)1 << 60;
+    return cols > ((int64_t)1 << 31) - 8192 || (rows > 0 && ld > most / rows) || rows > most;
+}
+
+int ue5m3_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, const void* weight, const void* bias,
+                     int weight_dtype, float eps, void* y, int64_t ldy, float* mean, float* rstd, void* stream) {
+    const ApiRange range_("ue5m3_layer_norm");
+    if (rows < 0 || cols <= 0 || ldx < cols || ldy < cols || !known_dtype(dtype) || !known_dtype(weight_dtype)) return UE5M3_ERR_INVALID_ARG;
+    if (!(eps >= 0.0f) || eps > 3.0e38f) return UE5M3_ERR_INVALID_ARG;
+    if (rows > 0 && (!x || !y)) return UE5M3_ERR_INVALID_ARG;
+    if (too_large(rows, cols, ldx) || too_large(rows, cols, ldy)) return UE5M3_ERR_UNSUPPORTED;
+    if (!aligned_to(x, dtype) || !aligned_to(y, dtype) || !aligned_to(weight, weight_dtype) || !aligned_to(bias, weight_dtype) ||
+        !aligned_to(mean, UE5M3_F32) || !aligned_to(rstd, UE5M3_F32))
+        return UE5M3_ERR_ALIGN;
+    int sms = 0;
+    const int bad = device_ready(sms);
+    if (bad != UE5M3_OK) return bad;
+    if (rows == 0) return UE5M3_OK;
+    LayerNormArgs a{};
+    a.x = x; a.ldx = ldx; a.weight = weight; a.bias = bias; a.y = y; a.ldy = ldy; a.mean = mean; a.rstd = rstd;
+    a.rows = rows; a.cols = cols; a.eps = eps;
+    return launch_layer_norm(a, dtype, weight_dtype, sms, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+}
+
+size_t ue5m3_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols <= 0 || too_large(rows, cols, cols)) return 0;
+    return (size_t)layer_norm_backward_groups(rows) * 2 * (size_t)cols * sizeof(float);
+}
+
+int ue5m3_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx,
+                              const void* weight, int weight_dtype, const float* mean, const float* rstd, void* dx, int64_t lddx,
+                              void* dweight, void* dbias, void* workspace, void* stream) {
+    const ApiRange range_("ue5m3_layer_norm_backward");
+    if (rows < 0 || cols <= 0 || ldx < cols || lddy < cols || lddx < cols || !known_dtype(dtype) || !known_dtype(weight_dtype))
+        return UE5M3_ERR_INVALID_ARG;
+    if (rows > 0 && (!x || !dy || !dx || !mean || !rstd)) return UE5M3_ERR_INVALID_ARG;
+    const bool sums = dweight || dbias;
+    if (sums && !workspace) return UE5M3_ERR_INVALID_ARG;
+    if (too_large(rows, cols, ldx) || too_large(rows, cols, lddy) || too_large(rows, cols, lddx)) return UE5M3_ERR_UNSUPPORTED;
+    if (!aligned_to(x, dtype) || !aligned_to(dy, dtype) || !aligned_to(dx, dtype) || !aligned_to(weight, weight_dtype) ||
+        !aligned_to(mean, UE5M3_F32) || !aligned_to(rstd, UE5M3_F32) || !aligned_to(dweight, weight_dtype) ||
+        !aligned_to(dbias, weight_dtype) || !aligned16(workspace))
+        return UE5M3_ERR_ALIGN;
+    int sms = 0;
+    const int bad = device_ready(sms);
+    if (bad != UE5M3_OK) return bad;
+    if (rows == 0 && !sums) return UE5M3_OK;
+    LayerNormArgs a{};
+    a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.weight = weight; a.y = dx; a.ldy = lddx;
+    a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+    a.dweight = dweight; a.dbias = dbias; a.partial = sums ? static_cast<float*>(workspace) : nullptr;
+    a.rows = rows; a.cols = cols;
+    return launch_layer_norm_backward(a, dtype, weight_dtype, sms, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+}
+
+int ue5m3_dropout_add(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype, int64_t rows, int64_t cols, float p,
+                      uint64_t seed, void* y, int64_t ldy, void* stream) {
+    const ApiRange range_("ue5m3_dropout_add");
+    if (rows < 0 || cols < 0 || ldx < cols || ldy < cols || (residual && ldr < cols) || !known_dtype(dtype)) return UE5M3_ERR_INVALID_ARG;
+    if (!(p >= 0.0f && p <= 1.0f)) return UE5M3_ERR_INVALID_ARG;
+    const bool empty = rows == 0 || cols == 0;
+    if (!empty && (!x || !y)) return UE5M3_ERR_INVALID_ARG;
+    if (too_large(rows, cols, ldx) || too_large(rows, cols, ldy) || (residual && too_large(rows, cols, ldr))) return UE5M3_ERR_UNSUPPORTED;
+    if (!aligned_to(x, dtype) || !aligned_to(residual, dtype) || !aligned_to(y, dtype)) return UE5M3_ERR_ALIGN;
+    int sms = 0;
+    const int bad = device_ready(sms);
+    if (bad != UE5M3_OK) return bad;
+    if (empty) return UE5M3_OK;
+    const uint32_t t = (uint32_t)((double)p * 65536.0 + 0.5);
+    DropoutArgs a{};
+    a.x = x; a.residual = residual; a.y = y; a.ldx = ldx; a.ldr = ldr; a.ldy = ldy; a.rows = rows; a.cols = cols; a.seed = seed;
+    a.drop = t != 0;
+    a.limit = t ? (t << 16) - 1u : 0u;                     // t = 65536: no draw is above it
+    a.inv_keep = t < 65536 ? (float)(65536.0 / (65536.0 - (double)t)) : 0.0f;
+    return launch_dropout_add(a, dtype, sms, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+}
+
+static int check_attention_shape(const ue5m3_attention_shape* s) {
+    if (!s || s->batch < 0 || s->q_len < 0 || s->k_len < 0 || s->heads <= 0 || s->kv_heads <= 0 || s->head_dim <= 0) return UE5M3_ERR_INVALID_ARG;
+    if (s->window_left < -1 || (s->causal != 0 && s->causal != 1) || !(s->scale > 0.0f) || s->scale > 3.0e38f) return UE5M3_ERR_INVALID_ARG;
+    if (!known_dtype(s->dtype)) return UE5M3_ERR_INVALID_ARG;
+    if ((s->head_dim % 8) || (s->heads % s->kv_heads)) return UE5M3_ERR_SHAPE;
+    if (s->dtype != UE5M3_BF16 || s->head_dim > 128) return UE5M3_ERR_UNSUPPORTED;
+    const int64_t most = (int64_t)1 << 30;
+    if (s->q_len > most || s->k_len > most || s->batch > most || s->heads > most || s->batch * s->heads > most) return UE5M3_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(s->k_lens) & 3u) return UE5M3_ERR_ALIGN;
+    return UE5M3_OK;
+}
+// One tensor [batch, tokens, heads, head_dim] of an attention call.
+static int check_heads(const ue5m3_heads* t, int64_t batch, int64_t tokens, int64_t heads) {
+    if (!t) return UE5M3_ERR_INVALID_ARG;
+    if (batch == 0 || tokens == 0) return UE5M3_OK;
+    if (!t->data) return UE5M3_ERR_INVALID_ARG;
+    if (!aligned16(t->data)) return UE5M3_ERR_ALIGN;
+    const int64_t sizes[3] = {batch, tokens, heads}, strides[3] = {t->batch_stride, t->token_stride, t->head_stride};
+    for (int i = 0; i < 3; ++i) {
+        if (sizes[i] <= 1) continue;
+        if (strides[i] <= 0 || strides[i] % 8) return UE5M3_ERR_ALIGN;
+        if (strides[i] >= ((int64_t)1 << 39)) return UE5M3_ERR_UNSUPPORTED;      // a tensor map's strides end at 2^40 bytes
+    }
+    return UE5M3_OK;
+}
+
+int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, const ue5m3_heads* k, const ue5m3_heads* v,
+                    const ue5m3_heads* o, float* lse, void* stream) {
+    const ApiRange range_("ue5m3_attention");
+    int bad = check_attention_shape(shape);
+    if (bad != UE5M3_OK) return bad;
+    const ue5m3_attention_shape& s = *shape;
+    for (const ue5m3_heads* t : {q, o})
+        if ((bad = check_heads(t, s.batch, s.q_len, s.heads)) != UE5M3_OK) return bad;
+    for (const ue5m3_heads* t : {k, v})
+        if ((bad = check_heads(t, s.batch, s.k_len, s.kv_heads)) != UE5M3_OK) return bad;
+    if (!lse && s.batch * s.q_len > 0) return UE5M3_ERR_INVALID_ARG;
+    if (!aligned_to(lse, UE5M3_F32)) return UE5M3_ERR_ALIGN;
+    int sms = 0;
+    if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
+    return launch_attention(s, *q, *k, *v, *o, lse, sms, (cudaStream_t)stream);
+}
+
+size_t ue5m3_attention_backward_workspace_bytes(const ue5m3_attention_shape* shape) {
+    if (check_attention_shape(shape) != UE5M3_OK) return 0;
+    return (size_t)shape->batch * (size_t)shape->heads * (size_t)attention_padded_q(shape->q_len) * 2 * sizeof(float);
+}
+
+int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_heads* dout, const ue5m3_heads* q, const ue5m3_heads* k,
+                             const ue5m3_heads* v, const ue5m3_heads* o, const float* lse, const ue5m3_heads* dq, const ue5m3_heads* dk,
+                             const ue5m3_heads* dv, void* workspace, void* stream) {
+    const ApiRange range_("ue5m3_attention_backward");
+    int bad = check_attention_shape(shape);
+    if (bad != UE5M3_OK) return bad;
+    const ue5m3_attention_shape& s = *shape;
+    for (const ue5m3_heads* t : {dout, q, o, dq})
+        if ((bad = check_heads(t, s.batch, s.q_len, s.heads)) != UE5M3_OK) return bad;
+    for (const ue5m3_heads* t : {k, v, dk, dv})
+        if ((bad = check_heads(t, s.batch, s.k_len, s.kv_heads)) != UE5M3_OK) return bad;
+    if ((!lse || !workspace) && s.batch * s.q_len > 0) return UE5M3_ERR_INVALID_ARG;
+    if (!aligned_to(lse, UE5M3_F32) || !aligned16(workspace)) return UE5M3_ERR_ALIGN;
+    int sms = 0;
+    if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
+    return launch_attention_backward(s, *dout, *q, *k, *v, *o, lse, *dq, *dk, *dv, static_cast<float*>(workspace), sms, (cudaStream_t)stream);
+}
+
 int ue5m3_last_device_status(void) {
     const int a = read_and_clear_device_status();
     const int b = read_and_clear_probe_status();
     const int c = read_and_clear_native_status();
-    return a != UE5M3_OK ? a : (b != UE5M3_OK ? b : c);
+    const int d = read_and_clear_attention_status();
+    const int e = read_and_clear_attention_backward_status();
+    for (int v : {a, b, c, d, e})
+        if (v != UE5M3_OK) return v;
+    return UE5M3_OK;
 }
 
 }  // extern "C"

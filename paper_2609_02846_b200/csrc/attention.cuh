@@ -1,0 +1,131 @@
+// What the attention kernels share: one-CTA tcgen05 wrappers, matrix descriptors, the mask and the tensor maps (sm_100a only).
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <cstdint>
+#include "../../include/ue5m3.h"
+#include "block_ops.h"
+#include "tcgen05.cuh"
+
+namespace ue5m3 {
+
+// ----------------------------------------------------------------------------- PTX wrappers (cta_group::1)
+__device__ __forceinline__ void tmem_alloc1(uint32_t dst_smem, uint32_t ncols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(ncols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc1(uint32_t taddr, uint32_t ncols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void umma1_ss(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma1_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Arrives on the barrier once every MMA issued so far by this thread has completed.
+__device__ __forceinline__ void umma1_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// Plain bulk copy of `bytes` (a multiple of 16, both addresses 16-byte aligned) into shared memory.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// ----------------------------------------------------------------------------- tiles in shared memory
+// A tile is ROWS x (64 * panels) BF16 values in panels of 64 columns: a panel is ROWS rows of 128 bytes, 128-byte swizzle, as a
+// tensor-map box of 64 x ROWS delivers it.  Read along the columns (contraction over the head dimension) it is a K-major
+// operand; read along the rows (contraction over queries or keys) an MN-major one.
+//
+// K-major: umma_smem_desc (8-row groups 1024 bytes apart); 16 columns further = 32 bytes, next panel = ROWS * 128 bytes.
+// MN-major: 64 consecutive columns per swizzle row; the next 64 (leading byte offset) are a panel further, the next 8 rows
+// of the contraction (stride byte offset) 1024 bytes further; 16 rows further = 2048 bytes.
+__device__ __forceinline__ uint64_t umma_mn_desc(uint32_t saddr, uint32_t panel_bytes) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(panel_bytes >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+// kind::f16 instruction descriptor: D = F32, A = B = BF16, M = 128, N given; b_mn: B is MN-major.
+__host__ __device__ constexpr uint32_t umma_idesc(uint32_t n, bool b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+// ----------------------------------------------------------------------------- which pairs exist
+struct AttentionParams {
+    int q_len, k_len, heads, group;      // group = heads per key/value head
+    int causal, left;                    // left < 0: all
+    int batch;
+    const int* k_lens;
+    float scale, scale_log2;             // scale * log2(e)
+    float* lse;                          // forward: [batch, heads, q_len]
+    const float* lse2;                   // backward: lse * log2(e) per query, padded to whole tiles (+inf: contributes nothing)
+    const float* delta;                  // backward: dout . o per query, padded
+    int q_pad;
+    long long wait_limit;
+
+    __device__ __forceinline__ int keys_of(int b) const {
+        if (!k_lens) return k_len;
+        const int n = __ldg(k_lens + b);
+        return n < 0 ? 0 : (n > k_len ? k_len : n);
+    }
+    // keys [lo, hi) that query i sees (empty when hi <= lo)
+    __device__ __forceinline__ int key_lo(int i) const { return left >= 0 ? max(0, i + (k_len - q_len) - left) : 0; }
+    __device__ __forceinline__ int key_hi(int i, int keys) const { return causal ? min(keys, i + (k_len - q_len) + 1) : keys; }
+    // queries [lo, hi) that see key j, given that j < keys
+    __device__ __forceinline__ int query_lo(int j) const { return causal ? max(0, j - (k_len - q_len)) : 0; }
+    __device__ __forceinline__ int query_hi(int j) const { return left >= 0 ? min(q_len, j - (k_len - q_len) + left + 1) : q_len; }
+};
+
+// ----------------------------------------------------------------------------- host side
+// [batch, tokens, heads, dim] with element strides -> map (dim, tokens, heads, batch); box 64 x rows.  Dimensions of size 1 get
+// a stride that is always valid.
+inline bool make_heads_map(CUtensorMap* m, const ue5m3_heads& t, int64_t batch, int64_t tokens, int64_t heads, int64_t dim, uint32_t rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)batch};
+    const cuuint64_t any = (cuuint64_t)((dim + 7) / 8 * 8) * 2;
+    cuuint64_t strides[3] = {tokens > 1 ? (cuuint64_t)t.token_stride * 2 : any, heads > 1 ? (cuuint64_t)t.head_stride * 2 : any,
+                             batch > 1 ? (cuuint64_t)t.batch_stride * 2 : any};
+    cuuint32_t box[4] = {64, rows, 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, t.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+inline AttentionParams attention_params(const ue5m3_attention_shape& s) {
+    AttentionParams p{};
+    p.q_len = (int)s.q_len; p.k_len = (int)s.k_len; p.heads = (int)s.heads; p.group = (int)(s.heads / s.kv_heads);
+    p.causal = s.causal; p.batch = (int)s.batch; p.k_lens = s.k_lens;
+    const int64_t all = s.q_len + s.k_len;                  // a window as long as this hides nothing
+    p.left = s.window_left < 0 ? -1 : (int)(s.window_left < all ? s.window_left : all);
+    p.scale = s.scale;
+    p.scale_log2 = s.scale * 1.4426950408889634f;
+    p.q_pad = (int)attention_padded_q(s.q_len);
+    p.wait_limit = WAIT_LIMIT_CYCLES;
+    return p;
+}
+
+}  // namespace ue5m3

@@ -1,0 +1,658 @@
+// Attention, backward, for sm_100a.  Nothing of the forward pass is kept but o and lse; with s = scale log2(e) q.k
+//     P_ij = 2^(s_ij - lse2_i),  dP_ij = dout_i . v_j,  dS_ij = P_ij (dP_ij - D_i),  D_i = dout_i . o_i
+//     dv_j = sum_i P_ij dout_i,  dk_j = scale sum_i dS_ij q_i,  dq_i = scale sum_j dS_ij k_j
+//
+// Three launches:
+//   rows     D_i and lse2_i = log2(e) lse_i of every query (padded to whole tiles; +inf where a query sees nothing, so that P = 0)
+//   keys     a CTA owns 128 keys of one key/value head and walks the queries that see them, through all query heads of the
+//            group: S^T = K Q^T, dP^T = V dO^T, then dV += P^T dO and dK += dS^T Q
+//   queries  a CTA owns 128 queries of one head and walks the keys they see: S = Q K^T, dP = dO V^T, dQ += dS K
+// S and dP are computed in both (7 products instead of 5): in exchange every gradient is summed by one CTA in one fixed order
+// in tensor memory; there is no binary32 copy of dq in memory, no atomic and nothing that changes from call to call.
+//
+// P and dS never touch shared memory: the softmax warps read S and dP from tensor memory and write P and dS (BF16) over them,
+// from where the tensor core takes them as the A operand.  Both kernels have the same roles:
+//   warp 0      copies     warp 1   issues the MMAs     warp 2   tensor-memory allocation
+//   warps 4-11  two groups of four; a thread owns one row of S (a key, or a query) and half of its 128 columns
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <cstdint>
+#include "../../include/ue5m3.h"
+#include "attention.cuh"
+#include "block_ops.h"
+#include "common.cuh"
+
+namespace ue5m3 {
+
+__device__ int g_attention_backward_status = 0;
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int B128 = 128;
+
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+    return mbar_wait_status(bar, parity, abort_flag, &g_attention_backward_status, limit);
+}
+
+// ------------------------------------------------------------------------------------------------ rows
+struct RowParams {
+    const __nv_bfloat16* o; const __nv_bfloat16* dout;
+    int64_t o_stride[3], d_stride[3];               // batch, token, head
+    const float* lse;
+    float* lse2; float* delta;
+    int q_len, q_pad, heads, dim;
+    int64_t rows;                                   // batch * heads * q_pad
+};
+// Eight threads per query, 16 bytes of o and dout at a time.
+__global__ void __launch_bounds__(256) attention_rows_kernel(const RowParams p) {
+    const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+    const int sub = threadIdx.x & 7;
+    if (r >= p.rows) return;                        // whole groups of eight
+    const int64_t bh = r / p.q_pad;
+    const int i = (int)(r - bh * p.q_pad), b = (int)(bh / p.heads), h = (int)(bh - (int64_t)b * p.heads);
+    float sum = 0.0f, lse2 = INFINITY;
+    if (i < p.q_len) {
+        const __nv_bfloat16* o = p.o + b * p.o_stride[0] + i * p.o_stride[1] + h * p.o_stride[2];
+        const __nv_bfloat16* d = p.dout + b * p.d_stride[0] + i * p.d_stride[1] + h * p.d_stride[2];
+        for (int c = sub * 8; c < p.dim; c += 64) {
+            float x[8], y[8];
+            unpack_bf16x8(ldg_nc_v4(o + c), x);
+            unpack_bf16x8(ldg_nc_v4(d + c), y);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum = fmaf(x[k], y[k], sum);
+        }
+        const float lse = p.lse[bh * p.q_len + i];
+        if (lse != -INFINITY) lse2 = lse * 1.4426950408889634f;
+    }
+#pragma unroll
+    for (int k = 4; k; k >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, k, 8);
+    if (sub == 0) { p.lse2[r] = lse2; p.delta[r] = sum; }
+}
+
+// ------------------------------------------------------------------------------------------------ shared pieces
+template <int DP> struct Tiles {
+    static constexpr int PANELS = DP / 64;
+    static constexpr int TILE = 128 * DP * 2;
+    static constexpr int PANEL = 128 * 128;
+};
+// tensor-memory columns: S, dP, then the accumulators
+constexpr uint32_t COL_S = 0, COL_DP = 128, COL_ACC0 = 256, COL_ACC1 = 384;
+
+// Writes a 128-row tile (this warp: 32 rows) of a binary32 accumulator times `f` as BF16 through shared memory.
+template <int DP>
+__device__ __forceinline__ void store_accumulator(uint32_t tm_lane, uint8_t* smem_gen, uint32_t smem, uint32_t tile_off, int q, int lane,
+                                                  const CUtensorMap* map, float f, bool zero, int row0, int head, int b) {
+#pragma unroll 1
+    for (int c = 0; c < DP / 64; ++c) {
+        const uint32_t off = tile_off + c * (128 * 128) + q * 4096;
+        uint8_t* mine = smem_gen + off + lane * 128;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            uint32_t o[32];
+            if (!zero) {
+                tmem_ld32(tm_lane + c * 64 + half * 32, o);
+                tmem_ld_wait();
+            }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                uint4 w = make_uint4(0, 0, 0, 0);
+                if (!zero) {
+                    w.x = pack_bf16x2(__uint_as_float(o[8 * v]) * f, __uint_as_float(o[8 * v + 1]) * f);
+                    w.y = pack_bf16x2(__uint_as_float(o[8 * v + 2]) * f, __uint_as_float(o[8 * v + 3]) * f);
+                    w.z = pack_bf16x2(__uint_as_float(o[8 * v + 4]) * f, __uint_as_float(o[8 * v + 5]) * f);
+                    w.w = pack_bf16x2(__uint_as_float(o[8 * v + 6]) * f, __uint_as_float(o[8 * v + 7]) * f);
+                }
+                *reinterpret_cast<uint4*>(mine + (((half * 4 + v) ^ (lane & 7)) << 4)) = w;
+            }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) tma_store_4d(map, smem + off, c * 64, row0, head, b);
+    }
+    if (lane == 0) tma_store_wait_all();
+}
+
+// ------------------------------------------------------------------------------------------------ keys: dK and dV
+template <int DP> struct KeySmem {
+    using T = Tiles<DP>;
+    static constexpr int STAGES = DP == 128 ? 2 : 4;
+    static constexpr int RING = 2 * T::TILE;                          // K, V, then STAGES x (Q, dO)
+    static constexpr int ROWS = RING + STAGES * 2 * T::TILE;          // STAGES x (128 lse2, 128 delta)
+    static constexpr int BAR = ROWS + STAGES * 1024;
+    static constexpr int SIZE = BAR + 256 + 1024;
+};
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
+                      const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                      const __grid_constant__ CUtensorMap map_dk, const __grid_constant__ CUtensorMap map_dv, const AttentionParams p,
+                      const int kv_heads) {
+    using T = Tiles<DP>;
+    using M = KeySmem<DP>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem - smem_u32(smem_raw));
+    const uint32_t bars = smem + M::BAR;
+    const uint32_t k_full = bars, v_full = bars + 8, s_full = bars + 16, dp_full = bars + 24, p_full = bars + 32, ds_full = bars + 40;
+    const uint32_t acc_full = bars + 48, drain = bars + 56, q_full = bars + 64, q_empty = q_full + 8 * M::STAGES;
+    const uint32_t d_full = q_empty + 8 * M::STAGES, d_empty = d_full + 8 * M::STAGES;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + M::BAR + 192);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + M::BAR + 196);
+
+    // key tiles of one head side by side, those that most queries see (causal: the first) at the front
+    const int bh_count = p.batch * kv_heads;
+    const int bh = blockIdx.x % bh_count, j0 = (int)(blockIdx.x / bh_count) * B128;
+    const int b = bh / kv_heads, kvh = bh - b * kv_heads;
+    const int keys = p.keys_of(b);
+    const int j1 = min(j0 + B128, keys) - 1;                          // last key of the tile
+    int lo = 0, hi = 0;                                               // query tiles
+    if (j0 < keys) {
+        const int a = p.query_lo(j0), z = p.query_hi(j1);
+        if (z > a) { lo = a / B128; hi = (z + B128 - 1) / B128; }
+    }
+    const int per_head = hi - lo, steps = per_head * p.group;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        const uint32_t ones[] = {k_full, v_full, s_full, dp_full, acc_full, drain};
+        for (uint32_t x : ones) mbar_init(x, 1);
+        mbar_init(p_full, 8);
+        mbar_init(ds_full, 8);
+        for (int s = 0; s < M::STAGES; ++s) {
+            mbar_init(q_full + 8 * s, 1); mbar_init(q_empty + 8 * s, 1);
+            mbar_init(d_full + 8 * s, 1); mbar_init(d_empty + 8 * s, 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_tmap(&map_q); prefetch_tmap(&map_do); prefetch_tmap(&map_k); prefetch_tmap(&map_v); prefetch_tmap(&map_dk); prefetch_tmap(&map_dv);
+    }
+    if (warp == 2) tmem_alloc1(smem_u32(tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ copies
+        if (lane == 0 && steps > 0) {
+            auto tile = [&](uint32_t dst, const CUtensorMap* m, uint32_t bar, int row, int head) {
+#pragma unroll
+                for (int c = 0; c < T::PANELS; ++c) tma_load_4d(dst + c * T::PANEL, m, bar, c * 64, row, head, b);
+            };
+            mbar_expect_tx(k_full, T::TILE);
+            tile(smem, &map_k, k_full, j0, kvh);
+            int it = 0;
+            bool v_out = false;
+            for (; it < steps; ++it) {
+                const int s = it % M::STAGES, h = kvh * p.group + it / per_head, i0 = (lo + it % per_head) * B128;
+                const uint32_t ph = (it / M::STAGES) & 1;
+                const uint32_t st = smem + M::RING + s * 2 * T::TILE, rows = smem + M::ROWS + s * 1024;
+                const int64_t row = ((int64_t)b * p.heads + h) * p.q_pad + i0;
+                if (!wait(q_empty + 8 * s, ph ^ 1, abort_flag, p.wait_limit)) break;
+                mbar_expect_tx(q_full + 8 * s, T::TILE + 1024);
+                tile(st, &map_q, q_full + 8 * s, i0, h);
+                bulk_load(rows, p.lse2 + row, 512, q_full + 8 * s);
+                bulk_load(rows + 512, p.delta + row, 512, q_full + 8 * s);
+                if (!v_out) {
+                    mbar_expect_tx(v_full, T::TILE);
+                    tile(smem + T::TILE, &map_v, v_full, j0, kvh);
+                    v_out = true;
+                }
+                if (!wait(d_empty + 8 * s, ph ^ 1, abort_flag, p.wait_limit)) {
+                    mbar_wait_drain(q_full + 8 * s, ph, &g_attention_backward_status, p.wait_limit);
+                    break;
+                }
+                mbar_expect_tx(d_full + 8 * s, T::TILE);
+                tile(st + T::TILE, &map_do, d_full + 8 * s, i0, h);
+            }
+            mbar_wait_drain(k_full, 0, &g_attention_backward_status, p.wait_limit);
+            if (v_out) mbar_wait_drain(v_full, 0, &g_attention_backward_status, p.wait_limit);
+            for (int back = 0; back < M::STAGES && back < it; ++back) {
+                const int j = it - 1 - back;
+                mbar_wait_drain(q_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, &g_attention_backward_status, p.wait_limit);
+                mbar_wait_drain(d_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, &g_attention_backward_status, p.wait_limit);
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        const bool elected = elect_one();
+        const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+        constexpr uint32_t id_s = umma_idesc(128, false), id_acc = umma_idesc(DP, true);
+        bool ok = true;
+        auto wait_all = [&](uint32_t bar, uint32_t parity) {
+            ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
+            tc_fence_after();
+            return ok;
+        };
+        auto stage = [&](int it) { return smem + M::RING + (uint32_t)(it % M::STAGES) * 2 * T::TILE; };
+        auto phase = [&](int it) { return (uint32_t)((it / M::STAGES) & 1); };
+        // [keys x queries] = (K or V) (Q or dO)^T, both K-major
+        auto issue_square = [&](uint32_t col, uint32_t a, uint32_t bt, uint32_t bar) {
+            const uint64_t ad = umma_smem_desc(a), bd = umma_smem_desc(bt);
+            if (elected) {
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    const uint32_t off = (k / 4) * (T::PANEL >> 4) + (k % 4) * 2;
+                    umma1_ss(tm + col, ad + off, bd + off, id_s, k != 0);
+                }
+                umma1_commit(bar);
+            }
+            __syncwarp();
+        };
+        // [keys x dim] += (P or dS)^T (dO or Q): A from tensor memory (each softmax group's 64 queries in its own half), B MN-major
+        auto issue_acc = [&](uint32_t col, uint32_t a_col, uint32_t bt, bool add, uint32_t bar) {
+            const uint64_t bd = umma_mn_desc(bt, T::PANEL);
+            if (elected) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    umma1_ts(tm + col, tm + a_col + (k / 4) * 64 + (k % 4) * 8, bd + k * (2048 >> 4), id_acc, add || k != 0);
+                umma1_commit(bar);
+            }
+            __syncwarp();
+        };
+        if (steps > 0 && wait_all(k_full, 0) && wait_all(q_full, 0)) {
+            issue_square(COL_S, smem, stage(0), s_full);
+            if (wait_all(v_full, 0) && wait_all(d_full, 0)) issue_square(COL_DP, smem + T::TILE, stage(0) + T::TILE, dp_full);
+        }
+        for (int it = 0; it < steps && ok; ++it) {
+            if (!wait_all(p_full, it & 1)) break;
+            issue_acc(COL_ACC0, COL_S, stage(it) + T::TILE, it != 0, d_empty + 8 * (it % M::STAGES));
+            if (it + 1 < steps) {
+                if (!wait_all(q_full + 8 * ((it + 1) % M::STAGES), phase(it + 1))) break;
+                issue_square(COL_S, smem, stage(it + 1), s_full);
+            }
+            if (!wait_all(ds_full, it & 1)) break;
+            issue_acc(COL_ACC1, COL_DP, stage(it), it != 0, q_empty + 8 * (it % M::STAGES));
+            if (it + 1 < steps) {
+                if (!wait_all(d_full + 8 * ((it + 1) % M::STAGES), phase(it + 1))) break;
+                issue_square(COL_DP, smem + T::TILE, stage(it + 1) + T::TILE, dp_full);
+            } else {
+                if (elected) umma1_commit(acc_full);
+                __syncwarp();
+            }
+        }
+        if (elected) {
+            umma1_commit(drain);
+            mbar_wait_drain(drain, 0, &g_attention_backward_status, p.wait_limit);
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ P, dS and the outputs
+        const int g = (warp - 4) >> 2, q = warp & 3;                  // column half, tensor-memory lane quarter
+        const int key = j0 + q * 32 + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
+        const uint32_t ts = lane_base + COL_S + g * 64, td = lane_base + COL_DP + g * 64;
+        const int q_lo = key < keys ? p.query_lo(key) : 0, q_hi = key < keys ? p.query_hi(key) : 0;
+        // query tiles [plain_lo, plain_hi) see every key of this tile
+        const int plain_lo = j0 + B128 <= keys ? (p.query_lo(j0 + B128 - 1) + B128 - 1) / B128 : hi;
+        const int plain_hi = p.left >= 0 ? max(p.query_hi(j0), 0) / B128 : p.q_len / B128 + 1;
+        bool ok = true;
+        for (int it = 0; it < steps; ++it) {
+            const int qt = lo + it % per_head;
+            const float* rows = reinterpret_cast<const float*>(smem_gen + M::ROWS + (it % M::STAGES) * 1024) + g * 64;
+            const bool plain = qt >= plain_lo && qt < plain_hi;
+            const int base = qt * B128 + g * 64 - q_lo, width = q_hi - q_lo;
+            if (!(ok = wait(s_full, it & 1, abort_flag, p.wait_limit))) break;
+            // this query tile's rows of lse2 and delta came with Q, whose barrier S waited for; seen by every thread
+            if (!(ok = wait(q_full + 8 * (it % M::STAGES), (it / M::STAGES) & 1, abort_flag, p.wait_limit))) break;
+            tc_fence_after();
+            uint32_t s[64];
+            tmem_ld32(ts, s);
+            tmem_ld32(ts + 32, s + 32);
+            tmem_ld_wait();
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+                const float4 e = *reinterpret_cast<const float4*>(rows + c);
+                s[c] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c]), p.scale_log2, -e.x)));
+                s[c + 1] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c + 1]), p.scale_log2, -e.y)));
+                s[c + 2] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c + 2]), p.scale_log2, -e.z)));
+                s[c + 3] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c + 3]), p.scale_log2, -e.w)));
+            }
+            if (!plain)
+#pragma unroll
+                for (int c = 0; c < 64; ++c)
+                    if (!(base + c >= 0 && base + c < width)) s[c] = 0u;
+            {
+                uint32_t pk[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) pk[i] = pack_bf16x2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+                tmem_st32(ts, pk);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full);
+            if (!(ok = wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
+            tc_fence_after();
+            uint32_t pk[32];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t d[32];
+                tmem_ld32(td + half * 32, d);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    const float4 e = *reinterpret_cast<const float4*>(rows + 128 + half * 32 + c);
+                    const uint32_t* pp = s + half * 32 + c;
+                    float x0 = __uint_as_float(pp[0]) * (__uint_as_float(d[c]) - e.x), x1 = __uint_as_float(pp[1]) * (__uint_as_float(d[c + 1]) - e.y);
+                    float x2 = __uint_as_float(pp[2]) * (__uint_as_float(d[c + 2]) - e.z), x3 = __uint_as_float(pp[3]) * (__uint_as_float(d[c + 3]) - e.w);
+                    if (!plain) {                                     // 0 * NaN where the pair does not exist
+                        x0 = pp[0] ? x0 : 0.0f; x1 = pp[1] ? x1 : 0.0f; x2 = pp[2] ? x2 : 0.0f; x3 = pp[3] ? x3 : 0.0f;
+                    }
+                    pk[half * 16 + c / 2] = pack_bf16x2(x0, x1);
+                    pk[half * 16 + c / 2 + 1] = pack_bf16x2(x2, x3);
+                }
+            }
+            tmem_st32(td, pk);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_full);
+        }
+        if (ok && steps > 0) {
+            ok = wait(acc_full, 0, abort_flag, p.wait_limit);
+            tc_fence_after();
+        }
+        // group 0 writes dV over V's tile, group 1 dK over K's: no MMA reads them any more (or they were never loaded)
+        if (ok && j0 + q * 32 < p.k_len) {
+            if (g == 0) store_accumulator<DP>(lane_base + COL_ACC0, smem_gen, smem, T::TILE, q, lane, &map_dv, 1.0f, steps == 0, j0 + q * 32, kvh, b);
+            else store_accumulator<DP>(lane_base + COL_ACC1, smem_gen, smem, 0, q, lane, &map_dk, p.scale, steps == 0, j0 + q * 32, kvh, b);
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 2) { tc_fence_after(); tmem_dealloc1(tmem, 512); }
+}
+
+// ------------------------------------------------------------------------------------------------ queries: dQ
+template <int DP> struct QuerySmem {
+    using T = Tiles<DP>;
+    static constexpr int STAGES = DP == 128 ? 5 : 8;                  // ring of K and V tiles
+    static constexpr int RING = 2 * T::TILE;                          // Q, dO
+    static constexpr int BAR = RING + STAGES * T::TILE;
+    static constexpr int SIZE = BAR + 256 + 1024;
+};
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
+                         const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                         const __grid_constant__ CUtensorMap map_dq, const AttentionParams p, const int q_tiles) {
+    using T = Tiles<DP>;
+    using M = QuerySmem<DP>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem - smem_u32(smem_raw));
+    const uint32_t bars = smem + M::BAR;
+    const uint32_t q_full = bars, d_full = bars + 8, s_full = bars + 16 /* two */, dp_full = bars + 32, s_free = bars + 40 /* two */;
+    const uint32_t ds_full = bars + 56, acc_full = bars + 64, drain = bars + 72, kv_full = bars + 80, kv_empty = kv_full + 8 * M::STAGES;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + M::BAR + 240);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + M::BAR + 244);
+    constexpr uint32_t COL_S1 = COL_ACC1;                             // S alternates between columns 0.. and 384..
+
+    const int bh_count = p.batch * p.heads;
+    const int bh = blockIdx.x % bh_count, i0 = (q_tiles - 1 - (int)(blockIdx.x / bh_count)) * B128;
+    const int b = bh / p.heads, h = bh - b * p.heads, kvh = h / p.group;
+    const int keys = p.keys_of(b);
+    const int i1 = min(i0 + B128, p.q_len) - 1;
+    int lo = 0, hi = 0;                                               // key tiles
+    {
+        const int a = p.key_lo(i0), z = p.key_hi(i1, keys);
+        if (z > a) { lo = a / B128; hi = (z + B128 - 1) / B128; }
+    }
+    const int steps = hi - lo;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        const uint32_t ones[] = {q_full, d_full, s_full, s_full + 8, dp_full, acc_full, drain}, eights[] = {s_free, s_free + 8, ds_full};
+        for (uint32_t x : ones) mbar_init(x, 1);
+        for (uint32_t x : eights) mbar_init(x, 8);
+        for (int s = 0; s < M::STAGES; ++s) { mbar_init(kv_full + 8 * s, 1); mbar_init(kv_empty + 8 * s, 1); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_tmap(&map_q); prefetch_tmap(&map_do); prefetch_tmap(&map_k); prefetch_tmap(&map_v); prefetch_tmap(&map_dq);
+    }
+    if (warp == 2) tmem_alloc1(smem_u32(tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ copies
+        if (lane == 0 && steps > 0) {
+            auto tile = [&](uint32_t dst, const CUtensorMap* m, uint32_t bar, int row, int head) {
+#pragma unroll
+                for (int c = 0; c < T::PANELS; ++c) tma_load_4d(dst + c * T::PANEL, m, bar, c * 64, row, head, b);
+            };
+            mbar_expect_tx(q_full, T::TILE);
+            tile(smem, &map_q, q_full, i0, h);
+            int it = 0;                                               // tile 2i = K, 2i + 1 = V of key tile lo + i
+            bool d_out = false;
+            for (; it < 2 * steps; ++it) {
+                const int s = it % M::STAGES;
+                if (!wait(kv_empty + 8 * s, ((it / M::STAGES) & 1) ^ 1, abort_flag, p.wait_limit)) break;
+                mbar_expect_tx(kv_full + 8 * s, T::TILE);
+                tile(smem + M::RING + s * T::TILE, (it & 1) ? &map_v : &map_k, kv_full + 8 * s, (lo + (it >> 1)) * B128, kvh);
+                if (!d_out) {
+                    mbar_expect_tx(d_full, T::TILE);
+                    tile(smem + T::TILE, &map_do, d_full, i0, h);
+                    d_out = true;
+                }
+            }
+            mbar_wait_drain(q_full, 0, &g_attention_backward_status, p.wait_limit);
+            if (d_out) mbar_wait_drain(d_full, 0, &g_attention_backward_status, p.wait_limit);
+            for (int back = 0; back < M::STAGES && back < it; ++back) {
+                const int j = it - 1 - back;
+                mbar_wait_drain(kv_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, &g_attention_backward_status, p.wait_limit);
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        // S runs one key tile ahead: S(0) dP(0) S(1) | dQ(0) dP(1) S(2) | dQ(1) dP(2) S(3) | ...
+        const bool elected = elect_one();
+        const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+        constexpr uint32_t id_s = umma_idesc(128, false), id_acc = umma_idesc(DP, true);
+        bool ok = true;
+        auto wait_all = [&](uint32_t bar, uint32_t parity) {
+            ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
+            tc_fence_after();
+            return ok;
+        };
+        auto stage = [&](int n) { return smem + M::RING + (uint32_t)(n % M::STAGES) * T::TILE; };
+        auto full = [&](int n) { return wait_all(kv_full + 8 * (n % M::STAGES), (n / M::STAGES) & 1); };
+        auto issue_square = [&](uint32_t col, uint32_t a, uint32_t bt, uint32_t bar) {
+            const uint64_t ad = umma_smem_desc(a), bd = umma_smem_desc(bt);
+            if (elected) {
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    const uint32_t off = (k / 4) * (T::PANEL >> 4) + (k % 4) * 2;
+                    umma1_ss(tm + col, ad + off, bd + off, id_s, k != 0);
+                }
+                umma1_commit(bar);
+            }
+            __syncwarp();
+        };
+        auto issue_s = [&](int it) {
+            if (!full(2 * it)) return;
+            const int valid = keys - (lo + it) * B128;
+            if (p.k_lens && valid < B128) {
+                // keys behind the sequence's end may hold anything (dS is zero there, and 0 * NaN is NaN): they become zeros
+                for (int i = valid * (DP / 8) + lane; i < B128 * (DP / 8); i += 32) {
+                    const int r = i / (DP / 8), c = i % (DP / 8);
+                    *reinterpret_cast<uint4*>(smem_gen + (stage(2 * it) - smem) + (c / 8) * T::PANEL + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_proxy_async();
+                __syncwarp();
+            }
+            // the softmax warps have read S(it - 2)
+            if (it >= 2 && !wait_all(s_free + 8 * (it & 1), ((it >> 1) & 1) ^ 1)) return;
+            issue_square((it & 1) ? COL_S1 : COL_S, smem, stage(2 * it), s_full + 8 * (it & 1));
+        };
+        auto issue_dp = [&](int it) {
+            if (!full(2 * it + 1)) return;
+            issue_square(COL_DP, smem + T::TILE, stage(2 * it + 1), dp_full);
+            if (elected) umma1_commit(kv_empty + 8 * ((2 * it + 1) % M::STAGES));
+            __syncwarp();
+        };
+        if (steps > 0 && wait_all(q_full, 0)) {
+            issue_s(0);
+            if (ok && wait_all(d_full, 0)) issue_dp(0);
+            if (ok && steps > 1) issue_s(1);
+        }
+        for (int it = 0; it < steps && ok; ++it) {
+            if (!wait_all(ds_full, it & 1)) break;
+            const uint64_t kd = umma_mn_desc(stage(2 * it), T::PANEL);
+            if (elected) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    umma1_ts(tm + COL_ACC0, tm + COL_DP + (k / 4) * 64 + (k % 4) * 8, kd + k * (2048 >> 4), id_acc, it != 0 || k != 0);
+                umma1_commit(kv_empty + 8 * ((2 * it) % M::STAGES));
+                if (it + 1 == steps) umma1_commit(acc_full);
+            }
+            __syncwarp();
+            if (it + 1 < steps) issue_dp(it + 1);
+            if (ok && it + 2 < steps) issue_s(it + 2);
+        }
+        if (elected) {
+            umma1_commit(drain);
+            mbar_wait_drain(drain, 0, &g_attention_backward_status, p.wait_limit);
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ P, dS and the output
+        const int g = (warp - 4) >> 2, q = warp & 3;
+        const int row = i0 + q * 32 + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
+        const uint32_t td = lane_base + COL_DP + g * 64;
+        const int k_lo = p.key_lo(row), k_hi = p.key_hi(row, keys);
+        const int plain_lo = p.left >= 0 ? (p.key_lo(i0 + B128 - 1) + B128 - 1) / B128 : 0;
+        const int plain_hi = max(p.key_hi(i0, keys), 0) / B128;
+        const int64_t at = ((int64_t)b * p.heads + h) * p.q_pad + row;
+        const float lse2 = __ldg(p.lse2 + at), delta = __ldg(p.delta + at);
+        bool ok = true;
+        for (int it = 0; it < steps; ++it) {
+            const int kt = lo + it;
+            const bool plain = kt >= plain_lo && kt < plain_hi;
+            const int base = kt * B128 + g * 64 - k_lo, width = k_hi - k_lo;
+            const uint32_t ts = lane_base + ((it & 1) ? COL_S1 : COL_S) + g * 64;
+            if (!(ok = wait(s_full + 8 * (it & 1), (it >> 1) & 1, abort_flag, p.wait_limit))) break;
+            tc_fence_after();
+            uint32_t s[64];
+            tmem_ld32(ts, s);
+            tmem_ld32(ts + 32, s + 32);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(s_free + 8 * (it & 1));
+#pragma unroll
+            for (int c = 0; c < 64; ++c) s[c] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c]), p.scale_log2, -lse2)));
+            if (!plain)
+#pragma unroll
+                for (int c = 0; c < 64; ++c)
+                    if (!(base + c >= 0 && base + c < width)) s[c] = 0u;
+            if (!(ok = wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
+            tc_fence_after();
+            uint32_t pk[32];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t d[32];
+                tmem_ld32(td + half * 32, d);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    const uint32_t* pp = s + half * 32 + c;
+                    float x0 = __uint_as_float(pp[0]) * (__uint_as_float(d[c]) - delta), x1 = __uint_as_float(pp[1]) * (__uint_as_float(d[c + 1]) - delta);
+                    if (!plain) { x0 = pp[0] ? x0 : 0.0f; x1 = pp[1] ? x1 : 0.0f; }
+                    pk[half * 16 + c / 2] = pack_bf16x2(x0, x1);
+                }
+            }
+            tmem_st32(td, pk);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_full);
+        }
+        if (ok && steps > 0) {
+            ok = wait(acc_full, 0, abort_flag, p.wait_limit);
+            tc_fence_after();
+        }
+        if (ok && g == 0 && i0 + q * 32 < p.q_len)
+            store_accumulator<DP>(lane_base + COL_ACC0, smem_gen, smem, 0, q, lane, &map_dq, p.scale, steps == 0, i0 + q * 32, h, b);
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 2) { tc_fence_after(); tmem_dealloc1(tmem, 512); }
+}
+
+struct Maps { CUtensorMap q, dout, k, v, dq, dk, dv; };
+
+template <int DP>
+int run(const ue5m3_attention_shape& s, const Maps& m, const AttentionParams& p, cudaStream_t st) {
+    const int64_t k_tiles = (s.k_len + 127) / 128, q_tiles = (s.q_len + 127) / 128;
+    const int64_t ck = k_tiles * s.batch * s.kv_heads, cq = q_tiles * s.batch * s.heads;
+    if (ck > 0x7FFFFFFF || cq > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
+    if (ck > 0) {
+        if (cudaFuncSetAttribute(attention_keys_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, KeySmem<DP>::SIZE) != cudaSuccess) return UE5M3_ERR_CUDA;
+        attention_keys_kernel<DP><<<(unsigned)ck, kThreads, KeySmem<DP>::SIZE, st>>>(m.q, m.dout, m.k, m.v, m.dk, m.dv, p, (int)s.kv_heads);
+        if (cudaGetLastError() != cudaSuccess) return UE5M3_ERR_CUDA;
+    }
+    if (cq > 0) {
+        if (cudaFuncSetAttribute(attention_queries_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, QuerySmem<DP>::SIZE) != cudaSuccess) return UE5M3_ERR_CUDA;
+        attention_queries_kernel<DP><<<(unsigned)cq, kThreads, QuerySmem<DP>::SIZE, st>>>(m.q, m.dout, m.k, m.v, m.dq, p, (int)q_tiles);
+        if (cudaGetLastError() != cudaSuccess) return UE5M3_ERR_CUDA;
+    }
+    return UE5M3_OK;
+}
+
+}  // namespace
+
+int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q, const ue5m3_heads& k,
+                              const ue5m3_heads& v, const ue5m3_heads& o, const float* lse, const ue5m3_heads& dq,
+                              const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace, int num_sms, cudaStream_t st) {
+    (void)num_sms;
+    if (s.batch == 0 || (s.q_len == 0 && s.k_len == 0)) return UE5M3_OK;
+    Maps m;
+    const int64_t B = s.batch, D = s.head_dim;
+    if (s.q_len > 0 && (!make_heads_map(&m.q, q, B, s.q_len, s.heads, D, 128) || !make_heads_map(&m.dout, dout, B, s.q_len, s.heads, D, 128) ||
+                        !make_heads_map(&m.dq, dq, B, s.q_len, s.heads, D, 32)))
+        return UE5M3_ERR_CUDA;
+    if (s.k_len > 0 && (!make_heads_map(&m.k, k, B, s.k_len, s.kv_heads, D, 128) || !make_heads_map(&m.v, v, B, s.k_len, s.kv_heads, D, 128) ||
+                        !make_heads_map(&m.dk, dk, B, s.k_len, s.kv_heads, D, 32) || !make_heads_map(&m.dv, dv, B, s.k_len, s.kv_heads, D, 32)))
+        return UE5M3_ERR_CUDA;
+    if (s.q_len == 0) m.q = m.dout = m.k;                  // an empty side is never read
+    if (s.k_len == 0) m.k = m.v = m.q;
+    AttentionParams p = attention_params(s);
+    if (s.q_len > 0) {
+        RowParams r{};
+        r.o = static_cast<const __nv_bfloat16*>(o.data); r.dout = static_cast<const __nv_bfloat16*>(dout.data);
+        r.o_stride[0] = o.batch_stride; r.o_stride[1] = o.token_stride; r.o_stride[2] = o.head_stride;
+        r.d_stride[0] = dout.batch_stride; r.d_stride[1] = dout.token_stride; r.d_stride[2] = dout.head_stride;
+        r.lse = lse;
+        r.q_len = (int)s.q_len; r.q_pad = p.q_pad; r.heads = (int)s.heads; r.dim = (int)D;
+        r.rows = B * s.heads * p.q_pad;
+        r.lse2 = workspace; r.delta = workspace + r.rows;
+        p.lse2 = r.lse2; p.delta = r.delta;
+        const int64_t grid = (r.rows * 8 + 255) / 256;
+        if (grid > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
+        attention_rows_kernel<<<(unsigned)grid, 256, 0, st>>>(r);
+        if (cudaGetLastError() != cudaSuccess) return UE5M3_ERR_CUDA;
+    }
+    return D <= 64 ? run<64>(s, m, p, st) : run<128>(s, m, p, st);
+}
+
+int read_and_clear_attention_backward_status() {
+    if (cudaDeviceSynchronize() != cudaSuccess) return UE5M3_ERR_CUDA;
+    int v = 0;
+    if (cudaMemcpyFromSymbol(&v, g_attention_backward_status, sizeof(int)) != cudaSuccess) return UE5M3_ERR_CUDA;
+    if (v != 0) {
+        const int zero = 0;
+        if (cudaMemcpyToSymbol(g_attention_backward_status, &zero, sizeof(int)) != cudaSuccess) return UE5M3_ERR_CUDA;
+    }
+    return v;
+}
+
+}  // namespace ue5m3

@@ -1,0 +1,48 @@
+// Host-side launch interface of the operators between the quantized linears (layer norm, dropout, attention).
+#pragma once
+#include <cuda_runtime.h>
+#include <cstdint>
+#include "../../include/ue5m3.h"
+
+namespace ue5m3 {
+
+struct LayerNormArgs {
+    const void* x; int64_t ldx;
+    const void* weight; const void* bias;
+    void* y; int64_t ldy;                 // backward: dx
+    const void* dy; int64_t lddy;         // backward only
+    float* mean; float* rstd;
+    void* dweight; void* dbias;           // backward only
+    float* partial;                       // backward only: [groups][2][cols]
+    int64_t rows, cols;
+    float eps;
+};
+// CTAs of the backward kernel = rows of column sums it leaves in the workspace
+int layer_norm_backward_groups(int64_t rows);
+cudaError_t launch_layer_norm(const LayerNormArgs& a, int dtype, int weight_dtype, int num_sms, cudaStream_t st);
+cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, int dtype, int weight_dtype, int num_sms, cudaStream_t st);
+
+struct DropoutArgs {
+    const void* x; const void* residual; void* y;
+    int64_t ldx, ldr, ldy, rows, cols;
+    uint32_t limit;                       // (t << 16) - 1: a draw in the upper 16 bits of a word keeps its element when above it
+    int drop;                             // 0: t = 0, nothing is dropped and no bits are drawn
+    float inv_keep;                       // 65536 / (65536 - t); 0 when t = 65536
+    uint64_t seed;
+};
+cudaError_t launch_dropout_add(const DropoutArgs& a, int dtype, int num_sms, cudaStream_t st);
+
+// returns a UE5M3_* status
+int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
+                     const ue5m3_heads& o, float* lse, int num_sms, cudaStream_t st);
+int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q,
+                              const ue5m3_heads& k, const ue5m3_heads& v, const ue5m3_heads& o, const float* lse,
+                              const ue5m3_heads& dq, const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace,
+                              int num_sms, cudaStream_t st);
+int read_and_clear_attention_status();            // both synchronise the device
+int read_and_clear_attention_backward_status();
+
+// Queries padded to whole tiles: rows of the backward pass's workspace.
+inline int64_t attention_padded_q(int64_t q_len) { return (q_len + 127) / 128 * 128; }
+
+}  // namespace ue5m3

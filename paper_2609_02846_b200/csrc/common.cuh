@@ -133,13 +133,15 @@ __device__ __forceinline__ void philox4x32(uint32_t c0, uint32_t c1, uint32_t c2
     out[0] = c0; out[1] = c1; out[2] = c2; out[3] = c3;
 }
 
-// The same generator for a counter (c0, 0, 0, 0): the first round has one product (the other factor is zero) and
-// leaves c0' = k[0], so the second round's first product is the launch constant m0k0: three products fewer.
+// The same generator for a counter (c0, 0, C2, 0) with C2 = 0 or 1: the first round has one product (the other one is 0 or
+// the multiplier itself, whose high half is zero) and leaves c0' = k[0], so the second round's first product is the launch
+// constant m0k0: three products fewer.
+template <uint32_t C2 = 0>
 __device__ __forceinline__ void philox4x32_c0(uint32_t c0, const PhiloxKeys& K, uint32_t out[4]) {
     const uint64_t q = (uint64_t)0xD2511F53u * c0;
-    // after round 0: (k[0], 0, hi(q) ^ k[1], lo(q));  round 1:
+    // after round 0: (k[0], C2 * 0xCD9E8D57, hi(q) ^ k[1], lo(q));  round 1:
     const uint64_t p1 = (uint64_t)0xCD9E8D57u * ((uint32_t)(q >> 32) ^ K.k[1]);
-    uint32_t a0 = (uint32_t)(p1 >> 32) ^ K.k[2];
+    uint32_t a0 = (uint32_t)(p1 >> 32) ^ (C2 * 0xCD9E8D57u) ^ K.k[2];
     uint32_t a1 = (uint32_t)p1;
     uint32_t a2 = K.m0k0_hi ^ (uint32_t)q ^ K.k[3];
     uint32_t a3 = K.m0k0_lo;
