@@ -1,4 +1,5 @@
-"""A linear layer whose three GEMMs run through the UE5M3-FP4 library, as a torch.autograd.Function.
+"""The library's calls as torch.autograd.Functions and modules: the linear layer whose three GEMMs run in UE5M3-FP4, and what
+stands between such linears in a transformer block (layer norm, attention, dropout added to the residual).
 
 Nothing is computed here: forward and backward only call `quantize`, `gemm` and `sample_amax` of the C ABI in
 the order the recipe prescribes (X and W rounded to nearest even, the upstream gradient rounded stochastically
@@ -117,3 +118,119 @@ class Ue5m3Linear(torch.nn.Module):
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         return _Ue5m3LinearFn.apply(x, self.weight, self, self.step)
+
+
+# ---------------------------------------------------------------------------------------------
+# Between the linears
+def _as_rows(t: torch.Tensor) -> torch.Tensor:
+    """[.., cols] as a matrix with contiguous rows (a copy only where the strides leave no other way, e.g. an expanded gradient)."""
+    t = t.reshape(-1, t.shape[-1])
+    ok = (t.stride(1) == 1 or t.shape[1] == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])
+    return t if ok else t.contiguous()
+
+
+def _as_heads(t: torch.Tensor) -> torch.Tensor:
+    """[batch, tokens, heads, dim] in a form that the attention calls take (a copy only where the strides or the start do not fit)."""
+    ok = (t.stride(3) == 1 or t.shape[3] == 1) and t.data_ptr() % 16 == 0 and \
+        all(t.shape[i] <= 1 or (t.stride(i) > 0 and t.stride(i) % 8 == 0) for i in range(3))
+    return t if ok else t.clone(memory_format=torch.contiguous_format)
+
+
+class _LayerNormFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        rows = _as_rows(x)
+        y, mean, rstd = B.layer_norm(rows, weight, bias, eps)
+        ctx.save_for_backward(rows, weight, mean, rstd)
+        ctx.shape, ctx.bias_dtype = x.shape, None if bias is None else bias.dtype
+        return y.view(x.shape)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        want_w, want_b = ctx.needs_input_grad[1], ctx.needs_input_grad[2]
+        dx, dw, db = B.layer_norm_backward(_as_rows(dy), x, weight, mean, rstd, want_weight=want_w, want_bias=want_b)
+        return dx.view(ctx.shape), dw, db if db is None else db.to(ctx.bias_dtype), None
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:
+    """Differentiable ue5m3_layer_norm over the last dimension of `x`."""
+    return _LayerNormFn.apply(x, weight, bias, eps)
+
+
+class LayerNorm(torch.nn.Module):
+    """Layer norm over the last dimension with learned weight and (by default) bias; the parameters may have another type than the
+    activations (float32 parameters with bfloat16 activations by default)."""
+
+    def __init__(self, features: int, eps: float = 1e-5, bias: bool = True, device="cuda", dtype=torch.float32):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.ones(features, device=device, dtype=dtype))
+        self.bias = torch.nn.Parameter(torch.zeros(features, device=device, dtype=dtype)) if bias else None
+        self.eps = float(eps)
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        return layer_norm(x, self.weight, self.bias, self.eps)
+
+
+class _DropoutAddFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, seed):
+        ctx.p, ctx.seed = p, seed
+        y = B.dropout_add(_as_rows(x), p, seed, None if residual is None else _as_rows(residual))
+        return y.view(x.shape)
+
+    @staticmethod
+    def backward(ctx, dy):
+        dx = B.dropout_add(_as_rows(dy), ctx.p, ctx.seed).view(dy.shape) if ctx.needs_input_grad[0] else None
+        return dx, dy if ctx.needs_input_grad[1] else None, None, None
+
+
+def dropout_add(x: torch.Tensor, p: float, seed: int, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Differentiable ue5m3_dropout_add: residual + dropout(x); the mask is drawn again from (seed, index) in the backward pass."""
+    return _DropoutAddFn.apply(x, residual, p, seed)
+
+
+class DropoutAdd(torch.nn.Module):
+    """residual + dropout(x) with a draw stream of its own per layer, rank and step (call `advance()` once per optimizer step, as for
+    Ue5m3Linear: within a step the same mask is drawn every time, so a recomputed forward pass meets the same one).  In
+    evaluation mode nothing is dropped."""
+
+    def __init__(self, p: float, seed: Optional[int] = None, group=None):
+        super().__init__()
+        if not 0.0 <= p <= 1.0:
+            raise ValueError(f"p = {p} is no probability")
+        global _layer_counter
+        self.p = float(p)
+        self.seed = _layer_counter if seed is None else int(seed)
+        _layer_counter += 1
+        self.rank = _group_rank(group)
+        self.step = 0
+
+    def advance(self) -> None:
+        self.step += 1
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        return dropout_add(x, self.p if self.training else 0.0, sr_stream_seed(self.seed, self.rank, self.step), residual)
+
+
+class _AttentionFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, causal, window_left, k_lens, scale):
+        q, k, v = (_as_heads(t) for t in (q, k, v))
+        o, lse = B.attention(q, k, v, causal, window_left, k_lens, scale)
+        ctx.save_for_backward(q, k, v, o, lse, k_lens)
+        ctx.args = causal, window_left, scale
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        q, k, v, o, lse, k_lens = ctx.saved_tensors
+        causal, window_left, scale = ctx.args
+        dq, dk, dv = B.attention_backward(_as_heads(do), q, k, v, o, lse, causal, window_left, k_lens, scale)
+        return dq, dk, dv, None, None, None, None
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, window_left: int = -1,
+              k_lens: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
+    """Differentiable ue5m3_attention: o [batch, tokens, heads, head_dim] (arguments as in the binding's `attention`)."""
+    return _AttentionFn.apply(q, k, v, causal, window_left, k_lens, scale)
