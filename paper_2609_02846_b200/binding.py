@@ -438,21 +438,50 @@ def last_device_status() -> int:
 
 
 # ---------------------------------------------------------------------------------------------
-# The operators between the quantized linears.
+# The operators between the quantized linears.  Small calls are bound by what the host does, so these wrappers ask torch for as
+# little as they can: sizes and strides once as tuples, outputs through new_empty, no device switch when the device is current.
+def _call(fn, where: str, x: torch.Tensor, *args) -> None:
+    """fn(*args, stream) on x's device and torch's current stream there."""
+    if not x.is_cuda:
+        raise ValueError("the library takes device tensors only")
+    index = x.get_device()
+    if index == torch.cuda.current_device():
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        raise Ue5m3Error(status, where)
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _differs(t: torch.Tensor, shape, like: torch.Tensor) -> bool:
+    return t.shape != shape or t.dtype != like.dtype or t.get_device() != like.get_device()
+
+
+def _unlike(t: torch.Tensor, shape, like: torch.Tensor) -> ValueError:
+    return ValueError(f"expected a tensor like [{tuple(shape)}, {like.dtype}, {like.device}], got [{tuple(t.shape)}, {t.dtype}, {t.device}]")
+
+
 def _rows(x: torch.Tensor, like: Optional[torch.Tensor] = None):
     """(rows, cols, leading dimension) of a 2-D tensor with contiguous rows; `like`: its shape, type and device are required."""
-    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+    if like is not None and _differs(x, like.shape, like):
+        raise _unlike(x, like.shape, like)
+    if x.dim() != 2:
         raise ValueError("expected a 2-D tensor whose rows are contiguous")
-    if like is not None and (x.shape != like.shape or x.dtype != like.dtype or x.device != like.device):
-        raise ValueError(f"expected a tensor like [{tuple(like.shape)}, {like.dtype}, {like.device}], got [{tuple(x.shape)}, {x.dtype}, {x.device}]")
-    rows, cols = x.shape
-    return rows, cols, x.stride(0) if rows > 1 else cols
+    (rows, cols), (ld, one) = x.shape, x.stride()
+    if one != 1 and cols > 1:
+        raise ValueError("expected a 2-D tensor whose rows are contiguous")
+    return rows, cols, ld if rows > 1 else cols
 
 
-def _vector(t: Optional[torch.Tensor], n: int, device, dtype=None):
-    if t is not None and (t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.device != device or (dtype is not None and t.dtype != dtype)):
-        raise ValueError(f"expected a contiguous vector of {n} values{'' if dtype is None else f' of {dtype}'} on {device}")
-    return t
+def _vector(t: Optional[torch.Tensor], n: int, like: torch.Tensor, dtype=None):
+    if t is not None and (t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.get_device() != like.get_device()
+                          or (dtype is not None and t.dtype != dtype)):
+        raise ValueError(f"expected a contiguous vector of {n} values{'' if dtype is None else f' of {dtype}'} on {like.device}")
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
@@ -461,16 +490,15 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     bfloat16, may be None.  mean and rstd (float32 [rows]) are what `layer_norm_backward` takes."""
     rows, cols, ldx = _rows(x)
     param = weight if weight is not None else bias
-    _vector(weight, cols, x.device)
-    _vector(bias, cols, x.device, None if param is None else param.dtype)
+    _vector(weight, cols, x)
+    _vector(bias, cols, x, None if param is None else param.dtype)
     if out is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    _, _, ldy = _rows(out, x)
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    with torch.cuda.device(x.device):
-        _check(_load().ue5m3_layer_norm(_dev_ptr(x), _dtype_code(x), rows, cols, ldx, _dev_ptr(weight), _dev_ptr(bias),
-                                        F32 if param is None else _dtype_code(param), eps, _dev_ptr(out), ldy, _dev_ptr(mean),
-                                        _dev_ptr(rstd), _stream(x)), "ue5m3_layer_norm")
+        out, ldy = x.new_empty((rows, cols)), cols
+    else:
+        ldy = _rows(out, x)[2]
+    mean, rstd = x.new_empty(rows, dtype=torch.float32), x.new_empty(rows, dtype=torch.float32)
+    _call(_load().ue5m3_layer_norm, "ue5m3_layer_norm", x, x.data_ptr(), _dtype_code(x), rows, cols, ldx, _ptr(weight), _ptr(bias),
+          F32 if param is None else _dtype_code(param), eps, out.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr())
     return out, mean, rstd
 
 
@@ -479,24 +507,23 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
     """ue5m3_layer_norm_backward: (dx, dweight, dbias).  dweight is None without a weight or when not wanted, dbias when not
     wanted; both have the weight's type (x's without a weight)."""
     rows, cols, ldx = _rows(x)
-    _, _, lddy = _rows(dy, x)
-    _vector(weight, cols, x.device)
-    _vector(mean, rows, x.device, torch.float32)
-    _vector(rstd, rows, x.device, torch.float32)
+    lddy = _rows(dy, x)[2]
+    _vector(weight, cols, x)
+    _vector(mean, rows, x, torch.float32)
+    _vector(rstd, rows, x, torch.float32)
     if out is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    _, _, lddx = _rows(out, x)
+        out, lddx = x.new_empty((rows, cols)), cols
+    else:
+        lddx = _rows(out, x)[2]
     param = weight if weight is not None else x
     lib = _load()
-    dw = torch.empty(cols, dtype=param.dtype, device=x.device) if want_weight and weight is not None else None
-    db = torch.empty(cols, dtype=param.dtype, device=x.device) if want_bias else None
+    dw = x.new_empty(cols, dtype=param.dtype) if want_weight and weight is not None else None
+    db = x.new_empty(cols, dtype=param.dtype) if want_bias else None
     ws = None
     if dw is not None or db is not None:
-        ws = torch.empty(lib.ue5m3_layer_norm_backward_workspace_bytes(rows, cols), dtype=torch.uint8, device=x.device)
-    with torch.cuda.device(x.device):
-        _check(lib.ue5m3_layer_norm_backward(_dev_ptr(dy), lddy, _dev_ptr(x), _dtype_code(x), rows, cols, ldx, _dev_ptr(weight),
-                                             _dtype_code(param), _dev_ptr(mean), _dev_ptr(rstd), _dev_ptr(out), lddx, _dev_ptr(dw),
-                                             _dev_ptr(db), _dev_ptr(ws), _stream(x)), "ue5m3_layer_norm_backward")
+        ws = x.new_empty(lib.ue5m3_layer_norm_backward_workspace_bytes(rows, cols), dtype=torch.uint8)
+    _call(lib.ue5m3_layer_norm_backward, "ue5m3_layer_norm_backward", x, dy.data_ptr(), lddy, x.data_ptr(), _dtype_code(x), rows, cols, ldx,
+          _ptr(weight), _dtype_code(param), mean.data_ptr(), rstd.data_ptr(), out.data_ptr(), lddx, _ptr(dw), _ptr(db), _ptr(ws))
     return out, dw, db
 
 
@@ -507,35 +534,34 @@ def dropout_add(x: torch.Tensor, p: float, seed: int, residual: Optional[torch.T
     rows, cols, ldx = _rows(x)
     ldr = 0 if residual is None else _rows(residual, x)[2]
     if out is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    _, _, ldy = _rows(out, x)
-    with torch.cuda.device(x.device):
-        _check(_load().ue5m3_dropout_add(_dev_ptr(x), ldx, _dev_ptr(residual), ldr, _dtype_code(x), rows, cols, p,
-                                         int(seed) & (2 ** 64 - 1), _dev_ptr(out), ldy, _stream(x)), "ue5m3_dropout_add")
+        out, ldy = x.new_empty((rows, cols)), cols
+    else:
+        ldy = _rows(out, x)[2]
+    _call(_load().ue5m3_dropout_add, "ue5m3_dropout_add", x, x.data_ptr(), ldx, _ptr(residual), ldr, _dtype_code(x), rows, cols, p,
+          int(seed) & (2 ** 64 - 1), out.data_ptr(), ldy)
     return out
 
 
-def _heads(t: torch.Tensor, shape: tuple, like: torch.Tensor) -> _Heads:
-    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"expected a tensor like [{tuple(shape)}, {like.dtype}, {like.device}], got [{tuple(t.shape)}, {t.dtype}, {t.device}]")
-    if not t.is_cuda:
-        raise ValueError("the library takes device tensors only")
-    if t.stride(3) != 1 and t.shape[3] > 1:
+def _heads(t: torch.Tensor, shape, like: torch.Tensor) -> _Heads:
+    if _differs(t, shape, like):
+        raise _unlike(t, shape, like)
+    batch, token, head, one = t.stride()
+    if one != 1 and shape[3] > 1:
         raise ValueError("expected tensors [batch, tokens, heads, head_dim] whose last dimension is contiguous")
-    return _Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return _Heads(t.data_ptr(), batch, token, head)
 
 
-def _attention_shape(q, k, v, causal, window_left, k_lens, scale) -> _AttentionShape:
+def _attention_shape(q, k, causal, window_left, k_lens, scale) -> _AttentionShape:
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("expected tensors [batch, tokens, heads, head_dim]")
-    B, Lq, H, D = q.shape
-    if k.shape[0] != B or k.shape[3] != D:
+    (B, Lq, H, D), (Bk, Lk, Hk, Dk) = q.shape, k.shape
+    if Bk != B or Dk != D:
         raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} differ in batch or head dimension")
     if k_lens is not None and (k_lens.dim() != 1 or k_lens.shape[0] != B or k_lens.dtype != torch.int32 or not k_lens.is_contiguous()
-                               or k_lens.device != q.device):
+                               or k_lens.get_device() != q.get_device()):
         raise ValueError("k_lens must be a contiguous int32 tensor with one length per sequence, on the queries' device")
-    return _AttentionShape(B, Lq, k.shape[1], H, k.shape[2], D, int(window_left), None if k_lens is None else k_lens.data_ptr(),
-                           D ** -0.5 if scale is None else float(scale), _dtype_code(q), 1 if causal else 0)
+    return _AttentionShape(B, Lq, Lk, H, Hk, D, int(window_left), _ptr(k_lens), D ** -0.5 if scale is None else float(scale),
+                           _dtype_code(q), 1 if causal else 0)
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, window_left: int = -1,
@@ -543,13 +569,12 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     """ue5m3_attention: (o, lse) for q [batch, tokens, heads, head_dim] and k, v [batch, keys, kv_heads, head_dim], bfloat16.  Any
     strides with a contiguous last dimension (views of a fused projection); `window_left` = keys a query sees before its own
     position (-1: all), `k_lens` int32 [batch] = valid keys of each sequence, `scale` defaults to head_dim ** -0.5."""
-    shape = _attention_shape(q, k, v, causal, window_left, k_lens, scale)
+    shape = _attention_shape(q, k, causal, window_left, k_lens, scale)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty((shape.batch, shape.heads, shape.q_len), dtype=torch.float32, device=q.device)
-    args = [_heads(q, q.shape, q), _heads(k, k.shape, q), _heads(v, k.shape, q), _heads(out, q.shape, q)]
-    with torch.cuda.device(q.device):
-        _check(_load().ue5m3_attention(shape, *args, _dev_ptr(lse), _stream(q)), "ue5m3_attention")
+        out = q.new_empty(q.shape)
+    lse = q.new_empty((shape.batch, shape.heads, shape.q_len), dtype=torch.float32)
+    _call(_load().ue5m3_attention, "ue5m3_attention", q, shape, _heads(q, q.shape, q), _heads(k, k.shape, q), _heads(v, k.shape, q),
+          _heads(out, q.shape, q), lse.data_ptr())
     return out, lse
 
 
@@ -559,18 +584,16 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     """ue5m3_attention_backward: (dq, dk, dv) from what `attention` returned (o, lse) and the gradient of o; the other arguments as
     in that call.  `out`: three tensors to write to (any strides with a contiguous last dimension, e.g. views of one fused
     gradient)."""
-    shape = _attention_shape(q, k, v, causal, window_left, k_lens, scale)
-    if lse.shape != (shape.batch, shape.heads, shape.q_len) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != q.device:
+    shape = _attention_shape(q, k, causal, window_left, k_lens, scale)
+    qs, ks = q.shape, k.shape
+    if lse.shape != (shape.batch, shape.heads, shape.q_len) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != q.get_device():
         raise ValueError("lse must be the contiguous float32 [batch, heads, tokens] tensor that attention returned")
-    if out is None:
-        out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dq, dk, dv = (q.new_empty(qs), k.new_empty(ks), k.new_empty(ks)) if out is None else out
     lib = _load()
-    ws = torch.empty(lib.ue5m3_attention_backward_workspace_bytes(shape), dtype=torch.uint8, device=q.device)
-    ins = [_heads(dout, q.shape, q), _heads(q, q.shape, q), _heads(k, k.shape, q), _heads(v, k.shape, q), _heads(o, q.shape, q)]
-    outs = [_heads(out[0], q.shape, q), _heads(out[1], k.shape, q), _heads(out[2], k.shape, q)]
-    with torch.cuda.device(q.device):
-        _check(lib.ue5m3_attention_backward(shape, *ins, _dev_ptr(lse), *outs, _dev_ptr(ws), _stream(q)), "ue5m3_attention_backward")
-    return tuple(out)
+    ws = q.new_empty(lib.ue5m3_attention_backward_workspace_bytes(shape), dtype=torch.uint8)
+    _call(lib.ue5m3_attention_backward, "ue5m3_attention_backward", q, shape, _heads(dout, qs, q), _heads(q, qs, q), _heads(k, ks, q),
+          _heads(v, ks, q), _heads(o, qs, q), lse.data_ptr(), _heads(dq, qs, q), _heads(dk, ks, q), _heads(dv, ks, q), ws.data_ptr())
+    return dq, dk, dv
 
 
 # ---------------------------------------------------------------------------------------------

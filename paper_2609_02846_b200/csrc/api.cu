@@ -411,7 +411,7 @@ int ue5m3_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int d
     a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
     a.dweight = dweight; a.dbias = dbias; a.partial = sums ? static_cast<float*>(workspace) : nullptr;
     a.rows = rows; a.cols = cols;
-    return launch_layer_norm_backward(a, dtype, weight_dtype, sms, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+    return launch_layer_norm_backward(a, dtype, weight_dtype, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
 int ue5m3_dropout_add(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype, int64_t rows, int64_t cols, float p,
@@ -508,7 +508,8 @@ int ue5m3_last_device_status(void) {
     const int c = read_and_clear_native_status();
     const int d = read_and_clear_attention_status();
     const int e = read_and_clear_attention_backward_status();
-    for (int v : {a, b, c, d, e})
+    const int f = read_and_clear_norm_status();
+    for (int v : {a, b, c, d, e, f})
         if (v != UE5M3_OK) return v;
     return UE5M3_OK;
 }

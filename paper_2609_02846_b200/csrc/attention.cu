@@ -338,7 +338,8 @@ int run(const ue5m3_attention_shape& s, const CUtensorMap& q, const CUtensorMap&
     using T = Tiles<DP>;
     const int64_t q_tiles = (s.q_len + 2 * BQ - 1) / (2 * BQ), ctas = q_tiles * s.batch * s.heads;
     if (ctas > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(attention_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM) != cudaSuccess) return UE5M3_ERR_CUDA;
+    static std::atomic<int> granted[64];
+    if (allow_smem(attention_kernel<DP>, T::SMEM, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
     attention_kernel<DP><<<(unsigned)ctas, kThreads, T::SMEM, st>>>(q, k, v, o, p, (int)q_tiles);
     return cudaGetLastError() == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }

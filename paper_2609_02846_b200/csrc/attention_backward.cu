@@ -596,12 +596,14 @@ int run(const ue5m3_attention_shape& s, const Maps& m, const AttentionParams& p,
     const int64_t ck = k_tiles * s.batch * s.kv_heads, cq = q_tiles * s.batch * s.heads;
     if (ck > 0x7FFFFFFF || cq > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
     if (ck > 0) {
-        if (cudaFuncSetAttribute(attention_keys_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, KeySmem<DP>::SIZE) != cudaSuccess) return UE5M3_ERR_CUDA;
+        static std::atomic<int> granted[64];
+        if (allow_smem(attention_keys_kernel<DP>, KeySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
         attention_keys_kernel<DP><<<(unsigned)ck, kThreads, KeySmem<DP>::SIZE, st>>>(m.q, m.dout, m.k, m.v, m.dk, m.dv, p, (int)s.kv_heads);
         if (cudaGetLastError() != cudaSuccess) return UE5M3_ERR_CUDA;
     }
     if (cq > 0) {
-        if (cudaFuncSetAttribute(attention_queries_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, QuerySmem<DP>::SIZE) != cudaSuccess) return UE5M3_ERR_CUDA;
+        static std::atomic<int> granted[64];
+        if (allow_smem(attention_queries_kernel<DP>, QuerySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
         attention_queries_kernel<DP><<<(unsigned)cq, kThreads, QuerySmem<DP>::SIZE, st>>>(m.q, m.dout, m.k, m.v, m.dq, p, (int)q_tiles);
         if (cudaGetLastError() != cudaSuccess) return UE5M3_ERR_CUDA;
     }

@@ -1,10 +1,24 @@
 // Host-side launch interface of the operators between the quantized linears (layer norm, dropout, attention).
 #pragma once
 #include <cuda_runtime.h>
+#include <atomic>
 #include <cstdint>
 #include "../../include/ue5m3.h"
 
 namespace ue5m3 {
+
+// Raises a kernel's limit of dynamic shared memory once per device (the attribute lasts as long as the device's context, and
+// asking for it again costs as much as half a launch).
+template <typename Kernel>
+inline cudaError_t allow_smem(Kernel* kernel, int bytes, std::atomic<int> (&granted)[64]) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64 && granted[dev].load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev >= 0 && dev < 64) granted[dev].store(bytes, std::memory_order_relaxed);
+    return e;
+}
 
 struct LayerNormArgs {
     const void* x; int64_t ldx;
@@ -20,7 +34,7 @@ struct LayerNormArgs {
 // CTAs of the backward kernel = rows of column sums it leaves in the workspace
 int layer_norm_backward_groups(int64_t rows);
 cudaError_t launch_layer_norm(const LayerNormArgs& a, int dtype, int weight_dtype, int num_sms, cudaStream_t st);
-cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, int dtype, int weight_dtype, int num_sms, cudaStream_t st);
+cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, int dtype, int weight_dtype, cudaStream_t st);
 
 struct DropoutArgs {
     const void* x; const void* residual; void* y;
@@ -39,7 +53,8 @@ int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads&
                               const ue5m3_heads& k, const ue5m3_heads& v, const ue5m3_heads& o, const float* lse,
                               const ue5m3_heads& dq, const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace,
                               int num_sms, cudaStream_t st);
-int read_and_clear_attention_status();            // both synchronise the device
+int read_and_clear_norm_status();                 // these three synchronise the device
+int read_and_clear_attention_status();
 int read_and_clear_attention_backward_status();
 
 // Queries padded to whole tiles: rows of the backward pass's workspace.

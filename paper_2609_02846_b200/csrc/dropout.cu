@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(kThreads) dropout_add_kernel(const DropoutPara
     const int64_t n = a.rows * a.cols, step = (int64_t)gridDim.x * kThreads;
     constexpr int U = LAYOUT == 2 ? 1 : 2;             // groups in flight per thread
     for (int64_t g0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; g0 < p.groups; g0 += U * step) {
-        if (LAYOUT == 2) {
+        if constexpr (LAYOUT == 2) {
             uint32_t w[4] = {};
             if (DROP) draw8<SMALL>(p.keys, (uint64_t)g0, w);
             int64_t row = g0 * 8 / a.cols, col = g0 * 8 - row * a.cols;
@@ -87,8 +87,7 @@ __global__ void __launch_bounds__(kThreads) dropout_add_kernel(const DropoutPara
                     if (++col == a.cols) { col = 0; ++row; }
                 }
             }
-            continue;
-        }
+        } else {
         Group8<T> vx[U], vr[U];
         int64_t ox[U], orr[U], oy[U];
 #pragma unroll
@@ -129,6 +128,7 @@ __global__ void __launch_bounds__(kThreads) dropout_add_kernel(const DropoutPara
                     put(y + i, res ? to_f32(res[i]) + k : k);
                 }
             }
+        }
         }
     }
 }

@@ -6,8 +6,9 @@
 // Both are bound by memory (2 and 3 elements moved per element, 8 and 14 operations).  The kernels are persistent: a group of
 // T threads owns a row at a time, every thread the same 16 columns of each of its rows, so the weights are read once per CTA
 // into registers, the column sums of dw and db stay in registers until the CTA ends, and the row itself stays in registers
-// between the reductions (the variance is that of the centred values: no cancellation for a large mean).  The next row's loads
-// are issued before the current row's reductions, which keeps the memory system busy across the two barriers of a row.
+// between the reductions (the variance is that of the centred values: no cancellation for a large mean).
+// Rows that are 16-byte aligned come through a ring in shared memory, filled by bulk copies several rows ahead: about 100 KB are
+// in flight per SM, which a prefetch in registers cannot hold.  Other rows are prefetched element by element, one row ahead.
 // Column sums leave as one binary32 row per CTA and are added by a second small kernel in a fixed order: no atomics.
 // Rows longer than 16 * 1024 columns take a kernel that re-reads the row instead.
 #include <cuda_bf16.h>
@@ -16,58 +17,81 @@
 #include "../../include/ue5m3.h"
 #include "block_ops.h"
 #include "common.cuh"
+#include "tcgen05.cuh"
 
 namespace ue5m3 {
+
+__device__ int g_norm_status = 0;
+
 namespace {
 
 constexpr int kPerThread = 16;                       // columns a thread holds at most
 constexpr int kMaxRowThreads = 1024;
+constexpr int64_t kRegisterCols = 16384;             // longest row the forward kernels hold in registers (backward: 8192)
 constexpr int kBwdGroups = 148;                      // CTAs of the backward kernel: one per SM of a B200
 
-// VEC consecutive elements of one row as they lie in memory.
-template <typename T, int VEC> struct Raw;
-template <> struct Raw<__nv_bfloat16, 8> { uint4 v; };
-template <> struct Raw<float, 4> { uint4 v; };
-template <> struct Raw<__nv_bfloat16, 1> { unsigned short v; };
-template <> struct Raw<float, 1> { float v; };
+// One element of a row as it lies in memory.
+template <typename T> struct Raw;
+template <> struct Raw<__nv_bfloat16> { unsigned short v; };
+template <> struct Raw<float> { float v; };
 
-__device__ __forceinline__ void load_raw(Raw<__nv_bfloat16, 8>& r, const __nv_bfloat16* p) { r.v = ldg_nc_v4(p); }
-__device__ __forceinline__ void load_raw(Raw<float, 4>& r, const float* p) { r.v = ldg_nc_v4(p); }
-__device__ __forceinline__ void load_raw(Raw<__nv_bfloat16, 1>& r, const __nv_bfloat16* p) { r.v = __ldg(reinterpret_cast<const unsigned short*>(p)); }
-__device__ __forceinline__ void load_raw(Raw<float, 1>& r, const float* p) { r.v = __ldg(p); }
-
-__device__ __forceinline__ void unpack(const Raw<__nv_bfloat16, 8>& r, float* f) { unpack_bf16x8(r.v, f); }
-__device__ __forceinline__ void unpack(const Raw<float, 4>& r, float* f) {
-    f[0] = __uint_as_float(r.v.x); f[1] = __uint_as_float(r.v.y); f[2] = __uint_as_float(r.v.z); f[3] = __uint_as_float(r.v.w);
-}
-__device__ __forceinline__ void unpack(const Raw<__nv_bfloat16, 1>& r, float* f) { f[0] = __uint_as_float((uint32_t)r.v << 16); }
-__device__ __forceinline__ void unpack(const Raw<float, 1>& r, float* f) { f[0] = r.v; }
+__device__ __forceinline__ void load_raw(Raw<__nv_bfloat16>& r, const __nv_bfloat16* p) { r.v = __ldg(reinterpret_cast<const unsigned short*>(p)); }
+__device__ __forceinline__ void load_raw(Raw<float>& r, const float* p) { r.v = __ldg(p); }
+__device__ __forceinline__ float unpack(const Raw<__nv_bfloat16>& r) { return __uint_as_float((uint32_t)r.v << 16); }
+__device__ __forceinline__ float unpack(const Raw<float>& r) { return r.v; }
 
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+__device__ __forceinline__ void store_one(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void store_one(float* p, float v) { *p = v; }
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+// VEC consecutive columns: one element, or 16 bytes
+template <int VEC> __device__ __forceinline__ void load_vec(float* f, const __nv_bfloat16* p) {
+    if constexpr (VEC == 8) unpack_bf16x8(*reinterpret_cast<const uint4*>(p), f);
+    else f[0] = __bfloat162float(*p);
+}
+template <int VEC> __device__ __forceinline__ void load_vec(float* f, const float* p) {
+    if constexpr (VEC == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+    } else {
+        f[0] = *p;
+    }
+}
 template <int VEC> __device__ __forceinline__ void store_vec(__nv_bfloat16* p, const float* f) {
     if constexpr (VEC == 8)
         *reinterpret_cast<uint4*>(p) = make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
-    else
-        *p = __float2bfloat16_rn(f[0]);
+    else *p = __float2bfloat16_rn(f[0]);
 }
 template <int VEC> __device__ __forceinline__ void store_vec(float* p, const float* f) {
     if constexpr (VEC == 4) *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
     else *p = f[0];
 }
-__device__ __forceinline__ float to_f32(float v) { return v; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
-// VEC parameters of type TW (read once per CTA: plain loads of the element type, 4 or 16 bytes wide where the compiler may)
-template <int VEC, typename TW> __device__ __forceinline__ void load_params(const TW* p, float* f) {
+// VEC parameters of type TW (16-byte aligned for VEC > 1)
+template <int VEC> __device__ __forceinline__ void load_params(const float* p, float* f) {
+    if constexpr (VEC > 1) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) f[j] = to_f32(p[j]);
+        for (int j = 0; j < VEC; j += 4) load_vec<4>(f + j, p + j);
+    } else {
+        f[0] = p[0];
+    }
+}
+template <int VEC> __device__ __forceinline__ void load_params(const __nv_bfloat16* p, float* f) {
+    if constexpr (VEC == 4) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        unpack_bf16x2(v.x, f[0], f[1]);
+        unpack_bf16x2(v.y, f[2], f[3]);
+    } else {
+        load_vec<VEC>(f, p);
+    }
 }
 
 // Sums of N values over the T threads of a row group (T a multiple of 32), the same order every time.  `scratch` is this
-// group's [2][32][N] floats; `turn` alternates between the two halves, so one barrier per sum is enough.
+// group's [2][N][32] floats, zero to begin with; `turn` alternates between the two halves, so one barrier per sum is enough.
 template <int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], float* scratch, int& turn, int threads, int barrier_id) {
 #pragma unroll
@@ -77,85 +101,164 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float* scratch, int& tu
     if (threads == 32) return;
     float* s = scratch + turn * 32 * N;
     turn ^= 1;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (lane == 0)
+    if ((threadIdx.x & 31) == 0) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) s[warp * N + k] = v[k];
+        for (int k = 0; k < N; ++k) s[k * 32 + (threadIdx.x >> 5)] = v[k];
+    }
     asm volatile("bar.sync %0, %1;" ::"r"(barrier_id), "r"(threads) : "memory");
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = lane < (threads >> 5) ? s[lane * N + k] : 0.0f;
+    for (int k = 0; k < N; ++k) v[k] = 0.0f;
+#pragma unroll 2
+    for (int w = 0; w < threads >> 5; w += 4) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1)
+        for (int k = 0; k < N; ++k) {
+            const float4 p = *reinterpret_cast<const float4*>(s + k * 32 + w);
+            v[k] += (p.x + p.y) + (p.z + p.w);
+        }
+    }
+}
+// Zeroes the CTA's scratch of `floats` values; the caller's __syncthreads follows.
+__device__ __forceinline__ void zero_scratch(float* scratch, int floats) {
+    for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < floats; i += blockDim.x * blockDim.y) scratch[i] = 0.0f;
+}
+
+// ------------------------------------------------------------------------------------------------ rows through a ring
+// A row group's ring of `slots` entries in shared memory: entry i % slots receives row `first + i * step` of one or two matrices.
+// Thread 0 of the group issues the copies; an entry is refilled once the whole group has read it into registers (behind the
+// barrier of the row's first sum).  Waits are bounded: one that gives up sets the status word and goes on with what is there.
+struct RowRing {
+    uint32_t base, bars, entry_bytes;
+    int slots;
+    int slot = 0;                      // entry of the current row, and its phase
+    uint32_t phase = 0;
+    __device__ __forceinline__ uint32_t entry() const { return base + (uint32_t)slot * entry_bytes; }
+    __device__ __forceinline__ uint32_t bar() const { return bars + 8u * (uint32_t)slot; }
+    __device__ __forceinline__ void wait() const {
+        if (!mbar_try_wait(bar(), phase)) mbar_wait_drain(bar(), phase, &g_norm_status, WAIT_LIMIT_CYCLES);
+    }
+    __device__ __forceinline__ void advance() {
+        if (++slot == slots) { slot = 0; phase ^= 1; }
+    }
+};
+// 16 bytes of a row (4 or 8 values) as pairs of binary32 values
+__device__ __forceinline__ void lds_pairs(f32x2 (&f)[4], uint32_t addr, const __nv_bfloat16*) {
+    uint32_t a, b, c, d;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr));
+    f[0] = f2_from_bf16x2(a); f[1] = f2_from_bf16x2(b); f[2] = f2_from_bf16x2(c); f[3] = f2_from_bf16x2(d);
+}
+__device__ __forceinline__ void lds_pairs(f32x2 (&f)[2], uint32_t addr, const float*) {
+    asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(f[0]), "=l"(f[1]) : "r"(addr));
+}
+__device__ __forceinline__ void stg_pairs(__nv_bfloat16* p, const f32x2 (&f)[4]) {
+    uint32_t o[4];
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+    for (int j = 0; j < 4; ++j) {
+        float lo, hi;
+        f2_unpack(f[j], lo, hi);
+        o[j] = bf16_pair(lo, hi);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+__device__ __forceinline__ void stg_pairs(float* p, const f32x2 (&f)[2]) { *reinterpret_cast<ulonglong2*>(p) = make_ulonglong2(f[0], f[1]); }
+__device__ __forceinline__ float f2_total(f32x2 v) {
+    float lo, hi;
+    f2_unpack(v, lo, hi);
+    return lo + hi;
 }
 
 // ------------------------------------------------------------------------------------------------ forward
-// blockDim = (T, R): R groups of T threads, a row each.  NV vectors of VEC columns per thread.  MAXT bounds the CTA: with up to
-// 512 threads there are registers for the weights; the 1024-thread CTA of rows over 8192 columns reads them per row (from L1).
-template <typename TX, typename TW, int VEC, int NV, int MAXT>
-__global__ void __launch_bounds__(MAXT)
-layer_norm_kernel(const LayerNormArgs a) {
-    constexpr bool KEEP = MAXT <= 512;
-    extern __shared__ float scratch_all[];
-    float* scratch = scratch_all + threadIdx.y * 64;
-    const int T = blockDim.x, bar_id = 1 + threadIdx.y;
+// blockDim = (T, R): R groups of T threads, a row each, NV 16-byte vectors per thread: 32 columns from 2048 columns on, 16 below.
+// What a row costs besides its columns (two sums through shuffles and a barrier, ~150 instructions per warp) made 16 columns per
+// thread issue-bound: 30.6 us at 8192 x 4096 BF16 against 24.7 us with 32.  FULL: the columns fill the group's threads exactly, so
+// nothing is conditional (a fifth of the instructions of a row go).
+template <typename TX, typename TW, int NV, bool FULL>
+__global__ void __launch_bounds__(512)
+layer_norm_ring_kernel(const LayerNormArgs a, const int slots) {
+    constexpr int VEC = 16 / sizeof(TX), PAIRS = VEC / 2;
+    extern __shared__ __align__(16) uint8_t ring_smem[];
+    const int T = blockDim.x, R = blockDim.y, bar_id = 1 + threadIdx.y;
+    const uint32_t row_bytes = (uint32_t)a.cols * sizeof(TX), smem = smem_u32(ring_smem);
+    // [R][64] scratch, [R][slots] rows, [R][slots] barriers
+    float* scratch = reinterpret_cast<float*>(ring_smem) + threadIdx.y * 64;
+    RowRing ring{smem + R * 256 + threadIdx.y * slots * row_bytes, smem + R * 256 + R * slots * row_bytes + threadIdx.y * slots * 8, row_bytes, slots};
     const int nvec = (int)(a.cols / VEC);
+    auto mine = [&](int k) { return FULL || threadIdx.x + k * T < nvec; };
+    const int64_t step = (int64_t)gridDim.x * R, first = (int64_t)blockIdx.x * R + threadIdx.y;
     const TX* x = static_cast<const TX*>(a.x);
-    TX* y = static_cast<TX*>(a.y);
-    auto params = [&](int vi, float* w, float* b) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) { w[j] = 1.0f; b[j] = 0.0f; }
-        if (vi < nvec) {
-            if (a.weight) load_params<VEC>(static_cast<const TW*>(a.weight) + (int64_t)vi * VEC, w);
-            if (a.bias) load_params<VEC>(static_cast<const TW*>(a.bias) + (int64_t)vi * VEC, b);
+    const TX* src = x + first * a.ldx;                     // the next row to be copied
+    int64_t next = first;
+    auto fill = [&](uint32_t entry, uint32_t bar) {
+        if (next < a.rows) {
+            mbar_expect_tx(bar, row_bytes);
+            bulk_load(entry, src, row_bytes, bar);
         }
+        next += step;
+        src += step * a.ldx;
     };
-    float w[KEEP ? NV : 1][VEC], b[KEEP ? NV : 1][VEC];
-    if constexpr (KEEP)
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < slots; ++i) mbar_init(ring.bars + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+        for (int i = 0; i < slots; ++i) fill(ring.base + i * row_bytes, ring.bars + 8 * i);
+    }
+    f32x2 w[NV][PAIRS], b[NV][PAIRS];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) params(threadIdx.x + k * T, w[k], b[k]);
+    for (int k = 0; k < NV; ++k) {
+        float t[VEC], u[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) { t[j] = 1.0f; u[j] = 0.0f; }
+        if (mine(k)) {
+            if (a.weight) load_params<VEC>(static_cast<const TW*>(a.weight) + (int64_t)(threadIdx.x + k * T) * VEC, t);
+            if (a.bias) load_params<VEC>(static_cast<const TW*>(a.bias) + (int64_t)(threadIdx.x + k * T) * VEC, u);
+        }
+#pragma unroll
+        for (int j = 0; j < PAIRS; ++j) { w[k][j] = f2_pack(t[2 * j], t[2 * j + 1]); b[k][j] = f2_pack(u[2 * j], u[2 * j + 1]); }
+    }
+    zero_scratch(reinterpret_cast<float*>(ring_smem), R * 64);
+    __syncthreads();                                       // the barriers and the scratch exist
     const float inv_n = 1.0f / (float)a.cols;
-    const int64_t step = (int64_t)gridDim.x * blockDim.y;
-    int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    Raw<TX, VEC> next[NV] = {};
-    if (row < a.rows)
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (threadIdx.x + k * T < nvec) load_raw(next[k], x + row * a.ldx + (int64_t)(threadIdx.x + k * T) * VEC);
     int turn = 0;
-    for (; row < a.rows; row += step) {
-        float f[NV][VEC];
+    TX* dst = static_cast<TX*>(a.y) + first * a.ldy + threadIdx.x * VEC;
+    for (int64_t row = first; row < a.rows; row += step, dst += step * a.ldy) {
+        f32x2 f[NV][PAIRS], acc = 0;
+        ring.wait();
 #pragma unroll
-        for (int k = 0; k < NV; ++k) unpack(next[k], f[k]);
-        if (row + step < a.rows)
+        for (int k = 0; k < NV; ++k) {
+            if constexpr (!FULL) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (threadIdx.x + k * T < nvec) load_raw(next[k], x + (row + step) * a.ldx + (int64_t)(threadIdx.x + k * T) * VEC);
-        float s[1] = {0.0f};
+                for (int j = 0; j < PAIRS; ++j) f[k][j] = 0;
+            }
+            if (mine(k)) lds_pairs(f[k], ring.entry() + (threadIdx.x + k * T) * 16, x);
+        }
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) s[0] += f[k][j];               // columns beyond the row hold zeros
+            for (int j = 0; j < PAIRS; ++j) acc = f2_add(acc, f[k][j]);   // columns beyond the row hold zeros
+        float s[1] = {f2_total(acc)};
         group_sum<1>(s, scratch, turn, T, bar_id);
+        __syncwarp();
+        if (threadIdx.x == 0) fill(ring.entry(), ring.bar());
+        ring.advance();
         const float mean = s[0] * inv_n;
-        float q[1] = {0.0f};
+        const f32x2 minus = f2_pack(-mean, -mean);
+        acc = 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (threadIdx.x + k * T < nvec)
+            if (mine(k)) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) { f[k][j] -= mean; q[0] = fmaf(f[k][j], f[k][j], q[0]); }
-        group_sum<1>(q, scratch, turn, T, bar_id);
-        const float rstd = 1.0f / sqrtf(fmaf(q[0], inv_n, a.eps));
+                for (int j = 0; j < PAIRS; ++j) { f[k][j] = f2_add(f[k][j], minus); acc = f2_fma(f[k][j], f[k][j], acc); }
+            }
+        s[0] = f2_total(acc);
+        group_sum<1>(s, scratch, turn, T, bar_id);
+        const float rstd = rsqrtf(fmaf(s[0], inv_n, a.eps));
+        const f32x2 rr = f2_pack(rstd, rstd);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (threadIdx.x + k * T < nvec) {
-                constexpr int one = KEEP ? 1 : 0;
-                if constexpr (!KEEP) params(threadIdx.x + k * T, w[0], b[0]);
-                float o[VEC];
+            if (mine(k)) {
+                f32x2 o[PAIRS];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) o[j] = fmaf(f[k][j] * rstd, w[k * one][j], b[k * one][j]);
-                store_vec<VEC>(y + row * a.ldy + (int64_t)(threadIdx.x + k * T) * VEC, o);
+                for (int j = 0; j < PAIRS; ++j) o[j] = f2_fma(f2_mul(f[k][j], rr), w[k][j], b[k][j]);
+                stg_pairs(dst + (int64_t)k * T * VEC, o);
             }
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -164,28 +267,106 @@ layer_norm_kernel(const LayerNormArgs a) {
     }
 }
 
-// Rows of any length: the row is read three times (from L1/L2 after the first).
-template <typename TX, typename TW>
-__global__ void __launch_bounds__(kMaxRowThreads) layer_norm_long_kernel(const LayerNormArgs a) {
-    __shared__ float scratch[64];
+// Rows without 16-byte alignment: NV single columns per thread, prefetched one row ahead; otherwise as above.
+template <typename TX, typename TW, int NV, int MAXT>
+__global__ void __launch_bounds__(MAXT)
+layer_norm_kernel(const LayerNormArgs a) {
+    constexpr bool KEEP = MAXT <= 512;
+    extern __shared__ __align__(16) float scratch_all[];
+    float* scratch = scratch_all + threadIdx.y * 64;
+    zero_scratch(scratch_all, blockDim.y * 64);
+    __syncthreads();
+    const int T = blockDim.x, bar_id = 1 + threadIdx.y, n = (int)a.cols;
+    const TX* x = static_cast<const TX*>(a.x);
+    TX* y = static_cast<TX*>(a.y);
+    auto weight = [&](int c) { return a.weight ? to_f32(static_cast<const TW*>(a.weight)[c]) : 1.0f; };
+    auto bias = [&](int c) { return a.bias ? to_f32(static_cast<const TW*>(a.bias)[c]) : 0.0f; };
+    float w[KEEP ? NV : 1], b[KEEP ? NV : 1];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = threadIdx.x + k * T;
+            w[k] = c < n ? weight(c) : 0.0f;
+            b[k] = c < n ? bias(c) : 0.0f;
+        }
+    }
     const float inv_n = 1.0f / (float)a.cols;
+    const int64_t step = (int64_t)gridDim.x * blockDim.y, first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    Raw<TX> next[NV] = {};
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (threadIdx.x + k * T < n) load_raw(next[k], x + r * a.ldx + threadIdx.x + k * T);
+    };
+    if (first < a.rows) fetch(first);
+    int turn = 0;
+    for (int64_t row = first; row < a.rows; row += step) {
+        float f[NV], s[1] = {0.0f};
+#pragma unroll
+        for (int k = 0; k < NV; ++k) { f[k] = unpack(next[k]); s[0] += f[k]; }      // columns beyond the row hold zeros
+        if (row + step < a.rows) fetch(row + step);
+        group_sum<1>(s, scratch, turn, T, bar_id);
+        const float mean = s[0] * inv_n;
+        s[0] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (threadIdx.x + k * T < n) { f[k] -= mean; s[0] = fmaf(f[k], f[k], s[0]); }
+        group_sum<1>(s, scratch, turn, T, bar_id);
+        const float rstd = rsqrtf(fmaf(s[0], inv_n, a.eps));
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = threadIdx.x + k * T;
+            if (c < n) store_one(y + row * a.ldy + c, fmaf(f[k] * rstd, KEEP ? w[KEEP ? k : 0] : weight(c), KEEP ? b[KEEP ? k : 0] : bias(c)));
+        }
+        if (threadIdx.x == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+    }
+}
+
+// Rows of any length: the row is read three times (from L1/L2 after the first), VEC columns per access.
+template <typename TX, typename TW, int VEC>
+__global__ void __launch_bounds__(kMaxRowThreads) layer_norm_long_kernel(const LayerNormArgs a) {
+    __shared__ __align__(16) float scratch[64];
+    zero_scratch(scratch, 64);
+    __syncthreads();
+    const float inv_n = 1.0f / (float)a.cols;
+    const int64_t stride = (int64_t)blockDim.x * VEC, c0 = (int64_t)threadIdx.x * VEC;
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const TX* x = static_cast<const TX*>(a.x) + row * a.ldx;
         TX* y = static_cast<TX*>(a.y) + row * a.ldy;
         float s[1] = {0.0f};
-        for (int64_t c = threadIdx.x; c < a.cols; c += blockDim.x) s[0] += to_f32(x[c]);
+#pragma unroll 2
+        for (int64_t c = c0; c < a.cols; c += stride) {
+            float f[VEC];
+            load_vec<VEC>(f, x + c);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) s[0] += f[j];
+        }
         group_sum<1>(s, scratch, turn, blockDim.x, 1);
         const float mean = s[0] * inv_n;
-        float q[1] = {0.0f};
-        for (int64_t c = threadIdx.x; c < a.cols; c += blockDim.x) { const float d = to_f32(x[c]) - mean; q[0] = fmaf(d, d, q[0]); }
-        group_sum<1>(q, scratch, turn, blockDim.x, 1);
-        const float rstd = 1.0f / sqrtf(fmaf(q[0], inv_n, a.eps));
-        for (int64_t c = threadIdx.x; c < a.cols; c += blockDim.x) {
-            const float w = a.weight ? to_f32(static_cast<const TW*>(a.weight)[c]) : 1.0f;
-            const float b = a.bias ? to_f32(static_cast<const TW*>(a.bias)[c]) : 0.0f;
-            const float o = fmaf((to_f32(x[c]) - mean) * rstd, w, b);
-            store_vec<1>(y + c, &o);
+        s[0] = 0.0f;
+#pragma unroll 2
+        for (int64_t c = c0; c < a.cols; c += stride) {
+            float f[VEC];
+            load_vec<VEC>(f, x + c);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) s[0] = fmaf(f[j] - mean, f[j] - mean, s[0]);
+        }
+        group_sum<1>(s, scratch, turn, blockDim.x, 1);
+        const float rstd = rsqrtf(fmaf(s[0], inv_n, a.eps));
+        for (int64_t c = c0; c < a.cols; c += stride) {
+            float f[VEC], w[VEC], b[VEC];
+            load_vec<VEC>(f, x + c);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) { w[j] = 1.0f; b[j] = 0.0f; }
+            if (a.weight) load_params<VEC>(static_cast<const TW*>(a.weight) + c, w);
+            if (a.bias) load_params<VEC>(static_cast<const TW*>(a.bias) + c, b);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f[j] = fmaf((f[j] - mean) * rstd, w[j], b[j]);
+            store_vec<VEC>(y + c, f);
         }
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -195,145 +376,275 @@ __global__ void __launch_bounds__(kMaxRowThreads) layer_norm_long_kernel(const L
 }
 
 // ------------------------------------------------------------------------------------------------ backward
-template <typename TX, typename TW, int VEC, int NV>
-__global__ void __launch_bounds__(512)
-layer_norm_backward_kernel(const LayerNormArgs a) {
-    extern __shared__ float smem[];                       // [R][128] reduction scratch, then [R][2][T * NV * VEC] column sums
-    asm volatile("griddepcontrol.launch_dependents;");    // the adding kernel may take its place; it waits for this grid's end
-    float* scratch = smem + threadIdx.y * 128;
-    const int T = blockDim.x, R = blockDim.y, bar_id = 1 + threadIdx.y;
-    const int nvec = (int)(a.cols / VEC);
-    const TX* x = static_cast<const TX*>(a.x);
-    const TX* dy = static_cast<const TX*>(a.dy);
-    TX* dx = static_cast<TX*>(a.y);
-    float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
+// The R groups' column sums, added in order by the first group, to this CTA's row of the workspace.  `get(which, k, j)` is this
+// thread's sum of column (thread + k T) VEC + j; `sums` has room for [R - 1][2][T * NV * VEC] values.
+template <int VEC, int NV, typename Get>
+__device__ __forceinline__ void leave_columns(const LayerNormArgs& a, float* sums, int nvec, Get get) {
+    const int T = blockDim.x, R = blockDim.y, per_group = T * NV * VEC;
+    __syncthreads();
+    if (threadIdx.y > 0) {
+        float* mine = sums + (threadIdx.y - 1) * 2 * per_group + threadIdx.x;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int vi = threadIdx.x + k * T;
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) { w[k][j] = 1.0f; dw[k][j] = 0.0f; db[k][j] = 0.0f; }
-        if (a.weight && vi < nvec) load_params<VEC>(static_cast<const TW*>(a.weight) + (int64_t)vi * VEC, w[k]);
+            for (int j = 0; j < VEC; ++j) {
+                // [.. ][k][j][thread]: a warp's stores fall into 32 different banks
+                mine[(k * VEC + j) * T] = get(0, k, j);
+                mine[per_group + (k * VEC + j) * T] = get(1, k, j);
+            }
     }
-    const float inv_n = 1.0f / (float)a.cols;
-    const int64_t step = (int64_t)gridDim.x * R;
-    int64_t row = (int64_t)blockIdx.x * R + threadIdx.y;
-    Raw<TX, VEC> nx[NV] = {}, ny[NV] = {};
-    float next_mean = 0.0f, next_rstd = 0.0f;
-    auto fetch = [&](int64_t r) {
+    __syncthreads();
+    if (threadIdx.y > 0) return;
+    float* out = a.partial + (int64_t)blockIdx.x * 2 * a.cols;
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int vi = threadIdx.x + k * T;
-            if (vi < nvec) {
-                load_raw(nx[k], x + r * a.ldx + (int64_t)vi * VEC);
-                load_raw(ny[k], dy + r * a.lddy + (int64_t)vi * VEC);
+            if (vi >= nvec) continue;
+            float v[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                v[j] = get(which, k, j);
+                for (int r = 0; r < R - 1; ++r) v[j] += sums[(r * 2 + which) * per_group + (k * VEC + j) * T + threadIdx.x];
+            }
+            float* p = out + which * a.cols + (int64_t)vi * VEC;
+            if constexpr (VEC % 4 == 0) {
+#pragma unroll
+                for (int j = 0; j < VEC; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            } else {
+                *p = v[0];
             }
         }
+}
+
+// Rows of x and dy come through the ring (an entry holds both).  Dynamic shared memory: [R][128] reduction scratch, [R][slots]
+// barriers, [R][slots][2] rows; at the end the column sums over them.
+template <typename TX, typename TW, int NV, bool FULL>
+__global__ void __launch_bounds__(512)
+layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
+    constexpr int VEC = 16 / sizeof(TX), PAIRS = VEC / 2;
+    extern __shared__ __align__(16) float smem[];
+    asm volatile("griddepcontrol.launch_dependents;");    // the adding kernel may take its place; it waits for this grid's end
+    const int T = blockDim.x, R = blockDim.y, bar_id = 1 + threadIdx.y;
+    float* scratch = smem + threadIdx.y * 128;
+    const int nvec = (int)(a.cols / VEC);
+    auto mine = [&](int k) { return FULL || threadIdx.x + k * T < nvec; };
+    const uint32_t row_bytes = (uint32_t)a.cols * sizeof(TX), bars = smem_u32(smem + R * 128), rows0 = (bars + R * slots * 8 + 15u) & ~15u;
+    RowRing ring{rows0 + threadIdx.y * slots * 2 * row_bytes, bars + threadIdx.y * slots * 8, 2 * row_bytes, slots};
+    const int64_t step = (int64_t)gridDim.x * R, first = (int64_t)blockIdx.x * R + threadIdx.y;
+    const TX* x = static_cast<const TX*>(a.x);
+    const TX* src_x = x + first * a.ldx;                  // the next row to be copied
+    const TX* src_dy = static_cast<const TX*>(a.dy) + first * a.lddy;
+    int64_t next = first;
+    auto fill = [&](uint32_t entry, uint32_t bar) {
+        if (next < a.rows) {
+            mbar_expect_tx(bar, 2 * row_bytes);
+            bulk_load(entry, src_x, row_bytes, bar);
+            bulk_load(entry + row_bytes, src_dy, row_bytes, bar);
+        }
+        next += step;
+        src_x += step * a.ldx;
+        src_dy += step * a.lddy;
+    };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < slots; ++i) mbar_init(ring.bars + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+        for (int i = 0; i < slots; ++i) fill(ring.base + i * 2 * row_bytes, ring.bars + 8 * i);
+    }
+    f32x2 w[NV][PAIRS], dw[NV][PAIRS], db[NV][PAIRS];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int vi = threadIdx.x + k * T;
+        float t[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) t[j] = 1.0f;
+        if (a.weight && mine(k)) load_params<VEC>(static_cast<const TW*>(a.weight) + (int64_t)vi * VEC, t);
+#pragma unroll
+        for (int j = 0; j < PAIRS; ++j) { w[k][j] = f2_pack(t[2 * j], t[2 * j + 1]); dw[k][j] = 0; db[k][j] = 0; }
+    }
+    zero_scratch(smem, R * 128);
+    __syncthreads();                                       // the barriers and the scratch exist
+    const float inv_n = 1.0f / (float)a.cols;
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    if (first < a.rows) { next_mean = __ldg(a.mean + first); next_rstd = __ldg(a.rstd + first); }
+    int turn = 0;
+    TX* dst = static_cast<TX*>(a.y) + first * a.ldy + threadIdx.x * VEC;
+    for (int64_t row = first; row < a.rows; row += step, dst += step * a.ldy) {
+        const float mean = next_mean, rstd = next_rstd;
+        if (row + step < a.rows) { next_mean = __ldg(a.mean + row + step); next_rstd = __ldg(a.rstd + row + step); }
+        const f32x2 minus = f2_pack(-mean, -mean), rr = f2_pack(rstd, rstd);
+        f32x2 xh[NV][PAIRS], g[NV][PAIRS], sg = 0, sgx = 0;
+        ring.wait();
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (mine(k)) {
+                lds_pairs(xh[k], ring.entry() + (threadIdx.x + k * T) * 16, x);
+                lds_pairs(g[k], ring.entry() + row_bytes + (threadIdx.x + k * T) * 16, x);
+#pragma unroll
+                for (int j = 0; j < PAIRS; ++j) {
+                    xh[k][j] = f2_mul(f2_add(xh[k][j], minus), rr);
+                    dw[k][j] = f2_fma(g[k][j], xh[k][j], dw[k][j]);
+                    db[k][j] = f2_add(db[k][j], g[k][j]);
+                    g[k][j] = f2_mul(g[k][j], w[k][j]);
+                    sg = f2_add(sg, g[k][j]);
+                    sgx = f2_fma(g[k][j], xh[k][j], sgx);
+                }
+            }
+        float s[2] = {f2_total(sg), f2_total(sgx)};
+        group_sum<2>(s, scratch, turn, T, bar_id);
+        __syncwarp();
+        if (threadIdx.x == 0) fill(ring.entry(), ring.bar());
+        ring.advance();
+        // dx = g rstd - xh (mean(g xh) rstd) - mean(g) rstd
+        const float mg = -s[0] * inv_n * rstd, mgx = -s[1] * inv_n * rstd;
+        const f32x2 mg2 = f2_pack(mg, mg), mgx2 = f2_pack(mgx, mgx);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (mine(k)) {
+                f32x2 o[PAIRS];
+#pragma unroll
+                for (int j = 0; j < PAIRS; ++j) o[j] = f2_fma(g[k][j], rr, f2_fma(xh[k][j], mgx2, mg2));
+                stg_pairs(dst + (int64_t)k * T * VEC, o);
+            }
+    }
+    if (!a.partial) return;
+    // every copy has been waited for: the rings' memory is free once all groups are here
+    leave_columns<VEC, NV>(a, smem + R * 128, nvec, [&](int which, int k, int j) {
+        float lo, hi;
+        f2_unpack(which ? db[k][j / 2] : dw[k][j / 2], lo, hi);
+        return (j & 1) ? hi : lo;
+    });
+}
+
+// Rows without 16-byte alignment: single columns, prefetched one row ahead.
+template <typename TX, typename TW, int NV>
+__global__ void __launch_bounds__(512)
+layer_norm_backward_kernel(const LayerNormArgs a) {
+    extern __shared__ __align__(16) float smem[];          // [R][128] reduction scratch, then the column sums
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int T = blockDim.x, R = blockDim.y, bar_id = 1 + threadIdx.y, n = (int)a.cols;
+    float* scratch = smem + threadIdx.y * 128;
+    zero_scratch(smem, R * 128);
+    __syncthreads();
+    const TX* x = static_cast<const TX*>(a.x);
+    const TX* dy = static_cast<const TX*>(a.dy);
+    TX* dx = static_cast<TX*>(a.y);
+    float w[NV], dw[NV], db[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = threadIdx.x + k * T;
+        w[k] = a.weight && c < n ? to_f32(static_cast<const TW*>(a.weight)[c]) : 1.0f;
+        dw[k] = db[k] = 0.0f;
+    }
+    const float inv_n = 1.0f / (float)a.cols;
+    const int64_t step = (int64_t)gridDim.x * R, first = (int64_t)blockIdx.x * R + threadIdx.y;
+    Raw<TX> nx[NV] = {}, ny[NV] = {};
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (threadIdx.x + k * T < n) {
+                load_raw(nx[k], x + r * a.ldx + threadIdx.x + k * T);
+                load_raw(ny[k], dy + r * a.lddy + threadIdx.x + k * T);
+            }
         next_mean = __ldg(a.mean + r);
         next_rstd = __ldg(a.rstd + r);
     };
-    if (row < a.rows) fetch(row);
+    if (first < a.rows) fetch(first);
     int turn = 0;
-    for (; row < a.rows; row += step) {
-        float xh[NV][VEC], g[NV][VEC];
+    for (int64_t row = first; row < a.rows; row += step) {
+        float xh[NV], g[NV], s[2] = {0.0f, 0.0f};
         const float mean = next_mean, rstd = next_rstd;
-        float s[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            unpack(nx[k], xh[k]);
-            unpack(ny[k], g[k]);
-            if (threadIdx.x + k * T < nvec)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    xh[k][j] = (xh[k][j] - mean) * rstd;
-                    dw[k][j] = fmaf(g[k][j], xh[k][j], dw[k][j]);
-                    db[k][j] += g[k][j];
-                    g[k][j] *= w[k][j];
-                    s[0] += g[k][j];
-                    s[1] = fmaf(g[k][j], xh[k][j], s[1]);
-                }
+            xh[k] = unpack(nx[k]);
+            g[k] = unpack(ny[k]);
+            if (threadIdx.x + k * T < n) {
+                xh[k] = (xh[k] - mean) * rstd;
+                dw[k] = fmaf(g[k], xh[k], dw[k]);
+                db[k] += g[k];
+                g[k] *= w[k];
+                s[0] += g[k];
+                s[1] = fmaf(g[k], xh[k], s[1]);
+            }
         }
         if (row + step < a.rows) fetch(row + step);
         group_sum<2>(s, scratch, turn, T, bar_id);
         const float mg = s[0] * inv_n, mgx = s[1] * inv_n;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (threadIdx.x + k * T < nvec) {
-                float o[VEC];
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) o[j] = rstd * (g[k][j] - mg - xh[k][j] * mgx);
-                store_vec<VEC>(dx + row * a.ldy + (int64_t)(threadIdx.x + k * T) * VEC, o);
+            if (threadIdx.x + k * T < n) {
+                store_one(dx + row * a.ldy + threadIdx.x + k * T, rstd * (g[k] - mg - xh[k] * mgx));
             }
     }
-    if (!a.partial) return;
-    // the R groups' column sums, added in order by the first group
-    const int per_group = T * NV * VEC;
-    float* sums = smem + R * 128;
-    if (threadIdx.y > 0)
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                // [.. ][k][j][thread]: a warp's stores fall into 32 different banks
-                sums[(threadIdx.y - 1) * 2 * per_group + (k * VEC + j) * T + threadIdx.x] = dw[k][j];
-                sums[(threadIdx.y - 1) * 2 * per_group + per_group + (k * VEC + j) * T + threadIdx.x] = db[k][j];
-            }
-    __syncthreads();
-    if (threadIdx.y > 0) return;
-    float* out = a.partial + (int64_t)blockIdx.x * 2 * a.cols;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int vi = threadIdx.x + k * T;
-        if (vi >= nvec) continue;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-            for (int r = 0; r < R - 1; ++r) {
-                dw[k][j] += sums[r * 2 * per_group + (k * VEC + j) * T + threadIdx.x];
-                db[k][j] += sums[r * 2 * per_group + per_group + (k * VEC + j) * T + threadIdx.x];
-            }
-        if constexpr (VEC % 4 == 0) {
-#pragma unroll
-            for (int j = 0; j < VEC; j += 4) {
-                *reinterpret_cast<float4*>(out + (int64_t)vi * VEC + j) = make_float4(dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]);
-                *reinterpret_cast<float4*>(out + a.cols + (int64_t)vi * VEC + j) = make_float4(db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]);
-            }
-        } else {
-            out[vi] = dw[k][0];
-            out[a.cols + vi] = db[k][0];
-        }
-    }
+    if (a.partial) leave_columns<1, NV>(a, smem + R * 128, n, [&](int which, int k, int) { return which ? db[k] : dw[k]; });
 }
 
-// Rows of any length: column sums are kept in this CTA's row of the workspace.
-template <typename TX, typename TW>
-__global__ void __launch_bounds__(kMaxRowThreads) layer_norm_backward_long_kernel(const LayerNormArgs a) {
-    __shared__ float scratch[128];
+// Rows of any length (over 8192 columns), one row per CTA at a time: x and dy are read twice, the second time from the caches.
+// The column sums stay in shared memory up to 24576 columns, beyond that in this CTA's row of the workspace; a thread always
+// has the same columns, so they need no order between threads.  VEC columns per access (1 where rows are not 16-byte aligned).
+template <typename TX, typename TW, int VEC>
+__global__ void __launch_bounds__(kMaxRowThreads) layer_norm_backward_long_kernel(const LayerNormArgs a, const int sums_in_smem) {
+    extern __shared__ __align__(16) float smem[];          // [128] reduction scratch, [2][cols] sums
     asm volatile("griddepcontrol.launch_dependents;");
+    zero_scratch(smem, 128);
     const float inv_n = 1.0f / (float)a.cols;
     float* out = a.partial ? a.partial + (int64_t)blockIdx.x * 2 * a.cols : nullptr;
-    if (out)
-        for (int64_t c = threadIdx.x; c < a.cols; c += blockDim.x) { out[c] = 0.0f; out[a.cols + c] = 0.0f; }   // own columns only
+    const int64_t stride = (int64_t)blockDim.x * VEC, c0 = (int64_t)threadIdx.x * VEC;
+    // where the sums of column c + j are: in shared memory a warp's threads side by side (no bank conflicts), else in order
+    float* sums = sums_in_smem ? smem + 128 : out;
+    const int64_t half = sums_in_smem ? (a.cols + stride - 1) / stride * stride : a.cols;
+    auto at = [&](int64_t c, int j) { return sums_in_smem ? (c - c0) + j * (int64_t)blockDim.x + threadIdx.x : c + j; };
+    if (sums)
+        for (int64_t c = c0; c < a.cols; c += stride)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) sums[at(c, j)] = sums[half + at(c, j)] = 0.0f;
+    __syncthreads();
+    const TW* wp = static_cast<const TW*>(a.weight);
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const TX* x = static_cast<const TX*>(a.x) + row * a.ldx;
         const TX* dy = static_cast<const TX*>(a.dy) + row * a.lddy;
         TX* dx = static_cast<TX*>(a.y) + row * a.ldy;
-        const TW* wp = static_cast<const TW*>(a.weight);
         const float mean = a.mean[row], rstd = a.rstd[row];
         float s[2] = {0.0f, 0.0f};
-        for (int64_t c = threadIdx.x; c < a.cols; c += blockDim.x) {
-            const float xh = (to_f32(x[c]) - mean) * rstd, d = to_f32(dy[c]), g = d * (wp ? to_f32(wp[c]) : 1.0f);
-            if (out) { out[c] = fmaf(d, xh, out[c]); out[a.cols + c] += d; }
-            s[0] += g;
-            s[1] = fmaf(g, xh, s[1]);
+#pragma unroll 2
+        for (int64_t c = c0; c < a.cols; c += stride) {
+            float xh[VEC], g[VEC], w[VEC];
+            load_vec<VEC>(xh, x + c);
+            load_vec<VEC>(g, dy + c);
+            if (wp) load_params<VEC>(wp + c, w);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                xh[j] = (xh[j] - mean) * rstd;
+                if (sums) {
+                    sums[at(c, j)] = fmaf(g[j], xh[j], sums[at(c, j)]);
+                    sums[half + at(c, j)] += g[j];
+                }
+                const float gw = wp ? g[j] * w[j] : g[j];
+                s[0] += gw;
+                s[1] = fmaf(gw, xh[j], s[1]);
+            }
         }
-        group_sum<2>(s, scratch, turn, blockDim.x, 1);
+        group_sum<2>(s, smem, turn, blockDim.x, 1);
         const float mg = s[0] * inv_n, mgx = s[1] * inv_n;
-        for (int64_t c = threadIdx.x; c < a.cols; c += blockDim.x) {
-            const float xh = (to_f32(x[c]) - mean) * rstd, g = to_f32(dy[c]) * (wp ? to_f32(wp[c]) : 1.0f);
-            const float o = rstd * (g - mg - xh * mgx);
-            store_vec<1>(dx + c, &o);
+#pragma unroll 2
+        for (int64_t c = c0; c < a.cols; c += stride) {
+            float xh[VEC], g[VEC], w[VEC];
+            load_vec<VEC>(xh, x + c);
+            load_vec<VEC>(g, dy + c);
+            if (wp) load_params<VEC>(wp + c, w);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) g[j] = rstd * ((wp ? g[j] * w[j] : g[j]) - mg - (xh[j] - mean) * rstd * mgx);
+            store_vec<VEC>(dx + c, g);
         }
     }
+    if (out && sums_in_smem)
+        for (int64_t c = c0; c < a.cols; c += stride)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) { out[c + j] = sums[at(c, j)]; out[a.cols + c + j] = sums[half + at(c, j)]; }
 }
 
 // Adds the CTAs' column sums: 32 columns of dw (blockIdx.y = 0) or db (1) per CTA, rows of sums dealt to 16 warps.
@@ -355,7 +666,7 @@ __global__ void __launch_bounds__(512) layer_norm_columns_kernel(const float* pa
     if (threadIdx.y == 0 && c < cols) {
 #pragma unroll
         for (int g = 1; g < 16; ++g) s += part[g][threadIdx.x];
-        store_vec<1>(out + c, &s);
+        store_one(out + c, s);
     }
 }
 
@@ -371,31 +682,62 @@ RowShape row_shape(int64_t cols, int per_thread, int cta) {
     return RowShape{t, r};
 }
 
-template <typename TX, typename TW, int VEC, int NV, int MAXT>
-cudaError_t run_forward(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
-    const RowShape s = row_shape(a.cols, VEC * NV, 128);
-    const size_t smem = (size_t)s.groups * 64 * sizeof(float);
-    int per_sm = 0;
-    cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, layer_norm_kernel<TX, TW, VEC, NV, MAXT>, s.threads * s.groups, smem);
+// Ring entries per row group: as many as fit into about 100 KB with all groups of the CTA, 2 to 8.
+int ring_slots(int groups, int64_t entry_bytes) {
+    const int64_t fit = (100 * 1024) / (groups * entry_bytes);
+    return (int)(fit < 2 ? 2 : (fit > 8 ? 8 : fit));
+}
+constexpr int kRingSmem = 200 * 1024;                    // dynamic shared memory asked for; the largest use is 2 x 64 KB + scratch
+
+template <typename TX, typename TW, int PER, bool FULL>
+cudaError_t run_forward_ring(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
+    constexpr int NV = PER * sizeof(TX) / 16;
+    RowShape s = row_shape(a.cols, PER, 512);
+    const int64_t spread = (a.rows + num_sms - 1) / num_sms;             // few rows: one group per SM rather than full CTAs
+    if (s.groups > spread) s.groups = (int)spread;
+    const int64_t row_bytes = a.cols * (int64_t)sizeof(TX);
+    const int slots = ring_slots(s.groups, row_bytes);
+    const size_t smem = (size_t)s.groups * (64 * sizeof(float) + slots * (row_bytes + 8));
+    static std::atomic<int> granted[64];
+    const cudaError_t e = allow_smem(layer_norm_ring_kernel<TX, TW, NV, FULL>, kRingSmem, granted);
     if (e != cudaSuccess) return e;
+    const int64_t need = (a.rows + s.groups - 1) / s.groups;
+    layer_norm_ring_kernel<TX, TW, NV, FULL><<<(unsigned)(need < num_sms ? need : num_sms), dim3(s.threads, s.groups), smem, st>>>(a, slots);
+    return cudaGetLastError();
+}
+
+template <typename TX, typename TW, int NV, int MAXT>
+cudaError_t run_forward(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
+    const RowShape s = row_shape(a.cols, NV, 128);
+    const size_t smem = (size_t)s.groups * 64 * sizeof(float);
+    // resident CTAs per SM of a CTA of so many warps: asked once (the library runs on one kind of device)
+    static std::atomic<int> resident[kMaxRowThreads / 32 + 1];
+    int per_sm = resident[s.threads * s.groups / 32].load(std::memory_order_relaxed);
+    if (per_sm == 0) {
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, layer_norm_kernel<TX, TW, NV, MAXT>, s.threads * s.groups, smem);
+        if (e != cudaSuccess) return e;
+        resident[s.threads * s.groups / 32].store(per_sm, std::memory_order_relaxed);
+    }
     const int64_t need = (a.rows + s.groups - 1) / s.groups, room = (int64_t)num_sms * (per_sm < 1 ? 1 : per_sm);
-    layer_norm_kernel<TX, TW, VEC, NV, MAXT><<<(unsigned)(need < room ? need : room), dim3(s.threads, s.groups), smem, st>>>(a);
+    layer_norm_kernel<TX, TW, NV, MAXT><<<(unsigned)(need < room ? need : room), dim3(s.threads, s.groups), smem, st>>>(a);
     return cudaGetLastError();
 }
 
 template <typename TX, typename TW>
 cudaError_t forward_of(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
     constexpr int V = 16 / sizeof(TX);
-    if (a.cols > (int64_t)kPerThread * kMaxRowThreads) {
-        layer_norm_long_kernel<TX, TW><<<(unsigned)(a.rows < 2 * num_sms ? a.rows : 2 * num_sms), kMaxRowThreads, 0, st>>>(a);
+    const bool vec = a.cols % V == 0 && (a.ldx * (int64_t)sizeof(TX)) % 16 == 0 && (a.ldy * (int64_t)sizeof(TX)) % 16 == 0 &&
+                     aligned(a.x, 16) && aligned(a.y, 16) && aligned(a.weight, 16) && aligned(a.bias, 16);
+    if (a.cols > kRegisterCols) {
+        const unsigned grid = (unsigned)(a.rows < 2 * num_sms ? a.rows : 2 * num_sms);
+        if (vec) layer_norm_long_kernel<TX, TW, V><<<grid, kMaxRowThreads, 0, st>>>(a);
+        else layer_norm_long_kernel<TX, TW, 1><<<grid, kMaxRowThreads, 0, st>>>(a);
         return cudaGetLastError();
     }
-    const bool vec = a.cols % V == 0 && (a.ldx * (int64_t)sizeof(TX)) % 16 == 0 && (a.ldy * (int64_t)sizeof(TX)) % 16 == 0 &&
-                     aligned(a.x, 16) && aligned(a.y, 16);
-    if (a.cols > kPerThread * 512)
-        return vec ? run_forward<TX, TW, V, kPerThread / V, kMaxRowThreads>(a, num_sms, st) : run_forward<TX, TW, 1, kPerThread, kMaxRowThreads>(a, num_sms, st);
-    if (vec) return run_forward<TX, TW, V, kPerThread / V, 512>(a, num_sms, st);
-    return a.cols <= 4 * 256 ? run_forward<TX, TW, 1, 4, 256>(a, num_sms, st) : run_forward<TX, TW, 1, kPerThread, 512>(a, num_sms, st);
+    if (vec && a.cols >= 2048) return a.cols % 1024 == 0 ? run_forward_ring<TX, TW, 32, true>(a, num_sms, st) : run_forward_ring<TX, TW, 32, false>(a, num_sms, st);
+    if (vec) return a.cols % 512 == 0 ? run_forward_ring<TX, TW, 16, true>(a, num_sms, st) : run_forward_ring<TX, TW, 16, false>(a, num_sms, st);
+    if (a.cols > kPerThread * 512) return run_forward<TX, TW, kPerThread, kMaxRowThreads>(a, num_sms, st);
+    return a.cols <= 4 * 256 ? run_forward<TX, TW, 4, 256>(a, num_sms, st) : run_forward<TX, TW, kPerThread, 512>(a, num_sms, st);
 }
 
 template <typename TW>
@@ -412,32 +754,56 @@ cudaError_t add_columns(const LayerNormArgs& a, int groups, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, layer_norm_columns_kernel<TW>, (const float*)a.partial, groups, a.cols, (TW*)a.dweight, (TW*)a.dbias);
 }
 
-template <typename TX, typename TW, int VEC, int NV>
-cudaError_t run_backward(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
-    const RowShape s = row_shape(a.cols, VEC * NV, 512);
-    const size_t smem = ((size_t)s.groups * 128 + (size_t)(s.groups - 1) * 2 * s.threads * NV * VEC) * sizeof(float);
-    cudaError_t e = cudaFuncSetAttribute(layer_norm_backward_kernel<TX, TW, VEC, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
+template <typename TX, typename TW, bool RING, bool FULL>
+cudaError_t run_backward(const LayerNormArgs& a, cudaStream_t st) {
+    RowShape s = row_shape(a.cols, kPerThread, 512);
+    const int64_t spread = (a.rows + kBwdGroups - 1) / kBwdGroups;
+    if (s.groups > spread) s.groups = spread < 1 ? 1 : (int)spread;
+    const int64_t row_bytes = a.cols * (int64_t)sizeof(TX);
+    const int slots = RING ? ring_slots(s.groups, 2 * row_bytes) : 0;
+    const size_t ring = (size_t)s.groups * slots * (2 * row_bytes + 8) + 16;
+    const size_t sums = (size_t)(s.groups - 1) * 2 * s.threads * kPerThread * sizeof(float);
+    const size_t smem = (size_t)s.groups * 128 * sizeof(float) + (ring > sums ? ring : sums);
     const int64_t need = (a.rows + s.groups - 1) / s.groups;
     const int grid = (int)(need < kBwdGroups ? need : kBwdGroups);
-    if (grid > 0) layer_norm_backward_kernel<TX, TW, VEC, NV><<<grid, dim3(s.threads, s.groups), smem, st>>>(a);
-    e = cudaGetLastError();
+    static std::atomic<int> granted[64];
+    cudaError_t e = cudaSuccess;
+    if constexpr (RING) {
+        constexpr int NV = kPerThread * sizeof(TX) / 16;
+        e = allow_smem(layer_norm_backward_ring_kernel<TX, TW, NV, FULL>, kRingSmem, granted);
+        if (e == cudaSuccess && grid > 0) layer_norm_backward_ring_kernel<TX, TW, NV, FULL><<<grid, dim3(s.threads, s.groups), smem, st>>>(a, slots);
+    } else {
+        e = allow_smem(layer_norm_backward_kernel<TX, TW, kPerThread>, kRingSmem, granted);
+        if (e == cudaSuccess && grid > 0) layer_norm_backward_kernel<TX, TW, kPerThread><<<grid, dim3(s.threads, s.groups), smem, st>>>(a);
+    }
+    if (e == cudaSuccess) e = cudaGetLastError();
     return e != cudaSuccess || !a.partial ? e : add_columns<TW>(a, grid, st);
 }
 
 template <typename TX, typename TW>
-cudaError_t backward_of(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
+cudaError_t backward_of(const LayerNormArgs& a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(TX);
+    const bool vec = a.cols % V == 0 && (a.ldx * (int64_t)sizeof(TX)) % 16 == 0 && (a.ldy * (int64_t)sizeof(TX)) % 16 == 0 &&
+                     (a.lddy * (int64_t)sizeof(TX)) % 16 == 0 && aligned(a.x, 16) && aligned(a.y, 16) && aligned(a.dy, 16) && aligned(a.weight, 16);
     if (a.cols > (int64_t)kPerThread * 512) {
         const int grid = (int)(a.rows < kBwdGroups ? a.rows : kBwdGroups);
-        if (grid > 0) layer_norm_backward_long_kernel<TX, TW><<<grid, kMaxRowThreads, 0, st>>>(a);
-        const cudaError_t e = cudaGetLastError();
+        const int in_smem = a.partial && a.cols <= 24576;
+        const int64_t whole = vec ? (int64_t)kMaxRowThreads * V : kMaxRowThreads;          // columns of one trip of the CTA
+        const size_t smem = 128 * sizeof(float) + (in_smem ? 2 * (size_t)((a.cols + whole - 1) / whole * whole) * sizeof(float) : 0);
+        static std::atomic<int> granted[2][64];
+        cudaError_t e = cudaSuccess;
+        if (vec) {
+            e = allow_smem(layer_norm_backward_long_kernel<TX, TW, V>, kRingSmem, granted[0]);
+            if (e == cudaSuccess && grid > 0) layer_norm_backward_long_kernel<TX, TW, V><<<grid, kMaxRowThreads, smem, st>>>(a, in_smem);
+        } else {
+            e = allow_smem(layer_norm_backward_long_kernel<TX, TW, 1>, kRingSmem, granted[1]);
+            if (e == cudaSuccess && grid > 0) layer_norm_backward_long_kernel<TX, TW, 1><<<grid, kMaxRowThreads, smem, st>>>(a, in_smem);
+        }
+        if (e == cudaSuccess) e = cudaGetLastError();
         return e != cudaSuccess || !a.partial ? e : add_columns<TW>(a, grid, st);
     }
-    const bool vec = a.cols % V == 0 && (a.ldx * (int64_t)sizeof(TX)) % 16 == 0 && (a.ldy * (int64_t)sizeof(TX)) % 16 == 0 &&
-                     (a.lddy * (int64_t)sizeof(TX)) % 16 == 0 && aligned(a.x, 16) && aligned(a.y, 16) && aligned(a.dy, 16);
-    if (vec) return run_backward<TX, TW, V, kPerThread / V>(a, num_sms, st);
-    return run_backward<TX, TW, 1, kPerThread>(a, num_sms, st);
+    if (!vec) return run_backward<TX, TW, false, false>(a, st);
+    return a.cols % (kPerThread * 32) == 0 ? run_backward<TX, TW, true, true>(a, st) : run_backward<TX, TW, true, false>(a, st);
 }
 
 }  // namespace
@@ -449,10 +815,21 @@ cudaError_t launch_layer_norm(const LayerNormArgs& a, int dtype, int weight_dtyp
         return weight_dtype == UE5M3_BF16 ? forward_of<__nv_bfloat16, __nv_bfloat16>(a, num_sms, st) : forward_of<__nv_bfloat16, float>(a, num_sms, st);
     return weight_dtype == UE5M3_BF16 ? forward_of<float, __nv_bfloat16>(a, num_sms, st) : forward_of<float, float>(a, num_sms, st);
 }
-cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, int dtype, int weight_dtype, int num_sms, cudaStream_t st) {
+cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, int dtype, int weight_dtype, cudaStream_t st) {
     if (dtype == UE5M3_BF16)
-        return weight_dtype == UE5M3_BF16 ? backward_of<__nv_bfloat16, __nv_bfloat16>(a, num_sms, st) : backward_of<__nv_bfloat16, float>(a, num_sms, st);
-    return weight_dtype == UE5M3_BF16 ? backward_of<float, __nv_bfloat16>(a, num_sms, st) : backward_of<float, float>(a, num_sms, st);
+        return weight_dtype == UE5M3_BF16 ? backward_of<__nv_bfloat16, __nv_bfloat16>(a, st) : backward_of<__nv_bfloat16, float>(a, st);
+    return weight_dtype == UE5M3_BF16 ? backward_of<float, __nv_bfloat16>(a, st) : backward_of<float, float>(a, st);
+}
+
+int read_and_clear_norm_status() {
+    if (cudaDeviceSynchronize() != cudaSuccess) return UE5M3_ERR_CUDA;
+    int v = 0;
+    if (cudaMemcpyFromSymbol(&v, g_norm_status, sizeof(int)) != cudaSuccess) return UE5M3_ERR_CUDA;
+    if (v != 0) {
+        const int zero = 0;
+        if (cudaMemcpyToSymbol(g_norm_status, &zero, sizeof(int)) != cudaSuccess) return UE5M3_ERR_CUDA;
+    }
+    return v;
 }
 
 }  // namespace ue5m3
