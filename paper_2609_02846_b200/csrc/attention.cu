@@ -6,10 +6,10 @@
 // A CTA owns two tiles of 128 queries of one head and walks the keys 128 at a time.  Both products run on the tensor core with
 // accumulators in tensor memory: S = Q K^T from shared memory, O += P V with P (BF16) taken from tensor memory, where it
 // overwrites S.  While one tile's softmax warps turn S into P, the tensor core works for the other tile.  Warp roles:
-//   warp 0      copies: Q once, then K and V tiles through a ring
+//   warp 0      tensor-memory allocation; copies: Q once, then K and V tiles through a ring
 //   warp 1      issues the MMAs (the whole warp runs the loop, one elected lane issues)
-//   warp 2      tensor-memory allocation
-//   warps 4-7 / 8-11   softmax of tile 0 / 1: thread = query row, so maxima and sums need no exchange between threads
+//   warps 4-7 / 8-11   softmax of tile 0 / 1: thread = query row, so maxima and sums need no exchange between threads; a thread
+//               holds a whole row of S (128 scores), so these warps take registers over from the first four
 // The running maximum that scales O is raised only when a row's maximum grew by more than 2^8 (then O is rescaled in tensor
 // memory by its softmax warps): p stays below 2^8, l and O in binary32 lose nothing, and o = O / l does not depend on m.
 // Tensor memory: S0, S1 (128 columns each), O0, O1 (head dimension columns each).
@@ -34,13 +34,17 @@ template <int DP> struct Tiles {                          // DP: head dimension 
     static constexpr int PANELS = DP / 64;
     static constexpr int TILE = 128 * DP * 2;             // bytes of a tile of 128 rows
     static constexpr int PANEL = 128 * 128;
-    static constexpr int STAGES = DP == 128 ? 5 : 8;
-    static constexpr int SMEM_BAR = 2 * TILE + STAGES * TILE;
+    static constexpr int RING = DP == 128 ? 5 : 9;        // K and V tiles in the ring, odd
+    static constexpr int PAIRS = (RING + 1) / 2;          // barriers: one for V of a key tile and K of the next together
+    static constexpr int SMEM_BAR = (2 + RING) * TILE;
     static constexpr int SMEM = SMEM_BAR + 256 + 1024;    // + alignment slack
 };
 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
-    return mbar_wait_status(bar, parity, abort_flag, &g_attention_status, limit);
+    return wait_inline(bar, parity, abort_flag, &g_attention_status, limit);
+}
+__device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+    wait_inline(bar, parity, abort_flag, &g_attention_status, limit, true);
 }
 
 template <int DP>
@@ -54,10 +58,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     uint8_t* smem_gen = smem_raw + (smem - smem_u32(smem_raw));
     const uint32_t ring = smem + 2 * T::TILE;
     const uint32_t bars = smem + T::SMEM_BAR;
-    const uint32_t q_full = bars, kv_full = bars + 16, kv_empty = kv_full + 8 * T::STAGES;
-    const uint32_t s_full = bars + 144, p_full = bars + 160, o_full = bars + 176, drain = bars + 192;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + T::SMEM_BAR + 200);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + T::SMEM_BAR + 204);
+    const uint32_t q_full = bars, kv_full = bars + 16, kv_empty = kv_full + 8 * T::PAIRS;
+    const uint32_t s_full = bars + 144, p_full = bars + 160 /* two halves per tile */, o_full = bars + 192, drain = bars + 208;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + T::SMEM_BAR + 224);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + T::SMEM_BAR + 228);
 
     // work of this CTA: heads fastest (heads that share keys run side by side), long query tiles first
     const int bh_count = p.batch * p.heads;
@@ -83,23 +87,25 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         for (int t = 0; t < 2; ++t) {
             mbar_init(q_full + 8 * t, 1);
             mbar_init(s_full + 8 * t, 1);
-            mbar_init(p_full + 8 * t, 4);
+            mbar_init(p_full + 16 * t, 4);
+            mbar_init(p_full + 16 * t + 8, 4);
             mbar_init(o_full + 8 * t, 1);
         }
-        for (int s = 0; s < T::STAGES; ++s) {
-            mbar_init(kv_full + 8 * s, 1);
+        for (int s = 0; s < T::PAIRS; ++s) {
+            mbar_init(kv_full + 8 * s, 2);                // V's copies and K's
             mbar_init(kv_empty + 8 * s, 1);
         }
         mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_tmap(&map_q); prefetch_tmap(&map_k); prefetch_tmap(&map_v); prefetch_tmap(&map_o);
     }
-    if (warp == 2) tmem_alloc1(smem_u32(tmem_slot), 512);
+    if (warp == 0) tmem_alloc1(smem_u32(tmem_slot), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
+    if (warp < 4) registers_few();
     if (warp == 0) {
         // ------------------------------------------------------------------ copies
         if (lane == 0) {
@@ -111,106 +117,127 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     for (int c = 0; c < T::PANELS; ++c)
                         tma_load_4d(smem + t * T::TILE + c * T::PANEL, &map_q, q_full + 8 * t, c * 64, q0 + t * BQ, h, b);
                 }
-            uint32_t it = 0;                              // tile 2i = K, 2i + 1 = V of key tile first + i
-            for (; it < 2u * (uint32_t)(last - first); ++it) {
-                const uint32_t s = it % T::STAGES, ph = (it / T::STAGES) & 1;
-                if (!wait(kv_empty + 8 * s, ph ^ 1, abort_flag, p.wait_limit)) break;
-                mbar_expect_tx(kv_full + 8 * s, T::TILE);
-                const CUtensorMap* m = (it & 1) ? &map_v : &map_k;
+            // Pair i: V of key tile first + i - 1 (none in the first) and K of key tile first + i (none in the last).  Its tiles are
+            // number 2i - 1 and 2i of the ring; the one takes the place of pair i - PAIRS's K, the other that of the next pair's V.
+            const int pairs = last > first ? last - first + 1 : 0;
+            auto emptied = [&](int pair) { return pair < 0 || wait(kv_empty + 8 * (pair % T::PAIRS), (pair / T::PAIRS) & 1, abort_flag, p.wait_limit); };
+            auto load = [&](int n, const CUtensorMap* m, uint32_t bar, int tile) {
+                mbar_expect_tx(bar, T::TILE);
 #pragma unroll
                 for (int c = 0; c < T::PANELS; ++c)
-                    tma_load_4d(ring + s * T::TILE + c * T::PANEL, m, kv_full + 8 * s, c * 64, (first + (int)(it >> 1)) * BK, kvh, b);
+                    tma_load_4d(ring + (n % T::RING) * T::TILE + c * T::PANEL, m, bar, c * 64, tile * BK, kvh, b);
+            };
+            int i = 0;
+            for (bool go = true; go && i < pairs; ++i) {
+                const uint32_t bar = kv_full + 8 * (i % T::PAIRS);
+                if (!emptied(i - T::PAIRS)) break;
+                if (i > 0) load(2 * i - 1, &map_v, bar, first + i - 1);
+                else mbar_arrive(bar);
+                go = emptied(i - T::PAIRS + 1);
+                if (go && i + 1 < pairs) load(2 * i, &map_k, bar, first + i);
+                else mbar_arrive(bar);
             }
             // copies in flight land before the shared memory goes away, whatever the other roles did
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-                if (hi[t] > lo[t]) mbar_wait_drain(q_full + 8 * t, 0, &g_attention_status, p.wait_limit);
-            for (uint32_t back = 0; back < T::STAGES && back < it; ++back) {
-                const uint32_t j = it - 1 - back;
-                mbar_wait_drain(kv_full + 8 * (j % T::STAGES), (j / T::STAGES) & 1, &g_attention_status, p.wait_limit);
+                if (hi[t] > lo[t]) drain_wait(q_full + 8 * t, 0, abort_flag, p.wait_limit);
+            for (int back = 0; back < T::PAIRS && back < i; ++back) {
+                const int j = i - 1 - back;
+                drain_wait(kv_full + 8 * (j % T::PAIRS), (j / T::PAIRS) & 1, abort_flag, p.wait_limit);
             }
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
+        // Per key tile j:  PV0 S0' | PV1 S1'  with S' = S of key tile j + 1.  The two query tiles stay half a period apart by this
+        // order (an issuing warp per tile let their softmax phases fall together: 293 us against 260 at 2 x 4096 tokens).
         const bool elected = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
         constexpr uint32_t id_s = umma_idesc(BK, false), id_o = umma_idesc(DP, true);
         bool ok = true;
         auto wait_all = [&](uint32_t bar, uint32_t parity) {
-            ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
-            tc_fence_after();
+            if (!__all_sync(0xFFFFFFFFu, try_wait_cta(bar, parity))) ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
             return ok;
         };
-        auto stage_of = [&](int n) { return ring + (uint32_t)(n % T::STAGES) * T::TILE; };
-        auto full = [&](int n) { return wait_all(kv_full + 8 * (n % T::STAGES), (n / T::STAGES) & 1); };
-        auto issue_s = [&](int t, int n) {                 // S_t = Q_t K^T, K in ring tile n
-            const uint64_t qd = umma_smem_desc(smem + t * T::TILE), kd = umma_smem_desc(stage_of(n));
+        uint32_t slot = 0, phase = 0, v_tile = T::RING - 1;          // of the next pair: barrier, and ring tile of its V
+        auto next_pair = [&](int j) {                      // waits for the pair with V of key tile j
+            wait_all(kv_full + 8 * slot, phase);
+            if (++slot == T::PAIRS) { slot = 0; phase ^= 1; }
+            const int valid = keys - j * BK;               // rows of this V tile that exist
+            if (p.k_lens && j >= first && valid < BK) {
+                // values behind the sequence's end may hold anything (0 * NaN is NaN): they become zeros
+                for (int i = valid * (DP / 8) + lane; i < BK * (DP / 8); i += 32) {
+                    const int r = i / (DP / 8), c = i % (DP / 8);
+                    *reinterpret_cast<uint4*>(smem_gen + (2 + v_tile) * T::TILE + (c / 8) * T::PANEL + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_proxy_async();
+                __syncwarp();
+            }
+            const uint32_t v = v_tile;
+            v_tile = v + 2 >= T::RING ? v + 2 - T::RING : v + 2;
+            return v;
+        };
+        auto k_tile = [&](uint32_t v) { return v + 1 == T::RING ? 0 : v + 1; };
+        const uint64_t qd = umma_smem_desc(smem), kd0 = umma_smem_desc(ring), vd0 = umma_mn_desc(ring, T::PANEL);
+        auto issue_s = [&](int t, uint32_t tile) {         // S_t = Q_t K^T
             if (elected) {
+                const uint64_t kd = kd0 + tile * (T::TILE >> 4);
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k) {
                     const uint32_t off = (k / 4) * (T::PANEL >> 4) + (k % 4) * 2;
-                    umma1_ss(tm + t * BK, qd + off, kd + off, id_s, k != 0);
+                    umma1_ss(tm + t * BK, qd + t * (T::TILE >> 4) + off, kd + off, id_s, k != 0);
                 }
                 umma1_commit(s_full + 8 * t);
             }
             __syncwarp();
         };
         uint32_t np[2] = {0, 0};                           // probability tiles consumed per query tile
+        auto issue_o = [&](int t, uint32_t tile, int half, bool end) {     // O_t += P_t V, 64 keys
+            if (!wait_all(p_full + 16 * t + 8 * half, np[t] & 1)) return;
+            tc_fence_after();
+            if (elected) {
+                const uint64_t vd = vd0 + tile * (T::TILE >> 4);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    umma1_ts(tm + 2 * BK + t * 128, tm + t * BK + half * 32 + k * 8, vd + (half * 4 + k) * (2048 >> 4), id_o, np[t] != 0 || half != 0 || k != 0);
+                if (end) umma1_commit(o_full + 8 * t);
+            }
+            __syncwarp();
+        };
         if (on0) wait_all(q_full, 0);
         if (on1) wait_all(q_full + 8, 0);
-        if (last > first && full(0)) {
+        uint32_t done = 0;                                 // barrier of the pair whose products are all issued
+        auto release = [&]() {
+            if (elected) umma1_commit(kv_empty + 8 * done);
+            if (++done == T::PAIRS) done = 0;
+        };
+        if (last > first && ok) {
+            const uint32_t k0 = k_tile(next_pair(first - 1));
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-                if (hi[t] > lo[t] && lo[t] == first) issue_s(t, 0);
-            if (elected) umma1_commit(kv_empty);
-            __syncwarp();
+                if (ok && hi[t] > lo[t] && lo[t] == first) issue_s(t, k0);
+            release();
         }
         for (int j = first; j < last && ok; ++j) {
-            const int nv = 2 * (j - first) + 1, nk = nv + 1;
-            if (!full(nv)) break;
-            const int valid = keys - j * BK;               // rows of this V tile that exist
-            if (p.k_lens && valid < BK) {
-                // values behind the sequence's end may hold anything (0 * NaN is NaN): they become zeros
-                for (int i = valid * (DP / 8) + lane; i < BK * (DP / 8); i += 32) {
-                    const int r = i / (DP / 8), c = i % (DP / 8);
-                    *reinterpret_cast<uint4*>(smem_gen + (stage_of(nv) - smem) + (c / 8) * T::PANEL + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
-                }
-                fence_proxy_async();
-                __syncwarp();
-            }
+            const uint32_t v = next_pair(j), k = k_tile(v);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const bool here = j >= lo[t] && j < hi[t], more = j + 1 < hi[t] && j + 1 >= lo[t];
-                if (here) {
-                    if (!wait_all(p_full + 8 * t, np[t] & 1)) break;
-                    const uint64_t vd = umma_mn_desc(stage_of(nv), T::PANEL);
-                    if (elected) {
-#pragma unroll
-                        for (int k = 0; k < BK / 16; ++k)
-                            umma1_ts(tm + 2 * BK + t * 128, tm + t * BK + k * 8, vd + k * (2048 >> 4), id_o, (np[t] | k) != 0);
-                        if (!more) umma1_commit(o_full + 8 * t);
-                    }
-                    __syncwarp();
+                if (here && ok) {
+                    issue_o(t, v, 0, false);
+                    if (ok) issue_o(t, v, 1, !more);
                     ++np[t];
                 }
-                if (more) {
-                    if (!full(nk)) break;
-                    issue_s(t, nk);
-                }
+                if (more && ok) issue_s(t, k);
             }
-            if (!ok) break;
-            if (elected) {
-                umma1_commit(kv_empty + 8 * (nv % T::STAGES));
-                if (j + 1 < last) umma1_commit(kv_empty + 8 * (nk % T::STAGES));
-            }
-            __syncwarp();
+            release();
         }
         if (elected) {
             umma1_commit(drain);
-            mbar_wait_drain(drain, 0, &g_attention_status, p.wait_limit);
+            drain_wait(drain, 0, abort_flag, p.wait_limit);
         }
         __syncwarp();
     } else if (warp >= 4) {
+        registers_many();
         // ------------------------------------------------------------------ softmax and output of one query tile
         const int t = (warp - 4) >> 2, q = warp & 3;       // tile, tensor-memory lane quarter
         const int r0 = q0 + t * BQ, row = r0 + q * 32 + lane;
@@ -221,7 +248,34 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         // key tiles [plain_lo, plain_hi) are seen whole by every row of the tile
         const int plain_lo = p.left >= 0 ? (p.key_lo(r0 + BQ - 1) + BK - 1) / BK : 0;
         const int plain_hi = max(p.key_hi(r0, keys), 0) / BK;
-        float m = -INFINITY, l = 0.0f;
+        float m = -INFINITY;
+        f32x2 l2 = 0;
+        const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2);
+        // raises the running maximum to at least `top`: l and (after the first tile) O are scaled down.  S of the current tile was
+        // issued after the previous P V, so O is at rest.
+        auto raise = [&](float top, bool first_tile) {
+            const float up = fmaxf(m, top);
+            const float f = m == up ? 1.0f : ex2(m - up);              // m = -inf: l and O hold zeros
+            m = up;
+            l2 = f2_mul(l2, f2_pack(f, f));
+            if (first_tile) return;
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(to + c, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tmem_st32(to + c, o);
+            }
+        };
+        auto publish = [&](int half, const uint32_t (&pk)[32]) {       // 64 probabilities per row, over S's first columns
+            tmem_st32(ts + half * 32, pk);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * half);
+        };
         bool ok = true;
         uint32_t n = 0;
         for (int j = n0; j < n1; ++j, ++n) {
@@ -231,58 +285,44 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, s + c * 32);
             tmem_ld_wait();
-            if (j < plain_lo || j >= plain_hi) {
-                const int base = j * BK - key_lo, width = key_hi - key_lo;
+            const bool masked = j < plain_lo || j >= plain_hi;
+            if (masked) hide_scores<128>(s, j * BK - key_lo, key_hi - key_lo);
+            uint32_t pk[32];
+            float base = m == -INFINITY ? 0.0f : m;
+            // The first half's exponentials are taken against the maximum so far, while this tile's is being found: it raises the
+            // running maximum (and makes them void) only in the first tiles of a row, as a rule.
+            f32x2 sum = 0;
+            exp_scores<32>(s, pk, sum, c2, f2_pack(-base, -base));
+            float top[4];
 #pragma unroll
-                for (int c = 0; c < 128; ++c)
-                    if (!(base + c >= 0 && base + c < width)) s[c] = 0xFF800000u;
+            for (int k = 0; k < 4; ++k) {
+                top[k] = __uint_as_float(s[k]);
+#pragma unroll
+                for (int c = k + 4; c + 4 < 128; c += 8) top[k] = max3(top[k], __uint_as_float(s[c]), __uint_as_float(s[c + 4]));
+                top[k] = fmaxf(top[k], __uint_as_float(s[124 + k]));
             }
-            float top0 = __uint_as_float(s[0]), top1 = __uint_as_float(s[1]), top2 = __uint_as_float(s[2]), top3 = __uint_as_float(s[3]);
-#pragma unroll
-            for (int c = 4; c < 128; c += 4) {
-                top0 = fmaxf(top0, __uint_as_float(s[c]));
-                top1 = fmaxf(top1, __uint_as_float(s[c + 1]));
-                top2 = fmaxf(top2, __uint_as_float(s[c + 2]));
-                top3 = fmaxf(top3, __uint_as_float(s[c + 3]));
+            const float tile_top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
+            if (__any_sync(0xFFFFFFFFu, tile_top > m + kRaise)) {
+                raise(tile_top, n == 0);
+                base = m == -INFINITY ? 0.0f : m;
+                sum = 0;
+                uint32_t again[64];                                    // S still stands in tensor memory
+                tmem_ld32(ts, again);
+                tmem_ld32(ts + 32, again + 32);
+                tmem_ld_wait();
+                if (masked) hide_scores<64>(again, j * BK - key_lo, key_hi - key_lo);
+                exp_scores<32>(again, pk, sum, c2, f2_pack(-base, -base));
             }
-            const float top = fmaxf(fmaxf(top0, top1), fmaxf(top2, top3)) * p.scale_log2;
-            if (n == 0) m = top;
-            else if (__any_sync(0xFFFFFFFFu, top > m + kRaise)) {
-                // S of this tile was issued after the previous P V, so O is at rest
-                const float up = fmaxf(m, top);
-                const float f = m == up ? 1.0f : ex2(m - up);          // m = -inf: O holds zeros
-                m = up;
-                l *= f;
-#pragma unroll 1
-                for (int c = 0; c < DP; c += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(to + c, o);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                    tmem_st32(to + c, o);
-                }
-            }
-            const float base = m == -INFINITY ? 0.0f : m;
-            float sum0 = 0.0f, sum1 = 0.0f;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t pk[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const float e0 = ex2(fmaf(__uint_as_float(s[c * 64 + 2 * i]), p.scale_log2, -base));
-                    const float e1 = ex2(fmaf(__uint_as_float(s[c * 64 + 2 * i + 1]), p.scale_log2, -base));
-                    sum0 += e0;
-                    sum1 += e1;
-                    pk[i] = pack_bf16x2(e0, e1);
-                }
-                tmem_st32(ts + c * 32, pk);
-            }
-            l += sum0 + sum1;
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 8 * t);
+            publish(0, pk);
+            exp_scores<32>(s + 64, pk, sum, c2, f2_pack(-base, -base));
+            publish(1, pk);
+            l2 = f2_add(l2, sum);
+        }
+        float l;
+        {
+            float a, b2;
+            f2_unpack(l2, a, b2);
+            l = a + b2;
         }
         if (row < p.q_len) {
             const float v = l > 0.0f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
@@ -329,7 +369,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         tc_fence_before();
     }
     __syncthreads();
-    if (warp == 2) { tc_fence_after(); tmem_dealloc1(tmem, 512); }
+    if (warp == 0) { tc_fence_after(); tmem_dealloc1(tmem, 512); }
 }
 
 template <int DP>

@@ -5,6 +5,7 @@
 #include <cstdint>
 #include "../../include/ue5m3.h"
 #include "block_ops.h"
+#include "common.cuh"
 #include "tcgen05.cuh"
 
 namespace ue5m3 {
@@ -44,6 +45,65 @@ __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+
+// Acquire at CTA scope: these kernels have no clusters, and the cluster-scope wait costs over a hundred cycles even when the phase
+// is complete (the issuing warp passes six of them per pair of tiles).
+__device__ __forceinline__ bool try_wait_cta(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded waits as in tcgen05.cuh, but without calls: a kernel that moves registers between its warps (setmaxnreg) may make none.
+// `drain`: for something this thread issued itself, whatever the other roles did (the abort flag is not looked at).
+__device__ __forceinline__ bool wait_inline(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status_word, long long limit, bool drain = false) {
+    if (try_wait_cta(bar, parity)) return true;
+    const long long t0 = clock64();
+#pragma unroll 1
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (try_wait_cta(bar, parity)) return true;
+        if (!drain && *abort_flag) return false;
+        if (clock64() - t0 > limit) {
+            if (!drain) *abort_flag = 1;
+            atomicExch(status_word, (int)UE5M3_ERR_TIMEOUT);
+            return false;
+        }
+    }
+}
+// 384 threads are launched with 168 registers each (64,512 in all): the four warps that copy and issue give theirs up, the eight
+// that do the arithmetic take them (128 x 88 + 256 x 208 = 64,512).
+__device__ __forceinline__ void registers_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+__device__ __forceinline__ void registers_many() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// Scores of pairs that do not exist become -inf: only columns with 0 <= base + column < width stay.
+template <int N>
+__device__ __forceinline__ void hide_scores(uint32_t* s, int base, int width) {
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+        if (!(base + c >= 0 && base + c < width)) s[c] = 0xFF800000u;
+}
+// 2^(s c - base) of 2 N scores: packed products, one exponential each.  Adds them to `sum` and packs them as BF16.
+template <int N>
+__device__ __forceinline__ void exp_scores(const uint32_t* s, uint32_t* packed, f32x2& sum, f32x2 c, f32x2 minus_base) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float a, b;
+        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c, minus_base), a, b);
+        a = ex2(a);
+        b = ex2(b);
+        sum = f2_add(sum, f2_pack(a, b));
+        packed[i] = pack_bf16x2(a, b);
+    }
 }
 
 // ----------------------------------------------------------------------------- tiles in shared memory
