@@ -81,7 +81,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     const int first = on0 ? (on1 ? min(lo[0], lo[1]) : lo[0]) : lo[1];
     const int last = on0 ? (on1 ? max(hi[0], hi[1]) : hi[0]) : (on1 ? hi[1] : first);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         *abort_flag = 0;
         for (int t = 0; t < 2; ++t) {

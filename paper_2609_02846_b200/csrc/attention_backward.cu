@@ -33,7 +33,10 @@ constexpr int kThreads = 384;
 constexpr int B128 = 128;
 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
-    return mbar_wait_status(bar, parity, abort_flag, &g_attention_backward_status, limit);
+    return wait_inline(bar, parity, abort_flag, &g_attention_backward_status, limit);
+}
+__device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+    wait_inline(bar, parity, abort_flag, &g_attention_backward_status, limit, true);
 }
 
 // ------------------------------------------------------------------------------------------------ rows
@@ -155,7 +158,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     }
     const int per_head = hi - lo, steps = per_head * p.group;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         *abort_flag = 0;
         const uint32_t ones[] = {k_full, v_full, s_full, dp_full, acc_full, drain};
@@ -202,18 +205,18 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     v_out = true;
                 }
                 if (!wait(d_empty + 8 * s, ph ^ 1, abort_flag, p.wait_limit)) {
-                    mbar_wait_drain(q_full + 8 * s, ph, &g_attention_backward_status, p.wait_limit);
+                    drain_wait(q_full + 8 * s, ph, abort_flag, p.wait_limit);
                     break;
                 }
                 mbar_expect_tx(d_full + 8 * s, T::TILE);
                 tile(st + T::TILE, &map_do, d_full + 8 * s, i0, h);
             }
-            mbar_wait_drain(k_full, 0, &g_attention_backward_status, p.wait_limit);
-            if (v_out) mbar_wait_drain(v_full, 0, &g_attention_backward_status, p.wait_limit);
+            drain_wait(k_full, 0, abort_flag, p.wait_limit);
+            if (v_out) drain_wait(v_full, 0, abort_flag, p.wait_limit);
             for (int back = 0; back < M::STAGES && back < it; ++back) {
                 const int j = it - 1 - back;
-                mbar_wait_drain(q_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, &g_attention_backward_status, p.wait_limit);
-                mbar_wait_drain(d_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, &g_attention_backward_status, p.wait_limit);
+                drain_wait(q_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, abort_flag, p.wait_limit);
+                drain_wait(d_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, abort_flag, p.wait_limit);
             }
         }
     } else if (warp == 1) {
@@ -276,7 +279,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         }
         if (elected) {
             umma1_commit(drain);
-            mbar_wait_drain(drain, 0, &g_attention_backward_status, p.wait_limit);
+            drain_wait(drain, 0, abort_flag, p.wait_limit);
         }
         __syncwarp();
     } else if (warp >= 4) {
@@ -405,7 +408,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     }
     const int steps = hi - lo;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         *abort_flag = 0;
         const uint32_t ones[] = {q_full, d_full, s_full, s_full + 8, dp_full, acc_full, drain}, eights[] = {s_free, s_free + 8, ds_full};
@@ -443,11 +446,11 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                     d_out = true;
                 }
             }
-            mbar_wait_drain(q_full, 0, &g_attention_backward_status, p.wait_limit);
-            if (d_out) mbar_wait_drain(d_full, 0, &g_attention_backward_status, p.wait_limit);
+            drain_wait(q_full, 0, abort_flag, p.wait_limit);
+            if (d_out) drain_wait(d_full, 0, abort_flag, p.wait_limit);
             for (int back = 0; back < M::STAGES && back < it; ++back) {
                 const int j = it - 1 - back;
-                mbar_wait_drain(kv_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, &g_attention_backward_status, p.wait_limit);
+                drain_wait(kv_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, abort_flag, p.wait_limit);
             }
         }
     } else if (warp == 1) {
@@ -519,7 +522,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         }
         if (elected) {
             umma1_commit(drain);
-            mbar_wait_drain(drain, 0, &g_attention_backward_status, p.wait_limit);
+            drain_wait(drain, 0, abort_flag, p.wait_limit);
         }
         __syncwarp();
     } else if (warp >= 4) {
