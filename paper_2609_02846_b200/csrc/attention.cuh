@@ -128,6 +128,43 @@ __host__ __device__ constexpr uint32_t umma_idesc(uint32_t n, bool b_mn) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
+// Issue of a whole product by an elected lane of the converged issuing warp.  Addresses and descriptors must be warp-uniform to the
+// compiler's eye, and so must the loops around: an operand that is not already in a uniform register is moved there before
+// every MMA, which takes longer than the MMA (75 cycles against 64).  So kernels take their loop bounds through uniform().
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+__device__ __forceinline__ uint64_t desc64(uint32_t high, uint32_t low) { return ((uint64_t)high << 32) | low; }
+constexpr uint32_t kDescHighK = (1024u >> 4) | (1u << 14) | (2u << 29);            // upper words: stride 1024, version, 128-byte swizzle
+__device__ __forceinline__ uint32_t desc_low_k(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_low_mn(uint32_t saddr, uint32_t panel_bytes) { return ((saddr & 0x3FFFFu) >> 4) | ((panel_bytes >> 4) << 16); }
+// D [128 x 128] = A B^T, both K-major tiles of 128 rows and DP columns.
+template <int DP>
+__device__ __forceinline__ void issue_square(bool elected, uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t bar) {
+    if (elected) {
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) {
+            const uint32_t off = (k / 4) * (128 * 128 >> 4) + (k % 4) * 2;
+            umma1_ss(d, desc64(kDescHighK, a_low + off), desc64(kDescHighK, b_low + off), umma_idesc(128, false), k != 0);
+        }
+        umma1_commit(bar);
+    }
+    __syncwarp();
+}
+// D [128 x DP] += A B over 16 K of the contraction: A (BF16) in tensor memory, B an MN-major tile.  The A columns of step k are
+// a + k * 8 + (k / 4) * gap: `gap` skips what lies between two groups of 64.
+template <int DP, int K>
+__device__ __forceinline__ void issue_accumulate(bool elected, uint32_t d, uint32_t a, uint32_t gap, uint32_t b_low, uint32_t add) {
+    if (elected) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            umma1_ts(d, a + k * 8 + (k / 4) * gap, desc64(kDescHighK, b_low + k * (2048 >> 4)), umma_idesc(DP, true), k == 0 ? add : 1u);
+    }
+    __syncwarp();
+}
+__device__ __forceinline__ void issue_commit(bool elected, uint32_t bar) {
+    if (elected) umma1_commit(bar);
+    __syncwarp();
+}
+
 // ----------------------------------------------------------------------------- which pairs exist
 struct AttentionParams {
     int q_len, k_len, heads, group;      // group = heads per key/value head

@@ -221,61 +221,52 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
+        // S(0) dP(0) | dV(0) S(1) dK(0) dP(1) | dV(1) S(2) dK(1) dP(2) | ...   S is in order behind dV, which reads P out of its columns
         const bool elected = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-        constexpr uint32_t id_s = umma_idesc(128, false), id_acc = umma_idesc(DP, true);
+        const int n = uniform(steps);
         bool ok = true;
-        auto wait_all = [&](uint32_t bar, uint32_t parity) {
-            ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
+        auto pass = [&](uint32_t bar, uint32_t parity) {   // the phase is complete, or `ok` is false in the whole warp
+            if (!__all_sync(0xFFFFFFFFu, try_wait_cta(bar, parity))) ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
             tc_fence_after();
-            return ok;
         };
-        auto stage = [&](int it) { return smem + M::RING + (uint32_t)(it % M::STAGES) * 2 * T::TILE; };
-        auto phase = [&](int it) { return (uint32_t)((it / M::STAGES) & 1); };
-        // [keys x queries] = (K or V) (Q or dO)^T, both K-major
-        auto issue_square = [&](uint32_t col, uint32_t a, uint32_t bt, uint32_t bar) {
-            const uint64_t ad = umma_smem_desc(a), bd = umma_smem_desc(bt);
-            if (elected) {
-#pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const uint32_t off = (k / 4) * (T::PANEL >> 4) + (k % 4) * 2;
-                    umma1_ss(tm + col, ad + off, bd + off, id_s, k != 0);
-                }
-                umma1_commit(bar);
-            }
-            __syncwarp();
-        };
-        // [keys x dim] += (P or dS)^T (dO or Q): A from tensor memory (each softmax group's 64 queries in its own half), B MN-major
-        auto issue_acc = [&](uint32_t col, uint32_t a_col, uint32_t bt, bool add, uint32_t bar) {
-            const uint64_t bd = umma_mn_desc(bt, T::PANEL);
-            if (elected) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    umma1_ts(tm + col, tm + a_col + (k / 4) * 64 + (k % 4) * 8, bd + k * (2048 >> 4), id_acc, add || k != 0);
-                umma1_commit(bar);
-            }
-            __syncwarp();
-        };
-        if (steps > 0 && wait_all(k_full, 0) && wait_all(q_full, 0)) {
-            issue_square(COL_S, smem, stage(0), s_full);
-            if (wait_all(v_full, 0) && wait_all(d_full, 0)) issue_square(COL_DP, smem + T::TILE, stage(0) + T::TILE, dp_full);
+        const uint32_t k_low = desc_low_k(smem), v_low = desc_low_k(smem + T::TILE);
+        const uint32_t q_k = desc_low_k(smem + M::RING), q_mn = desc_low_mn(smem + M::RING, T::PANEL);      // stage 0: Q, then dO
+        constexpr uint32_t DO = T::TILE >> 4, STAGE = 2 * T::TILE >> 4;
+        uint32_t s = 0, ph = 0;                            // ring stage of step it and its phase
+        if (n > 0) {
+            pass(k_full, 0);
+            pass(q_full, 0);
+            if (ok) issue_square<DP>(elected, tm + COL_S, k_low, q_k, s_full);
+            pass(v_full, 0);
+            pass(d_full, 0);
+            if (ok) issue_square<DP>(elected, tm + COL_DP, v_low, q_k + DO, dp_full);
         }
-        for (int it = 0; it < steps && ok; ++it) {
-            if (!wait_all(p_full, it & 1)) break;
-            issue_acc(COL_ACC0, COL_S, stage(it) + T::TILE, it != 0, d_empty + 8 * (it % M::STAGES));
-            if (it + 1 < steps) {
-                if (!wait_all(q_full + 8 * ((it + 1) % M::STAGES), phase(it + 1))) break;
-                issue_square(COL_S, smem, stage(it + 1), s_full);
+        for (int it = 0; it < n && ok; ++it) {
+            const uint32_t s1 = s + 1 == M::STAGES ? 0 : s + 1, ph1 = s + 1 == M::STAGES ? ph ^ 1 : ph;
+            const bool more = it + 1 < n;
+            pass(p_full, it & 1);
+            if (!ok) break;
+            issue_accumulate<DP, 8>(elected, tm + COL_ACC0, tm + COL_S, 32, q_mn + s * STAGE + DO, it != 0);
+            issue_commit(elected, d_empty + 8 * s);
+            if (more) {
+                pass(q_full + 8 * s1, ph1);
+                if (!ok) break;
+                issue_square<DP>(elected, tm + COL_S, k_low, q_k + s1 * STAGE, s_full);
             }
-            if (!wait_all(ds_full, it & 1)) break;
-            issue_acc(COL_ACC1, COL_DP, stage(it), it != 0, q_empty + 8 * (it % M::STAGES));
-            if (it + 1 < steps) {
-                if (!wait_all(d_full + 8 * ((it + 1) % M::STAGES), phase(it + 1))) break;
-                issue_square(COL_DP, smem + T::TILE, stage(it + 1) + T::TILE, dp_full);
+            pass(ds_full, it & 1);
+            if (!ok) break;
+            issue_accumulate<DP, 8>(elected, tm + COL_ACC1, tm + COL_DP, 32, q_mn + s * STAGE, it != 0);
+            issue_commit(elected, q_empty + 8 * s);
+            if (more) {
+                pass(d_full + 8 * s1, ph1);
+                if (!ok) break;
+                issue_square<DP>(elected, tm + COL_DP, v_low, q_k + s1 * STAGE + DO, dp_full);
             } else {
-                if (elected) umma1_commit(acc_full);
-                __syncwarp();
+                issue_commit(elected, acc_full);
             }
+            s = s1;
+            ph = ph1;
         }
         if (elected) {
             umma1_commit(drain);
@@ -458,67 +449,72 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         // S runs one key tile ahead: S(0) dP(0) S(1) | dQ(0) dP(1) S(2) | dQ(1) dP(2) S(3) | ...
         const bool elected = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-        constexpr uint32_t id_s = umma_idesc(128, false), id_acc = umma_idesc(DP, true);
+        const int n = uniform(steps), n_keys = uniform(keys), first = uniform(lo);
         bool ok = true;
-        auto wait_all = [&](uint32_t bar, uint32_t parity) {
-            ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
+        auto pass = [&](uint32_t bar, uint32_t parity) {   // the phase is complete, or `ok` is false in the whole warp
+            if (!__all_sync(0xFFFFFFFFu, try_wait_cta(bar, parity))) ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
             tc_fence_after();
-            return ok;
         };
-        auto stage = [&](int n) { return smem + M::RING + (uint32_t)(n % M::STAGES) * T::TILE; };
-        auto full = [&](int n) { return wait_all(kv_full + 8 * (n % M::STAGES), (n / M::STAGES) & 1); };
-        auto issue_square = [&](uint32_t col, uint32_t a, uint32_t bt, uint32_t bar) {
-            const uint64_t ad = umma_smem_desc(a), bd = umma_smem_desc(bt);
-            if (elected) {
-#pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const uint32_t off = (k / 4) * (T::PANEL >> 4) + (k % 4) * 2;
-                    umma1_ss(tm + col, ad + off, bd + off, id_s, k != 0);
-                }
-                umma1_commit(bar);
+        const uint32_t q_low = desc_low_k(smem), do_low = desc_low_k(smem + T::TILE);
+        const uint32_t r_k = desc_low_k(smem + M::RING), r_mn = desc_low_mn(smem + M::RING, T::PANEL);
+        constexpr uint32_t TILE = T::TILE >> 4;
+        uint32_t slot = 0, phase = 0;                      // of the next ring tile: K, V, K, V, ...
+        auto next_tile = [&]() {
+            const uint32_t s = slot;
+            pass(kv_full + 8 * s, phase);
+            if (++slot == M::STAGES) { slot = 0; phase ^= 1; }
+            return s;
+        };
+        auto clean_k = [&](int it, uint32_t s) {
+            // keys behind the sequence's end may hold anything (dS is zero there, and 0 * NaN is NaN): they become zeros
+            const int valid = n_keys - (first + it) * B128;
+            if (!p.k_lens || valid >= B128) return;
+            for (int i = valid * (DP / 8) + lane; i < B128 * (DP / 8); i += 32) {
+                const int r = i / (DP / 8), c = i % (DP / 8);
+                *reinterpret_cast<uint4*>(smem_gen + M::RING + s * T::TILE + (c / 8) * T::PANEL + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
             }
+            fence_proxy_async();
             __syncwarp();
         };
-        auto issue_s = [&](int it) {
-            if (!full(2 * it)) return;
-            const int valid = keys - (lo + it) * B128;
-            if (p.k_lens && valid < B128) {
-                // keys behind the sequence's end may hold anything (dS is zero there, and 0 * NaN is NaN): they become zeros
-                for (int i = valid * (DP / 8) + lane; i < B128 * (DP / 8); i += 32) {
-                    const int r = i / (DP / 8), c = i % (DP / 8);
-                    *reinterpret_cast<uint4*>(smem_gen + (stage(2 * it) - smem) + (c / 8) * T::PANEL + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
-                }
-                fence_proxy_async();
-                __syncwarp();
+        uint32_t k0 = 0, k1 = 0, k2 = 0, vs = 0;           // slots of K(it), K(it + 1), K(it + 2), V(it + 1)
+        if (n > 0) {
+            pass(q_full, 0);
+            k0 = next_tile();
+            clean_k(0, k0);
+            if (ok) issue_square<DP>(elected, tm + COL_S, q_low, r_k + k0 * TILE, s_full);
+            vs = next_tile();
+            pass(d_full, 0);
+            if (ok) issue_square<DP>(elected, tm + COL_DP, do_low, r_k + vs * TILE, dp_full);
+            issue_commit(elected, kv_empty + 8 * vs);
+            if (n > 1 && ok) {
+                k1 = next_tile();
+                clean_k(1, k1);
+                if (ok) issue_square<DP>(elected, tm + COL_S1, q_low, r_k + k1 * TILE, s_full + 8);
             }
-            // the softmax warps have read S(it - 2)
-            if (it >= 2 && !wait_all(s_free + 8 * (it & 1), ((it >> 1) & 1) ^ 1)) return;
-            issue_square((it & 1) ? COL_S1 : COL_S, smem, stage(2 * it), s_full + 8 * (it & 1));
-        };
-        auto issue_dp = [&](int it) {
-            if (!full(2 * it + 1)) return;
-            issue_square(COL_DP, smem + T::TILE, stage(2 * it + 1), dp_full);
-            if (elected) umma1_commit(kv_empty + 8 * ((2 * it + 1) % M::STAGES));
-            __syncwarp();
-        };
-        if (steps > 0 && wait_all(q_full, 0)) {
-            issue_s(0);
-            if (ok && wait_all(d_full, 0)) issue_dp(0);
-            if (ok && steps > 1) issue_s(1);
         }
-        for (int it = 0; it < steps && ok; ++it) {
-            if (!wait_all(ds_full, it & 1)) break;
-            const uint64_t kd = umma_mn_desc(stage(2 * it), T::PANEL);
-            if (elected) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    umma1_ts(tm + COL_ACC0, tm + COL_DP + (k / 4) * 64 + (k % 4) * 8, kd + k * (2048 >> 4), id_acc, it != 0 || k != 0);
-                umma1_commit(kv_empty + 8 * ((2 * it) % M::STAGES));
-                if (it + 1 == steps) umma1_commit(acc_full);
+        for (int it = 0; it < n && ok; ++it) {
+            const uint32_t odd = it & 1;
+            pass(ds_full, odd);
+            if (!ok) break;
+            issue_accumulate<DP, 8>(elected, tm + COL_ACC0, tm + COL_DP, 32, r_mn + k0 * TILE, it != 0);
+            issue_commit(elected, kv_empty + 8 * k0);
+            if (it + 1 < n) {
+                vs = next_tile();
+                if (!ok) break;
+                issue_square<DP>(elected, tm + COL_DP, do_low, r_k + vs * TILE, dp_full);
+                issue_commit(elected, kv_empty + 8 * vs);
+            } else {
+                issue_commit(elected, acc_full);
             }
-            __syncwarp();
-            if (it + 1 < steps) issue_dp(it + 1);
-            if (ok && it + 2 < steps) issue_s(it + 2);
+            if (it + 2 < n) {
+                k2 = next_tile();
+                clean_k(it + 2, k2);
+                pass(s_free + 8 * odd, (it >> 1) & 1);     // the softmax warps have read S(it)
+                if (!ok) break;
+                issue_square<DP>(elected, tm + (odd ? COL_S1 : COL_S), q_low, r_k + k2 * TILE, s_full + 8 * odd);
+            }
+            k0 = k1;
+            k1 = k2;
         }
         if (elected) {
             umma1_commit(drain);
