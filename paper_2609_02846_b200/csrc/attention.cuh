@@ -41,6 +41,12 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, uint32_t sr
                  ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
+// 16 consecutive 32-bit columns of this thread's tensor-memory lane.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t r[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -92,18 +98,44 @@ __device__ __forceinline__ void hide_scores(uint32_t* s, int base, int width) {
     for (int c = 0; c < N; ++c)
         if (!(base + c >= 0 && base + c < width)) s[c] = 0xFF800000u;
 }
+__device__ __forceinline__ f32x2 ex2_pair(f32x2 x) {
+    float a, b;
+    f2_unpack(x, a, b);
+    return f2_pack(ex2(a), ex2(b));
+}
+__device__ __forceinline__ uint32_t pack_pair(f32x2 x) {
+    float a, b;
+    f2_unpack(x, a, b);
+    return pack_bf16x2(a, b);
+}
+__device__ __forceinline__ f32x2 pair_of(const uint32_t* s) { return f2_pack(__uint_as_float(s[0]), __uint_as_float(s[1])); }
+
 // 2^(s c - base) of 2 N scores: packed products, one exponential each.  Adds them to `sum` and packs them as BF16.
 template <int N>
 __device__ __forceinline__ void exp_scores(const uint32_t* s, uint32_t* packed, f32x2& sum, f32x2 c, f32x2 minus_base) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        float a, b;
-        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c, minus_base), a, b);
-        a = ex2(a);
-        b = ex2(b);
-        sum = f2_add(sum, f2_pack(a, b));
-        packed[i] = pack_bf16x2(a, b);
+        const f32x2 x = ex2_pair(f2_fma(pair_of(s + 2 * i), c, minus_base));
+        sum = f2_add(sum, x);
+        packed[i] = pack_pair(x);
     }
+}
+// Probabilities of pairs that do not exist become zero: only columns with 0 <= base + column < width stay.
+template <int N>
+__device__ __forceinline__ void hide_pairs(f32x2* p, int base, int width) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float a, b;
+        f2_unpack(p[i], a, b);
+        p[i] = f2_pack(base + 2 * i >= 0 && base + 2 * i < width ? a : 0.0f, base + 2 * i + 1 >= 0 && base + 2 * i + 1 < width ? b : 0.0f);
+    }
+}
+// x where p is not zero (0 * NaN would be NaN where a pair does not exist)
+__device__ __forceinline__ f32x2 where_p(f32x2 p, f32x2 x) {
+    float a, b, u, v;
+    f2_unpack(p, a, b);
+    f2_unpack(x, u, v);
+    return f2_pack(a != 0.0f ? u : 0.0f, b != 0.0f ? v : 0.0f);
 }
 
 // ----------------------------------------------------------------------------- tiles in shared memory
@@ -149,14 +181,26 @@ __device__ __forceinline__ void issue_square(bool elected, uint32_t d, uint32_t 
     }
     __syncwarp();
 }
-// D [128 x DP] += A B over 16 K of the contraction: A (BF16) in tensor memory, B an MN-major tile.  The A columns of step k are
-// a + k * 8 + (k / 4) * gap: `gap` skips what lies between two groups of 64.
-template <int DP, int K>
-__device__ __forceinline__ void issue_accumulate(bool elected, uint32_t d, uint32_t a, uint32_t gap, uint32_t b_low, uint32_t add) {
+// The same with A in tensor memory (BF16 pairs, DP / 2 columns).
+template <int DP>
+__device__ __forceinline__ void issue_square_ts(bool elected, uint32_t d, uint32_t a, uint32_t b_low, uint32_t bar) {
     if (elected) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            umma1_ts(d, a + k * 8 + (k / 4) * gap, desc64(kDescHighK, b_low + k * (2048 >> 4)), umma_idesc(DP, true), k == 0 ? add : 1u);
+        for (int k = 0; k < DP / 16; ++k)
+            umma1_ts(d, a + k * 8, desc64(kDescHighK, b_low + (k / 4) * (128 * 128 >> 4) + (k % 4) * 2), umma_idesc(128, false), k != 0);
+        umma1_commit(bar);
+    }
+    __syncwarp();
+}
+// D [128 x DP] += A B over 128 of the contraction: A (BF16) in tensor memory, 64 values each from columns a and a + 64, B an
+// MN-major tile.  HALF 0 or 1: only the first or last 32 of each 64.
+template <int DP, int HALF = -1>
+__device__ __forceinline__ void issue_accumulate(bool elected, uint32_t d, uint32_t a, uint32_t b_low, uint32_t add) {
+    if (elected) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (HALF < 0 || ((k >> 1) & 1) == HALF)
+                umma1_ts(d, a + k * 8 + (k / 4) * 32, desc64(kDescHighK, b_low + k * (2048 >> 4)), umma_idesc(DP, true), k == 0 ? add : 1u);
     }
     __syncwarp();
 }
@@ -173,8 +217,8 @@ struct AttentionParams {
     const int* k_lens;
     float scale, scale_log2;             // scale * log2(e)
     float* lse;                          // forward: [batch, heads, q_len]
-    const float* lse2;                   // backward: lse * log2(e) per query, padded to whole tiles (+inf: contributes nothing)
-    const float* delta;                  // backward: dout . o per query, padded
+    const float* lse2;                   // backward: -lse * log2(e) per query, padded to whole tiles (-inf: contributes nothing)
+    const float* delta;                  // backward: -(dout . o) per query, padded
     int q_pad;
     long long wait_limit;
 

@@ -3,7 +3,7 @@
 //     dv_j = sum_i P_ij dout_i,  dk_j = scale sum_i dS_ij q_i,  dq_i = scale sum_j dS_ij k_j
 //
 // Three launches:
-//   rows     D_i and lse2_i = log2(e) lse_i of every query (padded to whole tiles; +inf where a query sees nothing, so that P = 0)
+//   rows     -D_i and -log2(e) lse_i of every query (padded to whole tiles; -inf where a query sees nothing, so that P = 0)
 //   keys     a CTA owns 128 keys of one key/value head and walks the queries that see them, through all query heads of the
 //            group: S^T = K Q^T, dP^T = V dO^T, then dV += P^T dO and dK += dS^T Q
 //   queries  a CTA owns 128 queries of one head and walks the keys they see: S = Q K^T, dP = dO V^T, dQ += dS K
@@ -50,12 +50,13 @@ struct RowParams {
 };
 // Eight threads per query, 16 bytes of o and dout at a time.
 __global__ void __launch_bounds__(256) attention_rows_kernel(const RowParams p) {
+    asm volatile("griddepcontrol.launch_dependents;");          // the keys kernel sets itself up meanwhile
     const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
     const int sub = threadIdx.x & 7;
     if (r >= p.rows) return;                        // whole groups of eight
     const int64_t bh = r / p.q_pad;
     const int i = (int)(r - bh * p.q_pad), b = (int)(bh / p.heads), h = (int)(bh - (int64_t)b * p.heads);
-    float sum = 0.0f, lse2 = INFINITY;
+    float sum = 0.0f, lse2 = -INFINITY;
     if (i < p.q_len) {
         const __nv_bfloat16* o = p.o + b * p.o_stride[0] + i * p.o_stride[1] + h * p.o_stride[2];
         const __nv_bfloat16* d = p.dout + b * p.d_stride[0] + i * p.d_stride[1] + h * p.d_stride[2];
@@ -67,11 +68,11 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const RowParams p) 
             for (int k = 0; k < 8; ++k) sum = fmaf(x[k], y[k], sum);
         }
         const float lse = p.lse[bh * p.q_len + i];
-        if (lse != -INFINITY) lse2 = lse * 1.4426950408889634f;
+        if (lse != -INFINITY) lse2 = lse * -1.4426950408889634f;
     }
 #pragma unroll
     for (int k = 4; k; k >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, k, 8);
-    if (sub == 0) { p.lse2[r] = lse2; p.delta[r] = sum; }
+    if (sub == 0) { p.lse2[r] = lse2; p.delta[r] = -sum; }
 }
 
 // ------------------------------------------------------------------------------------------------ shared pieces
@@ -140,10 +141,10 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     uint8_t* smem_gen = smem_raw + (smem - smem_u32(smem_raw));
     const uint32_t bars = smem + M::BAR;
     const uint32_t k_full = bars, v_full = bars + 8, s_full = bars + 16, dp_full = bars + 24, p_full = bars + 32, ds_full = bars + 40;
-    const uint32_t acc_full = bars + 48, drain = bars + 56, q_full = bars + 64, q_empty = q_full + 8 * M::STAGES;
+    const uint32_t acc_full = bars + 48, drain = bars + 56, p_half = bars + 64, q_full = bars + 72, q_empty = q_full + 8 * M::STAGES;
     const uint32_t d_full = q_empty + 8 * M::STAGES, d_empty = d_full + 8 * M::STAGES;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + M::BAR + 192);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + M::BAR + 196);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + M::BAR + 208);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + M::BAR + 212);
 
     // key tiles of one head side by side, those that most queries see (causal: the first) at the front
     const int bh_count = p.batch * kv_heads;
@@ -163,6 +164,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         *abort_flag = 0;
         const uint32_t ones[] = {k_full, v_full, s_full, dp_full, acc_full, drain};
         for (uint32_t x : ones) mbar_init(x, 1);
+        mbar_init(p_half, 8);
         mbar_init(p_full, 8);
         mbar_init(ds_full, 8);
         for (int s = 0; s < M::STAGES; ++s) {
@@ -177,6 +179,8 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    asm volatile("griddepcontrol.wait;" ::: "memory");           // the rows are there
+    asm volatile("griddepcontrol.launch_dependents;");            // the queries kernel needs nothing of this one: it may fill its tail
 
     if (warp == 0) {
         // ------------------------------------------------------------------ copies
@@ -245,9 +249,12 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         for (int it = 0; it < n && ok; ++it) {
             const uint32_t s1 = s + 1 == M::STAGES ? 0 : s + 1, ph1 = s + 1 == M::STAGES ? ph ^ 1 : ph;
             const bool more = it + 1 < n;
+            pass(p_half, it & 1);                          // half of dV's product runs under the other half's exponentials
+            if (!ok) break;
+            issue_accumulate<DP, 0>(elected, tm + COL_ACC0, tm + COL_S, q_mn + s * STAGE + DO, it != 0);
             pass(p_full, it & 1);
             if (!ok) break;
-            issue_accumulate<DP, 8>(elected, tm + COL_ACC0, tm + COL_S, 32, q_mn + s * STAGE + DO, it != 0);
+            issue_accumulate<DP, 1>(elected, tm + COL_ACC0, tm + COL_S, q_mn + s * STAGE + DO, 1);
             issue_commit(elected, d_empty + 8 * s);
             if (more) {
                 pass(q_full + 8 * s1, ph1);
@@ -256,7 +263,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             }
             pass(ds_full, it & 1);
             if (!ok) break;
-            issue_accumulate<DP, 8>(elected, tm + COL_ACC1, tm + COL_DP, 32, q_mn + s * STAGE, it != 0);
+            issue_accumulate<DP>(elected, tm + COL_ACC1, tm + COL_DP, q_mn + s * STAGE, it != 0);
             issue_commit(elected, q_empty + 8 * s);
             if (more) {
                 pass(d_full + 8 * s1, ph1);
@@ -283,6 +290,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         // query tiles [plain_lo, plain_hi) see every key of this tile
         const int plain_lo = j0 + B128 <= keys ? (p.query_lo(j0 + B128 - 1) + B128 - 1) / B128 : hi;
         const int plain_hi = p.left >= 0 ? max(p.query_hi(j0), 0) / B128 : p.q_len / B128 + 1;
+        const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2);
         bool ok = true;
         for (int it = 0; it < steps; ++it) {
             const int qt = lo + it % per_head;
@@ -297,28 +305,25 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             tmem_ld32(ts, s);
             tmem_ld32(ts + 32, s + 32);
             tmem_ld_wait();
+            f32x2 pr[32];
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const float4 e = *reinterpret_cast<const float4*>(rows + c);
-                s[c] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c]), p.scale_log2, -e.x)));
-                s[c + 1] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c + 1]), p.scale_log2, -e.y)));
-                s[c + 2] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c + 2]), p.scale_log2, -e.z)));
-                s[c + 3] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c + 3]), p.scale_log2, -e.w)));
+            for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                for (int c = half * 32; c < half * 32 + 32; c += 4) {
+                    const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(rows + c);          // -lse2 of four queries
+                    pr[c / 2] = ex2_pair(f2_fma(pair_of(s + c), c2, e.x));
+                    pr[c / 2 + 1] = ex2_pair(f2_fma(pair_of(s + c + 2), c2, e.y));
+                }
+                if (!plain) hide_pairs<16>(pr + half * 16, base + half * 32, width);
+                uint32_t pk[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) pk[i] = pack_pair(pr[half * 16 + i]);
+                tmem_st16(ts + half * 16, pk);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(half ? p_full : p_half);
             }
-            if (!plain)
-#pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    if (!(base + c >= 0 && base + c < width)) s[c] = 0u;
-            {
-                uint32_t pk[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) pk[i] = pack_bf16x2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
-                tmem_st32(ts, pk);
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full);
             if (!(ok = wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t pk[32];
@@ -329,15 +334,12 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 tmem_ld_wait();
 #pragma unroll
                 for (int c = 0; c < 32; c += 4) {
-                    const float4 e = *reinterpret_cast<const float4*>(rows + 128 + half * 32 + c);
-                    const uint32_t* pp = s + half * 32 + c;
-                    float x0 = __uint_as_float(pp[0]) * (__uint_as_float(d[c]) - e.x), x1 = __uint_as_float(pp[1]) * (__uint_as_float(d[c + 1]) - e.y);
-                    float x2 = __uint_as_float(pp[2]) * (__uint_as_float(d[c + 2]) - e.z), x3 = __uint_as_float(pp[3]) * (__uint_as_float(d[c + 3]) - e.w);
-                    if (!plain) {                                     // 0 * NaN where the pair does not exist
-                        x0 = pp[0] ? x0 : 0.0f; x1 = pp[1] ? x1 : 0.0f; x2 = pp[2] ? x2 : 0.0f; x3 = pp[3] ? x3 : 0.0f;
-                    }
-                    pk[half * 16 + c / 2] = pack_bf16x2(x0, x1);
-                    pk[half * 16 + c / 2 + 1] = pack_bf16x2(x2, x3);
+                    const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(rows + 128 + half * 32 + c);          // -delta
+                    const f32x2 p0 = pr[half * 16 + c / 2], p1 = pr[half * 16 + c / 2 + 1];
+                    f32x2 x = f2_mul(p0, f2_add(pair_of(d + c), e.x)), y = f2_mul(p1, f2_add(pair_of(d + c + 2), e.y));
+                    if (!plain) { x = where_p(p0, x); y = where_p(p1, y); }
+                    pk[half * 16 + c / 2] = pack_pair(x);
+                    pk[half * 16 + c / 2 + 1] = pack_pair(y);
                 }
             }
             tmem_st32(td, pk);
@@ -362,13 +364,16 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 }
 
 // ------------------------------------------------------------------------------------------------ queries: dQ
+// Q and dO stay with the CTA as A operands, so they move into tensor memory at the start: S and dP then read only K and V from
+// shared memory (with both operands there, a 128 x 128 product needs its whole bandwidth), and all of it is ring for K and V,
+// whose copies take up to 1500 cycles.
 template <int DP> struct QuerySmem {
     using T = Tiles<DP>;
-    static constexpr int STAGES = DP == 128 ? 5 : 8;                  // ring of K and V tiles
-    static constexpr int RING = 2 * T::TILE;                          // Q, dO
-    static constexpr int BAR = RING + STAGES * T::TILE;
+    static constexpr int STAGES = DP == 128 ? 7 : 10;                 // ring: Q, dO, then K and V tiles
+    static constexpr int BAR = STAGES * T::TILE;
     static constexpr int SIZE = BAR + 256 + 1024;
 };
+constexpr uint32_t COL_Q = 384, COL_DO = 448;                         // in place of the second accumulator
 
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -381,11 +386,10 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem - smem_u32(smem_raw));
     const uint32_t bars = smem + M::BAR;
-    const uint32_t q_full = bars, d_full = bars + 8, s_full = bars + 16 /* two */, dp_full = bars + 32, s_free = bars + 40 /* two */;
-    const uint32_t ds_full = bars + 56, acc_full = bars + 64, drain = bars + 72, kv_full = bars + 80, kv_empty = kv_full + 8 * M::STAGES;
+    const uint32_t qd_ready = bars, s_full = bars + 8, s_free = bars + 16, dp_full = bars + 24, ds_full = bars + 32, acc_full = bars + 40;
+    const uint32_t drain = bars + 48, full = bars + 56, empty = full + 8 * M::STAGES;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + M::BAR + 240);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + M::BAR + 244);
-    constexpr uint32_t COL_S1 = COL_ACC1;                             // S alternates between columns 0.. and 384..
 
     const int bh_count = p.batch * p.heads;
     const int bh = blockIdx.x % bh_count, i0 = (q_tiles - 1 - (int)(blockIdx.x / bh_count)) * B128;
@@ -402,10 +406,10 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         *abort_flag = 0;
-        const uint32_t ones[] = {q_full, d_full, s_full, s_full + 8, dp_full, acc_full, drain}, eights[] = {s_free, s_free + 8, ds_full};
+        const uint32_t ones[] = {s_full, dp_full, acc_full, drain}, eights[] = {qd_ready, s_free, ds_full};
         for (uint32_t x : ones) mbar_init(x, 1);
         for (uint32_t x : eights) mbar_init(x, 8);
-        for (int s = 0; s < M::STAGES; ++s) { mbar_init(kv_full + 8 * s, 1); mbar_init(kv_empty + 8 * s, 1); }
+        for (int s = 0; s < M::STAGES; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_tmap(&map_q); prefetch_tmap(&map_do); prefetch_tmap(&map_k); prefetch_tmap(&map_v); prefetch_tmap(&map_dq);
     }
@@ -422,31 +426,23 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
 #pragma unroll
                 for (int c = 0; c < T::PANELS; ++c) tma_load_4d(dst + c * T::PANEL, m, bar, c * 64, row, head, b);
             };
-            mbar_expect_tx(q_full, T::TILE);
-            tile(smem, &map_q, q_full, i0, h);
-            int it = 0;                                               // tile 2i = K, 2i + 1 = V of key tile lo + i
-            bool d_out = false;
-            for (; it < 2 * steps; ++it) {
+            int it = 0;                                               // ring: Q, dO, K(0), V(0), K(1), V(1), ...
+            for (; it < 2 * steps + 2; ++it) {
                 const int s = it % M::STAGES;
-                if (!wait(kv_empty + 8 * s, ((it / M::STAGES) & 1) ^ 1, abort_flag, p.wait_limit)) break;
-                mbar_expect_tx(kv_full + 8 * s, T::TILE);
-                tile(smem + M::RING + s * T::TILE, (it & 1) ? &map_v : &map_k, kv_full + 8 * s, (lo + (it >> 1)) * B128, kvh);
-                if (!d_out) {
-                    mbar_expect_tx(d_full, T::TILE);
-                    tile(smem + T::TILE, &map_do, d_full, i0, h);
-                    d_out = true;
-                }
+                if (!wait(empty + 8 * s, ((it / M::STAGES) & 1) ^ 1, abort_flag, p.wait_limit)) break;
+                mbar_expect_tx(full + 8 * s, T::TILE);
+                if (it < 2) tile(smem + s * T::TILE, it ? &map_do : &map_q, full + 8 * s, i0, h);
+                else tile(smem + s * T::TILE, (it & 1) ? &map_v : &map_k, full + 8 * s, (lo + (it >> 1) - 1) * B128, kvh);
             }
-            drain_wait(q_full, 0, abort_flag, p.wait_limit);
-            if (d_out) drain_wait(d_full, 0, abort_flag, p.wait_limit);
             for (int back = 0; back < M::STAGES && back < it; ++back) {
                 const int j = it - 1 - back;
-                drain_wait(kv_full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, abort_flag, p.wait_limit);
+                drain_wait(full + 8 * (j % M::STAGES), (j / M::STAGES) & 1, abort_flag, p.wait_limit);
             }
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
-        // S runs one key tile ahead: S(0) dP(0) S(1) | dQ(0) dP(1) S(2) | dQ(1) dP(2) S(3) | ...
+        // S(0) dP(0) S(1) | dQ(0) dP(1) S(2) | dQ(1) dP(2) S(3) | ...   S is read into registers at once, so it runs a step ahead; dP is in
+        // order behind the product that reads dS out of its columns
         const bool elected = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
         const int n = uniform(steps), n_keys = uniform(keys), first = uniform(lo);
@@ -455,13 +451,12 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             if (!__all_sync(0xFFFFFFFFu, try_wait_cta(bar, parity))) ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
             tc_fence_after();
         };
-        const uint32_t q_low = desc_low_k(smem), do_low = desc_low_k(smem + T::TILE);
-        const uint32_t r_k = desc_low_k(smem + M::RING), r_mn = desc_low_mn(smem + M::RING, T::PANEL);
+        const uint32_t r_k = desc_low_k(smem), r_mn = desc_low_mn(smem, T::PANEL);
         constexpr uint32_t TILE = T::TILE >> 4;
-        uint32_t slot = 0, phase = 0;                      // of the next ring tile: K, V, K, V, ...
+        uint32_t slot = 2, phase = 0;                      // of the next ring tile: K, V, K, V, ...
         auto next_tile = [&]() {
             const uint32_t s = slot;
-            pass(kv_full + 8 * s, phase);
+            pass(full + 8 * s, phase);
             if (++slot == M::STAGES) { slot = 0; phase ^= 1; }
             return s;
         };
@@ -471,48 +466,40 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             if (!p.k_lens || valid >= B128) return;
             for (int i = valid * (DP / 8) + lane; i < B128 * (DP / 8); i += 32) {
                 const int r = i / (DP / 8), c = i % (DP / 8);
-                *reinterpret_cast<uint4*>(smem_gen + M::RING + s * T::TILE + (c / 8) * T::PANEL + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(smem_gen + s * T::TILE + (c / 8) * T::PANEL + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
             }
             fence_proxy_async();
             __syncwarp();
         };
-        uint32_t k0 = 0, k1 = 0, k2 = 0, vs = 0;           // slots of K(it), K(it + 1), K(it + 2), V(it + 1)
+        uint32_t k0 = 0, k1 = 0, k2 = 0;                   // slots of K(it), K(it + 1), K(it + 2)
+        auto issue_s = [&](int it) {
+            const uint32_t s = next_tile();
+            clean_k(it, s);
+            if (it > 0) pass(s_free, (it - 1) & 1);        // the softmax warps have read S(it - 1)
+            if (ok) issue_square_ts<DP>(elected, tm + COL_S, tm + COL_Q, r_k + s * TILE, s_full);
+            return s;
+        };
+        auto issue_dp = [&]() {
+            const uint32_t s = next_tile();
+            if (ok) issue_square_ts<DP>(elected, tm + COL_DP, tm + COL_DO, r_k + s * TILE, dp_full);
+            if (ok) issue_commit(elected, empty + 8 * s);
+        };
         if (n > 0) {
-            pass(q_full, 0);
-            k0 = next_tile();
-            clean_k(0, k0);
-            if (ok) issue_square<DP>(elected, tm + COL_S, q_low, r_k + k0 * TILE, s_full);
-            vs = next_tile();
-            pass(d_full, 0);
-            if (ok) issue_square<DP>(elected, tm + COL_DP, do_low, r_k + vs * TILE, dp_full);
-            issue_commit(elected, kv_empty + 8 * vs);
-            if (n > 1 && ok) {
-                k1 = next_tile();
-                clean_k(1, k1);
-                if (ok) issue_square<DP>(elected, tm + COL_S1, q_low, r_k + k1 * TILE, s_full + 8);
-            }
+            pass(qd_ready, 0);
+            if (ok && elected) { mbar_arrive(empty); mbar_arrive(empty + 8); }
+            __syncwarp();
+            k0 = issue_s(0);
+            issue_dp();
+            if (n > 1 && ok) k1 = issue_s(1);
         }
         for (int it = 0; it < n && ok; ++it) {
-            const uint32_t odd = it & 1;
-            pass(ds_full, odd);
+            pass(ds_full, it & 1);
             if (!ok) break;
-            issue_accumulate<DP, 8>(elected, tm + COL_ACC0, tm + COL_DP, 32, r_mn + k0 * TILE, it != 0);
-            issue_commit(elected, kv_empty + 8 * k0);
-            if (it + 1 < n) {
-                vs = next_tile();
-                if (!ok) break;
-                issue_square<DP>(elected, tm + COL_DP, do_low, r_k + vs * TILE, dp_full);
-                issue_commit(elected, kv_empty + 8 * vs);
-            } else {
-                issue_commit(elected, acc_full);
-            }
-            if (it + 2 < n) {
-                k2 = next_tile();
-                clean_k(it + 2, k2);
-                pass(s_free + 8 * odd, (it >> 1) & 1);     // the softmax warps have read S(it)
-                if (!ok) break;
-                issue_square<DP>(elected, tm + (odd ? COL_S1 : COL_S), q_low, r_k + k2 * TILE, s_full + 8 * odd);
-            }
+            issue_accumulate<DP>(elected, tm + COL_ACC0, tm + COL_DP, r_mn + k0 * TILE, it != 0);
+            issue_commit(elected, empty + 8 * k0);
+            if (it + 1 == n) issue_commit(elected, acc_full);
+            else issue_dp();
+            if (it + 2 < n && ok) k2 = issue_s(it + 2);
             k0 = k1;
             k1 = k2;
         }
@@ -526,19 +513,37 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         const int g = (warp - 4) >> 2, q = warp & 3;
         const int row = i0 + q * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
-        const uint32_t td = lane_base + COL_DP + g * 64;
         const int k_lo = p.key_lo(row), k_hi = p.key_hi(row, keys);
         const int plain_lo = p.left >= 0 ? (p.key_lo(i0 + B128 - 1) + B128 - 1) / B128 : 0;
         const int plain_hi = max(p.key_hi(i0, keys), 0) / B128;
         const int64_t at = ((int64_t)b * p.heads + h) * p.q_pad + row;
-        const float lse2 = __ldg(p.lse2 + at), delta = __ldg(p.delta + at);
+        const float nl = __ldg(p.lse2 + at), nd = __ldg(p.delta + at);
+        const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2), nl2 = f2_pack(nl, nl), nd2 = f2_pack(nd, nd);
         bool ok = true;
-        for (int it = 0; it < steps; ++it) {
+        if (steps > 0) {
+            // group 0 moves Q into tensor memory, group 1 dO: a thread its own row, undoing the swizzle
+            ok = wait(full + 8 * g, 0, abort_flag, p.wait_limit);
+            if (ok) {
+#pragma unroll
+                for (int c = 0; c < T::PANELS; ++c) {
+                    const uint8_t* mine = smem_gen + g * T::TILE + c * T::PANEL + (q * 32 + lane) * 128;
+                    uint32_t w[32];
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4*>(w + 4 * v) = *reinterpret_cast<const uint4*>(mine + ((v ^ (lane & 7)) << 4));
+                    tmem_st32(lane_base + (g ? COL_DO : COL_Q) + c * 32, w);
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(qd_ready);
+            }
+        }
+        for (int it = 0; ok && it < steps; ++it) {
             const int kt = lo + it;
             const bool plain = kt >= plain_lo && kt < plain_hi;
             const int base = kt * B128 + g * 64 - k_lo, width = k_hi - k_lo;
-            const uint32_t ts = lane_base + ((it & 1) ? COL_S1 : COL_S) + g * 64;
-            if (!(ok = wait(s_full + 8 * (it & 1), (it >> 1) & 1, abort_flag, p.wait_limit))) break;
+            const uint32_t ts = lane_base + COL_S + g * 64, td = lane_base + COL_DP + g * 64;
+            if (!(ok = wait(s_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t s[64];
             tmem_ld32(ts, s);
@@ -546,13 +551,11 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             tmem_ld_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(s_free + 8 * (it & 1));
+            if (lane == 0) mbar_arrive(s_free);
+            f32x2 pr[32];
 #pragma unroll
-            for (int c = 0; c < 64; ++c) s[c] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c]), p.scale_log2, -lse2)));
-            if (!plain)
-#pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    if (!(base + c >= 0 && base + c < width)) s[c] = 0u;
+            for (int i = 0; i < 32; ++i) pr[i] = ex2_pair(f2_fma(pair_of(s + 2 * i), c2, nl2));
+            if (!plain) hide_pairs<32>(pr, base, width);
             if (!(ok = wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t pk[32];
@@ -562,11 +565,11 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 tmem_ld32(td + half * 32, d);
                 tmem_ld_wait();
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    const uint32_t* pp = s + half * 32 + c;
-                    float x0 = __uint_as_float(pp[0]) * (__uint_as_float(d[c]) - delta), x1 = __uint_as_float(pp[1]) * (__uint_as_float(d[c + 1]) - delta);
-                    if (!plain) { x0 = pp[0] ? x0 : 0.0f; x1 = pp[1] ? x1 : 0.0f; }
-                    pk[half * 16 + c / 2] = pack_bf16x2(x0, x1);
+                for (int i = 0; i < 16; ++i) {
+                    const f32x2 pp = pr[half * 16 + i];
+                    f32x2 x = f2_mul(pp, f2_add(pair_of(d + 2 * i), nd2));
+                    if (!plain) x = where_p(pp, x);
+                    pk[half * 16 + i] = pack_pair(x);
                 }
             }
             tmem_st32(td, pk);
@@ -585,9 +588,26 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     }
     __syncthreads();
     if (warp == 2) { tc_fence_after(); tmem_dealloc1(tmem, 512); }
+    asm volatile("griddepcontrol.wait;" ::: "memory");           // this grid ends after the keys kernel: what follows is behind both
 }
 
 struct Maps { CUtensorMap q, dout, k, v, dq, dk, dv; };
+
+// A launch that may begin before the one in front of it has ended (`early`): the kernel says itself what it waits for.
+template <typename... Args>
+int launch(void (*kernel)(Args...), int64_t grid, int smem, bool early, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+}
 
 template <int DP>
 int run(const ue5m3_attention_shape& s, const Maps& m, const AttentionParams& p, cudaStream_t st) {
@@ -597,14 +617,14 @@ int run(const ue5m3_attention_shape& s, const Maps& m, const AttentionParams& p,
     if (ck > 0) {
         static std::atomic<int> granted[64];
         if (allow_smem(attention_keys_kernel<DP>, KeySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-        attention_keys_kernel<DP><<<(unsigned)ck, kThreads, KeySmem<DP>::SIZE, st>>>(m.q, m.dout, m.k, m.v, m.dk, m.dv, p, (int)s.kv_heads);
-        if (cudaGetLastError() != cudaSuccess) return UE5M3_ERR_CUDA;
+        const int r = launch(attention_keys_kernel<DP>, ck, KeySmem<DP>::SIZE, cq > 0, st, m.q, m.dout, m.k, m.v, m.dk, m.dv, p, (int)s.kv_heads);
+        if (r != UE5M3_OK) return r;
     }
     if (cq > 0) {
         static std::atomic<int> granted[64];
         if (allow_smem(attention_queries_kernel<DP>, QuerySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-        attention_queries_kernel<DP><<<(unsigned)cq, kThreads, QuerySmem<DP>::SIZE, st>>>(m.q, m.dout, m.k, m.v, m.dq, p, (int)q_tiles);
-        if (cudaGetLastError() != cudaSuccess) return UE5M3_ERR_CUDA;
+        const int r = launch(attention_queries_kernel<DP>, cq, QuerySmem<DP>::SIZE, ck > 0, st, m.q, m.dout, m.k, m.v, m.dq, p, (int)q_tiles);
+        if (r != UE5M3_OK) return r;
     }
     return UE5M3_OK;
 }
