@@ -371,9 +371,13 @@ typedef struct {
  *   [batch, heads, q_len] contiguous.
  *   head_dim a multiple of 8 up to 128, heads a multiple of kv_heads (UE5M3_ERR_SHAPE); pointers 16-byte aligned and
  *   strides multiples of 8 elements, positive where the dimension is larger than 1 (UE5M3_ERR_ALIGN).
+ *   workspace  device, ue5m3_attention_workspace_bytes(shape) bytes, 16-byte aligned; 0 bytes (and a null pointer) unless there
+ *              are few queries for many keys: the keys of a query are then shared out among several CTAs, whose results (binary32
+ *              o and lse) pass through the workspace and are joined by a second kernel in a fixed order.
  */
+UE5M3_API size_t ue5m3_attention_workspace_bytes(const ue5m3_attention_shape* shape);
 UE5M3_API int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, const ue5m3_heads* k,
-                              const ue5m3_heads* v, const ue5m3_heads* o, float* lse, void* stream);
+                              const ue5m3_heads* v, const ue5m3_heads* o, float* lse, void* workspace, void* stream);
 
 /*
  * Backward pass of ue5m3_attention: nothing of the forward pass but o and lse is kept, the probabilities are recomputed.

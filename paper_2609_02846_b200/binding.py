@@ -24,8 +24,8 @@ FPROP, DGRAD, WGRAD = 0, 1, 2
 SYMBOLS = ("ue5m3_sample_amax", "ue5m3_quantize", "ue5m3_quantize_dual", "ue5m3_quantize_current", "ue5m3_gemm",
            "ue5m3_gemm_probe_matched", "ue5m3_gemm_stall_selftest", "ue5m3_scales_bytes", "ue5m3_unswizzle_scales",
            "ue5m3_last_device_status", "ue5m3_status_string", "ue5m3_layer_norm", "ue5m3_layer_norm_backward_workspace_bytes",
-           "ue5m3_layer_norm_backward", "ue5m3_dropout_add", "ue5m3_attention", "ue5m3_attention_backward_workspace_bytes",
-           "ue5m3_attention_backward")
+           "ue5m3_layer_norm_backward", "ue5m3_dropout_add", "ue5m3_attention_workspace_bytes", "ue5m3_attention",
+           "ue5m3_attention_backward_workspace_bytes", "ue5m3_attention_backward")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libue5m3.so")
@@ -99,7 +99,9 @@ def _load() -> C.CDLL:
         L.ue5m3_dropout_add.argtypes = [vp, i64, vp, i64, ci, i64, i64, f32, u64, vp, i64, vp]
         shape, heads = C.POINTER(_AttentionShape), C.POINTER(_Heads)
         L.ue5m3_attention.restype = ci
-        L.ue5m3_attention.argtypes = [shape, heads, heads, heads, heads, vp, vp]
+        L.ue5m3_attention.argtypes = [shape, heads, heads, heads, heads, vp, vp, vp]
+        L.ue5m3_attention_workspace_bytes.restype = C.c_size_t
+        L.ue5m3_attention_workspace_bytes.argtypes = [shape]
         L.ue5m3_attention_backward_workspace_bytes.restype = C.c_size_t
         L.ue5m3_attention_backward_workspace_bytes.argtypes = [shape]
         L.ue5m3_attention_backward.restype = ci
@@ -573,8 +575,11 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     if out is None:
         out = q.new_empty(q.shape)
     lse = q.new_empty((shape.batch, shape.heads, shape.q_len), dtype=torch.float32)
-    _call(_load().ue5m3_attention, "ue5m3_attention", q, shape, _heads(q, q.shape, q), _heads(k, k.shape, q), _heads(v, k.shape, q),
-          _heads(out, q.shape, q), lse.data_ptr())
+    lib = _load()
+    need = lib.ue5m3_attention_workspace_bytes(shape)
+    ws = q.new_empty(need, dtype=torch.uint8) if need else None
+    _call(lib.ue5m3_attention, "ue5m3_attention", q, shape, _heads(q, q.shape, q), _heads(k, k.shape, q), _heads(v, k.shape, q),
+          _heads(out, q.shape, q), lse.data_ptr(), _ptr(ws))
     return out, lse
 
 

@@ -462,8 +462,16 @@ static int check_heads(const ue5m3_heads* t, int64_t batch, int64_t tokens, int6
     return UE5M3_OK;
 }
 
+// Binary32 o and lse of every part.
+size_t ue5m3_attention_workspace_bytes(const ue5m3_attention_shape* shape) {
+    if (check_attention_shape(shape) != UE5M3_OK) return 0;
+    const int parts = attention_splits(*shape);
+    if (parts <= 1) return 0;
+    return (size_t)parts * (size_t)shape->batch * (size_t)shape->heads * (size_t)shape->q_len * (size_t)(shape->head_dim + 4) * sizeof(float);
+}
+
 int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, const ue5m3_heads* k, const ue5m3_heads* v,
-                    const ue5m3_heads* o, float* lse, void* stream) {
+                    const ue5m3_heads* o, float* lse, void* workspace, void* stream) {
     const ApiRange range_("ue5m3_attention");
     int bad = check_attention_shape(shape);
     if (bad != UE5M3_OK) return bad;
@@ -473,10 +481,11 @@ int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, co
     for (const ue5m3_heads* t : {k, v})
         if ((bad = check_heads(t, s.batch, s.k_len, s.kv_heads)) != UE5M3_OK) return bad;
     if (!lse && s.batch * s.q_len > 0) return UE5M3_ERR_INVALID_ARG;
-    if (!aligned_to(lse, UE5M3_F32)) return UE5M3_ERR_ALIGN;
+    if (!workspace && attention_splits(s) > 1) return UE5M3_ERR_INVALID_ARG;
+    if (!aligned_to(lse, UE5M3_F32) || !aligned16(workspace)) return UE5M3_ERR_ALIGN;
     int sms = 0;
     if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
-    return launch_attention(s, *q, *k, *v, *o, lse, sms, (cudaStream_t)stream);
+    return launch_attention(s, *q, *k, *v, *o, lse, static_cast<float*>(workspace), (cudaStream_t)stream);
 }
 
 size_t ue5m3_attention_backward_workspace_bytes(const ue5m3_attention_shape* shape) {
@@ -499,7 +508,7 @@ int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_hea
     if (!aligned_to(lse, UE5M3_F32) || !aligned16(workspace)) return UE5M3_ERR_ALIGN;
     int sms = 0;
     if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
-    return launch_attention_backward(s, *dout, *q, *k, *v, *o, lse, *dq, *dk, *dv, static_cast<float*>(workspace), sms, (cudaStream_t)stream);
+    return launch_attention_backward(s, *dout, *q, *k, *v, *o, lse, *dq, *dk, *dv, static_cast<float*>(workspace), (cudaStream_t)stream);
 }
 
 int ue5m3_last_device_status(void) {

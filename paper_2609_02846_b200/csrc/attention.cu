@@ -14,6 +14,7 @@
 // memory by its softmax warps): p stays below 2^8, l and O in binary32 lose nothing, and o = O / l does not depend on m.
 // Tensor memory: S0, S1 (128 columns each), O0, O1 (head dimension columns each).
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
 #include "../../include/ue5m3.h"
@@ -47,7 +48,8 @@ __device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity, volati
     wait_inline(bar, parity, abort_flag, &g_attention_status, limit, true);
 }
 
-template <int DP>
+// PARTS: a CTA takes a share of the keys and leaves binary32 results for attention_join_kernel.
+template <int DP, bool PARTS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const AttentionParams p,
@@ -65,7 +67,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 
     // work of this CTA: heads fastest (heads that share keys run side by side), long query tiles first
     const int bh_count = p.batch * p.heads;
-    const int bh = blockIdx.x % bh_count, qt = q_tiles - 1 - blockIdx.x / bh_count;
+    const int part = PARTS ? (int)(blockIdx.x % p.parts) : 0, block = PARTS ? (int)(blockIdx.x / p.parts) : (int)blockIdx.x;
+    const int bh = block % bh_count, qt = q_tiles - 1 - block / bh_count;
     const int b = bh / p.heads, h = bh - b * p.heads, kvh = h / p.group;
     const int q0 = qt * 2 * BQ;
     const int keys = p.keys_of(b);
@@ -76,6 +79,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const int a = p.key_lo(r0), z = r0 < p.q_len ? p.key_hi(r1, keys) : 0;
         lo[t] = a / BK;
         hi[t] = z > a ? (z + BK - 1) / BK : lo[t];
+        if (PARTS) {                                      // this part's share of all key tiles
+            const int n = (p.k_len + BK - 1) / BK;
+            lo[t] = max(lo[t], (int)((int64_t)n * part / p.parts));
+            hi[t] = max(min(hi[t], (int)((int64_t)n * (part + 1) / p.parts)), lo[t]);
+        }
     }
     const bool on0 = hi[0] > lo[0], on1 = hi[1] > lo[1];
     const int first = on0 ? (on1 ? min(lo[0], lo[1]) : lo[0]) : lo[1];
@@ -99,6 +107,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_tmap(&map_q); prefetch_tmap(&map_k); prefetch_tmap(&map_v); prefetch_tmap(&map_o);
     }
+    if (PARTS) asm volatile("griddepcontrol.launch_dependents;");    // the joining kernel waits for this grid's end
     if (warp == 0) tmem_alloc1(smem_u32(tmem_slot), 512);
     tc_fence_before();
     __syncthreads();
@@ -324,9 +333,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             f2_unpack(l2, a, b2);
             l = a + b2;
         }
+        const int64_t lse_at = (((int64_t)part * p.batch + b) * p.heads + h) * p.q_len + row;
         if (row < p.q_len) {
             const float v = l > 0.0f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-            p.lse[((int64_t)b * p.heads + h) * p.q_len + row] = v;
+            (PARTS ? p.part_lse : p.lse)[lse_at] = v;
         }
         const int box0 = r0 + q * 32;                      // this warp's 32 rows
         bool any = n1 > n0;
@@ -334,7 +344,25 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             ok = wait(o_full + 8 * t, 0, abort_flag, p.wait_limit);
             tc_fence_after();
         }
-        if (ok && box0 < p.q_len) {
+        if (PARTS) {
+            const float f = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+            if (any && ok) {
+#pragma unroll 1
+                for (int c = 0; c < DP; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(to + c, o);
+                    tmem_ld_wait();
+                    if (row < p.q_len) {
+                        float* dst = p.part_o + lse_at * p.dim + c;
+#pragma unroll
+                        for (int v = 0; v < 32; v += 4)
+                            if (c + v < p.dim)
+                                *reinterpret_cast<float4*>(dst + v) = f == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f)
+                                    : make_float4(__uint_as_float(o[v]) * f, __uint_as_float(o[v + 1]) * f, __uint_as_float(o[v + 2]) * f, __uint_as_float(o[v + 3]) * f);
+                    }
+                }
+            }
+        } else if (ok && box0 < p.q_len) {
             // staged over this tile's Q (no MMA reads it any more, or it was never loaded)
             const float f = l > 0.0f || l != l ? 1.0f / l : 0.0f;
             const uint32_t stage = t * T::TILE + q * 4096;
@@ -372,23 +400,64 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     if (warp == 0) { tc_fence_after(); tmem_dealloc1(tmem, 512); }
 }
 
-template <int DP>
+// Joins the parts of a query:  lse = log sum exp lse_p,  o = sum exp(lse_p - lse) o_p, parts in order.  A warp per query; a part that
+// saw no key (lse = -inf) has written no o and is not read.
+__global__ void __launch_bounds__(256) attention_join_kernel(const AttentionParams p, __nv_bfloat16* o, const int64_t batch_stride,
+                                                             const int64_t token_stride, const int64_t head_stride) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int64_t rows = (int64_t)p.batch * p.heads * p.q_len, r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (r >= rows) return;
+    const int lane = threadIdx.x & 31;
+    float top = -INFINITY;
+    for (int k = 0; k < p.parts; ++k) top = fmaxf(top, p.part_lse[k * rows + r]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < p.parts; ++k) {
+        const float lse = p.part_lse[k * rows + r];
+        if (lse == -INFINITY) continue;
+        const float w = exp2f((lse - base) * 1.4426950408889634f);
+        sum += w;
+        if (lane * 4 < p.dim) {
+            const float4 v = *reinterpret_cast<const float4*>(p.part_o + (k * rows + r) * p.dim + lane * 4);
+            acc[0] = fmaf(w, v.x, acc[0]); acc[1] = fmaf(w, v.y, acc[1]); acc[2] = fmaf(w, v.z, acc[2]); acc[3] = fmaf(w, v.w, acc[3]);
+        }
+    }
+    const float f = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const int64_t i = r % p.q_len, bh = r / p.q_len, b = bh / p.heads, h = bh - b * p.heads;
+    if (lane * 4 < p.dim) {
+        uint2 w = make_uint2(0, 0);
+        if (f != 0.0f) w = make_uint2(pack_bf16x2(acc[0] * f, acc[1] * f), pack_bf16x2(acc[2] * f, acc[3] * f));
+        *reinterpret_cast<uint2*>(o + b * batch_stride + i * token_stride + h * head_stride + lane * 4) = w;
+    }
+    if (lane == 0) p.lse[r] = sum > 0.0f || sum != sum ? base + logf(sum) : -INFINITY;
+}
+
+template <int DP, bool PARTS>
 int run(const ue5m3_attention_shape& s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& o,
         const AttentionParams& p, cudaStream_t st) {
     using T = Tiles<DP>;
-    const int64_t q_tiles = (s.q_len + 2 * BQ - 1) / (2 * BQ), ctas = q_tiles * s.batch * s.heads;
+    const int64_t q_tiles = (s.q_len + 2 * BQ - 1) / (2 * BQ), ctas = q_tiles * s.batch * s.heads * p.parts;
     if (ctas > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
     static std::atomic<int> granted[64];
-    if (allow_smem(attention_kernel<DP>, T::SMEM, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-    attention_kernel<DP><<<(unsigned)ctas, kThreads, T::SMEM, st>>>(q, k, v, o, p, (int)q_tiles);
+    if (allow_smem(attention_kernel<DP, PARTS>, T::SMEM, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
+    attention_kernel<DP, PARTS><<<(unsigned)ctas, kThreads, T::SMEM, st>>>(q, k, v, o, p, (int)q_tiles);
     return cudaGetLastError() == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
 }  // namespace
 
+// Key tiles are shared out when the query tiles alone leave at least half of the 148 SMs idle, into as many parts as fill them but
+// none below two key tiles (a part costs its set-up, and its results a pass through memory).
+int attention_splits(const ue5m3_attention_shape& s) {
+    const int64_t ctas = (s.q_len + 2 * BQ - 1) / (2 * BQ) * s.batch * s.heads, tiles = (s.k_len + BK - 1) / BK;
+    if (ctas == 0 || ctas > 74) return 1;
+    const int64_t fill = 148 / ctas, most = tiles / 2;
+    const int64_t n = fill < most ? fill : most;
+    return n < 1 ? 1 : (int)n;
+}
+
 int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
-                     const ue5m3_heads& o, float* lse, int num_sms, cudaStream_t st) {
-    (void)num_sms;
+                     const ue5m3_heads& o, float* lse, float* workspace, cudaStream_t st) {
     if (s.batch == 0 || s.q_len == 0) return UE5M3_OK;
     CUtensorMap mq, mk, mv, mo;
     if (!make_heads_map(&mq, q, s.batch, s.q_len, s.heads, s.head_dim, BQ) || !make_heads_map(&mo, o, s.batch, s.q_len, s.heads, s.head_dim, 32))
@@ -398,7 +467,24 @@ int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const
         return UE5M3_ERR_CUDA;
     AttentionParams p = attention_params(s);
     p.lse = lse;
-    return s.head_dim <= 64 ? run<64>(s, mq, mk, mv, mo, p, st) : run<128>(s, mq, mk, mv, mo, p, st);
+    p.parts = attention_splits(s);
+    if (p.parts == 1) return s.head_dim <= 64 ? run<64, false>(s, mq, mk, mv, mo, p, st) : run<128, false>(s, mq, mk, mv, mo, p, st);
+    const int64_t rows = s.batch * s.heads * s.q_len;
+    p.part_o = workspace;
+    p.part_lse = workspace + p.parts * rows * s.head_dim;
+    const int r = s.head_dim <= 64 ? run<64, true>(s, mq, mk, mv, mo, p, st) : run<128, true>(s, mq, mk, mv, mo, p, st);
+    if (r != UE5M3_OK) return r;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((rows + 7) / 8));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attention_join_kernel, p, static_cast<__nv_bfloat16*>(o.data), o.batch_stride, o.token_stride, o.head_stride) == cudaSuccess
+               ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
 int read_and_clear_attention_status() {

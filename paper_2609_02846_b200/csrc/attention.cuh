@@ -220,6 +220,8 @@ struct AttentionParams {
     const float* lse2;                   // backward: -lse * log2(e) per query, padded to whole tiles (-inf: contributes nothing)
     const float* delta;                  // backward: -(dout . o) per query, padded
     int q_pad;
+    int dim, parts;                      // forward: head dimension; parts into which the key tiles are shared out
+    float* part_o; float* part_lse;      // forward with parts > 1: [parts][batch][heads][q_len][dim] and [..][q_len]
     long long wait_limit;
 
     __device__ __forceinline__ int keys_of(int b) const {
@@ -261,6 +263,8 @@ inline AttentionParams attention_params(const ue5m3_attention_shape& s) {
     p.scale_log2 = s.scale * 1.4426950408889634f;
     p.q_pad = (int)attention_padded_q(s.q_len);
     p.wait_limit = WAIT_LIMIT_CYCLES;
+    p.dim = (int)s.head_dim;
+    p.parts = 1;
     return p;
 }
 

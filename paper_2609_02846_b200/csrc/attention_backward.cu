@@ -633,8 +633,7 @@ int run(const ue5m3_attention_shape& s, const Maps& m, const AttentionParams& p,
 
 int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q, const ue5m3_heads& k,
                               const ue5m3_heads& v, const ue5m3_heads& o, const float* lse, const ue5m3_heads& dq,
-                              const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace, int num_sms, cudaStream_t st) {
-    (void)num_sms;
+                              const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace, cudaStream_t st) {
     if (s.batch == 0 || (s.q_len == 0 && s.k_len == 0)) return UE5M3_OK;
     Maps m;
     const int64_t B = s.batch, D = s.head_dim;

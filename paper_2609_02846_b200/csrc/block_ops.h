@@ -48,11 +48,12 @@ cudaError_t launch_dropout_add(const DropoutArgs& a, int dtype, int num_sms, cud
 
 // returns a UE5M3_* status
 int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
-                     const ue5m3_heads& o, float* lse, int num_sms, cudaStream_t st);
+                     const ue5m3_heads& o, float* lse, float* workspace, cudaStream_t st);
+int attention_splits(const ue5m3_attention_shape& s);      // parts into which the keys are shared out (1: none)
 int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q,
                               const ue5m3_heads& k, const ue5m3_heads& v, const ue5m3_heads& o, const float* lse,
                               const ue5m3_heads& dq, const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace,
-                              int num_sms, cudaStream_t st);
+                              cudaStream_t st);
 int read_and_clear_norm_status();                 // these three synchronise the device
 int read_and_clear_attention_status();
 int read_and_clear_attention_backward_status();

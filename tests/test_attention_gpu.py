@@ -233,3 +233,21 @@ def test_refusals():
         lib.attention_backward(do[:, :19], q, k, v, o, lse)
     with pytest.raises(ValueError):
         lib.attention(q.cpu(), k.cpu(), v.cpu())
+
+
+@pytest.mark.parametrize("Lq,Lk", [(1, 8192), (1, 300), (3, 2000), (130, 4097), (300, 3000)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_few_queries_for_many_keys(Lq, Lk, causal):
+    """The keys are shared out among CTAs and joined: one head and several, empty and short sequences, windows that leave parts
+    without a key, any strides of the output."""
+    check(*make(1, Lq, Lk, 1, 1, 128, seed=Lk), causal=causal)
+    q, k, v, do = make(3, Lq, Lk, 4, 2, 72, seed=Lk + 1)
+    lens = torch.tensor([Lk, 0, Lk // 3], dtype=torch.int32, device=DEV)
+    o, lse, _ = check(q, k, v, do, causal=causal, lens=lens)
+    out = torch.full((3, 4, Lq, 72), 3.0, dtype=torch.bfloat16, device=DEV).transpose(1, 2)
+    again = lib.attention(q, k, v, causal=causal, k_lens=lens, out=out)
+    assert torch.equal(again[0], o) and torch.equal(again[1], lse)
+    check(q, k, v, do, causal=True, left=200)
+    v2 = v.clone()
+    v2[2, Lk // 3:] = float("nan")
+    assert torch.equal(lib.attention(q, k, v2, causal=causal, k_lens=lens)[0], o)
