@@ -490,7 +490,11 @@ int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, co
 
 size_t ue5m3_attention_backward_workspace_bytes(const ue5m3_attention_shape* shape) {
     if (check_attention_shape(shape) != UE5M3_OK) return 0;
-    return (size_t)shape->batch * (size_t)shape->heads * (size_t)attention_padded_q(shape->q_len) * 2 * sizeof(float);
+    const int parts = attention_backward_splits(*shape);
+    const size_t heads = (size_t)shape->batch * (size_t)shape->heads;
+    // two numbers per query, padded to whole tiles; binary32 dq of every part
+    return (heads * (size_t)attention_padded_q(shape->q_len) * 2 +
+            (parts > 1 ? (size_t)parts * heads * (size_t)shape->q_len * (size_t)shape->head_dim : 0)) * sizeof(float);
 }
 
 int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_heads* dout, const ue5m3_heads* q, const ue5m3_heads* k,

@@ -220,8 +220,8 @@ struct AttentionParams {
     const float* lse2;                   // backward: -lse * log2(e) per query, padded to whole tiles (-inf: contributes nothing)
     const float* delta;                  // backward: -(dout . o) per query, padded
     int q_pad;
-    int dim, parts;                      // forward: head dimension; parts into which the key tiles are shared out
-    float* part_o; float* part_lse;      // forward with parts > 1: [parts][batch][heads][q_len][dim] and [..][q_len]
+    int dim, parts;                      // head dimension; parts into which the key tiles of a query are shared out
+    float* part_o; float* part_lse;      // parts > 1: o (backward: dq) [parts][batch][heads][q_len][dim]; forward: lse [..][q_len]
     long long wait_limit;
 
     __device__ __forceinline__ int keys_of(int b) const {

@@ -375,7 +375,8 @@ template <int DP> struct QuerySmem {
 };
 constexpr uint32_t COL_Q = 384, COL_DO = 448;                         // in place of the second accumulator
 
-template <int DP>
+// PARTS: a CTA takes a share of the keys and leaves a binary32 sum for attention_sum_kernel.
+template <int DP, bool PARTS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
                          const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -392,7 +393,8 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + M::BAR + 244);
 
     const int bh_count = p.batch * p.heads;
-    const int bh = blockIdx.x % bh_count, i0 = (q_tiles - 1 - (int)(blockIdx.x / bh_count)) * B128;
+    const int part = PARTS ? (int)(blockIdx.x % p.parts) : 0, block = PARTS ? (int)(blockIdx.x / p.parts) : (int)blockIdx.x;
+    const int bh = block % bh_count, i0 = (q_tiles - 1 - block / bh_count) * B128;
     const int b = bh / p.heads, h = bh - b * p.heads, kvh = h / p.group;
     const int keys = p.keys_of(b);
     const int i1 = min(i0 + B128, p.q_len) - 1;
@@ -400,6 +402,11 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     {
         const int a = p.key_lo(i0), z = p.key_hi(i1, keys);
         if (z > a) { lo = a / B128; hi = (z + B128 - 1) / B128; }
+        if (PARTS) {                                                  // this part's share of all key tiles
+            const int n = (p.k_len + B128 - 1) / B128;
+            lo = max(lo, (int)((int64_t)n * part / p.parts));
+            hi = max(min(hi, (int)((int64_t)n * (part + 1) / p.parts)), lo);
+        }
     }
     const int steps = hi - lo;
 
@@ -413,6 +420,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_tmap(&map_q); prefetch_tmap(&map_do); prefetch_tmap(&map_k); prefetch_tmap(&map_v); prefetch_tmap(&map_dq);
     }
+    if (PARTS) asm volatile("griddepcontrol.launch_dependents;");      // the adding kernel waits for this grid's end
     if (warp == 2) tmem_alloc1(smem_u32(tmem_slot), 512);
     tc_fence_before();
     __syncthreads();
@@ -582,7 +590,25 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             ok = wait(acc_full, 0, abort_flag, p.wait_limit);
             tc_fence_after();
         }
-        if (ok && g == 0 && i0 + q * 32 < p.q_len)
+        if (PARTS) {
+            if (ok && g == 0) {
+                float* dst = p.part_o + ((((int64_t)part * p.batch + b) * p.heads + h) * p.q_len + row) * p.dim;
+#pragma unroll 1
+                for (int c = 0; c < DP; c += 32) {
+                    uint32_t o[32];
+                    if (steps > 0) {
+                        tmem_ld32(lane_base + COL_ACC0 + c, o);
+                        tmem_ld_wait();
+                    }
+                    if (row < p.q_len)
+#pragma unroll
+                        for (int v = 0; v < 32; v += 4)
+                            if (c + v < p.dim)
+                                *reinterpret_cast<float4*>(dst + c + v) = steps == 0 ? make_float4(0.0f, 0.0f, 0.0f, 0.0f)
+                                    : make_float4(__uint_as_float(o[v]), __uint_as_float(o[v + 1]), __uint_as_float(o[v + 2]), __uint_as_float(o[v + 3]));
+                }
+            }
+        } else if (ok && g == 0 && i0 + q * 32 < p.q_len)
             store_accumulator<DP>(lane_base + COL_ACC0, smem_gen, smem, 0, q, lane, &map_dq, p.scale, steps == 0, i0 + q * 32, h, b);
         tc_fence_before();
     }
@@ -591,14 +617,32 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     asm volatile("griddepcontrol.wait;" ::: "memory");           // this grid ends after the keys kernel: what follows is behind both
 }
 
+// dq of a query from its parts, added in order: four values per thread.
+__global__ void __launch_bounds__(256) attention_sum_kernel(const AttentionParams p, __nv_bfloat16* dq, const int64_t batch_stride,
+                                                            const int64_t token_stride, const int64_t head_stride) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int per_row = p.dim / 4;
+    const int64_t rows = (int64_t)p.batch * p.heads * p.q_len, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= rows * per_row) return;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int k = 0; k < p.parts; ++k) {
+        const float4 v = reinterpret_cast<const float4*>(p.part_o)[k * rows * per_row + at];
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const int64_t r = at / per_row, i = r % p.q_len, bh = r / p.q_len, b = bh / p.heads, h = bh - b * p.heads;
+    *reinterpret_cast<uint2*>(dq + b * batch_stride + i * token_stride + h * head_stride + (at - r * per_row) * 4) =
+        make_uint2(pack_bf16x2(s.x * p.scale, s.y * p.scale), pack_bf16x2(s.z * p.scale, s.w * p.scale));
+}
+
 struct Maps { CUtensorMap q, dout, k, v, dq, dk, dv; };
 
 // A launch that may begin before the one in front of it has ended (`early`): the kernel says itself what it waits for.
 template <typename... Args>
-int launch(void (*kernel)(Args...), int64_t grid, int smem, bool early, cudaStream_t st, Args... args) {
+int launch(void (*kernel)(Args...), int64_t grid, int threads, int smem, bool early, cudaStream_t st, Args... args) {
+    if (grid > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -609,27 +653,45 @@ int launch(void (*kernel)(Args...), int64_t grid, int smem, bool early, cudaStre
     return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
+template <int DP, bool PARTS>
+int run_queries(const Maps& m, const AttentionParams& p, int64_t grid, int q_tiles, bool early, cudaStream_t st) {
+    static std::atomic<int> granted[64];
+    if (allow_smem(attention_queries_kernel<DP, PARTS>, QuerySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
+    return launch(attention_queries_kernel<DP, PARTS>, grid, kThreads, QuerySmem<DP>::SIZE, early, st, m.q, m.dout, m.k, m.v, m.dq, p, q_tiles);
+}
+
 template <int DP>
-int run(const ue5m3_attention_shape& s, const Maps& m, const AttentionParams& p, cudaStream_t st) {
+int run(const ue5m3_attention_shape& s, const ue5m3_heads& dq, const Maps& m, const AttentionParams& p, cudaStream_t st) {
     const int64_t k_tiles = (s.k_len + 127) / 128, q_tiles = (s.q_len + 127) / 128;
-    const int64_t ck = k_tiles * s.batch * s.kv_heads, cq = q_tiles * s.batch * s.heads;
-    if (ck > 0x7FFFFFFF || cq > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
+    const int64_t ck = k_tiles * s.batch * s.kv_heads, cq = q_tiles * s.batch * s.heads * p.parts;
     if (ck > 0) {
         static std::atomic<int> granted[64];
         if (allow_smem(attention_keys_kernel<DP>, KeySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-        const int r = launch(attention_keys_kernel<DP>, ck, KeySmem<DP>::SIZE, cq > 0, st, m.q, m.dout, m.k, m.v, m.dk, m.dv, p, (int)s.kv_heads);
+        const int r = launch(attention_keys_kernel<DP>, ck, kThreads, KeySmem<DP>::SIZE, cq > 0, st, m.q, m.dout, m.k, m.v, m.dk, m.dv, p, (int)s.kv_heads);
         if (r != UE5M3_OK) return r;
     }
-    if (cq > 0) {
-        static std::atomic<int> granted[64];
-        if (allow_smem(attention_queries_kernel<DP>, QuerySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-        const int r = launch(attention_queries_kernel<DP>, cq, QuerySmem<DP>::SIZE, ck > 0, st, m.q, m.dout, m.k, m.v, m.dq, p, (int)q_tiles);
-        if (r != UE5M3_OK) return r;
-    }
-    return UE5M3_OK;
+    if (cq == 0) return UE5M3_OK;
+    if (p.parts == 1) return run_queries<DP, false>(m, p, cq, (int)q_tiles, ck > 0, st);
+    const int r = run_queries<DP, true>(m, p, cq, (int)q_tiles, ck > 0, st);
+    if (r != UE5M3_OK) return r;
+    const int64_t rows = s.batch * s.heads * s.q_len;
+    return launch(attention_sum_kernel, (rows * (s.head_dim / 4) + 255) / 256, 256, 0, true, st, p, static_cast<__nv_bfloat16*>(dq.data),
+                  dq.batch_stride, dq.token_stride, dq.head_stride);
 }
 
 }  // namespace
+
+// As attention_splits, for the tiles of 128 queries of the queries kernel, but no part below 16 key tiles: this kernel runs into the
+// tail of the keys kernel, so SMs are rarely idle for it.  Whole against shared out, us of the whole backward pass: one query on
+// 8192 keys, 32 heads 147 / 89; 100 on 8192, 16 heads 129 / 82.  Smaller parts: 600 on 2000, 8 heads 32.4 / 36.0 (of 8 tiles), 1 on
+// 512, 8 heads 13.1 / 18.0 and 1000 on 1000, 8 heads 20.6 / 28.0 (of 2).
+int attention_backward_splits(const ue5m3_attention_shape& s) {
+    const int64_t ctas = (s.q_len + 127) / 128 * s.batch * s.heads, tiles = (s.k_len + 127) / 128;
+    if (ctas == 0 || ctas > 74) return 1;
+    const int64_t fill = 148 / ctas, most = tiles / 16;
+    const int64_t n = fill < most ? fill : most;
+    return n < 1 ? 1 : (int)n;
+}
 
 int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q, const ue5m3_heads& k,
                               const ue5m3_heads& v, const ue5m3_heads& o, const float* lse, const ue5m3_heads& dq,
@@ -656,12 +718,14 @@ int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads&
         r.rows = B * s.heads * p.q_pad;
         r.lse2 = workspace; r.delta = workspace + r.rows;
         p.lse2 = r.lse2; p.delta = r.delta;
+        p.parts = attention_backward_splits(s);
+        p.part_o = workspace + 2 * r.rows;
         const int64_t grid = (r.rows * 8 + 255) / 256;
         if (grid > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
         attention_rows_kernel<<<(unsigned)grid, 256, 0, st>>>(r);
         if (cudaGetLastError() != cudaSuccess) return UE5M3_ERR_CUDA;
     }
-    return D <= 64 ? run<64>(s, m, p, st) : run<128>(s, m, p, st);
+    return D <= 64 ? run<64>(s, dq, m, p, st) : run<128>(s, dq, m, p, st);
 }
 
 int read_and_clear_attention_backward_status() {

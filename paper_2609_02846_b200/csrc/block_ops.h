@@ -54,6 +54,7 @@ int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads&
                               const ue5m3_heads& k, const ue5m3_heads& v, const ue5m3_heads& o, const float* lse,
                               const ue5m3_heads& dq, const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace,
                               cudaStream_t st);
+int attention_backward_splits(const ue5m3_attention_shape& s);        // the same for the queries' gradient
 int read_and_clear_norm_status();                 // these three synchronise the device
 int read_and_clear_attention_status();
 int read_and_clear_attention_backward_status();
