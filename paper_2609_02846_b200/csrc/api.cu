@@ -422,6 +422,7 @@ int ue5m3_dropout_add(const void* x, int64_t ldx, const void* residual, int64_t 
     const bool empty = rows == 0 || cols == 0;
     if (!empty && (!x || !y)) return UE5M3_ERR_INVALID_ARG;
     if (too_large(rows, cols, ldx) || too_large(rows, cols, ldy) || (residual && too_large(rows, cols, ldr))) return UE5M3_ERR_UNSUPPORTED;
+    if (rows * cols > ((int64_t)1 << 40)) return UE5M3_ERR_UNSUPPORTED;      // blocks of 2048 elements are counted in 31 bits
     if (!aligned_to(x, dtype) || !aligned_to(residual, dtype) || !aligned_to(y, dtype)) return UE5M3_ERR_ALIGN;
     int sms = 0;
     const int bad = device_ready(sms);
@@ -433,7 +434,7 @@ int ue5m3_dropout_add(const void* x, int64_t ldx, const void* residual, int64_t 
     a.drop = t != 0;
     a.limit = t ? (t << 16) - 1u : 0u;                     // t = 65536: no draw is above it
     a.inv_keep = t < 65536 ? (float)(65536.0 / (65536.0 - (double)t)) : 0.0f;
-    return launch_dropout_add(a, dtype, sms, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+    return launch_dropout_add(a, dtype, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
 static int check_attention_shape(const ue5m3_attention_shape* s) {

@@ -44,7 +44,7 @@ struct DropoutArgs {
     float inv_keep;                       // 65536 / (65536 - t); 0 when t = 65536
     uint64_t seed;
 };
-cudaError_t launch_dropout_add(const DropoutArgs& a, int dtype, int num_sms, cudaStream_t st);
+cudaError_t launch_dropout_add(const DropoutArgs& a, int dtype, cudaStream_t st);
 
 // returns a UE5M3_* status
 int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,

@@ -2,9 +2,10 @@
 //
 //   y_i = residual_i + [r_i >= t] x_i 65536 / (65536 - t),   r_i = 16 bits of Philox4x32-7(key = seed, counter = (i >> 3, 0, 1, 0))
 //
-// One call of the generator serves a group of eight consecutive elements: 16 bytes of BF16, 32 bytes of FP32.  A thread takes a
-// group per trip; two groups are in flight per thread (loads first, then the generator, whose ~70 instructions hide behind
-// the memory latency of the other warps).  Bound by memory: 6 bytes per BF16 element with a residual, 4 without.
+// One call of the generator serves a group of eight consecutive elements: 16 bytes of BF16, 32 bytes of FP32.  A thread takes one
+// group, its loads first; the generator's ~70 instructions hide behind the memory latency of the other warps.
+// Bound by memory: 6 bytes per BF16 element with a residual, 4 without; without one the generator begins to show.  16384 x 4096 BF16
+// with a residual: 57.5 us, 7.0 TB/s (two groups per thread 57.8, a persistent grid 66.8); without 45.4 us, 5.9 TB/s (48.6, 56.2).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -71,73 +72,48 @@ __global__ void __launch_bounds__(kThreads) dropout_add_kernel(const DropoutPara
     const T* x = static_cast<const T*>(a.x);
     const T* res = static_cast<const T*>(a.residual);
     T* y = static_cast<T*>(a.y);
-    const int64_t n = a.rows * a.cols, step = (int64_t)gridDim.x * kThreads;
-    constexpr int U = LAYOUT == 2 ? 1 : 2;             // groups in flight per thread
-    for (int64_t g0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; g0 < p.groups; g0 += U * step) {
-        if constexpr (LAYOUT == 2) {
-            uint32_t w[4] = {};
-            if (DROP) draw8<SMALL>(p.keys, (uint64_t)g0, w);
-            int64_t row = g0 * 8 / a.cols, col = g0 * 8 - row * a.cols;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (g0 * 8 + j < n) {
-                    const float v = to_f32(x[row * a.ldx + col]);
-                    const float k = !DROP || kept(w, j, a.limit) ? v * a.inv_keep : 0.0f;
-                    put(y + row * a.ldy + col, res ? to_f32(res[row * a.ldr + col]) + k : k);
-                    if (++col == a.cols) { col = 0; ++row; }
-                }
-            }
-        } else {
-        Group8<T> vx[U], vr[U];
-        int64_t ox[U], orr[U], oy[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t g = g0 + u * step;
-            if (LAYOUT == 0) { ox[u] = orr[u] = oy[u] = g * 8; }
-            else {
-                const int64_t row = g * 8 / a.cols, col = g * 8 - row * a.cols;
-                ox[u] = row * a.ldx + col; orr[u] = row * a.ldr + col; oy[u] = row * a.ldy + col;
-            }
-            if (g * 8 + 8 <= n) {
-                vx[u].load(x + ox[u]);
-                if (res) vr[u].load(res + orr[u]);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t g = g0 + u * step;
-            if (g >= p.groups) break;
-            uint32_t w[4] = {};
-            if (DROP) draw8<SMALL>(p.keys, (uint64_t)g, w);
-            if (g * 8 + 8 <= n) {
-                float f[8], r[8];
-                vx[u].get(f);
-                if (res) vr[u].get(r);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float k = !DROP || kept(w, j, a.limit) ? f[j] * a.inv_keep : 0.0f;
-                    f[j] = res ? r[j] + k : k;
-                }
-                Group8<T>::store(y + oy[u], f);
-            } else {                                   // LAYOUT 0 only: the last, short group
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int64_t i = g * 8 + j;
-                    if (i >= n) break;
-                    const float k = !DROP || kept(w, j, a.limit) ? to_f32(x[i]) * a.inv_keep : 0.0f;
-                    put(y + i, res ? to_f32(res[i]) + k : k);
-                }
-            }
-        }
-        }
+    const int64_t g = (int64_t)blockIdx.x * kThreads + threadIdx.x, n = a.rows * a.cols;
+    if (g >= p.groups) return;
+    int64_t row = 0, col = g * 8;                      // where the group begins; LAYOUT 0: all one row
+    if (LAYOUT != 0) {
+        row = g * 8 / a.cols;
+        col = g * 8 - row * a.cols;
     }
+    if (LAYOUT == 2 || g * 8 + 8 > n) {
+        uint32_t w[4] = {};
+        if (DROP) draw8<SMALL>(p.keys, (uint64_t)g, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (g * 8 + j < n) {
+                const float v = to_f32(x[row * a.ldx + col]);
+                const float k = !DROP || kept(w, j, a.limit) ? v * a.inv_keep : 0.0f;
+                put(y + row * a.ldy + col, res ? to_f32(res[row * a.ldr + col]) + k : k);
+                ++col;
+                if (LAYOUT != 0 && col == a.cols) { col = 0; ++row; }
+            }
+        }
+        return;
+    }
+    Group8<T> vx, vr;
+    vx.load(x + row * a.ldx + col);
+    if (res) vr.load(res + row * a.ldr + col);
+    uint32_t w[4] = {};
+    if (DROP) draw8<SMALL>(p.keys, (uint64_t)g, w);
+    float f[8], r[8];
+    vx.get(f);
+    if (res) vr.get(r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float k = !DROP || kept(w, j, a.limit) ? f[j] * a.inv_keep : 0.0f;
+        f[j] = res ? r[j] + k : k;
+    }
+    Group8<T>::store(y + row * a.ldy + col, f);
 }
 
 template <typename T, int LAYOUT>
-cudaError_t run(const DropoutParams& p, int num_sms, cudaStream_t st) {
+cudaError_t run(const DropoutParams& p, cudaStream_t st) {
     const bool small = p.groups < ((int64_t)1 << 32);
-    const int64_t need = (p.groups + kThreads - 1) / kThreads, room = (int64_t)num_sms * 8;
-    const unsigned grid = (unsigned)(need < room ? need : room);
+    const unsigned grid = (unsigned)((p.groups + kThreads - 1) / kThreads);
     if (!p.a.drop) dropout_add_kernel<T, LAYOUT, false, true><<<grid, kThreads, 0, st>>>(p);
     else if (small) dropout_add_kernel<T, LAYOUT, true, true><<<grid, kThreads, 0, st>>>(p);
     else dropout_add_kernel<T, LAYOUT, true, false><<<grid, kThreads, 0, st>>>(p);
@@ -145,23 +121,23 @@ cudaError_t run(const DropoutParams& p, int num_sms, cudaStream_t st) {
 }
 
 template <typename T>
-cudaError_t run_of(const DropoutParams& p, int num_sms, cudaStream_t st) {
+cudaError_t run_of(const DropoutParams& p, cudaStream_t st) {
     const DropoutArgs& a = p.a;
     auto at16 = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
     const int64_t sz = sizeof(T);
     const bool ptrs = at16(a.x) && at16(a.y) && at16(a.residual);
     const bool contiguous = a.rows == 1 || (a.ldx == a.cols && a.ldy == a.cols && (!a.residual || a.ldr == a.cols));
-    if (ptrs && contiguous) return run<T, 0>(p, num_sms, st);
+    if (ptrs && contiguous) return run<T, 0>(p, st);
     const bool lds = (a.ldx * sz) % 16 == 0 && (a.ldy * sz) % 16 == 0 && (!a.residual || (a.ldr * sz) % 16 == 0);
-    if (ptrs && lds && a.cols % 8 == 0) return run<T, 1>(p, num_sms, st);
-    return run<T, 2>(p, num_sms, st);
+    if (ptrs && lds && a.cols % 8 == 0) return run<T, 1>(p, st);
+    return run<T, 2>(p, st);
 }
 
 }  // namespace
 
-cudaError_t launch_dropout_add(const DropoutArgs& a, int dtype, int num_sms, cudaStream_t st) {
+cudaError_t launch_dropout_add(const DropoutArgs& a, int dtype, cudaStream_t st) {
     DropoutParams p{a, philox_round_keys(a.seed), (a.rows * a.cols + 7) / 8};
-    return dtype == UE5M3_BF16 ? run_of<__nv_bfloat16>(p, num_sms, st) : run_of<float>(p, num_sms, st);
+    return dtype == UE5M3_BF16 ? run_of<__nv_bfloat16>(p, st) : run_of<float>(p, st);
 }
 
 }  // namespace ue5m3
