@@ -486,7 +486,7 @@ int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, co
     if (!aligned_to(lse, UE5M3_F32) || !aligned16(workspace)) return UE5M3_ERR_ALIGN;
     int sms = 0;
     if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
-    return launch_attention(s, *q, *k, *v, *o, lse, static_cast<float*>(workspace), (cudaStream_t)stream);
+    return launch_attention(s, *q, *k, *v, *o, lse, static_cast<float*>(workspace), sms, (cudaStream_t)stream);
 }
 
 size_t ue5m3_attention_backward_workspace_bytes(const ue5m3_attention_shape* shape) {

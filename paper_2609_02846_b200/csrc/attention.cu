@@ -48,12 +48,51 @@ __device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity, volati
     wait_inline(bar, parity, abort_flag, &g_attention_status, limit, true);
 }
 
-// PARTS: a CTA takes a share of the keys and leaves binary32 results for attention_join_kernel.
+struct OutputParams { __nv_bfloat16* o; int64_t batch_stride, token_stride, head_stride; };
+
+// One piece of work: two tiles of 128 queries of one head (PARTS: on a share of the keys).
+struct Item {
+    int b, h, part, q0, keys;
+    int lo[2], hi[2];                                     // key tiles of the two query tiles
+    int first, last;                                      // ... and of both together
+    __device__ __forceinline__ bool on(int t) const { return hi[t] > lo[t]; }
+};
+// Heads fastest (heads that share keys run side by side), long query tiles first.
+template <bool PARTS>
+__device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int q_tiles) {
+    Item w;
+    w.part = PARTS ? index % p.parts : 0;
+    const int bh_count = p.batch * p.heads, block = PARTS ? index / p.parts : index;
+    const int bh = block % bh_count;
+    w.b = bh / p.heads;
+    w.h = bh - w.b * p.heads;
+    w.q0 = (q_tiles - 1 - block / bh_count) * 2 * BQ;
+    w.keys = p.keys_of(w.b);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int r0 = w.q0 + t * BQ, r1 = min(r0 + BQ, p.q_len) - 1;
+        const int a = p.key_lo(r0), z = r0 < p.q_len ? p.key_hi(r1, w.keys) : 0;
+        w.lo[t] = a / BK;
+        w.hi[t] = z > a ? (z + BK - 1) / BK : w.lo[t];
+        if (PARTS) {                                      // this part's share of all key tiles
+            const int n = (p.k_len + BK - 1) / BK;
+            w.lo[t] = max(w.lo[t], (int)((int64_t)n * w.part / p.parts));
+            w.hi[t] = max(min(w.hi[t], (int)((int64_t)n * (w.part + 1) / p.parts)), w.lo[t]);
+        }
+    }
+    w.first = w.on(0) ? (w.on(1) ? min(w.lo[0], w.lo[1]) : w.lo[0]) : w.lo[1];
+    w.last = w.on(0) ? (w.on(1) ? max(w.hi[0], w.hi[1]) : w.hi[0]) : (w.on(1) ? w.hi[1] : w.first);
+    return w;
+}
+
+// Persistent: a CTA takes items in turn (forwards, then backwards, so that long and short ones even out) and every role walks them
+// by itself: the next item's Q is copied as soon as the last S of this one is done, its first S runs under this one's last softmax
+// and output.  With a CTA per item the SM stood still for 14,700 cycles at each (set-up, first copies, last product, output).
+// PARTS: binary32 results for attention_join_kernel.
 template <int DP, bool PARTS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                 const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const AttentionParams p,
-                 const int q_tiles) {
+                 const __grid_constant__ CUtensorMap map_v, const AttentionParams p, const OutputParams out, const int q_tiles, const int items) {
     using T = Tiles<DP>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -61,33 +100,12 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     const uint32_t ring = smem + 2 * T::TILE;
     const uint32_t bars = smem + T::SMEM_BAR;
     const uint32_t q_full = bars, kv_full = bars + 16, kv_empty = kv_full + 8 * T::PAIRS;
-    const uint32_t s_full = bars + 144, p_full = bars + 160 /* two halves per tile */, o_full = bars + 192, drain = bars + 208;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + T::SMEM_BAR + 224);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + T::SMEM_BAR + 228);
-
-    // work of this CTA: heads fastest (heads that share keys run side by side), long query tiles first
-    const int bh_count = p.batch * p.heads;
-    const int part = PARTS ? (int)(blockIdx.x % p.parts) : 0, block = PARTS ? (int)(blockIdx.x / p.parts) : (int)blockIdx.x;
-    const int bh = block % bh_count, qt = q_tiles - 1 - block / bh_count;
-    const int b = bh / p.heads, h = bh - b * p.heads, kvh = h / p.group;
-    const int q0 = qt * 2 * BQ;
-    const int keys = p.keys_of(b);
-    int lo[2], hi[2];                                     // key tiles of the two query tiles
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int r0 = q0 + t * BQ, r1 = min(r0 + BQ, p.q_len) - 1;
-        const int a = p.key_lo(r0), z = r0 < p.q_len ? p.key_hi(r1, keys) : 0;
-        lo[t] = a / BK;
-        hi[t] = z > a ? (z + BK - 1) / BK : lo[t];
-        if (PARTS) {                                      // this part's share of all key tiles
-            const int n = (p.k_len + BK - 1) / BK;
-            lo[t] = max(lo[t], (int)((int64_t)n * part / p.parts));
-            hi[t] = max(min(hi[t], (int)((int64_t)n * (part + 1) / p.parts)), lo[t]);
-        }
-    }
-    const bool on0 = hi[0] > lo[0], on1 = hi[1] > lo[1];
-    const int first = on0 ? (on1 ? min(lo[0], lo[1]) : lo[0]) : lo[1];
-    const int last = on0 ? (on1 ? max(hi[0], hi[1]) : hi[0]) : (on1 ? hi[1] : first);
+    const uint32_t s_full = bars + 96, p_full = bars + 112 /* two halves per tile */, o_full = bars + 144, q_empty = bars + 160, o_empty = bars + 176;
+    const uint32_t drain = bars + 192;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + T::SMEM_BAR + 200);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + T::SMEM_BAR + 204);
+    const int G = gridDim.x;
+    auto item_at = [&](int turn) { return turn * G + ((turn & 1) ? G - 1 - (int)blockIdx.x : (int)blockIdx.x); };
 
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -98,6 +116,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             mbar_init(p_full + 16 * t, 4);
             mbar_init(p_full + 16 * t + 8, 4);
             mbar_init(o_full + 8 * t, 1);
+            mbar_init(q_empty + 8 * t, 1);
+            mbar_init(o_empty + 8 * t, 4);
         }
         for (int s = 0; s < T::PAIRS; ++s) {
             mbar_init(kv_full + 8 * s, 2);                // V's copies and K's
@@ -105,7 +125,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        prefetch_tmap(&map_q); prefetch_tmap(&map_k); prefetch_tmap(&map_v); prefetch_tmap(&map_o);
+        prefetch_tmap(&map_q); prefetch_tmap(&map_k); prefetch_tmap(&map_v);
     }
     if (PARTS) asm volatile("griddepcontrol.launch_dependents;");    // the joining kernel waits for this grid's end
     if (warp == 0) tmem_alloc1(smem_u32(tmem_slot), 512);
@@ -118,40 +138,48 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     if (warp == 0) {
         // ------------------------------------------------------------------ copies
         if (lane == 0) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-                if (hi[t] > lo[t]) {
-                    mbar_expect_tx(q_full + 8 * t, T::TILE);
+            // Pair i of an item: V of key tile first + i - 1 (none in the first) and K of key tile first + i (none in the last).  Pairs are
+            // numbered through all items; pair n's tiles are number 2n - 1 and 2n of the ring, of which the one takes the place of pair
+            // n - PAIRS's K, the other that of the next pair's V.
+            auto emptied = [&](int pair) { return pair < 0 || wait(kv_empty + 8 * (pair % T::PAIRS), (pair / T::PAIRS) & 1, abort_flag, p.wait_limit); };
+            int n = 0, q_uses[2] = {0, 0};
+            bool go = true;
+            for (int turn = 0, index; go && (index = item_at(turn)) < items; ++turn) {
+                const Item w = item_of<PARTS>(p, index, q_tiles);
+                const int kvh = w.h / p.group, pairs = w.last > w.first ? w.last - w.first + 1 : 0;
+                auto load = [&](int tile_n, const CUtensorMap* m, uint32_t bar, int tile) {
+                    mbar_expect_tx(bar, T::TILE);
 #pragma unroll
                     for (int c = 0; c < T::PANELS; ++c)
-                        tma_load_4d(smem + t * T::TILE + c * T::PANEL, &map_q, q_full + 8 * t, c * 64, q0 + t * BQ, h, b);
-                }
-            // Pair i: V of key tile first + i - 1 (none in the first) and K of key tile first + i (none in the last).  Its tiles are
-            // number 2i - 1 and 2i of the ring; the one takes the place of pair i - PAIRS's K, the other that of the next pair's V.
-            const int pairs = last > first ? last - first + 1 : 0;
-            auto emptied = [&](int pair) { return pair < 0 || wait(kv_empty + 8 * (pair % T::PAIRS), (pair / T::PAIRS) & 1, abort_flag, p.wait_limit); };
-            auto load = [&](int n, const CUtensorMap* m, uint32_t bar, int tile) {
-                mbar_expect_tx(bar, T::TILE);
+                        tma_load_4d(ring + (tile_n % T::RING) * T::TILE + c * T::PANEL, m, bar, c * 64, tile * BK, kvh, w.b);
+                };
 #pragma unroll
-                for (int c = 0; c < T::PANELS; ++c)
-                    tma_load_4d(ring + (n % T::RING) * T::TILE + c * T::PANEL, m, bar, c * 64, tile * BK, kvh, b);
-            };
-            int i = 0;
-            for (bool go = true; go && i < pairs; ++i) {
-                const uint32_t bar = kv_full + 8 * (i % T::PAIRS);
-                if (!emptied(i - T::PAIRS)) break;
-                if (i > 0) load(2 * i - 1, &map_v, bar, first + i - 1);
-                else mbar_arrive(bar);
-                go = emptied(i - T::PAIRS + 1);
-                if (go && i + 1 < pairs) load(2 * i, &map_k, bar, first + i);
-                else mbar_arrive(bar);
+                for (int t = 0; t < 2; ++t)
+                    if (go && w.on(t)) {
+                        go = wait(q_empty + 8 * t, (q_uses[t] & 1) ^ 1, abort_flag, p.wait_limit);
+                        if (!go) break;
+                        ++q_uses[t];
+                        mbar_expect_tx(q_full + 8 * t, T::TILE);
+#pragma unroll
+                        for (int c = 0; c < T::PANELS; ++c)
+                            tma_load_4d(smem + t * T::TILE + c * T::PANEL, &map_q, q_full + 8 * t, c * 64, w.q0 + t * BQ, w.h, w.b);
+                    }
+                for (int i = 0; go && i < pairs; ++i, ++n) {
+                    const uint32_t bar = kv_full + 8 * (n % T::PAIRS);
+                    if (!(go = emptied(n - T::PAIRS))) break;
+                    if (i > 0) load(2 * n - 1, &map_v, bar, w.first + i - 1);
+                    else mbar_arrive(bar);
+                    go = emptied(n - T::PAIRS + 1);
+                    if (go && i + 1 < pairs) load(2 * n, &map_k, bar, w.first + i);
+                    else mbar_arrive(bar);
+                }
             }
             // copies in flight land before the shared memory goes away, whatever the other roles did
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-                if (hi[t] > lo[t]) drain_wait(q_full + 8 * t, 0, abort_flag, p.wait_limit);
-            for (int back = 0; back < T::PAIRS && back < i; ++back) {
-                const int j = i - 1 - back;
+                if (q_uses[t] > 0) drain_wait(q_full + 8 * t, (q_uses[t] - 1) & 1, abort_flag, p.wait_limit);
+            for (int back = 0; back < T::PAIRS && back < n; ++back) {
+                const int j = n - 1 - back;
                 drain_wait(kv_full + 8 * (j % T::PAIRS), (j / T::PAIRS) & 1, abort_flag, p.wait_limit);
             }
         }
@@ -168,11 +196,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             return ok;
         };
         uint32_t slot = 0, phase = 0, v_tile = T::RING - 1;          // of the next pair: barrier, and ring tile of its V
-        auto next_pair = [&](int j) {                      // waits for the pair with V of key tile j
+        auto next_pair = [&](const Item& w, int j) {       // waits for the pair with V of key tile j
             wait_all(kv_full + 8 * slot, phase);
             if (++slot == T::PAIRS) { slot = 0; phase ^= 1; }
-            const int valid = keys - j * BK;               // rows of this V tile that exist
-            if (p.k_lens && j >= first && valid < BK) {
+            const int valid = w.keys - j * BK;             // rows of this V tile that exist
+            if (p.k_lens && j >= w.first && valid < BK) {
                 // values behind the sequence's end may hold anything (0 * NaN is NaN): they become zeros
                 for (int i = valid * (DP / 8) + lane; i < BK * (DP / 8); i += 32) {
                     const int r = i / (DP / 8), c = i % (DP / 8);
@@ -199,46 +227,59 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             }
             __syncwarp();
         };
-        uint32_t np[2] = {0, 0};                           // probability tiles consumed per query tile
-        auto issue_o = [&](int t, uint32_t tile, int half, bool end) {     // O_t += P_t V, 64 keys
+        uint32_t np[2] = {0, 0}, uses[2] = {0, 0};         // probability tiles consumed and items begun, per query tile
+        auto issue_o = [&](int t, uint32_t tile, int half, bool begin, bool end) {     // O_t (+)= P_t V, 64 keys
             if (!wait_all(p_full + 16 * t + 8 * half, np[t] & 1)) return;
             tc_fence_after();
             if (elected) {
                 const uint64_t vd = vd0 + tile * (T::TILE >> 4);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    umma1_ts(tm + 2 * BK + t * 128, tm + t * BK + half * 32 + k * 8, vd + (half * 4 + k) * (2048 >> 4), id_o, np[t] != 0 || half != 0 || k != 0);
+                    umma1_ts(tm + 2 * BK + t * 128, tm + t * BK + half * 32 + k * 8, vd + (half * 4 + k) * (2048 >> 4), id_o, !begin || half != 0 || k != 0);
                 if (end) umma1_commit(o_full + 8 * t);
             }
             __syncwarp();
         };
-        if (on0) wait_all(q_full, 0);
-        if (on1) wait_all(q_full + 8, 0);
         uint32_t done = 0;                                 // barrier of the pair whose products are all issued
         auto release = [&]() {
             if (elected) umma1_commit(kv_empty + 8 * done);
             if (++done == T::PAIRS) done = 0;
         };
-        if (last > first && ok) {
-            const uint32_t k0 = k_tile(next_pair(first - 1));
+        for (int turn = 0, index; ok && (index = item_at(turn)) < items; ++turn) {
+            const Item w = item_of<PARTS>(p, index, q_tiles);
+            if (w.last <= w.first) continue;
+            const uint32_t k0 = k_tile(next_pair(w, w.first - 1));
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-                if (ok && hi[t] > lo[t] && lo[t] == first) issue_s(t, k0);
-            release();
-        }
-        for (int j = first; j < last && ok; ++j) {
-            const uint32_t v = next_pair(j), k = k_tile(v);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const bool here = j >= lo[t] && j < hi[t], more = j + 1 < hi[t] && j + 1 >= lo[t];
-                if (here && ok) {
-                    issue_o(t, v, 0, false);
-                    if (ok) issue_o(t, v, 1, !more);
-                    ++np[t];
+                if (ok && w.on(t)) {
+                    wait_all(q_full + 8 * t, uses[t] & 1);
+                    ++uses[t];
+                    if (ok && w.lo[t] == w.first) {
+                        issue_s(t, k0);
+                        if (w.hi[t] == w.first + 1 && elected) umma1_commit(q_empty + 8 * t);
+                    }
                 }
-                if (more && ok) issue_s(t, k);
-            }
             release();
+            for (int j = w.first; j < w.last && ok; ++j) {
+                const uint32_t v = next_pair(w, j), k = k_tile(v);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const bool here = j >= w.lo[t] && j < w.hi[t], more = j + 1 < w.hi[t] && j + 1 >= w.lo[t];
+                    if (here && ok) {
+                        const bool begin = j == w.lo[t];
+                        // the item before has read its O_t out
+                        if (begin && !wait_all(o_empty + 8 * t, uses[t] & 1)) break;
+                        issue_o(t, v, 0, begin, false);
+                        if (ok) issue_o(t, v, 1, false, !more);
+                        ++np[t];
+                    }
+                    if (more && ok) {
+                        issue_s(t, k);
+                        if (j + 2 == w.hi[t] && elected) umma1_commit(q_empty + 8 * t);       // the last S of this tile: Q is free behind it
+                    }
+                }
+                release();
+            }
         }
         if (elected) {
             umma1_commit(drain);
@@ -249,17 +290,21 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         registers_many();
         // ------------------------------------------------------------------ softmax and output of one query tile
         const int t = (warp - 4) >> 2, q = warp & 3;       // tile, tensor-memory lane quarter
-        const int r0 = q0 + t * BQ, row = r0 + q * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
         const uint32_t ts = lane_base + t * BK, to = lane_base + 2 * BK + t * 128;
-        const int key_lo = p.key_lo(row), key_hi = p.key_hi(row, keys);
-        const int n0 = t == 0 ? lo[0] : lo[1], n1 = t == 0 ? hi[0] : hi[1];
+        const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2);
+        uint32_t n = 0, uses = 0;                          // S tiles and items of this query tile so far
+        bool ok = true;
+        for (int turn = 0, index; ok && (index = item_at(turn)) < items; ++turn) {
+        const Item w = item_of<PARTS>(p, index, q_tiles);
+        const int r0 = w.q0 + t * BQ, row = r0 + q * 32 + lane;
+        const int key_lo = p.key_lo(row), key_hi = p.key_hi(row, w.keys);
+        const int n0 = t == 0 ? w.lo[0] : w.lo[1], n1 = t == 0 ? w.hi[0] : w.hi[1];
         // key tiles [plain_lo, plain_hi) are seen whole by every row of the tile
         const int plain_lo = p.left >= 0 ? (p.key_lo(r0 + BQ - 1) + BK - 1) / BK : 0;
-        const int plain_hi = max(p.key_hi(r0, keys), 0) / BK;
+        const int plain_hi = max(p.key_hi(r0, w.keys), 0) / BK;
         float m = -INFINITY;
         f32x2 l2 = 0;
-        const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2);
         // raises the running maximum to at least `top`: l and (after the first tile) O are scaled down.  S of the current tile was
         // issued after the previous P V, so O is at rest.
         auto raise = [&](float top, bool first_tile) {
@@ -285,8 +330,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             __syncwarp();
             if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * half);
         };
-        bool ok = true;
-        uint32_t n = 0;
         for (int j = n0; j < n1; ++j, ++n) {
             if (!(ok = wait(s_full + 8 * t, n & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
@@ -312,7 +355,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             }
             const float tile_top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
             if (__any_sync(0xFFFFFFFFu, tile_top > m + kRaise)) {
-                raise(tile_top, n == 0);
+                raise(tile_top, j == n0);
                 base = m == -INFINITY ? 0.0f : m;
                 sum = 0;
                 uint32_t again[64];                                    // S still stands in tensor memory
@@ -333,66 +376,55 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             f2_unpack(l2, a, b2);
             l = a + b2;
         }
-        const int64_t lse_at = (((int64_t)part * p.batch + b) * p.heads + h) * p.q_len + row;
-        if (row < p.q_len) {
-            const float v = l > 0.0f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-            (PARTS ? p.part_lse : p.lse)[lse_at] = v;
-        }
-        const int box0 = r0 + q * 32;                      // this warp's 32 rows
-        bool any = n1 > n0;
+        const int64_t lse_at = (((int64_t)w.part * p.batch + w.b) * p.heads + w.h) * p.q_len + row;
+        const bool some = l > 0.0f || l != l;              // this query sees a key
+        if (row < p.q_len) (PARTS ? p.part_lse : p.lse)[lse_at] = some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        const bool any = n1 > n0;
         if (any && ok) {
-            ok = wait(o_full + 8 * t, 0, abort_flag, p.wait_limit);
+            ok = wait(o_full + 8 * t, uses & 1, abort_flag, p.wait_limit);
+            ++uses;
             tc_fence_after();
         }
-        if (PARTS) {
-            const float f = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-            if (any && ok) {
+        if (!ok) break;
+        const float f = some ? 1.0f / l : 0.0f;
+        __nv_bfloat16* dst = out.o + w.b * out.batch_stride + row * out.token_stride + w.h * out.head_stride;
 #pragma unroll 1
-                for (int c = 0; c < DP; c += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(to + c, o);
-                    tmem_ld_wait();
-                    if (row < p.q_len) {
-                        float* dst = p.part_o + lse_at * p.dim + c;
-#pragma unroll
-                        for (int v = 0; v < 32; v += 4)
-                            if (c + v < p.dim)
-                                *reinterpret_cast<float4*>(dst + v) = f == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f)
-                                    : make_float4(__uint_as_float(o[v]) * f, __uint_as_float(o[v + 1]) * f, __uint_as_float(o[v + 2]) * f, __uint_as_float(o[v + 3]) * f);
-                    }
+        for (int c = 0; c < DP; c += 32) {
+            uint32_t o[32];
+            if (any) {
+                tmem_ld32(to + c, o);
+                tmem_ld_wait();
+                if (c + 32 >= DP) {
+                    // O has been read: the next item's first product may overwrite it
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(o_empty + 8 * t);
                 }
             }
-        } else if (ok && box0 < p.q_len) {
-            // staged over this tile's Q (no MMA reads it any more, or it was never loaded)
-            const float f = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-            const uint32_t stage = t * T::TILE + q * 4096;
-#pragma unroll 1
-            for (int c = 0; c < T::PANELS; ++c) {
-                uint8_t* mine = smem_gen + stage + c * T::PANEL + lane * 128;
+            if (!any || !some) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t o[32];
-                    if (any) {
-                        tmem_ld32(to + c * 64 + half * 32, o);
-                        tmem_ld_wait();
-                    }
+                for (int v = 0; v < 32; ++v) o[v] = 0u;
+            }
+            if (row < p.q_len && (!PARTS || any)) {                   // a part without keys: lse says so, o is not read
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        uint4 w = make_uint4(0, 0, 0, 0);
-                        if (any && f != 0.0f) {
-                            w.x = pack_bf16x2(__uint_as_float(o[8 * v]) * f, __uint_as_float(o[8 * v + 1]) * f);
-                            w.y = pack_bf16x2(__uint_as_float(o[8 * v + 2]) * f, __uint_as_float(o[8 * v + 3]) * f);
-                            w.z = pack_bf16x2(__uint_as_float(o[8 * v + 4]) * f, __uint_as_float(o[8 * v + 5]) * f);
-                            w.w = pack_bf16x2(__uint_as_float(o[8 * v + 6]) * f, __uint_as_float(o[8 * v + 7]) * f);
+                for (int v = 0; v < 4; ++v) {
+                    float x[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(o[8 * v + k]) * f;
+                    if (c + 8 * v < p.dim) {
+                        if constexpr (PARTS) {
+                            float4* to4 = reinterpret_cast<float4*>(p.part_o + lse_at * p.dim + c + 8 * v);
+                            to4[0] = make_float4(x[0], x[1], x[2], x[3]);
+                            to4[1] = make_float4(x[4], x[5], x[6], x[7]);
+                        } else {
+                            *reinterpret_cast<uint4*>(dst + c + 8 * v) =
+                                make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
                         }
-                        *reinterpret_cast<uint4*>(mine + (((half * 4 + v) ^ (lane & 7)) << 4)) = w;
                     }
                 }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) tma_store_4d(&map_o, smem + stage + c * T::PANEL, c * 64, box0, h, b);
             }
-            if (lane == 0) tma_store_wait_all();
+            __syncwarp();
+        }
         }
         tc_fence_before();
     }
@@ -433,14 +465,14 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionPara
 }
 
 template <int DP, bool PARTS>
-int run(const ue5m3_attention_shape& s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& o,
-        const AttentionParams& p, cudaStream_t st) {
+int run(const ue5m3_attention_shape& s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
+        const OutputParams& o, int num_sms, cudaStream_t st) {
     using T = Tiles<DP>;
-    const int64_t q_tiles = (s.q_len + 2 * BQ - 1) / (2 * BQ), ctas = q_tiles * s.batch * s.heads * p.parts;
-    if (ctas > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
+    const int64_t q_tiles = (s.q_len + 2 * BQ - 1) / (2 * BQ), items = q_tiles * s.batch * s.heads * p.parts;
+    if (items > 0x7FFFFFFF - 2 * num_sms) return UE5M3_ERR_UNSUPPORTED;
     static std::atomic<int> granted[64];
     if (allow_smem(attention_kernel<DP, PARTS>, T::SMEM, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-    attention_kernel<DP, PARTS><<<(unsigned)ctas, kThreads, T::SMEM, st>>>(q, k, v, o, p, (int)q_tiles);
+    attention_kernel<DP, PARTS><<<(unsigned)(items < num_sms ? items : num_sms), kThreads, T::SMEM, st>>>(q, k, v, p, o, (int)q_tiles, (int)items);
     return cudaGetLastError() == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
@@ -459,22 +491,22 @@ int attention_splits(const ue5m3_attention_shape& s) {
 }
 
 int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
-                     const ue5m3_heads& o, float* lse, float* workspace, cudaStream_t st) {
+                     const ue5m3_heads& o, float* lse, float* workspace, int num_sms, cudaStream_t st) {
     if (s.batch == 0 || s.q_len == 0) return UE5M3_OK;
-    CUtensorMap mq, mk, mv, mo;
-    if (!make_heads_map(&mq, q, s.batch, s.q_len, s.heads, s.head_dim, BQ) || !make_heads_map(&mo, o, s.batch, s.q_len, s.heads, s.head_dim, 32))
-        return UE5M3_ERR_CUDA;
+    CUtensorMap mq, mk, mv;
+    if (!make_heads_map(&mq, q, s.batch, s.q_len, s.heads, s.head_dim, BQ)) return UE5M3_ERR_CUDA;
     if (s.k_len == 0) mk = mv = mq;                        // no key tile is ever read
     else if (!make_heads_map(&mk, k, s.batch, s.k_len, s.kv_heads, s.head_dim, BK) || !make_heads_map(&mv, v, s.batch, s.k_len, s.kv_heads, s.head_dim, BK))
         return UE5M3_ERR_CUDA;
     AttentionParams p = attention_params(s);
     p.lse = lse;
     p.parts = attention_splits(s);
-    if (p.parts == 1) return s.head_dim <= 64 ? run<64, false>(s, mq, mk, mv, mo, p, st) : run<128, false>(s, mq, mk, mv, mo, p, st);
+    const OutputParams out{static_cast<__nv_bfloat16*>(o.data), o.batch_stride, o.token_stride, o.head_stride};
+    if (p.parts == 1) return s.head_dim <= 64 ? run<64, false>(s, mq, mk, mv, p, out, num_sms, st) : run<128, false>(s, mq, mk, mv, p, out, num_sms, st);
     const int64_t rows = s.batch * s.heads * s.q_len;
     p.part_o = workspace;
     p.part_lse = workspace + p.parts * rows * s.head_dim;
-    const int r = s.head_dim <= 64 ? run<64, true>(s, mq, mk, mv, mo, p, st) : run<128, true>(s, mq, mk, mv, mo, p, st);
+    const int r = s.head_dim <= 64 ? run<64, true>(s, mq, mk, mv, p, out, num_sms, st) : run<128, true>(s, mq, mk, mv, p, out, num_sms, st);
     if (r != UE5M3_OK) return r;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((rows + 7) / 8));

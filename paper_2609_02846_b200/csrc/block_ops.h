@@ -48,7 +48,7 @@ cudaError_t launch_dropout_add(const DropoutArgs& a, int dtype, cudaStream_t st)
 
 // returns a UE5M3_* status
 int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
-                     const ue5m3_heads& o, float* lse, float* workspace, cudaStream_t st);
+                     const ue5m3_heads& o, float* lse, float* workspace, int num_sms, cudaStream_t st);
 int attention_splits(const ue5m3_attention_shape& s);      // parts into which the keys are shared out (1: none)
 int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q,
                               const ue5m3_heads& k, const ue5m3_heads& v, const ue5m3_heads& o, const float* lse,
