@@ -338,7 +338,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, s + c * 32);
             tmem_ld_wait();
             const bool masked = j < plain_lo || j >= plain_hi;
-            if (masked) hide_scores<128>(s, j * BK - key_lo, key_hi - key_lo);
+            const int from = key_lo - j * BK, to = key_hi - j * BK;    // columns of this tile that the row sees
+            if (masked) hide_scores<128>(s, from, to, p.left >= 0);
             uint32_t pk[32];
             float base = m == -INFINITY ? 0.0f : m;
             // The first half's exponentials are taken against the maximum so far, while this tile's is being found: it raises the
@@ -362,7 +363,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 tmem_ld32(ts, again);
                 tmem_ld32(ts + 32, again + 32);
                 tmem_ld_wait();
-                if (masked) hide_scores<64>(again, j * BK - key_lo, key_hi - key_lo);
+                if (masked) hide_scores<64>(again, from, to, p.left >= 0);
                 exp_scores<32>(again, pk, sum, c2, f2_pack(-base, -base));
             }
             publish(0, pk);

@@ -91,12 +91,16 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// Scores of pairs that do not exist become -inf: only columns with 0 <= base + column < width stay.
+// Scores of pairs that do not exist become -inf: only columns from <= column < to stay (`from` is looked at where it can be above 0).
 template <int N>
-__device__ __forceinline__ void hide_scores(uint32_t* s, int base, int width) {
+__device__ __forceinline__ void hide_scores(uint32_t* s, int from, int to, bool window) {
+    if (window) {
 #pragma unroll
-    for (int c = 0; c < N; ++c)
-        if (!(base + c >= 0 && base + c < width)) s[c] = 0xFF800000u;
+        for (int c = 0; c < N; ++c) s[c] = c >= from && c < to ? s[c] : 0xFF800000u;
+    } else {
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] = c < to ? s[c] : 0xFF800000u;
+    }
 }
 __device__ __forceinline__ f32x2 ex2_pair(f32x2 x) {
     float a, b;
@@ -120,14 +124,14 @@ __device__ __forceinline__ void exp_scores(const uint32_t* s, uint32_t* packed, 
         packed[i] = pack_pair(x);
     }
 }
-// Probabilities of pairs that do not exist become zero: only columns with 0 <= base + column < width stay.
+// Probabilities of pairs that do not exist become zero: only columns from <= column < to stay.
 template <int N>
-__device__ __forceinline__ void hide_pairs(f32x2* p, int base, int width) {
+__device__ __forceinline__ void hide_pairs(f32x2* p, int from, int to) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         float a, b;
         f2_unpack(p[i], a, b);
-        p[i] = f2_pack(base + 2 * i >= 0 && base + 2 * i < width ? a : 0.0f, base + 2 * i + 1 >= 0 && base + 2 * i + 1 < width ? b : 0.0f);
+        p[i] = f2_pack(2 * i >= from && 2 * i < to ? a : 0.0f, 2 * i + 1 >= from && 2 * i + 1 < to ? b : 0.0f);
     }
 }
 // x where p is not zero (0 * NaN would be NaN where a pair does not exist)

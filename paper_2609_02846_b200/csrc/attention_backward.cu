@@ -314,7 +314,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     pr[c / 2] = ex2_pair(f2_fma(pair_of(s + c), c2, e.x));
                     pr[c / 2 + 1] = ex2_pair(f2_fma(pair_of(s + c + 2), c2, e.y));
                 }
-                if (!plain) hide_pairs<16>(pr + half * 16, base + half * 32, width);
+                if (!plain) hide_pairs<16>(pr + half * 16, -base - half * 32, width - base - half * 32);
                 uint32_t pk[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) pk[i] = pack_pair(pr[half * 16 + i]);
@@ -563,7 +563,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             f32x2 pr[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) pr[i] = ex2_pair(f2_fma(pair_of(s + 2 * i), c2, nl2));
-            if (!plain) hide_pairs<32>(pr, base, width);
+            if (!plain) hide_pairs<32>(pr, -base, width - base);
             if (!(ok = wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t pk[32];
