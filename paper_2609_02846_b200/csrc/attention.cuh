@@ -124,14 +124,31 @@ __device__ __forceinline__ void exp_scores(const uint32_t* s, uint32_t* packed, 
         packed[i] = pack_pair(x);
     }
 }
-// Probabilities of pairs that do not exist become zero: only columns from <= column < to stay.
+// Probabilities of pairs that do not exist become zero: only columns from <= column < to stay.  `lower`, `upper`: which of the two
+// bounds the mask has at all.
 template <int N>
-__device__ __forceinline__ void hide_pairs(f32x2* p, int from, int to) {
+__device__ __forceinline__ void hide_pairs(f32x2* p, int from, int to, bool lower, bool upper) {
+    if (lower && upper) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float a, b;
-        f2_unpack(p[i], a, b);
-        p[i] = f2_pack(2 * i >= from && 2 * i < to ? a : 0.0f, 2 * i + 1 >= from && 2 * i + 1 < to ? b : 0.0f);
+        for (int i = 0; i < N; ++i) {
+            float a, b;
+            f2_unpack(p[i], a, b);
+            p[i] = f2_pack(2 * i >= from && 2 * i < to ? a : 0.0f, 2 * i + 1 >= from && 2 * i + 1 < to ? b : 0.0f);
+        }
+    } else if (upper) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float a, b;
+            f2_unpack(p[i], a, b);
+            p[i] = f2_pack(2 * i < to ? a : 0.0f, 2 * i + 1 < to ? b : 0.0f);
+        }
+    } else if (lower) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float a, b;
+            f2_unpack(p[i], a, b);
+            p[i] = f2_pack(2 * i >= from ? a : 0.0f, 2 * i + 1 >= from ? b : 0.0f);
+        }
     }
 }
 // x where p is not zero (0 * NaN would be NaN where a pair does not exist)

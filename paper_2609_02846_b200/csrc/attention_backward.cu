@@ -290,6 +290,8 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         // query tiles [plain_lo, plain_hi) see every key of this tile
         const int plain_lo = j0 + B128 <= keys ? (p.query_lo(j0 + B128 - 1) + B128 - 1) / B128 : hi;
         const int plain_hi = p.left >= 0 ? max(p.query_hi(j0), 0) / B128 : p.q_len / B128 + 1;
+        const bool short_tile = j0 + B128 > keys;                     // some keys of the tile do not exist: their rows see no query
+        const bool upper = p.left >= 0 || short_tile;
         const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2);
         bool ok = true;
         for (int it = 0; it < steps; ++it) {
@@ -314,7 +316,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     pr[c / 2] = ex2_pair(f2_fma(pair_of(s + c), c2, e.x));
                     pr[c / 2 + 1] = ex2_pair(f2_fma(pair_of(s + c + 2), c2, e.y));
                 }
-                if (!plain) hide_pairs<16>(pr + half * 16, -base - half * 32, width - base - half * 32);
+                if (!plain) hide_pairs<16>(pr + half * 16, -base - half * 32, width - base - half * 32, p.causal, upper);
                 uint32_t pk[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) pk[i] = pack_pair(pr[half * 16 + i]);
@@ -336,11 +338,13 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 for (int c = 0; c < 32; c += 4) {
                     const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(rows + 128 + half * 32 + c);          // -delta
                     const f32x2 p0 = pr[half * 16 + c / 2], p1 = pr[half * 16 + c / 2 + 1];
-                    f32x2 x = f2_mul(p0, f2_add(pair_of(d + c), e.x)), y = f2_mul(p1, f2_add(pair_of(d + c + 2), e.y));
-                    if (!plain) { x = where_p(p0, x); y = where_p(p1, y); }
-                    pk[half * 16 + c / 2] = pack_pair(x);
-                    pk[half * 16 + c / 2 + 1] = pack_pair(y);
+                    pk[half * 16 + c / 2] = pack_pair(f2_mul(p0, f2_add(pair_of(d + c), e.x)));
+                    pk[half * 16 + c / 2 + 1] = pack_pair(f2_mul(p1, f2_add(pair_of(d + c + 2), e.y)));
                 }
+            }
+            if (short_tile) {                                         // what stands behind the sequence's end may be NaN, and so then is dP
+#pragma unroll
+                for (int i = 0; i < 32; ++i) pk[i] = key < keys ? pk[i] : 0u;
             }
             tmem_st32(td, pk);
             tmem_st_wait();
@@ -563,7 +567,8 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             f32x2 pr[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) pr[i] = ex2_pair(f2_fma(pair_of(s + 2 * i), c2, nl2));
-            if (!plain) hide_pairs<32>(pr, -base, width - base);
+            if (!plain) hide_pairs<32>(pr, -base, width - base, p.left >= 0, true);
+            const bool short_tile = p.k_lens && (kt + 1) * B128 > keys;           // values behind the end may be NaN, and so then is dP
             if (!(ok = wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t pk[32];
@@ -576,7 +581,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 for (int i = 0; i < 16; ++i) {
                     const f32x2 pp = pr[half * 16 + i];
                     f32x2 x = f2_mul(pp, f2_add(pair_of(d + 2 * i), nd2));
-                    if (!plain) x = where_p(pp, x);
+                    if (short_tile) x = where_p(pp, x);
                     pk[half * 16 + i] = pack_pair(x);
                 }
             }
