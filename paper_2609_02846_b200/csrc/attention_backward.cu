@@ -60,14 +60,22 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const RowParams p) 
     if (i < p.q_len) {
         const __nv_bfloat16* o = p.o + b * p.o_stride[0] + i * p.o_stride[1] + h * p.o_stride[2];
         const __nv_bfloat16* d = p.dout + b * p.d_stride[0] + i * p.d_stride[1] + h * p.d_stride[2];
-        for (int c = sub * 8; c < p.dim; c += 64) {
-            float x[8], y[8];
-            unpack_bf16x8(ldg_nc_v4(o + c), x);
-            unpack_bf16x8(ldg_nc_v4(d + c), y);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum = fmaf(x[k], y[k], sum);
-        }
         const float lse = p.lse[bh * p.q_len + i];
+        uint4 u[2], w[2];                           // head dimension up to 128: all four loads at once
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int c = sub * 8 + k * 64;
+            u[k] = c < p.dim ? ldg_nc_v4(o + c) : make_uint4(0, 0, 0, 0);
+            w[k] = c < p.dim ? ldg_nc_v4(d + c) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float x[8], y[8];
+            unpack_bf16x8(u[k], x);
+            unpack_bf16x8(w[k], y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(x[j], y[j], sum);
+        }
         if (lse != -INFINITY) lse2 = lse * -1.4426950408889634f;
     }
 #pragma unroll
