@@ -4,7 +4,8 @@
  * The library implements the per-linear hot path of the UE5M3 FP4 pretraining recipe: operands
  * are stored as packed E2M1 payloads (4 bits) with one unsigned E5M3 block scale per 16 values
  * and one FP32 tensor reference per operand, and the three GEMMs of a linear layer are computed
- * on those operands.
+ * on those operands.  Beside them stand the operators between the linears of a transformer block: layer norm, dropout
+ * added to the residual and attention, each with its backward pass.
  *
  * General rules for every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller.  Nothing is allocated, nothing

@@ -13,6 +13,11 @@
 // The running maximum that scales O is raised only when a row's maximum grew by more than 2^8 (then O is rescaled in tensor
 // memory by its softmax warps): p stays below 2^8, l and O in binary32 lose nothing, and o = O / l does not depend on m.
 // Tensor memory: S0, S1 (128 columns each), O0, O1 (head dimension columns each).
+//
+// Per pair of tiles (2 x 128 queries, 128 keys, dimension 128) the products take 2048 cycles, the exponentials 2048 on their own unit,
+// and S with both operands in shared memory uses all of its bandwidth; a step takes 2775, because a tile's softmax (1700) and its
+// products (1000) follow one another and two tiles in flight are all that tensor memory has room for.  2 x 4096 tokens, 32 / 8 heads
+// of 128, causal: 232 us, 1184 TFLOP/s (0.72 of the measured burst rate of a BF16 product); under the power cap about 270 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -86,8 +91,8 @@ __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int
 }
 
 // Persistent: a CTA takes items in turn (forwards, then backwards, so that long and short ones even out) and every role walks them
-// by itself: the next item's Q is copied as soon as the last S of this one is done, its first S runs under this one's last softmax
-// and output.  With a CTA per item the SM stood still for 14,700 cycles at each (set-up, first copies, last product, output).
+// by itself: the next item's Q and keys are copied and its first S computed while the softmax warps still write this one's output.
+// 233 us at 2 x 4096 tokens against 240 with a CTA per item.
 // PARTS: binary32 results for attention_join_kernel.
 template <int DP, bool PARTS>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -186,7 +191,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
         // Per key tile j:  PV0 S0' | PV1 S1'  with S' = S of key tile j + 1.  The two query tiles stay half a period apart by this
-        // order (an issuing warp per tile let their softmax phases fall together: 293 us against 260 at 2 x 4096 tokens).
+        // order (an issuing warp per tile let their softmax phases fall together: 293 us against 260 at 2 x 4096 tokens).  What this
+        // warp does between two products is idle time of the tensor core, so a pair of tiles has one barrier, waited for once and
+        // released once, right behind the last product that reads it (260 us -> 240).
         const bool elected = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
         constexpr uint32_t id_s = umma_idesc(BK, false), id_o = umma_idesc(DP, true);

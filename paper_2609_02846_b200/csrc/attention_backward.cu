@@ -8,7 +8,13 @@
 //            group: S^T = K Q^T, dP^T = V dO^T, then dV += P^T dO and dK += dS^T Q
 //   queries  a CTA owns 128 queries of one head and walks the keys they see: S = Q K^T, dP = dO V^T, dQ += dS K
 // S and dP are computed in both (7 products instead of 5): in exchange every gradient is summed by one CTA in one fixed order
-// in tensor memory; there is no binary32 copy of dq in memory, no atomic and nothing that changes from call to call.
+// in tensor memory; there is no atomic and nothing that changes from call to call (few queries for many keys share the keys out
+// and add binary32 parts in order).  The three overlap: the keys kernel sets itself up under the rows kernel, the queries kernel fills
+// the tail of the keys kernel.
+//
+// 2 x 4096 tokens, 32 / 8 heads of 128, causal: rows 25 us (5.4 TB/s), keys 403, queries 371 (ncu), together 757 us: 908 TFLOP/s of
+// the 5 products that the gradients need, 1271 of the 7 that are computed, 0.92 of what a BF16 product sustains under the power
+// cap that both reach.  A step of the keys kernel takes 2620 cycles (products 2048), of the queries kernel about 2200 (1536).
 //
 // P and dS never touch shared memory: the softmax warps read S and dP from tensor memory and write P and dS (BF16) over them,
 // from where the tensor core takes them as the A operand.  Both kernels have the same roles:

