@@ -251,3 +251,28 @@ def test_few_queries_for_many_keys(Lq, Lk, causal):
     v2 = v.clone()
     v2[2, Lk // 3:] = float("nan")
     assert torch.equal(lib.attention(q, k, v2, causal=causal, k_lens=lens)[0], o)
+
+
+def test_offsets_over_32_bits():
+    """Tokens 2^30 elements apart: offsets pass 2^32 elements and bytes in every tensor, read and written."""
+    big = torch.zeros((1 << 32) + 8192, dtype=torch.bfloat16, device=DEV)
+    far = lambda at: big[at:].as_strided((1, 5, 2, 64), (8, 1 << 30, 64, 1))
+    src = make(1, 5, 5, 2, 2, 64, seed=12)
+    q, k, v, do = (far(128 * i).copy_(t) for i, t in enumerate(src))
+    o, lse = lib.attention(q, k, v, causal=True, out=far(512))
+    grads = lib.attention_backward(do, q, k, v, o, lse, causal=True, out=(far(640), far(768), far(896)))
+    want = lib.attention(*src[:3], causal=True)
+    gwant = lib.attention_backward(src[3], *src[:3], *want, causal=True)
+    assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    for a, b in zip(grads, gwant):
+        assert torch.equal(a, b)
+
+
+def test_one_key_per_query():
+    """With a single key the probability is 1: o is v, dv the sum of do over the group, dq and dk vanish."""
+    q, k, v, do = make(3, 4, 1, 4, 2, 64, seed=13)
+    o, lse = lib.attention(q, k, v)
+    assert torch.equal(o, v.repeat_interleave(2, 2).expand(3, 4, 4, 64))
+    dq, dk, dv = lib.attention_backward(do, q, k, v, o, lse)
+    size = float(do.abs().max() * v.abs().max() * 64) * float(torch.maximum(q.abs().max(), k.abs().max())) * 4
+    assert float(dq.abs().max()) <= 2.0 ** -20 * size and float(dk.abs().max()) <= 2.0 ** -20 * size

@@ -1,0 +1,66 @@
+"""Host-side rules of the operators between the linears: workspace sizes and the splits behind them (no GPU)."""
+import ctypes as C
+
+import pytest
+
+import paper_2609_02846_b200.binding as B
+from paper_2609_02846_b200.build import build_library
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build_library()
+    return B._load()
+
+
+def _shape(batch, q_len, k_len, heads, kv_heads, dim, left=-1, scale=0.1, dtype=B.BF16, causal=0):
+    return B._AttentionShape(batch, q_len, k_len, heads, kv_heads, dim, left, None, scale, dtype, causal)
+
+
+def test_layer_norm_workspace(lib):
+    f = lib.ue5m3_layer_norm_backward_workspace_bytes
+    assert f(1, 100) == 2 * 100 * 4 and f(148, 64) == f(10 ** 6, 64) == 148 * 2 * 64 * 4
+    assert f(0, 64) > 0 and f(-1, 64) == 0 and f(5, 0) == 0
+
+
+def test_attention_workspace_is_asked_for_only_when_keys_are_shared_out(lib):
+    f = lib.ue5m3_attention_workspace_bytes
+    assert f(_shape(2, 4096, 4096, 32, 8, 128)) == 0                 # enough query tiles
+    assert f(_shape(1, 1, 200, 8, 2, 64)) == 0                       # two key tiles: nothing to share out
+    # 32 query tiles of CTAs, 64 key tiles: four parts of binary32 o and lse
+    assert f(_shape(1, 1, 8192, 32, 8, 128)) == 4 * 32 * (128 + 4) * 4
+    assert f(_shape(1, 0, 8192, 32, 8, 128)) == f(_shape(0, 1, 8192, 32, 8, 128)) == f(_shape(1, 1, 0, 32, 8, 128)) == 0
+
+
+def test_attention_backward_workspace(lib):
+    f = lib.ue5m3_attention_backward_workspace_bytes
+    rows = lambda batch, heads, q_len: batch * heads * ((q_len + 127) // 128 * 128) * 2 * 4
+    assert f(_shape(2, 200, 200, 8, 8, 64)) == rows(2, 8, 200)
+    assert f(_shape(1, 1, 8192, 32, 8, 128)) == rows(1, 32, 1) + 4 * 32 * 128 * 4
+    assert f(_shape(1, 0, 8192, 32, 8, 128)) == 0
+
+
+@pytest.mark.parametrize("bad", [dict(dim=60), dict(dim=136), dict(heads=6, kv_heads=4), dict(scale=0.0), dict(scale=float("nan")), dict(left=-2),
+                                 dict(dtype=7), dict(causal=2), dict(q_len=-1), dict(kv_heads=0)])
+def test_shapes_that_no_call_takes_have_no_workspace(lib, bad):
+    args = dict(batch=1, q_len=1, k_len=8192, heads=32, kv_heads=8, dim=128)
+    args.update(bad)
+    s = _shape(**args)
+    assert lib.ue5m3_attention_workspace_bytes(s) == 0 and lib.ue5m3_attention_backward_workspace_bytes(s) == 0
+
+
+def test_calls_refuse_before_they_look_for_a_device(lib):
+    """Argument errors come first, so they are the same with and without a GPU."""
+    invalid, shape, align = 1, 2, 3
+    p = C.c_void_p(1 << 20)
+    assert lib.ue5m3_dropout_add(p, 8, None, 0, B.BF16, 4, 8, 1.5, 0, p, 8, None) == invalid
+    assert lib.ue5m3_dropout_add(p, 7, None, 0, B.BF16, 4, 8, 0.5, 0, p, 8, None) == invalid
+    assert lib.ue5m3_dropout_add(C.c_void_p((1 << 20) + 1), 8, None, 0, B.BF16, 4, 8, 0.5, 0, p, 8, None) == align
+    assert lib.ue5m3_layer_norm(p, B.BF16, 4, 0, 8, p, p, B.F32, 1e-5, p, 8, p, p, None) == invalid
+    assert lib.ue5m3_layer_norm(p, B.BF16, 4, 8, 8, C.c_void_p((1 << 20) + 2), p, B.F32, 1e-5, p, 8, p, p, None) == align
+    assert lib.ue5m3_layer_norm_backward(p, 8, p, B.F32, 4, 8, 8, p, B.F32, p, p, p, 8, p, p, None, None) == invalid     # sums without a workspace
+    t = B._Heads(1 << 20, 1024, 128, 64)
+    odd = B._Heads(1 << 20, 1024, 132, 64)
+    assert lib.ue5m3_attention(_shape(2, 8, 8, 2, 2, 60), t, t, t, t, p, None, None) == shape
+    assert lib.ue5m3_attention(_shape(2, 8, 8, 2, 2, 64), odd, t, t, t, p, None, None) == align
+    assert lib.ue5m3_attention(_shape(2, 8, 8, 2, 2, 64), t, t, t, t, None, None, None) == invalid
