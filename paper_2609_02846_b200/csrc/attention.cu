@@ -21,6 +21,8 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include "../../include/ue5m3.h"
 #include "attention.cuh"
@@ -55,28 +57,38 @@ __device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity, volati
 
 struct OutputParams { __nv_bfloat16* o; int64_t batch_stride, token_stride, head_stride; };
 
-// One piece of work: two tiles of 128 queries of one head (PARTS: on a share of the keys).
+// One piece of work: two tiles of 128 queries of one head (PARTS: on a share of the keys).  PACK (few queries per head): a tile holds
+// the queries of `pack` heads that share keys, row = head * q_len + query; h is the first of them in tile 0, tile 1 goes on behind.
 struct Item {
-    int b, h, part, q0, keys;
+    int b, h, h_end, kvh, part, q0, keys;                 // h_end: heads of the group of h end there (PACK)
     int lo[2], hi[2];                                     // key tiles of the two query tiles
     int first, last;                                      // ... and of both together
     __device__ __forceinline__ bool on(int t) const { return hi[t] > lo[t]; }
 };
 // Heads fastest (heads that share keys run side by side), long query tiles first.
-template <bool PARTS>
+template <bool PARTS, bool PACK>
 __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int q_tiles) {
     Item w;
     w.part = PARTS ? index % p.parts : 0;
-    const int bh_count = p.batch * p.heads, block = PARTS ? index / p.parts : index;
-    const int bh = block % bh_count;
-    w.b = bh / p.heads;
-    w.h = bh - w.b * p.heads;
-    w.q0 = (q_tiles - 1 - block / bh_count) * 2 * BQ;
+    const int heads = PACK ? p.kv_heads : p.heads, bh_count = p.batch * heads, block = PARTS ? index / p.parts : index;
+    const int turn = block / bh_count, bh = block - turn * bh_count;
+    w.b = bh / heads;
+    w.h = bh - w.b * heads;
+    w.h_end = 0;
+    if (PACK) {
+        w.kvh = w.h;
+        w.h = w.kvh * p.group + turn * 2 * p.pack;
+        w.h_end = (w.kvh + 1) * p.group;
+        w.q0 = 0;
+    } else {
+        w.kvh = w.h / p.group;
+        w.q0 = (q_tiles - 1 - turn) * 2 * BQ;
+    }
     w.keys = p.keys_of(w.b);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int r0 = w.q0 + t * BQ, r1 = min(r0 + BQ, p.q_len) - 1;
-        const int a = p.key_lo(r0), z = r0 < p.q_len ? p.key_hi(r1, w.keys) : 0;
+        const int r0 = PACK ? 0 : w.q0 + t * BQ, r1 = min(r0 + BQ, p.q_len) - 1;
+        const int a = p.key_lo(r0), z = (PACK ? w.h + t * p.pack < w.h_end : r0 < p.q_len) ? p.key_hi(r1, w.keys) : 0;
         w.lo[t] = a / BK;
         w.hi[t] = z > a ? (z + BK - 1) / BK : w.lo[t];
         if (PARTS) {                                      // this part's share of all key tiles
@@ -94,7 +106,7 @@ __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int
 // by itself: the next item's Q and keys are copied and its first S computed while the softmax warps still write this one's output.
 // 233 us at 2 x 4096 tokens against 240 with a CTA per item.
 // PARTS: binary32 results for attention_join_kernel.
-template <int DP, bool PARTS>
+template <int DP, bool PARTS, bool PACK>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                  const __grid_constant__ CUtensorMap map_v, const AttentionParams p, const OutputParams out, const int q_tiles, const int items) {
@@ -150,13 +162,13 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             int n = 0, q_uses[2] = {0, 0};
             bool go = true;
             for (int turn = 0, index; go && (index = item_at(turn)) < items; ++turn) {
-                const Item w = item_of<PARTS>(p, index, q_tiles);
-                const int kvh = w.h / p.group, pairs = w.last > w.first ? w.last - w.first + 1 : 0;
+                const Item w = item_of<PARTS, PACK>(p, index, q_tiles);
+                const int pairs = w.last > w.first ? w.last - w.first + 1 : 0;
                 auto load = [&](int tile_n, const CUtensorMap* m, uint32_t bar, int tile) {
                     mbar_expect_tx(bar, T::TILE);
 #pragma unroll
                     for (int c = 0; c < T::PANELS; ++c)
-                        tma_load_4d(ring + (tile_n % T::RING) * T::TILE + c * T::PANEL, m, bar, c * 64, tile * BK, kvh, w.b);
+                        tma_load_4d(ring + (tile_n % T::RING) * T::TILE + c * T::PANEL, m, bar, c * 64, tile * BK, w.kvh, w.b);
                 };
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -164,10 +176,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         go = wait(q_empty + 8 * t, (q_uses[t] & 1) ^ 1, abort_flag, p.wait_limit);
                         if (!go) break;
                         ++q_uses[t];
-                        mbar_expect_tx(q_full + 8 * t, T::TILE);
+                        mbar_expect_tx(q_full + 8 * t, PACK ? p.pack * p.q_len * DP * 2 : T::TILE);
 #pragma unroll
                         for (int c = 0; c < T::PANELS; ++c)
-                            tma_load_4d(smem + t * T::TILE + c * T::PANEL, &map_q, q_full + 8 * t, c * 64, w.q0 + t * BQ, w.h, w.b);
+                            tma_load_4d(smem + t * T::TILE + c * T::PANEL, &map_q, q_full + 8 * t, c * 64, PACK ? 0 : w.q0 + t * BQ, PACK ? w.h + t * p.pack : w.h, w.b);
                     }
                 for (int i = 0; go && i < pairs; ++i, ++n) {
                     const uint32_t bar = kv_full + 8 * (n % T::PAIRS);
@@ -253,7 +265,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (++done == T::PAIRS) done = 0;
         };
         for (int turn = 0, index; ok && (index = item_at(turn)) < items; ++turn) {
-            const Item w = item_of<PARTS>(p, index, q_tiles);
+            const Item w = item_of<PARTS, PACK>(p, index, q_tiles);
             if (w.last <= w.first) continue;
             const uint32_t k0 = k_tile(next_pair(w, w.first - 1));
 #pragma unroll
@@ -300,15 +312,19 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
         const uint32_t ts = lane_base + t * BK, to = lane_base + 2 * BK + t * 128;
         const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2);
+        // this thread's row of the tile; PACK: head and query in it.  Rows that no copy fills hold anything and stay among themselves.
+        const int r = q * 32 + lane, r_head = PACK ? r / p.q_len : 0, r_query = PACK ? r - r_head * p.q_len : r;
         uint32_t n = 0, uses = 0;                          // S tiles and items of this query tile so far
         bool ok = true;
         for (int turn = 0, index; ok && (index = item_at(turn)) < items; ++turn) {
-        const Item w = item_of<PARTS>(p, index, q_tiles);
-        const int r0 = w.q0 + t * BQ, row = r0 + q * 32 + lane;
+        const Item w = item_of<PARTS, PACK>(p, index, q_tiles);
+        const int r0 = PACK ? 0 : w.q0 + t * BQ, r_last = PACK ? p.q_len - 1 : r0 + BQ - 1;
+        const int h = PACK ? w.h + t * p.pack + r_head : w.h, row = r0 + r_query;
+        const bool exists = PACK ? r_head < p.pack && h < w.h_end : row < p.q_len;
         const int key_lo = p.key_lo(row), key_hi = p.key_hi(row, w.keys);
         const int n0 = t == 0 ? w.lo[0] : w.lo[1], n1 = t == 0 ? w.hi[0] : w.hi[1];
         // key tiles [plain_lo, plain_hi) are seen whole by every row of the tile
-        const int plain_lo = p.left >= 0 ? (p.key_lo(r0 + BQ - 1) + BK - 1) / BK : 0;
+        const int plain_lo = p.left >= 0 ? (p.key_lo(r_last) + BK - 1) / BK : 0;
         const int plain_hi = max(p.key_hi(r0, w.keys), 0) / BK;
         float m = -INFINITY;
         f32x2 l2 = 0;
@@ -361,7 +377,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 for (int c = k + 4; c + 4 < 128; c += 8) top[k] = max3(top[k], __uint_as_float(s[c]), __uint_as_float(s[c + 4]));
                 top[k] = fmaxf(top[k], __uint_as_float(s[124 + k]));
             }
-            const float tile_top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
+            float tile_top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
+            if (PACK && !exists) tile_top = -INFINITY;
             if (__any_sync(0xFFFFFFFFu, tile_top > m + kRaise)) {
                 raise(tile_top, j == n0);
                 base = m == -INFINITY ? 0.0f : m;
@@ -384,9 +401,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             f2_unpack(l2, a, b2);
             l = a + b2;
         }
-        const int64_t lse_at = (((int64_t)w.part * p.batch + w.b) * p.heads + w.h) * p.q_len + row;
+        const int64_t lse_at = (((int64_t)w.part * p.batch + w.b) * p.heads + h) * p.q_len + row;
         const bool some = l > 0.0f || l != l;              // this query sees a key
-        if (row < p.q_len) (PARTS ? p.part_lse : p.lse)[lse_at] = some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        if (exists) (PARTS ? p.part_lse : p.lse)[lse_at] = some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
         const bool any = n1 > n0;
         if (any && ok) {
             ok = wait(o_full + 8 * t, uses & 1, abort_flag, p.wait_limit);
@@ -395,7 +412,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         if (!ok) break;
         const float f = some ? 1.0f / l : 0.0f;
-        __nv_bfloat16* dst = out.o + w.b * out.batch_stride + row * out.token_stride + w.h * out.head_stride;
+        __nv_bfloat16* dst = out.o + w.b * out.batch_stride + row * out.token_stride + h * out.head_stride;
 #pragma unroll 1
         for (int c = 0; c < DP; c += 32) {
             uint32_t o[32];
@@ -413,7 +430,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 #pragma unroll
                 for (int v = 0; v < 32; ++v) o[v] = 0u;
             }
-            if (row < p.q_len && (!PARTS || any)) {                   // a part without keys: lse says so, o is not read
+            if (exists && (!PARTS || any)) {                   // a part without keys: lse says so, o is not read
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     float x[8];
@@ -440,26 +457,41 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     if (warp == 0) { tc_fence_after(); tmem_dealloc1(tmem, 512); }
 }
 
-// Joins the parts of a query:  lse = log sum exp lse_p,  o = sum exp(lse_p - lse) o_p, parts in order.  A warp per query; a part that
-// saw no key (lse = -inf) has written no o and is not read.
+// Joins the parts of a query:  lse = log sum exp lse_p,  o = sum exp(lse_p - lse) o_p, parts in order.  A warp per query.  A part
+// that saw no key (lse = -inf) has written no o: what is loaded there, before lse is known, is not used.
 __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionParams p, __nv_bfloat16* o, const int64_t batch_stride,
                                                              const int64_t token_stride, const int64_t head_stride) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int64_t rows = (int64_t)p.batch * p.heads * p.q_len, r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (r >= rows) return;
     const int lane = threadIdx.x & 31;
-    float top = -INFINITY;
-    for (int k = 0; k < p.parts; ++k) top = fmaxf(top, p.part_lse[k * rows + r]);
+    auto lse_of = [&](int k) { return k < p.parts ? p.part_lse[k * rows + r] : -INFINITY; };
+    const float mine = lse_of(lane);                       // a lane per part
+    float top = mine;
+    for (int k = lane + 32; k < p.parts; k += 32) top = fmaxf(top, lse_of(k));
+    float4 v[4];
+    auto load = [&](int k0) {                              // four at a time; they do not wait for lse
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (k0 + u < p.parts && lane * 4 < p.dim) v[u] = *reinterpret_cast<const float4*>(p.part_o + ((k0 + u) * rows + r) * p.dim + lane * 4);
+    };
+    load(0);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
     const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < p.parts; ++k) {
-        const float lse = p.part_lse[k * rows + r];
-        if (lse == -INFINITY) continue;
-        const float w = exp2f((lse - base) * 1.4426950408889634f);
-        sum += w;
-        if (lane * 4 < p.dim) {
-            const float4 v = *reinterpret_cast<const float4*>(p.part_o + (k * rows + r) * p.dim + lane * 4);
-            acc[0] = fmaf(w, v.x, acc[0]); acc[1] = fmaf(w, v.y, acc[1]); acc[2] = fmaf(w, v.z, acc[2]); acc[3] = fmaf(w, v.w, acc[3]);
+    float sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, weight = 0.0f;
+    for (int k0 = 0; k0 < p.parts; k0 += 4) {
+        if (k0 > 0) load(k0);
+        if ((k0 & 31) == 0) {
+            const float lse = k0 == 0 ? mine : lse_of(k0 + lane);
+            weight = lse == -INFINITY ? -1.0f : exp2f((lse - base) * 1.4426950408889634f);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float w = __shfl_sync(0xFFFFFFFFu, weight, (k0 + u) & 31);
+            if (w == -1.0f) continue;                      // no keys, or no such part
+            sum += w;
+            acc[0] = fmaf(w, v[u].x, acc[0]); acc[1] = fmaf(w, v[u].y, acc[1]); acc[2] = fmaf(w, v[u].z, acc[2]); acc[3] = fmaf(w, v[u].w, acc[3]);
         }
     }
     const float f = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
@@ -472,49 +504,77 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionPara
     if (lane == 0) p.lse[r] = sum > 0.0f || sum != sum ? base + logf(sum) : -INFINITY;
 }
 
-template <int DP, bool PARTS>
+// Heads of a group whose queries share a tile of 128 rows, evenly over the tiles they need; 0: a head's queries have their own tiles.
+// Few queries leave most rows of a tile empty, and every head of a group walks the same keys: together they walk them once.  On their
+// own / together, us, 32 heads on 8 key/value heads of 128: one query on 8192 keys 31.1 / 16.8; 16 sequences of that 338 / 89.6
+// (6.0 TB/s, 0.91 of the measured copy rate); 4 x 8 on 4096 47.8 / 22.5; 1 on 300 9.3 / 9.0.  A group that needs more than one tile puts two
+// of them into a CTA, one behind the other: that pays once the heads alone are more than the 148 SMs take at a time (8 x 100 on
+// 2000 53.4 / 36.2, 8 x 100 on 128 12.5 / 9.9) and costs before (4 x 100 on 128 8.0 / 9.4, 61 on 61, 8 heads 5.9 / 7.5).
+int packed_heads(const ue5m3_attention_shape& s) {
+    const int64_t group = s.heads / s.kv_heads;
+    if (group == 1 || s.q_len == 0 || s.q_len > BQ || (s.q_len * group > BQ && s.batch * s.heads <= 148)) return 0;
+    const int64_t most = BQ / s.q_len, tiles = (group + most - 1) / most;
+    return (int)((group + tiles - 1) / tiles);
+}
+// Pairs of query tiles.
+int64_t query_pairs(const ue5m3_attention_shape& s) {
+    const int64_t pack = packed_heads(s), group = s.heads / s.kv_heads;
+    return pack ? s.batch * s.kv_heads * ((group + 2 * pack - 1) / (2 * pack)) : (s.q_len + 2 * BQ - 1) / (2 * BQ) * s.batch * s.heads;
+}
+
+template <int DP, bool PARTS, bool PACK>
 int run(const ue5m3_attention_shape& s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
         const OutputParams& o, int num_sms, cudaStream_t st) {
     using T = Tiles<DP>;
-    const int64_t q_tiles = (s.q_len + 2 * BQ - 1) / (2 * BQ), items = q_tiles * s.batch * s.heads * p.parts;
+    const int64_t q_tiles = (s.q_len + 2 * BQ - 1) / (2 * BQ), items = query_pairs(s) * p.parts;
     if (items > 0x7FFFFFFF - 2 * num_sms) return UE5M3_ERR_UNSUPPORTED;
     static std::atomic<int> granted[64];
-    if (allow_smem(attention_kernel<DP, PARTS>, T::SMEM, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-    attention_kernel<DP, PARTS><<<(unsigned)(items < num_sms ? items : num_sms), kThreads, T::SMEM, st>>>(q, k, v, p, o, (int)q_tiles, (int)items);
+    if (allow_smem(attention_kernel<DP, PARTS, PACK>, T::SMEM, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
+    attention_kernel<DP, PARTS, PACK><<<(unsigned)(items < num_sms ? items : num_sms), kThreads, T::SMEM, st>>>(q, k, v, p, o, (int)q_tiles, (int)items);
     return cudaGetLastError() == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+}
+template <bool PARTS>
+int run(const ue5m3_attention_shape& s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
+        const OutputParams& o, int num_sms, cudaStream_t st) {
+    if (p.pack) return s.head_dim <= 64 ? run<64, PARTS, true>(s, q, k, v, p, o, num_sms, st) : run<128, PARTS, true>(s, q, k, v, p, o, num_sms, st);
+    return s.head_dim <= 64 ? run<64, PARTS, false>(s, q, k, v, p, o, num_sms, st) : run<128, PARTS, false>(s, q, k, v, p, o, num_sms, st);
 }
 
 }  // namespace
 
-// Key tiles are shared out when the query tiles alone leave at least half of the 148 SMs idle, into as many parts as fill them but
-// none below two key tiles (a part costs its set-up, and its results a pass through memory).  Whole against shared out, us: one
-// query on 8192 keys, 32 heads 88.9 / 29.6; 100 on 8192, 16 heads 91.0 / 27.4; 600 on 2000, 8 heads 33.4 / 24.2; 1 on 512, 8 heads
-// 9.9 / 10.0.  Parts of one key tile: 128 on 384, 16 heads 10.1 / 12.8.
+// Parts into which the key tiles are shared out when the query tiles alone leave at least half of the 148 SMs idle: as many as fill
+// them, none below two key tiles, and no more than pay (a quarter of the time at least).  In units of a key tile's step (1.5 us) a call takes tiles / n, and sharing
+// out costs 2 (the second kernel) and, per part, its binary32 results through memory twice at about 5 TB/s: rows * dim / 0.9e6.  Whole
+// against shared out, us: one query on 8192 keys, 32 heads 88.9 / 29.6; 100 on 8192, 16 heads 91.0 / 25.3; 600 on 2000, 8 heads
+// 33.4 / 22.4; and where it does not pay: 100 on 512, 32 heads 11.1 / 13.4; 8 x 64 on 1000, 32 / 8 heads 23.0 / 28.8.
 int attention_splits(const ue5m3_attention_shape& s) {
-    const int64_t ctas = (s.q_len + 2 * BQ - 1) / (2 * BQ) * s.batch * s.heads, tiles = (s.k_len + BK - 1) / BK;
-    if (ctas == 0 || ctas > 74) return 1;
-    const int64_t fill = 148 / ctas, most = tiles / 2;
-    const int64_t n = fill < most ? fill : most;
-    return n < 1 ? 1 : (int)n;
+    const int64_t ctas = query_pairs(s), tiles = (s.k_len + BK - 1) / BK;
+    if (ctas == 0 || ctas > 74 || tiles < 4) return 1;
+    const double part = (double)s.batch * s.heads * s.q_len * s.head_dim / 0.9e6;
+    const int64_t fill = 148 / ctas, most = tiles / 2, pays = (int64_t)sqrt((double)tiles / part);
+    const int64_t n = std::min(std::min(fill, most), pays);
+    return n > 1 && (double)tiles / n + 2 + n * part < 0.75 * (double)tiles ? (int)n : 1;
 }
 
 int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
                      const ue5m3_heads& o, float* lse, float* workspace, int num_sms, cudaStream_t st) {
     if (s.batch == 0 || s.q_len == 0) return UE5M3_OK;
     CUtensorMap mq, mk, mv;
-    if (!make_heads_map(&mq, q, s.batch, s.q_len, s.heads, s.head_dim, BQ)) return UE5M3_ERR_CUDA;
+    const int pack = packed_heads(s);
+    if (!make_heads_map(&mq, q, s.batch, s.q_len, s.heads, s.head_dim, pack ? (uint32_t)s.q_len : BQ, pack ? pack : 1)) return UE5M3_ERR_CUDA;
     if (s.k_len == 0) mk = mv = mq;                        // no key tile is ever read
     else if (!make_heads_map(&mk, k, s.batch, s.k_len, s.kv_heads, s.head_dim, BK) || !make_heads_map(&mv, v, s.batch, s.k_len, s.kv_heads, s.head_dim, BK))
         return UE5M3_ERR_CUDA;
     AttentionParams p = attention_params(s);
     p.lse = lse;
     p.parts = attention_splits(s);
+    p.pack = pack;
     const OutputParams out{static_cast<__nv_bfloat16*>(o.data), o.batch_stride, o.token_stride, o.head_stride};
-    if (p.parts == 1) return s.head_dim <= 64 ? run<64, false>(s, mq, mk, mv, p, out, num_sms, st) : run<128, false>(s, mq, mk, mv, p, out, num_sms, st);
+    if (p.parts == 1) return run<false>(s, mq, mk, mv, p, out, num_sms, st);
     const int64_t rows = s.batch * s.heads * s.q_len;
     p.part_o = workspace;
     p.part_lse = workspace + p.parts * rows * s.head_dim;
-    const int r = s.head_dim <= 64 ? run<64, true>(s, mq, mk, mv, p, out, num_sms, st) : run<128, true>(s, mq, mk, mv, p, out, num_sms, st);
+    const int r = run<true>(s, mq, mk, mv, p, out, num_sms, st);
     if (r != UE5M3_OK) return r;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((rows + 7) / 8));

@@ -241,6 +241,7 @@ struct AttentionParams {
     const float* lse2;                   // backward: -lse * log2(e) per query, padded to whole tiles (-inf: contributes nothing)
     const float* delta;                  // backward: -(dout . o) per query, padded
     int q_pad;
+    int kv_heads, pack;                         // forward: heads that share a query tile (0: none do)
     int dim, parts;                      // head dimension; parts into which the key tiles of a query are shared out
     float* part_o; float* part_lse;      // parts > 1: o (backward: dq) [parts][batch][heads][q_len][dim]; forward: lse [..][q_len]
     long long wait_limit;
@@ -259,16 +260,16 @@ struct AttentionParams {
 };
 
 // ----------------------------------------------------------------------------- host side
-// [batch, tokens, heads, dim] with element strides -> map (dim, tokens, heads, batch); box 64 x rows.  Dimensions of size 1 get
+// [batch, tokens, heads, dim] with element strides -> map (dim, tokens, heads, batch); box 64 x rows (x box_heads).  Dimensions of size 1 get
 // a stride that is always valid.
-inline bool make_heads_map(CUtensorMap* m, const ue5m3_heads& t, int64_t batch, int64_t tokens, int64_t heads, int64_t dim, uint32_t rows) {
+inline bool make_heads_map(CUtensorMap* m, const ue5m3_heads& t, int64_t batch, int64_t tokens, int64_t heads, int64_t dim, uint32_t rows, uint32_t box_heads = 1) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)batch};
     const cuuint64_t any = (cuuint64_t)((dim + 7) / 8 * 8) * 2;
     cuuint64_t strides[3] = {tokens > 1 ? (cuuint64_t)t.token_stride * 2 : any, heads > 1 ? (cuuint64_t)t.head_stride * 2 : any,
                              batch > 1 ? (cuuint64_t)t.batch_stride * 2 : any};
-    cuuint32_t box[4] = {64, rows, 1, 1};
+    cuuint32_t box[4] = {64, rows, box_heads, 1};
     cuuint32_t estr[4] = {1, 1, 1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, t.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -277,7 +278,7 @@ inline bool make_heads_map(CUtensorMap* m, const ue5m3_heads& t, int64_t batch, 
 inline AttentionParams attention_params(const ue5m3_attention_shape& s) {
     AttentionParams p{};
     p.q_len = (int)s.q_len; p.k_len = (int)s.k_len; p.heads = (int)s.heads; p.group = (int)(s.heads / s.kv_heads);
-    p.causal = s.causal; p.batch = (int)s.batch; p.k_lens = s.k_lens;
+    p.kv_heads = (int)s.kv_heads; p.causal = s.causal; p.batch = (int)s.batch; p.k_lens = s.k_lens;
     const int64_t all = s.q_len + s.k_len;                  // a window as long as this hides nothing
     p.left = s.window_left < 0 ? -1 : (int)(s.window_left < all ? s.window_left : all);
     p.scale = s.scale;

@@ -276,3 +276,18 @@ def test_one_key_per_query():
     dq, dk, dv = lib.attention_backward(do, q, k, v, o, lse)
     size = float(do.abs().max() * v.abs().max() * 64) * float(torch.maximum(q.abs().max(), k.abs().max())) * 4
     assert float(dq.abs().max()) <= 2.0 ** -20 * size and float(dk.abs().max()) <= 2.0 ** -20 * size
+
+
+@pytest.mark.parametrize("B,Lq,Lk,H,Hk,D", [(1, 1, 700, 4, 1, 64), (2, 1, 1500, 32, 8, 128), (16, 1, 300, 20, 10, 128), (3, 33, 400, 12, 2, 80), (1, 40, 900, 4, 1, 128),
+                                            (2, 43, 300, 7, 1, 64), (1, 64, 100, 10, 2, 64), (1, 9, 4500, 28, 2, 128), (1, 1, 9000, 200, 1, 64), (2, 65, 513, 6, 2, 128),
+                                            (1, 128, 384, 6, 2, 128), (1, 127, 130, 3, 1, 16)])
+def test_few_queries_of_grouped_heads(B, Lq, Lk, H, Hk, D):
+    """Queries of several heads in one tile: whole, partial and several tiles to a group, on keys that are shared out or not; the
+    next group's head behind a partial tile; no mask, causal, a window, lengths."""
+    q, k, v, do = make(B, Lq, Lk, H, Hk, D, seed=Lq + H)
+    lens = torch.tensor([(Lk * (3 * b + 1)) // (3 * B) for b in range(B)], dtype=torch.int32, device=DEV)
+    for causal, left, l in ((False, -1, None), (True, -1, None), (True, 70, None), (True, -1, lens)):
+        o, lse, _ = check(q, k, v, do, causal=causal, left=left, lens=l)
+        out = torch.full((B, H, Lq, D), 7.0, dtype=torch.bfloat16, device=DEV).transpose(1, 2)
+        lib.attention(q, k, v, causal=causal, window_left=left, k_lens=l, out=out)
+        assert torch.equal(o, out)

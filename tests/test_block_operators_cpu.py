@@ -27,8 +27,9 @@ def test_attention_workspace_is_asked_for_only_when_keys_are_shared_out(lib):
     f = lib.ue5m3_attention_workspace_bytes
     assert f(_shape(2, 4096, 4096, 32, 8, 128)) == 0                 # enough query tiles
     assert f(_shape(1, 1, 200, 8, 2, 64)) == 0                       # two key tiles: nothing to share out
-    # 32 query tiles of CTAs, 64 key tiles: four parts of binary32 o and lse
-    assert f(_shape(1, 1, 8192, 32, 8, 128)) == 4 * 32 * (128 + 4) * 4
+    # eight tiles, each of the four heads that share keys; 64 key tiles: 18 parts of binary32 o and lse
+    assert f(_shape(1, 1, 8192, 32, 8, 128)) == 18 * 32 * (128 + 4) * 4
+    assert f(_shape(1, 100, 512, 32, 8, 128)) == 0                   # four key tiles: sharing out costs more than it saves
     assert f(_shape(1, 0, 8192, 32, 8, 128)) == f(_shape(0, 1, 8192, 32, 8, 128)) == f(_shape(1, 1, 0, 32, 8, 128)) == 0
 
 
