@@ -519,9 +519,12 @@ layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
     });
 }
 
-// Rows without 16-byte alignment: single columns, prefetched one row ahead.
-template <typename TX, typename TW, int NV>
-__global__ void __launch_bounds__(512)
+// Rows without 16-byte alignment: single columns, prefetched one row ahead.  The fewer columns a thread has, the more loads of
+// different rows are in flight and the shorter a row's chain, until a wide row's group leaves no second one beside it.  us at
+// 4 columns per thread (768 threads) / 6 (768) / 16 (512):  FP32 1000 x 1537 11.3 / 11.6 / 16.6, 8000 x 1537 57.1 / 42.3 / 58.3; BF16
+// 3000 x 1023 13.9 / 15.5 / -, 10000 x 333 15.0 / 15.5 / 25.0.  So 4 to 1024 columns, 6 as far as 768 threads reach, 16 beyond.
+template <typename TX, typename TW, int NV, int MAXT>
+__global__ void __launch_bounds__(MAXT)
 layer_norm_backward_kernel(const LayerNormArgs a) {
     extern __shared__ __align__(16) float smem[];          // [R][128] reduction scratch, then the column sums
     asm volatile("griddepcontrol.launch_dependents;");
@@ -756,27 +759,27 @@ cudaError_t add_columns(const LayerNormArgs& a, int groups, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, layer_norm_columns_kernel<TW>, (const float*)a.partial, groups, a.cols, (TW*)a.dweight, (TW*)a.dbias);
 }
 
-template <typename TX, typename TW, bool RING, bool FULL>
+template <typename TX, typename TW, bool RING, bool FULL, int PER, int CTA>
 cudaError_t run_backward(const LayerNormArgs& a, cudaStream_t st) {
-    RowShape s = row_shape(a.cols, kPerThread, 512);
+    RowShape s = row_shape(a.cols, PER, CTA);
     const int64_t spread = (a.rows + kBwdGroups - 1) / kBwdGroups;
     if (s.groups > spread) s.groups = spread < 1 ? 1 : (int)spread;
     const int64_t row_bytes = a.cols * (int64_t)sizeof(TX);
     const int slots = RING ? ring_slots(s.groups, 2 * row_bytes) : 0;
     const size_t ring = (size_t)s.groups * slots * (2 * row_bytes + 8) + 16;
-    const size_t sums = (size_t)(s.groups - 1) * 2 * s.threads * kPerThread * sizeof(float);
+    const size_t sums = (size_t)(s.groups - 1) * 2 * s.threads * PER * sizeof(float);
     const size_t smem = (size_t)s.groups * 128 * sizeof(float) + (ring > sums ? ring : sums);
     const int64_t need = (a.rows + s.groups - 1) / s.groups;
     const int grid = (int)(need < kBwdGroups ? need : kBwdGroups);
     static std::atomic<int> granted[64];
     cudaError_t e = cudaSuccess;
     if constexpr (RING) {
-        constexpr int NV = kPerThread * sizeof(TX) / 16;
+        constexpr int NV = PER * sizeof(TX) / 16;
         e = allow_smem(layer_norm_backward_ring_kernel<TX, TW, NV, FULL>, kRingSmem, granted);
         if (e == cudaSuccess && grid > 0) layer_norm_backward_ring_kernel<TX, TW, NV, FULL><<<grid, dim3(s.threads, s.groups), smem, st>>>(a, slots);
     } else {
-        e = allow_smem(layer_norm_backward_kernel<TX, TW, kPerThread>, kRingSmem, granted);
-        if (e == cudaSuccess && grid > 0) layer_norm_backward_kernel<TX, TW, kPerThread><<<grid, dim3(s.threads, s.groups), smem, st>>>(a);
+        e = allow_smem(layer_norm_backward_kernel<TX, TW, PER, CTA>, kRingSmem, granted);
+        if (e == cudaSuccess && grid > 0) layer_norm_backward_kernel<TX, TW, PER, CTA><<<grid, dim3(s.threads, s.groups), smem, st>>>(a);
     }
     if (e == cudaSuccess) e = cudaGetLastError();
     return e != cudaSuccess || !a.partial ? e : add_columns<TW>(a, grid, st);
@@ -804,8 +807,10 @@ cudaError_t backward_of(const LayerNormArgs& a, cudaStream_t st) {
         if (e == cudaSuccess) e = cudaGetLastError();
         return e != cudaSuccess || !a.partial ? e : add_columns<TW>(a, grid, st);
     }
-    if (!vec) return run_backward<TX, TW, false, false>(a, st);
-    return a.cols % (kPerThread * 32) == 0 ? run_backward<TX, TW, true, true>(a, st) : run_backward<TX, TW, true, false>(a, st);
+    if (!vec && a.cols <= 1024) return run_backward<TX, TW, false, false, 4, 768>(a, st);
+    if (!vec && a.cols <= 6 * 768) return run_backward<TX, TW, false, false, 6, 768>(a, st);
+    if (!vec) return run_backward<TX, TW, false, false, kPerThread, 512>(a, st);
+    return a.cols % (kPerThread * 32) == 0 ? run_backward<TX, TW, true, true, kPerThread, 512>(a, st) : run_backward<TX, TW, true, false, kPerThread, 512>(a, st);
 }
 
 }  // namespace

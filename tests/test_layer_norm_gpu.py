@@ -182,3 +182,14 @@ def test_refusals():
         lib.layer_norm_backward(dy[:7], x, w, mean, rstd)
     with pytest.raises(ValueError):
         lib.layer_norm_backward(dy, x, w, mean[:7], rstd)
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("rows,cols", [(700, 33), (700, 1023), (300, 1024), (300, 1025), (900, 2047), (300, 4607), (300, 4608), (300, 4609), (301, 8192)])
+def test_rows_without_alignment(rows, cols, dt):
+    """Widths around the limits of the columns a thread holds, every row at another offset from 16 bytes."""
+    x, w, b, dy = make(rows, cols, dt, F, seed=cols)
+    def odd(t):
+        wide = torch.zeros(rows, cols + 3 + cols % 2, dtype=t.dtype, device=DEV)
+        return wide[:, 1:cols + 1].copy_(t)
+    check(odd(x), w, b, odd(dy))
