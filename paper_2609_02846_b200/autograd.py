@@ -64,6 +64,27 @@ def _check_dims(M: int, K: int, N: int, multiple: int = 128) -> None:
             raise ValueError(f"{name} = {v}: the three GEMMs of this linear need every dimension to be a multiple of {multiple}")
 
 
+class _NoSecondDerivative(torch.autograd.Function):
+    """A gradient as a value: the library has no derivative of its backward passes, so going through one is an error."""
+
+    @staticmethod
+    def forward(ctx, name, grad, *sources):
+        ctx.name = name
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{ctx.name} has no second derivative")
+
+
+def _once(name, grads, *sources):
+    """`grads` as a backward pass returns them.  Asked for with a graph (create_graph), they hang on the tensors they depend on, so
+    that a second derivative is refused in place of being left out of the sum.  (torch's once_differentiable looks at the upstream
+    gradient alone, which need not require one.)"""
+    sources = [t for t in sources if t is not None and t.requires_grad] if torch.is_grad_enabled() else []
+    return tuple(None if g is None else _NoSecondDerivative.apply(name, g, *sources) for g in grads) if sources else tuple(grads)
+
+
 class _Ue5m3LinearFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, layer, step):
@@ -75,18 +96,19 @@ class _Ue5m3LinearFn(torch.autograd.Function):
         y, _, qw = B.linear_forward(x, w, ax, aw, layer.target_T, x.dtype, grid_denominator=layer.grid_denominator)
         ctx.save_for_backward(x)
         ctx.qw, ctx.ax, ctx.layer, ctx.step = qw, ax, layer, step
+        ctx.w = w                               # only to refuse a second derivative: the weight may change after the forward pass
         return y
 
     @staticmethod
     def backward(ctx, dy):
         (x,) = ctx.saved_tensors
-        layer, step = ctx.layer, ctx.step
+        layer, step, upstream = ctx.layer, ctx.step, dy
         dy = dy.contiguous()
         ag = layer.scale_dy.get(dy, step)
         dx, dw = B.linear_backward(dy, x, ctx.qw, ag, ctx.ax, seed=sr_stream_seed(layer.seed, layer.rank, step), target_T=layer.target_T,
                                    target_T_wgrad_dy=layer.target_T_wgrad_dy, out_dtype=dy.dtype,
                                    grid_denominator=layer.grid_denominator, grad_rounding=layer.grad_rounding)
-        return dx, dw, None, None
+        return *_once("Ue5m3Linear", (dx, dw), upstream, x, ctx.w), None, None
 
 
 class Ue5m3Linear(torch.nn.Module):
@@ -141,16 +163,16 @@ class _LayerNormFn(torch.autograd.Function):
     def forward(ctx, x, weight, bias, eps):
         rows = _as_rows(x)
         y, mean, rstd = B.layer_norm(rows, weight, bias, eps)
-        ctx.save_for_backward(rows, weight, mean, rstd)
-        ctx.shape, ctx.bias_dtype = x.shape, None if bias is None else bias.dtype
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.bias_dtype = None if bias is None else bias.dtype
         return y.view(x.shape)
 
     @staticmethod
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
         want_w, want_b = ctx.needs_input_grad[1], ctx.needs_input_grad[2]
-        dx, dw, db = B.layer_norm_backward(_as_rows(dy), x, weight, mean, rstd, want_weight=want_w, want_bias=want_b)
-        return dx.view(ctx.shape), dw, db if db is None else db.to(ctx.bias_dtype), None
+        dx, dw, db = B.layer_norm_backward(_as_rows(dy), _as_rows(x), weight, mean, rstd, want_weight=want_w, want_bias=want_b)
+        return *_once("layer_norm", (dx.view(x.shape), dw, db if db is None else db.to(ctx.bias_dtype)), dy, x, weight), None
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:
@@ -181,7 +203,7 @@ class _DropoutAddFn(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
-        dx = B.dropout_add(_as_rows(dy), ctx.p, ctx.seed).view(dy.shape) if ctx.needs_input_grad[0] else None
+        dx = dropout_add(dy, ctx.p, ctx.seed) if ctx.needs_input_grad[0] else None         # the same linear map, differentiable again
         return dx, dy if ctx.needs_input_grad[1] else None, None, None
 
 
@@ -216,8 +238,7 @@ class DropoutAdd(torch.nn.Module):
 class _AttentionFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, causal, window_left, k_lens, scale):
-        q, k, v = (_as_heads(t) for t in (q, k, v))
-        o, lse = B.attention(q, k, v, causal, window_left, k_lens, scale)
+        o, lse = B.attention(_as_heads(q), _as_heads(k), _as_heads(v), causal, window_left, k_lens, scale)
         ctx.save_for_backward(q, k, v, o, lse, k_lens)
         ctx.args = causal, window_left, scale
         return o
@@ -226,8 +247,8 @@ class _AttentionFn(torch.autograd.Function):
     def backward(ctx, do):
         q, k, v, o, lse, k_lens = ctx.saved_tensors
         causal, window_left, scale = ctx.args
-        dq, dk, dv = B.attention_backward(_as_heads(do), q, k, v, o, lse, causal, window_left, k_lens, scale)
-        return dq, dk, dv, None, None, None, None
+        grads = B.attention_backward(*(_as_heads(t) for t in (do, q, k, v)), o, lse, causal, window_left, k_lens, scale)
+        return *_once("attention", grads, do, q, k, v), None, None, None, None
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, window_left: int = -1,
