@@ -53,6 +53,13 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 
+// Load at device scope: from where every SM sees the same value, not from this SM's first-level cache or the read-only path.
+__device__ __forceinline__ float load_device(const float* p) {
+    float r;
+    asm volatile("ld.relaxed.gpu.global.f32 %0, [%1];" : "=f"(r) : "l"(p) : "memory");
+    return r;
+}
+
 // Acquire at CTA scope: these kernels have no clusters, and the cluster-scope wait costs over a hundred cycles even when the phase
 // is complete (the issuing warp passes six of them per pair of tiles).
 __device__ __forceinline__ bool try_wait_cta(uint32_t bar, uint32_t parity) {

@@ -194,7 +194,10 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     asm volatile("griddepcontrol.wait;" ::: "memory");           // the rows are there
-    asm volatile("griddepcontrol.launch_dependents;");            // the queries kernel needs nothing of this one: it may fill its tail
+    // The queries kernel needs nothing of this one and may fill its tail.  It does need the rows, and has no wait of its own in front of
+    // them (that would be a wait for this grid's end): it starts once every CTA of this grid is past the line above, so once the rows grid
+    // has ended and its writes have been performed at device scope, and reads them with loads of that scope.
+    asm volatile("griddepcontrol.launch_dependents;");
 
     if (warp == 0) {
         // ------------------------------------------------------------------ copies
@@ -543,7 +546,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         const int plain_lo = p.left >= 0 ? (p.key_lo(i0 + B128 - 1) + B128 - 1) / B128 : 0;
         const int plain_hi = max(p.key_hi(i0, keys), 0) / B128;
         const int64_t at = ((int64_t)b * p.heads + h) * p.q_pad + row;
-        const float nl = __ldg(p.lse2 + at), nd = __ldg(p.delta + at);
+        const float nl = load_device(p.lse2 + at), nd = load_device(p.delta + at);         // visible: see launch_dependents in the keys kernel
         const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2), nl2 = f2_pack(nl, nl), nd2 = f2_pack(nd, nd);
         bool ok = true;
         if (steps > 0) {
