@@ -396,6 +396,16 @@ UE5M3_API int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const
                               void* stream);
 
 /*
+ * Failure-detection self-test of the attention kernels, as ue5m3_gemm_stall_selftest: a small problem with the copies switched
+ * off and every wait bounded by wait_limit_cycles.  All roles give up, drain, release tensor memory and return;
+ * ue5m3_last_device_status() then returns UE5M3_ERR_TIMEOUT once, and the context stays usable.
+ *   which    0 = attention, 1 = attention with few queries (keys shared out; the joining kernel runs behind it), 2 = attention backward.
+ *   buffer   device, 16-byte aligned, at least UE5M3_BLOCK_SELFTEST_BYTES: the problem's tensors, o first.  o is not written by 0.
+ */
+#define UE5M3_BLOCK_SELFTEST_BYTES ((size_t)4 << 20)
+UE5M3_API int ue5m3_block_stall_selftest(int which, void* buffer, size_t bytes, int64_t wait_limit_cycles, void* stream);
+
+/*
  * Bytes a scale buffer needs.  rows/cols are those of the SOURCE tensor given to ue5m3_quantize.
  * (Section 3.2: one scale per block of B = 16; Section 3.3: one per 16x16 weight tile.)
  * Returns 0 for invalid arguments.

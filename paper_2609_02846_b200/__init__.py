@@ -11,5 +11,5 @@ from .binding import (  # noqa: F401
     SCALE_1D, SCALE_1D_TILED, SCALE_2D, SCALES_ROWMAJOR, SCALES_TILED,
     AmaxCache, QuantizedOperand, Ue5m3Error, gemm, gemm_fp16, gemm_native, gemm_native_workspace, gemm_static, native_windows, gemm_probe_matched, gemm_stall_selftest, last_device_status, library_path, linear_backward,
     linear_forward, quantize, quantize_current, quantize_dual, sample_amax, scales_bytes, status_string, unswizzle_scales,
-    attention, attention_backward, dropout_add, layer_norm, layer_norm_backward,
+    attention, attention_backward, block_stall_selftest, dropout_add, layer_norm, layer_norm_backward,
 )

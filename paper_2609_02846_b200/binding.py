@@ -25,7 +25,7 @@ SYMBOLS = ("ue5m3_sample_amax", "ue5m3_quantize", "ue5m3_quantize_dual", "ue5m3_
            "ue5m3_gemm_probe_matched", "ue5m3_gemm_stall_selftest", "ue5m3_scales_bytes", "ue5m3_unswizzle_scales",
            "ue5m3_last_device_status", "ue5m3_status_string", "ue5m3_layer_norm", "ue5m3_layer_norm_backward_workspace_bytes",
            "ue5m3_layer_norm_backward", "ue5m3_dropout_add", "ue5m3_attention_workspace_bytes", "ue5m3_attention",
-           "ue5m3_attention_backward_workspace_bytes", "ue5m3_attention_backward")
+           "ue5m3_attention_backward_workspace_bytes", "ue5m3_attention_backward", "ue5m3_block_stall_selftest")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libue5m3.so")
@@ -106,6 +106,8 @@ def _load() -> C.CDLL:
         L.ue5m3_attention_backward_workspace_bytes.argtypes = [shape]
         L.ue5m3_attention_backward.restype = ci
         L.ue5m3_attention_backward.argtypes = [shape, heads, heads, heads, heads, heads, vp, heads, heads, heads, vp, vp]
+        L.ue5m3_block_stall_selftest.restype = ci
+        L.ue5m3_block_stall_selftest.argtypes = [ci, vp, C.c_size_t, i64, vp]
         L.ue5m3_status_string.restype = C.c_char_p
         L.ue5m3_status_string.argtypes = [ci]
         _lib = L
@@ -599,6 +601,13 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     _call(lib.ue5m3_attention_backward, "ue5m3_attention_backward", q, shape, _heads(dout, qs, q), _heads(q, qs, q), _heads(k, ks, q),
           _heads(v, ks, q), _heads(o, qs, q), lse.data_ptr(), _heads(dq, qs, q), _heads(dk, ks, q), _heads(dv, ks, q), ws.data_ptr())
     return dq, dk, dv
+
+
+def block_stall_selftest(which: int, buffer: torch.Tensor, wait_limit_cycles: int = 2_000_000) -> None:
+    """ue5m3_block_stall_selftest: launches a small attention (0), attention with few queries (1) or attention backward (2) with its
+    copies switched off and every wait bounded by `wait_limit_cycles`; `last_device_status()` then reports the timeout once."""
+    _call(_load().ue5m3_block_stall_selftest, "ue5m3_block_stall_selftest", buffer, int(which), buffer.data_ptr(),
+          buffer.numel() * buffer.element_size(), int(wait_limit_cycles))
 
 
 # ---------------------------------------------------------------------------------------------

@@ -516,6 +516,42 @@ int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_hea
     return launch_attention_backward(s, *dout, *q, *k, *v, *o, lse, *dq, *dk, *dv, static_cast<float*>(workspace), (cudaStream_t)stream);
 }
 
+// Self-test problems: one sequence, heads of 64 that share one key/value head, 300 queries of two heads on 300 keys or one query of
+// four on 4096 (one tile for all heads, keys shared out).  The tensors lie one behind the other in the caller's buffer.
+int ue5m3_block_stall_selftest(int which, void* buffer, size_t bytes, int64_t wait_limit_cycles, void* stream) {
+    const ApiRange range_("ue5m3_block_stall_selftest");
+    if (which < 0 || which > 2 || !buffer || bytes < UE5M3_BLOCK_SELFTEST_BYTES) return UE5M3_ERR_INVALID_ARG;
+    if (wait_limit_cycles < 1000 || wait_limit_cycles > 4000000000LL) return UE5M3_ERR_INVALID_ARG;
+    if (!aligned16(buffer)) return UE5M3_ERR_ALIGN;
+    int sms = 0;
+    const int bad = device_ready(sms);
+    if (bad != UE5M3_OK) return bad;
+    const StallTest stall{wait_limit_cycles};
+    char* at = static_cast<char*>(buffer);
+    auto take = [&](size_t n) { char* p = at; at += (n + 255) / 256 * 256; return static_cast<void*>(p); };
+    ue5m3_attention_shape s{};
+    s.batch = s.kv_heads = 1;
+    s.heads = which == 1 ? 4 : 2;
+    s.q_len = which == 1 ? 1 : 300;
+    s.k_len = which == 1 ? 4096 : 300;
+    s.head_dim = 64;
+    s.window_left = -1;
+    s.scale = 0.125f;
+    s.dtype = UE5M3_BF16;
+    auto tensor = [&](int64_t tokens, int64_t heads) {
+        return ue5m3_heads{take((size_t)(tokens * heads * s.head_dim) * 2), tokens * heads * s.head_dim, heads * s.head_dim, s.head_dim};
+    };
+    const ue5m3_heads o = tensor(s.q_len, s.heads), q = tensor(s.q_len, s.heads), k = tensor(s.k_len, 1), v = tensor(s.k_len, 1);
+    float* lse = static_cast<float*>(take((size_t)(s.heads * s.q_len) * sizeof(float)));
+    if (which < 2) {
+        float* ws = static_cast<float*>(take(ue5m3_attention_workspace_bytes(&s)));
+        return launch_attention(s, q, k, v, o, lse, ws, sms, (cudaStream_t)stream, stall);
+    }
+    const ue5m3_heads dout = tensor(s.q_len, s.heads), dq = tensor(s.q_len, s.heads), dk = tensor(s.k_len, 1), dv = tensor(s.k_len, 1);
+    float* ws = static_cast<float*>(take(ue5m3_attention_backward_workspace_bytes(&s)));
+    return launch_attention_backward(s, dout, q, k, v, o, lse, dq, dk, dv, ws, (cudaStream_t)stream, stall);
+}
+
 int ue5m3_last_device_status(void) {
     const int a = read_and_clear_device_status();
     const int b = read_and_clear_probe_status();

@@ -51,6 +51,9 @@ template <int DP> struct Tiles {                          // DP: head dimension 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
     return wait_inline(bar, parity, abort_flag, &g_attention_status, limit);
 }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+    return wait_warp(bar, parity, abort_flag, &g_attention_status, limit);
+}
 __device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
     wait_inline(bar, parity, abort_flag, &g_attention_status, limit, true);
 }
@@ -160,7 +163,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             // n - PAIRS's K, the other that of the next pair's V.
             auto emptied = [&](int pair) { return pair < 0 || wait(kv_empty + 8 * (pair % T::PAIRS), (pair / T::PAIRS) & 1, abort_flag, p.wait_limit); };
             int n = 0, q_uses[2] = {0, 0};
-            bool go = true;
+            bool go = !p.stall;
             for (int turn = 0, index; go && (index = item_at(turn)) < items; ++turn) {
                 const Item w = item_of<PARTS, PACK>(p, index, q_tiles);
                 const int pairs = w.last > w.first ? w.last - w.first + 1 : 0;
@@ -354,7 +357,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * half);
         };
         for (int j = n0; j < n1; ++j, ++n) {
-            if (!(ok = wait(s_full + 8 * t, n & 1, abort_flag, p.wait_limit))) break;
+            if (!(ok = warp_wait(s_full + 8 * t, n & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t s[128];
 #pragma unroll
@@ -395,6 +398,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             publish(1, pk);
             l2 = f2_add(l2, sum);
         }
+        if (!ok) break;
         float l;
         {
             float a, b2;
@@ -405,8 +409,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const bool some = l > 0.0f || l != l;              // this query sees a key
         if (exists) (PARTS ? p.part_lse : p.lse)[lse_at] = some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
         const bool any = n1 > n0;
-        if (any && ok) {
-            ok = wait(o_full + 8 * t, uses & 1, abort_flag, p.wait_limit);
+        if (any) {
+            ok = warp_wait(o_full + 8 * t, uses & 1, abort_flag, p.wait_limit);
             ++uses;
             tc_fence_after();
         }
@@ -557,7 +561,7 @@ int attention_splits(const ue5m3_attention_shape& s) {
 }
 
 int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
-                     const ue5m3_heads& o, float* lse, float* workspace, int num_sms, cudaStream_t st) {
+                     const ue5m3_heads& o, float* lse, float* workspace, int num_sms, cudaStream_t st, const StallTest& stall) {
     if (s.batch == 0 || s.q_len == 0) return UE5M3_OK;
     CUtensorMap mq, mk, mv;
     const int pack = packed_heads(s);
@@ -569,6 +573,7 @@ int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const
     p.lse = lse;
     p.parts = attention_splits(s);
     p.pack = pack;
+    if (stall.wait_limit > 0) { p.wait_limit = stall.wait_limit; p.stall = 1; }
     const OutputParams out{static_cast<__nv_bfloat16*>(o.data), o.batch_stride, o.token_stride, o.head_stride};
     if (p.parts == 1) return run<false>(s, mq, mk, mv, p, out, num_sms, st);
     const int64_t rows = s.batch * s.heads * s.q_len;

@@ -88,6 +88,11 @@ __device__ __forceinline__ bool wait_inline(uint32_t bar, uint32_t parity, volat
         }
     }
 }
+// The same for a whole warp: complete for every lane, or given up by every lane.  A lane that gave up alone (the clock and the abort
+// flag are read lane by lane) would leave the others in front of tensor-memory instructions and votes that want the whole warp.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status_word, long long limit) {
+    return __all_sync(0xFFFFFFFFu, wait_inline(bar, parity, abort_flag, status_word, limit));
+}
 // 384 threads are launched with 168 registers each (64,512 in all): the four warps that copy and issue give theirs up, the eight
 // that do the arithmetic take them (128 x 88 + 256 x 208 = 64,512).
 __device__ __forceinline__ void registers_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
@@ -252,6 +257,7 @@ struct AttentionParams {
     int dim, parts;                      // head dimension; parts into which the key tiles of a query are shared out
     float* part_o; float* part_lse;      // parts > 1: o (backward: dq) [parts][batch][heads][q_len][dim]; forward: lse [..][q_len]
     long long wait_limit;
+    int stall;                           // self-test: no copy is issued, so every wait for one runs out
 
     __device__ __forceinline__ int keys_of(int b) const {
         if (!k_lens) return k_len;

@@ -41,6 +41,9 @@ constexpr int B128 = 128;
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
     return wait_inline(bar, parity, abort_flag, &g_attention_backward_status, limit);
 }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+    return wait_warp(bar, parity, abort_flag, &g_attention_backward_status, limit);
+}
 __device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
     wait_inline(bar, parity, abort_flag, &g_attention_backward_status, limit, true);
 }
@@ -201,7 +204,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 
     if (warp == 0) {
         // ------------------------------------------------------------------ copies
-        if (lane == 0 && steps > 0) {
+        if (lane == 0 && steps > 0 && !p.stall) {
             auto tile = [&](uint32_t dst, const CUtensorMap* m, uint32_t bar, int row, int head) {
 #pragma unroll
                 for (int c = 0; c < T::PANELS; ++c) tma_load_4d(dst + c * T::PANEL, m, bar, c * 64, row, head, b);
@@ -316,9 +319,9 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             const float* rows = reinterpret_cast<const float*>(smem_gen + M::ROWS + (it % M::STAGES) * 1024) + g * 64;
             const bool plain = qt >= plain_lo && qt < plain_hi;
             const int base = qt * B128 + g * 64 - q_lo, width = q_hi - q_lo;
-            if (!(ok = wait(s_full, it & 1, abort_flag, p.wait_limit))) break;
+            if (!(ok = warp_wait(s_full, it & 1, abort_flag, p.wait_limit))) break;
             // this query tile's rows of lse2 and delta came with Q, whose barrier S waited for; seen by every thread
-            if (!(ok = wait(q_full + 8 * (it % M::STAGES), (it / M::STAGES) & 1, abort_flag, p.wait_limit))) break;
+            if (!(ok = warp_wait(q_full + 8 * (it % M::STAGES), (it / M::STAGES) & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t s[64];
             tmem_ld32(ts, s);
@@ -343,7 +346,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 __syncwarp();
                 if (lane == 0) mbar_arrive(half ? p_full : p_half);
             }
-            if (!(ok = wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
+            if (!(ok = warp_wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t pk[32];
 #pragma unroll
@@ -370,7 +373,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             if (lane == 0) mbar_arrive(ds_full);
         }
         if (ok && steps > 0) {
-            ok = wait(acc_full, 0, abort_flag, p.wait_limit);
+            ok = warp_wait(acc_full, 0, abort_flag, p.wait_limit);
             tc_fence_after();
         }
         // group 0 writes dV over V's tile, group 1 dK over K's: no MMA reads them any more (or they were never loaded)
@@ -450,7 +453,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
 
     if (warp == 0) {
         // ------------------------------------------------------------------ copies
-        if (lane == 0 && steps > 0) {
+        if (lane == 0 && steps > 0 && !p.stall) {
             auto tile = [&](uint32_t dst, const CUtensorMap* m, uint32_t bar, int row, int head) {
 #pragma unroll
                 for (int c = 0; c < T::PANELS; ++c) tma_load_4d(dst + c * T::PANEL, m, bar, c * 64, row, head, b);
@@ -551,7 +554,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         bool ok = true;
         if (steps > 0) {
             // group 0 moves Q into tensor memory, group 1 dO: a thread its own row, undoing the swizzle
-            ok = wait(full + 8 * g, 0, abort_flag, p.wait_limit);
+            ok = warp_wait(full + 8 * g, 0, abort_flag, p.wait_limit);
             if (ok) {
 #pragma unroll
                 for (int c = 0; c < T::PANELS; ++c) {
@@ -572,7 +575,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             const bool plain = kt >= plain_lo && kt < plain_hi;
             const int base = kt * B128 + g * 64 - k_lo, width = k_hi - k_lo;
             const uint32_t ts = lane_base + COL_S + g * 64, td = lane_base + COL_DP + g * 64;
-            if (!(ok = wait(s_full, it & 1, abort_flag, p.wait_limit))) break;
+            if (!(ok = warp_wait(s_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t s[64];
             tmem_ld32(ts, s);
@@ -586,7 +589,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             for (int i = 0; i < 32; ++i) pr[i] = ex2_pair(f2_fma(pair_of(s + 2 * i), c2, nl2));
             if (!plain) hide_pairs<32>(pr, -base, width - base, p.left >= 0, true);
             const bool short_tile = p.k_lens && (kt + 1) * B128 > keys;           // values behind the end may be NaN, and so then is dP
-            if (!(ok = wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
+            if (!(ok = warp_wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t pk[32];
 #pragma unroll
@@ -609,7 +612,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             if (lane == 0) mbar_arrive(ds_full);
         }
         if (ok && steps > 0) {
-            ok = wait(acc_full, 0, abort_flag, p.wait_limit);
+            ok = warp_wait(acc_full, 0, abort_flag, p.wait_limit);
             tc_fence_after();
         }
         if (PARTS) {
@@ -717,7 +720,7 @@ int attention_backward_splits(const ue5m3_attention_shape& s) {
 
 int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q, const ue5m3_heads& k,
                               const ue5m3_heads& v, const ue5m3_heads& o, const float* lse, const ue5m3_heads& dq,
-                              const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace, cudaStream_t st) {
+                              const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace, cudaStream_t st, const StallTest& stall) {
     if (s.batch == 0 || (s.q_len == 0 && s.k_len == 0)) return UE5M3_OK;
     Maps m;
     const int64_t B = s.batch, D = s.head_dim;
@@ -730,6 +733,7 @@ int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads&
     if (s.q_len == 0) m.q = m.dout = m.k;                  // an empty side is never read
     if (s.k_len == 0) m.k = m.v = m.q;
     AttentionParams p = attention_params(s);
+    if (stall.wait_limit > 0) { p.wait_limit = stall.wait_limit; p.stall = 1; }
     if (s.q_len > 0) {
         RowParams r{};
         r.o = static_cast<const __nv_bfloat16*>(o.data); r.dout = static_cast<const __nv_bfloat16*>(dout.data);

@@ -20,6 +20,9 @@ inline cudaError_t allow_smem(Kernel* kernel, int bytes, std::atomic<int> (&gran
     return e;
 }
 
+// Failure-detection self-test: the bound of every device-side wait in SM clocks, with the copies switched off (0: a normal launch).
+struct StallTest { long long wait_limit = 0; };
+
 struct LayerNormArgs {
     const void* x; int64_t ldx;
     const void* weight; const void* bias;
@@ -48,12 +51,12 @@ cudaError_t launch_dropout_add(const DropoutArgs& a, int dtype, cudaStream_t st)
 
 // returns a UE5M3_* status
 int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
-                     const ue5m3_heads& o, float* lse, float* workspace, int num_sms, cudaStream_t st);
+                     const ue5m3_heads& o, float* lse, float* workspace, int num_sms, cudaStream_t st, const StallTest& stall = {});
 int attention_splits(const ue5m3_attention_shape& s);      // parts into which the keys are shared out (1: none)
 int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q,
                               const ue5m3_heads& k, const ue5m3_heads& v, const ue5m3_heads& o, const float* lse,
                               const ue5m3_heads& dq, const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace,
-                              cudaStream_t st);
+                              cudaStream_t st, const StallTest& stall = {});
 int attention_backward_splits(const ue5m3_attention_shape& s);        // the same for the queries' gradient
 int read_and_clear_norm_status();                 // these three synchronise the device
 int read_and_clear_attention_status();
