@@ -604,8 +604,8 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
 
 
 def block_stall_selftest(which: int, buffer: torch.Tensor, wait_limit_cycles: int = 2_000_000) -> None:
-    """ue5m3_block_stall_selftest: launches a small attention (0), attention with few queries (1) or attention backward (2) with its
-    copies switched off and every wait bounded by `wait_limit_cycles`; `last_device_status()` then reports the timeout once."""
+    """ue5m3_block_stall_selftest: launches a small attention (0), attention with few queries (1), attention backward (2), layer
+    norm (3) or layer norm backward (4) with its copies switched off and every wait bounded by `wait_limit_cycles`; `last_device_status()` then reports the timeout once."""
     _call(_load().ue5m3_block_stall_selftest, "ue5m3_block_stall_selftest", buffer, int(which), buffer.data_ptr(),
           buffer.numel() * buffer.element_size(), int(wait_limit_cycles))
 

@@ -379,7 +379,7 @@ int ue5m3_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64
     if (rows == 0) return UE5M3_OK;
     LayerNormArgs a{};
     a.x = x; a.ldx = ldx; a.weight = weight; a.bias = bias; a.y = y; a.ldy = ldy; a.mean = mean; a.rstd = rstd;
-    a.rows = rows; a.cols = cols; a.eps = eps;
+    a.rows = a.copy_rows = rows; a.cols = cols; a.eps = eps;
     return launch_layer_norm(a, dtype, weight_dtype, sms, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
@@ -410,7 +410,7 @@ int ue5m3_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int d
     a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.weight = weight; a.y = dx; a.ldy = lddx;
     a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
     a.dweight = dweight; a.dbias = dbias; a.partial = sums ? static_cast<float*>(workspace) : nullptr;
-    a.rows = rows; a.cols = cols;
+    a.rows = a.copy_rows = rows; a.cols = cols;
     return launch_layer_norm_backward(a, dtype, weight_dtype, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
@@ -516,11 +516,11 @@ int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_hea
     return launch_attention_backward(s, *dout, *q, *k, *v, *o, lse, *dq, *dk, *dv, static_cast<float*>(workspace), (cudaStream_t)stream);
 }
 
-// Self-test problems: one sequence, heads of 64 that share one key/value head, 300 queries of two heads on 300 keys or one query of
+// Self-test problems: 4500 rows of 64 columns in BF16, three to each of the 148 x 15 row groups; one sequence, heads of 64 that share one key/value head, 300 queries of two heads on 300 keys or one query of
 // four on 4096 (one tile for all heads, keys shared out).  The tensors lie one behind the other in the caller's buffer.
 int ue5m3_block_stall_selftest(int which, void* buffer, size_t bytes, int64_t wait_limit_cycles, void* stream) {
     const ApiRange range_("ue5m3_block_stall_selftest");
-    if (which < 0 || which > 2 || !buffer || bytes < UE5M3_BLOCK_SELFTEST_BYTES) return UE5M3_ERR_INVALID_ARG;
+    if (which < 0 || which > 4 || !buffer || bytes < UE5M3_BLOCK_SELFTEST_BYTES) return UE5M3_ERR_INVALID_ARG;
     if (wait_limit_cycles < 1000 || wait_limit_cycles > 4000000000LL) return UE5M3_ERR_INVALID_ARG;
     if (!aligned16(buffer)) return UE5M3_ERR_ALIGN;
     int sms = 0;
@@ -529,6 +529,25 @@ int ue5m3_block_stall_selftest(int which, void* buffer, size_t bytes, int64_t wa
     const StallTest stall{wait_limit_cycles};
     char* at = static_cast<char*>(buffer);
     auto take = [&](size_t n) { char* p = at; at += (n + 255) / 256 * 256; return static_cast<void*>(p); };
+    if (which >= 3) {
+        const int64_t rows = 4500, cols = 64;
+        const size_t matrix = (size_t)(rows * cols) * 2;
+        LayerNormArgs a{};
+        a.y = take(matrix);
+        a.x = take(matrix);
+        a.ldx = a.ldy = a.lddy = a.cols = cols;
+        a.mean = static_cast<float*>(take(rows * sizeof(float)));
+        a.rstd = static_cast<float*>(take(rows * sizeof(float)));
+        a.rows = rows;
+        a.copy_rows = rows / 2;                           // the second row that a row group takes arrives or does not, its third does not
+        a.wait_limit = wait_limit_cycles;
+        if (which == 3) return launch_layer_norm(a, UE5M3_BF16, UE5M3_F32, sms, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+        a.dy = take(matrix);
+        a.dweight = take(cols * sizeof(float));
+        a.dbias = take(cols * sizeof(float));
+        a.partial = static_cast<float*>(take(ue5m3_layer_norm_backward_workspace_bytes(rows, cols)));
+        return launch_layer_norm_backward(a, UE5M3_BF16, UE5M3_F32, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+    }
     ue5m3_attention_shape s{};
     s.batch = s.kv_heads = 1;
     s.heads = which == 1 ? 4 : 2;

@@ -125,16 +125,40 @@ __device__ __forceinline__ void zero_scratch(float* scratch, int floats) {
 // ------------------------------------------------------------------------------------------------ rows through a ring
 // A row group's ring of `slots` entries in shared memory: entry i % slots receives row `first + i * step` of one or two matrices.
 // Thread 0 of the group issues the copies; an entry is refilled once the whole group has read it into registers (behind the
-// barrier of the row's first sum).  Waits are bounded: one that gives up sets the status word and goes on with what is there.
+// barrier of the row's first sum).  Waits are bounded.  One that gives up sets the status word and the CTA's flag, and the threads, which
+// still have to meet at the barriers, go through the rows that are left with what is there: no wait is tried a second time, nothing
+// more is copied (an entry is refilled only by a thread that has seen its copy end), and the copies in flight are seen out at the end.
+struct RingHead {                      // at the front of the shared memory
+    int gave_up;
+    struct { int64_t from, to; } lost[15];         // per row group: rows that were being copied when its thread 0 gave up
+};
+constexpr int kRingHead = 256;
+static_assert(sizeof(RingHead) <= kRingHead, "RingHead");
+constexpr int64_t kNoMore = (int64_t)1 << 61;      // the next row to be copied, of a thread 0 that gave up (rows end at 2^60)
 struct RowRing {
     uint32_t base, bars, entry_bytes;
     int slots;
     int slot = 0;                      // entry of the current row, and its phase
     uint32_t phase = 0;
+    static __device__ __forceinline__ long long bound(const LayerNormArgs& a) { return a.wait_limit > 0 ? a.wait_limit : WAIT_LIMIT_CYCLES; }
     __device__ __forceinline__ uint32_t entry() const { return base + (uint32_t)slot * entry_bytes; }
     __device__ __forceinline__ uint32_t bar() const { return bars + 8u * (uint32_t)slot; }
-    __device__ __forceinline__ void wait() const {
-        if (!mbar_try_wait(bar(), phase)) mbar_wait_drain(bar(), phase, &g_norm_status, WAIT_LIMIT_CYCLES);
+    __device__ __forceinline__ void wait(const LayerNormArgs& a, RingHead* head, int64_t row, int64_t& next) const {
+        if (mbar_try_wait(bar(), phase)) return;
+        volatile int* gave_up = &head->gave_up;
+        if (!*gave_up && mbar_wait_slow(bar(), phase, gave_up, &g_norm_status, bound(a))) return;
+        if (threadIdx.x == 0 && next < kNoMore) {
+            head->lost[threadIdx.y] = {row, min(next, a.copy_rows)};
+            next = kNoMore;
+        }
+    }
+    // Thread 0 of a group, behind its last row: if it gave up, waits, bounded, for the copies in flight.
+    __device__ __forceinline__ void drain(const LayerNormArgs& a, const RingHead* head, int64_t first, int64_t step, int64_t next) const {
+        if (next < kNoMore) return;
+        for (int64_t row = head->lost[threadIdx.y].from; row < head->lost[threadIdx.y].to; row += step) {
+            const int64_t i = (row - first) / step;
+            mbar_wait_drain(bars + 8u * (uint32_t)(i % slots), (uint32_t)(i / slots) & 1u, &g_norm_status, bound(a));
+        }
     }
     __device__ __forceinline__ void advance() {
         if (++slot == slots) { slot = 0; phase ^= 1; }
@@ -175,10 +199,12 @@ template <typename TX, typename TW, int NV, bool FULL>
 __global__ void __launch_bounds__(512)
 layer_norm_ring_kernel(const LayerNormArgs a, const int slots) {
     constexpr int VEC = 16 / sizeof(TX), PAIRS = VEC / 2;
-    extern __shared__ __align__(16) uint8_t ring_smem[];
+    extern __shared__ __align__(16) uint8_t ring_raw[];
+    RingHead* head = reinterpret_cast<RingHead*>(ring_raw);
+    uint8_t* ring_smem = ring_raw + kRingHead;
     const int T = blockDim.x, R = blockDim.y, bar_id = 1 + threadIdx.y;
     const uint32_t row_bytes = (uint32_t)a.cols * sizeof(TX), smem = smem_u32(ring_smem);
-    // [R][64] scratch, [R][slots] rows, [R][slots] barriers
+    // the head, [R][64] scratch, [R][slots] rows, [R][slots] barriers
     float* scratch = reinterpret_cast<float*>(ring_smem) + threadIdx.y * 64;
     RowRing ring{smem + R * 256 + threadIdx.y * slots * row_bytes, smem + R * 256 + R * slots * row_bytes + threadIdx.y * slots * 8, row_bytes, slots};
     const int nvec = (int)(a.cols / VEC);
@@ -188,7 +214,7 @@ layer_norm_ring_kernel(const LayerNormArgs a, const int slots) {
     const TX* src = x + first * a.ldx;                     // the next row to be copied
     int64_t next = first;
     auto fill = [&](uint32_t entry, uint32_t bar) {
-        if (next < a.rows) {
+        if (next < a.copy_rows) {
             mbar_expect_tx(bar, row_bytes);
             bulk_load(entry, src, row_bytes, bar);
         }
@@ -215,13 +241,14 @@ layer_norm_ring_kernel(const LayerNormArgs a, const int slots) {
         for (int j = 0; j < PAIRS; ++j) { w[k][j] = f2_pack(t[2 * j], t[2 * j + 1]); b[k][j] = f2_pack(u[2 * j], u[2 * j + 1]); }
     }
     zero_scratch(reinterpret_cast<float*>(ring_smem), R * 64);
-    __syncthreads();                                       // the barriers and the scratch exist
+    if (threadIdx.x == 0 && threadIdx.y == 0) head->gave_up = 0;
+    __syncthreads();                                       // the barriers, the scratch and the flag exist
     const float inv_n = 1.0f / (float)a.cols;
     int turn = 0;
     TX* dst = static_cast<TX*>(a.y) + first * a.ldy + threadIdx.x * VEC;
     for (int64_t row = first; row < a.rows; row += step, dst += step * a.ldy) {
         f32x2 f[NV][PAIRS], acc = 0;
-        ring.wait();
+        ring.wait(a, head, row, next);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             if constexpr (!FULL) {
@@ -265,6 +292,7 @@ layer_norm_ring_kernel(const LayerNormArgs a, const int slots) {
             if (a.rstd) a.rstd[row] = rstd;
         }
     }
+    if (threadIdx.x == 0) ring.drain(a, head, first, step, next);
 }
 
 // Rows without 16-byte alignment: NV single columns per thread, prefetched one row ahead; otherwise as above.
@@ -418,14 +446,16 @@ __device__ __forceinline__ void leave_columns(const LayerNormArgs& a, float* sum
         }
 }
 
-// Rows of x and dy come through the ring (an entry holds both).  Dynamic shared memory: [R][128] reduction scratch, [R][slots]
+// Rows of x and dy come through the ring (an entry holds both).  Dynamic shared memory: the head, [R][128] reduction scratch, [R][slots]
 // barriers, [R][slots][2] rows; at the end the column sums over them.  16 columns per thread: weights, both column sums and both rows
 // are 80 registers already.  16384 x 4096 BF16 with the adding kernel: 72 us, 5.6 TB/s (0.86 of the measured copy).
 template <typename TX, typename TW, int NV, bool FULL>
 __global__ void __launch_bounds__(512)
 layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
     constexpr int VEC = 16 / sizeof(TX), PAIRS = VEC / 2;
-    extern __shared__ __align__(16) float smem[];
+    extern __shared__ __align__(16) uint8_t ring_raw[];
+    RingHead* head = reinterpret_cast<RingHead*>(ring_raw);
+    float* smem = reinterpret_cast<float*>(ring_raw + kRingHead);
     asm volatile("griddepcontrol.launch_dependents;");    // the adding kernel may take its place; it waits for this grid's end
     const int T = blockDim.x, R = blockDim.y, bar_id = 1 + threadIdx.y;
     float* scratch = smem + threadIdx.y * 128;
@@ -439,7 +469,7 @@ layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
     const TX* src_dy = static_cast<const TX*>(a.dy) + first * a.lddy;
     int64_t next = first;
     auto fill = [&](uint32_t entry, uint32_t bar) {
-        if (next < a.rows) {
+        if (next < a.copy_rows) {
             mbar_expect_tx(bar, 2 * row_bytes);
             bulk_load(entry, src_x, row_bytes, bar);
             bulk_load(entry + row_bytes, src_dy, row_bytes, bar);
@@ -466,7 +496,8 @@ layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
         for (int j = 0; j < PAIRS; ++j) { w[k][j] = f2_pack(t[2 * j], t[2 * j + 1]); dw[k][j] = 0; db[k][j] = 0; }
     }
     zero_scratch(smem, R * 128);
-    __syncthreads();                                       // the barriers and the scratch exist
+    if (threadIdx.x == 0 && threadIdx.y == 0) head->gave_up = 0;
+    __syncthreads();                                       // the barriers, the scratch and the flag exist
     const float inv_n = 1.0f / (float)a.cols;
     float next_mean = 0.0f, next_rstd = 0.0f;
     if (first < a.rows) { next_mean = __ldg(a.mean + first); next_rstd = __ldg(a.rstd + first); }
@@ -477,7 +508,7 @@ layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
         if (row + step < a.rows) { next_mean = __ldg(a.mean + row + step); next_rstd = __ldg(a.rstd + row + step); }
         const f32x2 minus = f2_pack(-mean, -mean), rr = f2_pack(rstd, rstd);
         f32x2 xh[NV][PAIRS], g[NV][PAIRS], sg = 0, sgx = 0;
-        ring.wait();
+        ring.wait(a, head, row, next);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (mine(k)) {
@@ -510,6 +541,7 @@ layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
                 stg_pairs(dst + (int64_t)k * T * VEC, o);
             }
     }
+    if (threadIdx.x == 0) ring.drain(a, head, first, step, next);
     if (!a.partial) return;
     // every copy has been waited for: the rings' memory is free once all groups are here
     leave_columns<VEC, NV>(a, smem + R * 128, nvec, [&](int which, int k, int j) {
@@ -702,7 +734,7 @@ cudaError_t run_forward_ring(const LayerNormArgs& a, int num_sms, cudaStream_t s
     if (s.groups > spread) s.groups = (int)spread;
     const int64_t row_bytes = a.cols * (int64_t)sizeof(TX);
     const int slots = ring_slots(s.groups, row_bytes);
-    const size_t smem = (size_t)s.groups * (64 * sizeof(float) + slots * (row_bytes + 8));
+    const size_t smem = (size_t)s.groups * (64 * sizeof(float) + slots * (row_bytes + 8)) + kRingHead;
     static std::atomic<int> granted[64];
     const cudaError_t e = allow_smem(layer_norm_ring_kernel<TX, TW, NV, FULL>, kRingSmem, granted);
     if (e != cudaSuccess) return e;
@@ -768,7 +800,7 @@ cudaError_t run_backward(const LayerNormArgs& a, cudaStream_t st) {
     const int slots = RING ? ring_slots(s.groups, 2 * row_bytes) : 0;
     const size_t ring = (size_t)s.groups * slots * (2 * row_bytes + 8) + 16;
     const size_t sums = (size_t)(s.groups - 1) * 2 * s.threads * PER * sizeof(float);
-    const size_t smem = (size_t)s.groups * 128 * sizeof(float) + (ring > sums ? ring : sums);
+    const size_t smem = (RING ? kRingHead : 0) + (size_t)s.groups * 128 * sizeof(float) + (ring > sums ? ring : sums);
     const int64_t need = (a.rows + s.groups - 1) / s.groups;
     const int grid = (int)(need < kBwdGroups ? need : kBwdGroups);
     static std::atomic<int> granted[64];

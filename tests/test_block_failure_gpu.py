@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2609_02846_b200 as lib
+import test_layer_norm_gpu as norm
 from test_attention_gpu import check, make
 
 pytestmark = pytest.mark.gpu
@@ -13,7 +14,7 @@ ERR_TIMEOUT = 6
 BYTES = 4 << 20
 
 
-@pytest.mark.parametrize("which", [0, 1, 2])
+@pytest.mark.parametrize("which", [0, 1, 2, 3, 4])
 def test_waits_run_out_and_are_reported_once(which):
     buffer = torch.full((BYTES // 2,), 3.0, dtype=torch.bfloat16, device=DEV)
     torch.cuda.synchronize()
@@ -30,6 +31,7 @@ def test_waits_run_out_and_are_reported_once(which):
         assert bool((buffer[:300 * 2 * 64] == 3.0).all())
     check(*make(1, 300, 300, 2, 1, 64, seed=which))
     check(*make(1, 1, 4096, 4, 1, 64, seed=which))
+    norm.check(*norm.make(600, 512, torch.bfloat16, torch.float32, seed=which))
 
 
 def test_selftest_rejects_bad_arguments():
