@@ -371,7 +371,9 @@ typedef struct {
  *   q [batch, q_len, heads, head_dim], k and v [batch, k_len, kv_heads, head_dim], o like q; lse device, binary32
  *   [batch, heads, q_len] contiguous.
  *   head_dim a multiple of 8 up to 128, heads a multiple of kv_heads (UE5M3_ERR_SHAPE); pointers 16-byte aligned and
- *   strides multiples of 8 elements, positive where the dimension is larger than 1 (UE5M3_ERR_ALIGN).
+ *   strides multiples of 8 elements, positive where the dimension is larger than 1 (UE5M3_ERR_ALIGN).  o may be q (same pointer and
+ *   strides) and else has no element in common with q, k or v (UE5M3_ERR_INVALID_ARG where that is found out, as for all views of one
+ *   buffer); inputs may overlap one another.
  *   workspace  device, ue5m3_attention_workspace_bytes(shape) bytes, 16-byte aligned; 0 bytes (and a null pointer) unless there
  *              are few queries for many keys: the keys of a query are then shared out among several CTAs, whose results (binary32
  *              o and lse) pass through the workspace and are joined by a second kernel in a fixed order.
@@ -386,7 +388,8 @@ UE5M3_API int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_he
  *     dv_j = sum_i P_ij dout_i,   dS_ij = P_ij (dout_i . v_j - D_i),   dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i
  * dk and dv are summed over the query heads that share a key/value head, in binary32 and in a fixed order (no atomics).
  * Gradients of keys and values that no query sees, and of queries that see no key, are zero.
- *   dout, o, dq like q; dk, dv like k (each with strides of its own).
+ *   dout, o, dq like q; dk, dv like k (each with strides of its own).  dq, dk and dv have no element in common with one another nor
+ *   with dout, q, k or v: parts of them are written while others are computed (UE5M3_ERR_INVALID_ARG as above).  dq may be o.
  *   workspace  device, ue5m3_attention_backward_workspace_bytes(shape) bytes, 16-byte aligned.
  */
 UE5M3_API size_t ue5m3_attention_backward_workspace_bytes(const ue5m3_attention_shape* shape);

@@ -572,7 +572,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
               k_lens: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> tuple:
     """ue5m3_attention: (o, lse) for q [batch, tokens, heads, head_dim] and k, v [batch, keys, kv_heads, head_dim], bfloat16.  Any
     strides with a contiguous last dimension (views of a fused projection); `window_left` = keys a query sees before its own
-    position (-1: all), `k_lens` int32 [batch] = valid keys of each sequence, `scale` defaults to head_dim ** -0.5."""
+    position (-1: all), `k_lens` int32 [batch] = valid keys of each sequence, `scale` defaults to head_dim ** -0.5.  `out` may be q;
+    any other overlap with an input is refused."""
     shape = _attention_shape(q, k, causal, window_left, k_lens, scale)
     if out is None:
         out = q.new_empty(q.shape)
@@ -590,7 +591,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
                        scale: Optional[float] = None, out: Optional[tuple] = None) -> tuple:
     """ue5m3_attention_backward: (dq, dk, dv) from what `attention` returned (o, lse) and the gradient of o; the other arguments as
     in that call.  `out`: three tensors to write to (any strides with a contiguous last dimension, e.g. views of one fused
-    gradient)."""
+    gradient) that overlap neither one another nor dout, q, k, v."""
     shape = _attention_shape(q, k, causal, window_left, k_lens, scale)
     qs, ks = q.shape, k.shape
     if lse.shape != (shape.batch, shape.heads, shape.q_len) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != q.get_device():

@@ -1,6 +1,7 @@
 // C ABI of the UE5M3-FP4 library: argument checks on the host, then kernel launches.
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
+#include <algorithm>
 #include <cstdint>
 #include <mutex>
 #include "../../include/ue5m3.h"
@@ -448,6 +449,53 @@ static int check_attention_shape(const ue5m3_attention_shape* s) {
     if (reinterpret_cast<uintptr_t>(s->k_lens) & 3u) return UE5M3_ERR_ALIGN;
     return UE5M3_OK;
 }
+// Where the elements of a tensor of an attention call lie, in units of eight elements (16 bytes): pointers, strides and the head
+// dimension are whole numbers of them.  Dimensions of size 1 have no stride.
+struct Extent { int64_t base, sizes[4], strides[4], last; };             // last: units from the first to the last
+static Extent extent_of(const ue5m3_heads& t, int64_t batch, int64_t tokens, int64_t heads, int64_t dim) {
+    Extent e{(int64_t)(reinterpret_cast<uintptr_t>(t.data) >> 4), {batch, tokens, heads, dim / 8},
+             {t.batch_stride / 8, t.token_stride / 8, t.head_stride / 8, 1}, 0};
+    for (int i = 0; i < 4; ++i) e.last += (e.sizes[i] - 1) * (e.sizes[i] > 1 ? e.strides[i] : 0);
+    return e;
+}
+// Do two tensors have an element in common?  base_a - base_b + sum of strides * indices of a - those of b = 0 is solved stride by stride
+// from the largest down: what the smaller ones reach leaves one or two values of each index where rows do not lie on one another, as in
+// all views of a buffer.  Layouts that need more than a few thousand steps are taken as apart: this check finds mistakes, and the
+// caller's promise covers the rest.
+struct Term { int64_t stride, lo, hi; };
+static bool meets(const Term* t, int n, int64_t r, int& budget) {
+    if (n == 0) return r == 0;
+    int64_t least = 0, most = 0;
+    for (int i = 1; i < n; ++i) { least += t[i].lo * t[i].stride; most += t[i].hi * t[i].stride; }
+    auto down = [](int64_t a, int64_t b) { return a >= 0 ? a / b : -((-a + b - 1) / b); };
+    const int64_t from = std::max(t[0].lo, -down(r + most, t[0].stride)), to = std::min(t[0].hi, down(-r - least, t[0].stride));
+    for (int64_t x = from; x <= to && budget-- > 0; ++x)
+        if (meets(t + 1, n - 1, r + x * t[0].stride, budget)) return true;
+    return false;
+}
+static bool overlap(const Extent& a, const Extent& b) {
+    if (a.base > b.base + b.last || b.base > a.base + a.last) return false;
+    Term t[8];
+    int n = 0;
+    auto add = [&](int64_t stride, int64_t lo, int64_t hi) {
+        for (int i = 0; i < n; ++i)
+            if (t[i].stride == stride) { t[i].lo += lo; t[i].hi += hi; return; }
+        t[n++] = Term{stride, lo, hi};
+    };
+    for (int i = 0; i < 4; ++i) {
+        if (a.sizes[i] > 1) add(a.strides[i], 0, a.sizes[i] - 1);
+        if (b.sizes[i] > 1) add(b.strides[i], 1 - b.sizes[i], 0);
+    }
+    std::sort(t, t + n, [](const Term& x, const Term& y) { return x.stride > y.stride; });
+    int budget = 4096;
+    return meets(t, n, a.base - b.base, budget);
+}
+static bool same_layout(const Extent& a, const Extent& b) {               // of tensors of the same sizes
+    for (int i = 0; i < 3; ++i)
+        if (a.sizes[i] > 1 && a.strides[i] != b.strides[i]) return false;
+    return a.base == b.base;
+}
+
 // One tensor [batch, tokens, heads, head_dim] of an attention call.
 static int check_heads(const ue5m3_heads* t, int64_t batch, int64_t tokens, int64_t heads) {
     if (!t) return UE5M3_ERR_INVALID_ARG;
@@ -459,6 +507,7 @@ static int check_heads(const ue5m3_heads* t, int64_t batch, int64_t tokens, int6
         if (sizes[i] <= 1) continue;
         if (strides[i] <= 0 || strides[i] % 8) return UE5M3_ERR_ALIGN;
         if (strides[i] >= ((int64_t)1 << 39)) return UE5M3_ERR_UNSUPPORTED;      // a tensor map's strides end at 2^40 bytes
+        if (sizes[i] > ((int64_t)1 << 58) / strides[i]) return UE5M3_ERR_UNSUPPORTED;       // no such memory
     }
     return UE5M3_OK;
 }
@@ -483,6 +532,14 @@ int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, co
         if ((bad = check_heads(t, s.batch, s.k_len, s.kv_heads)) != UE5M3_OK) return bad;
     if (!lse && s.batch * s.q_len > 0) return UE5M3_ERR_INVALID_ARG;
     if (!workspace && attention_splits(s) > 1) return UE5M3_ERR_INVALID_ARG;
+    if (s.batch * s.q_len > 0) {
+        const Extent eo = extent_of(*o, s.batch, s.q_len, s.heads, s.head_dim), eq = extent_of(*q, s.batch, s.q_len, s.heads, s.head_dim);
+        // in place of q: a CTA that writes rows of o is the only one that reads these rows of q, and has read them
+        if (!same_layout(eo, eq) && overlap(eo, eq)) return UE5M3_ERR_INVALID_ARG;
+        if (s.k_len > 0)
+            for (const ue5m3_heads* t : {k, v})
+                if (overlap(eo, extent_of(*t, s.batch, s.k_len, s.kv_heads, s.head_dim))) return UE5M3_ERR_INVALID_ARG;
+    }
     if (!aligned_to(lse, UE5M3_F32) || !aligned16(workspace)) return UE5M3_ERR_ALIGN;
     int sms = 0;
     if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
@@ -510,6 +567,24 @@ int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_hea
     for (const ue5m3_heads* t : {k, v, dk, dv})
         if ((bad = check_heads(t, s.batch, s.k_len, s.kv_heads)) != UE5M3_OK) return bad;
     if ((!lse || !workspace) && s.batch * s.q_len > 0) return UE5M3_ERR_INVALID_ARG;
+    {
+        // dk and dv are written while dq still reads the inputs, and the other way round; o is read before either
+        Extent e[7];                                          // dq, dk, dv, then what they may not meet
+        int n = 0;
+        bool is_output[7];
+        auto take = [&](const ue5m3_heads* t, int64_t tokens, int64_t heads, bool output) {
+            if (s.batch * tokens == 0) return;
+            is_output[n] = output;
+            e[n++] = extent_of(*t, s.batch, tokens, heads, s.head_dim);
+        };
+        take(dq, s.q_len, s.heads, true);
+        for (const ue5m3_heads* t : {dk, dv}) take(t, s.k_len, s.kv_heads, true);
+        for (const ue5m3_heads* t : {dout, q}) take(t, s.q_len, s.heads, false);
+        for (const ue5m3_heads* t : {k, v}) take(t, s.k_len, s.kv_heads, false);
+        for (int i = 0; i < n && is_output[i]; ++i)
+            for (int j = i + 1; j < n; ++j)
+                if (overlap(e[i], e[j])) return UE5M3_ERR_INVALID_ARG;
+    }
     if (!aligned_to(lse, UE5M3_F32) || !aligned16(workspace)) return UE5M3_ERR_ALIGN;
     int sms = 0;
     if ((bad = device_ready(sms)) != UE5M3_OK) return bad;

@@ -25,3 +25,29 @@ def test_rows_of_an_earlier_call_are_not_seen():
     for turn in range(60):
         got = lib.attention_backward(*sets[turn % 3])
         assert all(torch.equal(a, b) for a, b in zip(got, want[turn % 3])), turn
+
+
+@pytest.mark.parametrize("B,Lq,Lk,H,Hk,D", [(2, 700, 700, 4, 2, 128), (1, 1, 8192, 32, 8, 128), (3, 33, 400, 12, 2, 80), (1, 300, 3000, 2, 2, 64), (40, 65, 513, 6, 2, 128)])
+def test_output_in_place_of_the_queries(B, Lq, Lk, H, Hk, D):
+    """Whole tiles, keys shared out, heads in one tile (with a partial tile in front of the next group's heads)."""
+    q, k, v, do = make(B, Lq, Lk, H, Hk, D, seed=Lq)
+    o, lse = lib.attention(q, k, v, causal=True)
+    again = q.clone()
+    got, got_lse = lib.attention(again, k, v, causal=True, out=again)
+    assert got is again and torch.equal(got, o) and torch.equal(got_lse, lse)
+    grads = lib.attention_backward(do, q, k, v, o, lse, causal=True)
+    over = o.clone()
+    for a, b in zip(grads, lib.attention_backward(do, q, k, v, over, lse, causal=True, out=(over, torch.empty_like(k), torch.empty_like(v)))):
+        assert torch.equal(a, b)
+
+
+def test_outputs_over_inputs_are_refused():
+    q, k, v, do = make(1, 64, 64, 2, 2, 64)
+    o, lse = lib.attention(q, k, v)
+    for out in (k, v):
+        with pytest.raises(lib.Ue5m3Error, match="INVALID_ARG"):
+            lib.attention(q, k, v, out=out)
+    fine = [torch.empty_like(t) for t in (q, k, v)]
+    for i, out in ((0, q), (0, do), (1, k), (2, v), (1, fine[0]), (2, q)):
+        with pytest.raises(lib.Ue5m3Error, match="INVALID_ARG"):
+            lib.attention_backward(do, q, k, v, o, lse, out=tuple(out if j == i else t for j, t in enumerate(fine)))

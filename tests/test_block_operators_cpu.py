@@ -65,3 +65,73 @@ def test_calls_refuse_before_they_look_for_a_device(lib):
     assert lib.ue5m3_attention(_shape(2, 8, 8, 2, 2, 60), t, t, t, t, p, None, None) == shape
     assert lib.ue5m3_attention(_shape(2, 8, 8, 2, 2, 64), odd, t, t, t, p, None, None) == align
     assert lib.ue5m3_attention(_shape(2, 8, 8, 2, 2, 64), t, t, t, t, None, None, None) == invalid
+
+
+# ---- outputs that share memory with inputs ------------------------------------------------------
+def _elements(t, sizes, dim):
+    """The 16-byte units that a tensor [batch, tokens, heads, dim] covers."""
+    out = set()
+    for b in range(sizes[0]):
+        for i in range(sizes[1]):
+            for h in range(sizes[2]):
+                at = t.data // 16 + (b * t.batch_stride + i * t.token_stride + h * t.head_stride) // 8
+                out.update(range(at, at + dim // 8))
+    return out
+
+
+# An lse pointer that is not aligned is refused (3) behind the check of overlaps (1): no call reaches a device.
+ODD = C.c_void_p((1 << 20) + 1)
+
+
+def _forward_status(lib, s, q, k, v, o):
+    return lib.ue5m3_attention(s, q, k, v, o, ODD, None, None)
+
+
+def _backward_status(lib, s, dout, q, k, v, o, dq, dk, dv):
+    return lib.ue5m3_attention_backward(s, dout, q, k, v, o, ODD, dq, dk, dv, C.c_void_p(1 << 20), None)
+
+
+def test_attention_refuses_an_output_over_its_inputs(lib):
+    overlap, none = 1, 3
+    s = _shape(2, 40, 40, 4, 4, 64)
+    at = lambda n: B._Heads((1 << 20) + n * (1 << 16), 40 * 256, 256, 64)
+    q, k, v, o = (at(n) for n in range(4))
+    assert _forward_status(lib, s, q, k, v, o) == none
+    assert _forward_status(lib, s, q, k, v, q) == none                      # o in place of q
+    assert _forward_status(lib, s, q, k, v, k) == overlap and _forward_status(lib, s, q, k, v, v) == overlap
+    later = B._Heads(q.data + 256 * 2, 40 * 256, 256, 64)                   # q from its second token on
+    assert _forward_status(lib, s, q, k, v, later) == overlap
+    ins, outs = [at(n) for n in (4, 0, 1, 2, 3)], [at(n) for n in (5, 6, 7)]
+    assert _backward_status(lib, s, *ins, *outs) == none
+    assert _backward_status(lib, s, *ins, ins[4], *outs[1:]) == none         # dq in place of o
+    for i in range(3):
+        for other in ins[:4] + [t for j, t in enumerate(outs) if j != i]:
+            assert _backward_status(lib, s, *ins, *(other if j == i else t for j, t in enumerate(outs))) == overlap
+
+
+def test_attention_takes_interleaved_views_and_refuses_what_meets(lib):
+    """Random layouts, against the sets of elements: views of one buffer interleave without an element in common, or with one."""
+    import random
+    rng = random.Random(5)
+    seen = {1: 0, 3: 0}
+    for _ in range(3000):
+        batch, tokens, heads, dim = rng.randint(1, 3), rng.randint(1, 4), rng.randint(1, 3), 8 * rng.randint(1, 3)
+        sizes = (batch, tokens, heads)
+
+        def tensor(width):
+            order = rng.choice([(2, 1, 0), (1, 2, 0), (2, 0, 1)])           # which dimension is innermost
+            strides, step = [8, 8, 8], width
+            for i in order:
+                strides[i] = step
+                step *= sizes[i] + rng.choice([0, 0, 1])
+            return B._Heads((1 << 20) + 16 * rng.randint(0, 12), *strides)
+        width = dim + 8 * rng.randint(0, 3)
+        q, o = tensor(width), tensor(rng.choice([width, dim + 8 * rng.randint(0, 3)]))
+        far = B._Heads(1 << 30, *([8 * 64] * 3))
+        s = _shape(batch, tokens, tokens, heads, heads, dim)
+        same = all(getattr(q, n) == getattr(o, n) for n, size in (("data", 0), ("batch_stride", batch), ("token_stride", tokens), ("head_stride", heads))
+                   if n == "data" or size > 1)
+        want = 1 if not same and _elements(q, sizes, dim) & _elements(o, sizes, dim) else 3
+        assert _forward_status(lib, s, q, far, far, o) == want
+        seen[want] += 1
+    assert min(seen.values()) > 300
