@@ -365,8 +365,8 @@ typedef struct {
  * j <= position (causal) and j >= position - window_left (window_left >= 0).  Query head h uses key/value head
  * h / (heads / kv_heads).
  *     S_ij = scale * q_i . k_j,   lse_i = log sum_j exp S_ij,   o_i = sum_j exp(S_ij - lse_i) v_j      over the keys it sees
- * A query that sees no key gets o = 0 and lse = -inf.  Keys and values at positions >= k_lens[b] are never used, whatever
- * they hold (NaN included).  Products of BF16 values are accumulated in binary32; the probabilities are rounded to BF16
+ * A query that sees no key gets o = 0 and lse = -inf.  Keys and values at positions >= k_lens[b], and those in front of every
+ * query's window, are never used, whatever they hold (NaN included).  Products of BF16 values are accumulated in binary32; the probabilities are rounded to BF16
  * for the second product; maximum, sum and lse are binary32.
  *   q [batch, q_len, heads, head_dim], k and v [batch, k_len, kv_heads, head_dim], o like q; lse device, binary32
  *   [batch, heads, q_len] contiguous.

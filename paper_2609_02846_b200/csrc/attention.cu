@@ -221,16 +221,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         auto next_pair = [&](const Item& w, int j) {       // waits for the pair with V of key tile j
             wait_all(kv_full + 8 * slot, phase);
             if (++slot == T::PAIRS) { slot = 0; phase ^= 1; }
-            const int valid = w.keys - j * BK;             // rows of this V tile that exist
-            if (p.k_lens && j >= w.first && valid < BK) {
-                // values behind the sequence's end may hold anything (0 * NaN is NaN): they become zeros
-                for (int i = valid * (DP / 8) + lane; i < BK * (DP / 8); i += 32) {
-                    const int r = i / (DP / 8), c = i % (DP / 8);
-                    *reinterpret_cast<uint4*>(smem_gen + (2 + v_tile) * T::TILE + (c / 8) * T::PANEL + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
-                }
-                fence_proxy_async();
-                __syncwarp();
-            }
+            // values behind the sequence's end and in front of every window may hold anything: they become zeros
+            const int from = p.first_key - j * BK, valid = w.keys - j * BK;
+            if (j >= w.first && ((p.k_lens && valid < BK) || from > 0)) keep_rows<DP>(smem_gen + (2 + v_tile) * T::TILE, from, valid, lane);
             const uint32_t v = v_tile;
             v_tile = v + 2 >= T::RING ? v + 2 - T::RING : v + 2;
             return v;

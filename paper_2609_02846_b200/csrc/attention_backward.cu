@@ -310,8 +310,10 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         // query tiles [plain_lo, plain_hi) see every key of this tile
         const int plain_lo = j0 + B128 <= keys ? (p.query_lo(j0 + B128 - 1) + B128 - 1) / B128 : hi;
         const int plain_hi = p.left >= 0 ? max(p.query_hi(j0), 0) / B128 : p.q_len / B128 + 1;
-        const bool short_tile = j0 + B128 > keys;                     // some keys of the tile do not exist: their rows see no query
-        const bool upper = p.left >= 0 || short_tile;
+        const bool upper = p.left >= 0 || j0 + B128 > keys;
+        // Some keys of the tile take no part (behind the sequence's end, in front of every window): what they hold may be NaN, and so then
+        // is their dP.
+        const bool idle_keys = j0 + B128 > keys || j0 < p.first_key;
         const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2);
         bool ok = true;
         for (int it = 0; it < steps; ++it) {
@@ -362,9 +364,9 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     pk[half * 16 + c / 2 + 1] = pack_pair(f2_mul(p1, f2_add(pair_of(d + c + 2), e.y)));
                 }
             }
-            if (short_tile) {                                         // what stands behind the sequence's end may be NaN, and so then is dP
+            if (idle_keys) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) pk[i] = key < keys ? pk[i] : 0u;
+                for (int i = 0; i < 32; ++i) pk[i] = q_lo < q_hi ? pk[i] : 0u;
             }
             tmem_st32(td, pk);
             tmem_st_wait();
@@ -493,15 +495,9 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             return s;
         };
         auto clean_k = [&](int it, uint32_t s) {
-            // keys behind the sequence's end may hold anything (dS is zero there, and 0 * NaN is NaN): they become zeros
-            const int valid = n_keys - (first + it) * B128;
-            if (!p.k_lens || valid >= B128) return;
-            for (int i = valid * (DP / 8) + lane; i < B128 * (DP / 8); i += 32) {
-                const int r = i / (DP / 8), c = i % (DP / 8);
-                *reinterpret_cast<uint4*>(smem_gen + s * T::TILE + (c / 8) * T::PANEL + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
-            }
-            fence_proxy_async();
-            __syncwarp();
+            // keys behind the sequence's end and in front of every window may hold anything (dS is zero there): they become zeros
+            const int from = p.first_key - (first + it) * B128, valid = n_keys - (first + it) * B128;
+            if ((p.k_lens && valid < B128) || from > 0) keep_rows<DP>(smem_gen + s * T::TILE, from, valid, lane);
         };
         uint32_t k0 = 0, k1 = 0, k2 = 0;                   // slots of K(it), K(it + 1), K(it + 2)
         auto issue_s = [&](int it) {
@@ -588,7 +584,8 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
 #pragma unroll
             for (int i = 0; i < 32; ++i) pr[i] = ex2_pair(f2_fma(pair_of(s + 2 * i), c2, nl2));
             if (!plain) hide_pairs<32>(pr, -base, width - base, p.left >= 0, true);
-            const bool short_tile = p.k_lens && (kt + 1) * B128 > keys;           // values behind the end may be NaN, and so then is dP
+            // values that take no part may be NaN, and so then is dP
+            const bool idle_keys = (p.k_lens && (kt + 1) * B128 > keys) || kt * B128 < p.first_key;
             if (!(ok = warp_wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t pk[32];
@@ -601,7 +598,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 for (int i = 0; i < 16; ++i) {
                     const f32x2 pp = pr[half * 16 + i];
                     f32x2 x = f2_mul(pp, f2_add(pair_of(d + 2 * i), nd2));
-                    if (short_tile) x = where_p(pp, x);
+                    if (idle_keys) x = where_p(pp, x);
                     pk[half * 16 + i] = pack_pair(x);
                 }
             }

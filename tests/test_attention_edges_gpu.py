@@ -51,3 +51,26 @@ def test_outputs_over_inputs_are_refused():
     for i, out in ((0, q), (0, do), (1, k), (2, v), (1, fine[0]), (2, q)):
         with pytest.raises(lib.Ue5m3Error, match="INVALID_ARG"):
             lib.attention_backward(do, q, k, v, o, lse, out=tuple(out if j == i else t for j, t in enumerate(fine)))
+
+
+def _call(q, k, v, do, o=None, **kw):
+    out, lse = lib.attention(q, k, v, **kw)
+    return out, lse, *lib.attention_backward(do, q, k, v, out if o is None else o, lse, **kw)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Lq,Lk,left", [(1, 700, 100), (3, 1000, 300), (130, 900, 65), (300, 700, 17), (128, 4097, 500)])
+def test_garbage_in_keys_in_front_of_every_window(Lq, Lk, left, D):
+    """Keys and values that no query's window reaches, as a cache that is written round holds them."""
+    q, k, v, do = make(2, Lq, Lk, 4, 2, D, seed=Lk)
+    first = Lk - Lq - left
+    assert first > 0
+    for kl in (None, torch.tensor([Lk, Lk - 5], dtype=torch.int32, device=DEV)):
+        kw = dict(causal=True, window_left=left, k_lens=kl)
+        want = _call(q, k, v, do, **kw)
+        assert bool((want[3][:, :first] == 0).all()) and bool((want[4][:, :first] == 0).all())
+        k2, v2 = k.clone(), v.clone()
+        k2[:, :first], v2[:, :first] = float("nan"), float("inf")
+        v2[:, :first:3] = float("nan")
+        for a, b in zip(want, _call(q, k2, v2, do, **kw)):
+            assert torch.equal(a, b)
