@@ -387,7 +387,8 @@ UE5M3_API int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_he
  * With P_ij = exp(S_ij - lse_i) and D_i = dout_i . o_i:
  *     dv_j = sum_i P_ij dout_i,   dS_ij = P_ij (dout_i . v_j - D_i),   dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i
  * dk and dv are summed over the query heads that share a key/value head, in binary32 and in a fixed order (no atomics).
- * Gradients of keys and values that no query sees, and of queries that see no key, are zero.
+ * Gradients of keys and values that no query sees, and of queries that see no key, are zero, and none of these is used, whatever
+ * q, dout, k and v hold there.
  *   dout, o, dq like q; dk, dv like k (each with strides of its own).  dq, dk and dv have no element in common with one another nor
  *   with dout, q, k or v: parts of them are written while others are computed (UE5M3_ERR_INVALID_ARG as above).  dq may be o.
  *   workspace  device, ue5m3_attention_backward_workspace_bytes(shape) bytes, 16-byte aligned.

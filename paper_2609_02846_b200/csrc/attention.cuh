@@ -268,6 +268,7 @@ struct AttentionParams {
     const float* delta;                  // backward: -(dout . o) per query, padded
     int q_pad;
     int first_key;                       // keys in front of this one lie before every query's window
+    int first_query;                     // queries in front of this one stand before every key (causal)
     int kv_heads, pack;                         // forward: heads that share a query tile (0: none do)
     int dim, parts;                      // head dimension; parts into which the key tiles of a query are shared out
     float* part_o; float* part_lse;      // parts > 1: o (backward: dq) [parts][batch][heads][q_len][dim]; forward: lse [..][q_len]
@@ -282,6 +283,8 @@ struct AttentionParams {
     // keys [lo, hi) that query i sees (empty when hi <= lo)
     __device__ __forceinline__ int key_lo(int i) const { return left >= 0 ? max(0, i + (k_len - q_len) - left) : 0; }
     __device__ __forceinline__ int key_hi(int i, int keys) const { return causal ? min(keys, i + (k_len - q_len) + 1) : keys; }
+    // queries from this one on see no key: their windows begin behind the sequence's end
+    __device__ __forceinline__ int queries_end(int keys) const { return left >= 0 ? min(q_len, keys - k_len + q_len + left) : q_len; }
     // queries [lo, hi) that see key j, given that j < keys
     __device__ __forceinline__ int query_lo(int j) const { return causal ? max(0, j - (k_len - q_len)) : 0; }
     __device__ __forceinline__ int query_hi(int j) const { return left >= 0 ? min(q_len, j - (k_len - q_len) + left + 1) : q_len; }
@@ -313,6 +316,7 @@ inline AttentionParams attention_params(const ue5m3_attention_shape& s) {
     p.scale_log2 = s.scale * 1.4426950408889634f;
     p.q_pad = (int)attention_padded_q(s.q_len);
     p.wait_limit = WAIT_LIMIT_CYCLES;
+    p.first_query = p.causal ? (int)std::max<int64_t>(0, s.q_len - s.k_len) : 0;
     p.first_key = p.left >= 0 ? (int)std::max<int64_t>(0, s.k_len - s.q_len - p.left) : 0;
     p.dim = (int)s.head_dim;
     p.parts = 1;

@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const RowParams p) 
     const int64_t bh = r / p.q_pad;
     const int i = (int)(r - bh * p.q_pad), b = (int)(bh / p.heads), h = (int)(bh - (int64_t)b * p.heads);
     float sum = 0.0f, lse2 = -INFINITY;
+    bool seen = true;
     if (i < p.q_len) {
         const __nv_bfloat16* o = p.o + b * p.o_stride[0] + i * p.o_stride[1] + h * p.o_stride[2];
         const __nv_bfloat16* d = p.dout + b * p.d_stride[0] + i * p.d_stride[1] + h * p.d_stride[2];
@@ -86,10 +87,11 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const RowParams p) 
             for (int j = 0; j < 8; ++j) sum = fmaf(x[j], y[j], sum);
         }
         if (lse != -INFINITY) lse2 = lse * -1.4426950408889634f;
+        else seen = false;
     }
 #pragma unroll
     for (int k = 4; k; k >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, k, 8);
-    if (sub == 0) { p.lse2[r] = lse2; p.delta[r] = -sum; }
+    if (sub == 0) { p.lse2[r] = lse2; p.delta[r] = seen ? -sum : 0.0f; }       // a query that sees nothing: dout may hold anything
 }
 
 // ------------------------------------------------------------------------------------------------ shared pieces
@@ -145,7 +147,9 @@ template <int DP> struct KeySmem {
     static constexpr int SIZE = BAR + 256 + 1024;
 };
 
-template <int DP>
+// IDLE: queries that see no key may exist.  Looking for their tiles takes the issuing warp 1 to 2 % of the kernel's time (2501 tokens,
+// window 511: 66.9 us against 65.8 of the whole backward pass), so calls without such queries do not.
+template <int DP, bool IDLE>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
                       const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -248,12 +252,18 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         // S(0) dP(0) | dV(0) S(1) dK(0) dP(1) | dV(1) S(2) dK(1) dP(2) | ...   S is in order behind dV, which reads P out of its columns
         const bool elected = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-        const int n = uniform(steps);
+        const int n = uniform(steps), q_end = uniform(p.queries_end(keys)), i_first = uniform(lo) * B128, i_end = uniform(hi) * B128;
         bool ok = true;
         auto pass = [&](uint32_t bar, uint32_t parity) {   // the phase is complete, or `ok` is false in the whole warp
             if (!__all_sync(0xFFFFFFFFu, try_wait_cta(bar, parity))) ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
             tc_fence_after();
         };
+        // Q and dO of queries that see no key may hold anything (P and dS are zero there): they become zeros.  Rows behind q_len are.
+        auto clean = [&](uint32_t tile, int i0) {
+            if (!IDLE) return;
+            if (i0 < p.first_query || (q_end < p.q_len && i0 + B128 > q_end)) keep_rows<DP>(smem_gen + M::RING + tile * T::TILE, p.first_query - i0, q_end - i0, lane);
+        };
+        int i0 = i_first;                                  // first query of the tile whose S was issued last
         const uint32_t k_low = desc_low_k(smem), v_low = desc_low_k(smem + T::TILE);
         const uint32_t q_k = desc_low_k(smem + M::RING), q_mn = desc_low_mn(smem + M::RING, T::PANEL);      // stage 0: Q, then dO
         constexpr uint32_t DO = T::TILE >> 4, STAGE = 2 * T::TILE >> 4;
@@ -261,9 +271,11 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         if (n > 0) {
             pass(k_full, 0);
             pass(q_full, 0);
+            clean(0, i0);
             if (ok) issue_square<DP>(elected, tm + COL_S, k_low, q_k, s_full);
             pass(v_full, 0);
             pass(d_full, 0);
+            clean(1, i0);
             if (ok) issue_square<DP>(elected, tm + COL_DP, v_low, q_k + DO, dp_full);
         }
         for (int it = 0; it < n && ok; ++it) {
@@ -279,6 +291,8 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             if (more) {
                 pass(q_full + 8 * s1, ph1);
                 if (!ok) break;
+                i0 = i0 + B128 == i_end ? i_first : i0 + B128;
+                clean(2 * s1, i0);
                 issue_square<DP>(elected, tm + COL_S, k_low, q_k + s1 * STAGE, s_full);
             }
             pass(ds_full, it & 1);
@@ -288,6 +302,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             if (more) {
                 pass(d_full + 8 * s1, ph1);
                 if (!ok) break;
+                clean(2 * s1 + 1, i0);
                 issue_square<DP>(elected, tm + COL_DP, v_low, q_k + s1 * STAGE + DO, dp_full);
             } else {
                 issue_commit(elected, acc_full);
@@ -544,6 +559,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         const int k_lo = p.key_lo(row), k_hi = p.key_hi(row, keys);
         const int plain_lo = p.left >= 0 ? (p.key_lo(i0 + B128 - 1) + B128 - 1) / B128 : 0;
         const int plain_hi = max(p.key_hi(i0, keys), 0) / B128;
+        const bool idle_queries = i0 < p.first_query || i1 >= p.queries_end(keys);
         const int64_t at = ((int64_t)b * p.heads + h) * p.q_pad + row;
         const float nl = load_device(p.lse2 + at), nd = load_device(p.delta + at);         // visible: see launch_dependents in the keys kernel
         const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2), nl2 = f2_pack(nl, nl), nd2 = f2_pack(nd, nd);
@@ -584,8 +600,8 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
 #pragma unroll
             for (int i = 0; i < 32; ++i) pr[i] = ex2_pair(f2_fma(pair_of(s + 2 * i), c2, nl2));
             if (!plain) hide_pairs<32>(pr, -base, width - base, p.left >= 0, true);
-            // values that take no part may be NaN, and so then is dP
-            const bool idle_keys = (p.k_lens && (kt + 1) * B128 > keys) || kt * B128 < p.first_key;
+            // values, and dO of queries, that take no part may be NaN, and so then is dP
+            const bool idle = (p.k_lens && (kt + 1) * B128 > keys) || kt * B128 < p.first_key || idle_queries;
             if (!(ok = warp_wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
             uint32_t pk[32];
@@ -598,7 +614,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 for (int i = 0; i < 16; ++i) {
                     const f32x2 pp = pr[half * 16 + i];
                     f32x2 x = f2_mul(pp, f2_add(pair_of(d + 2 * i), nd2));
-                    if (idle_keys) x = where_p(pp, x);
+                    if (idle) x = where_p(pp, x);
                     pk[half * 16 + i] = pack_pair(x);
                 }
             }
@@ -682,14 +698,21 @@ int run_queries(const Maps& m, const AttentionParams& p, int64_t grid, int q_til
     return launch(attention_queries_kernel<DP, PARTS>, grid, kThreads, QuerySmem<DP>::SIZE, early, st, m.q, m.dout, m.k, m.v, m.dq, p, q_tiles);
 }
 
+template <int DP, bool IDLE>
+int run_keys(const Maps& m, const AttentionParams& p, int64_t grid, int kv_heads, bool early, cudaStream_t st) {
+    static std::atomic<int> granted[64];
+    if (allow_smem(attention_keys_kernel<DP, IDLE>, KeySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
+    return launch(attention_keys_kernel<DP, IDLE>, grid, kThreads, KeySmem<DP>::SIZE, early, st, m.q, m.dout, m.k, m.v, m.dk, m.dv, p, kv_heads);
+}
+
 template <int DP>
 int run(const ue5m3_attention_shape& s, const ue5m3_heads& dq, const Maps& m, const AttentionParams& p, cudaStream_t st) {
     const int64_t k_tiles = (s.k_len + 127) / 128, q_tiles = (s.q_len + 127) / 128;
     const int64_t ck = k_tiles * s.batch * s.kv_heads, cq = q_tiles * s.batch * s.heads * p.parts;
     if (ck > 0) {
-        static std::atomic<int> granted[64];
-        if (allow_smem(attention_keys_kernel<DP>, KeySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-        const int r = launch(attention_keys_kernel<DP>, ck, kThreads, KeySmem<DP>::SIZE, cq > 0, st, m.q, m.dout, m.k, m.v, m.dk, m.dv, p, (int)s.kv_heads);
+        // queries in front of every key, or with a window that begins behind the end of their sequence
+        const bool idle = p.first_query > 0 || (p.left >= 0 && p.k_lens);
+        const int r = idle ? run_keys<DP, true>(m, p, ck, (int)s.kv_heads, cq > 0, st) : run_keys<DP, false>(m, p, ck, (int)s.kv_heads, cq > 0, st);
         if (r != UE5M3_OK) return r;
     }
     if (cq == 0) return UE5M3_OK;

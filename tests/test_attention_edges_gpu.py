@@ -58,6 +58,34 @@ def _call(q, k, v, do, o=None, **kw):
     return out, lse, *lib.attention_backward(do, q, k, v, out if o is None else o, lse, **kw)
 
 
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Lq,Lk,causal,left,lens", [
+    (300, 200, True, -1, None), (700, 130, True, -1, None),                  # the first Lq - Lk queries stand in front of every key
+    (515, 515, True, 40, [515, 100, 300]), (400, 400, False, 3, [1, 129, 400]),     # queries whose window begins behind their sequence's end
+    (20, 200, True, 10, [200, 130, 175])])
+def test_garbage_in_queries_that_see_no_key(Lq, Lk, causal, left, lens, D, value):
+    """q and dout of such queries change no output and no gradient, and their own are zero."""
+    B = 1 if lens is None else len(lens)
+    q, k, v, do = make(B, Lq, Lk, 4, 2, D, seed=Lq + D)
+    kl = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+    kw = dict(causal=causal, window_left=left, k_lens=kl)
+    want = _call(q, k, v, do, **kw)
+    at = torch.arange(Lq, device=DEV) + Lk - Lq
+    q2, do2 = q.clone(), do.clone()
+    some = False
+    for b in range(B):
+        n = Lk if lens is None else lens[b]
+        dead = ((at < 0) if causal else torch.zeros_like(at, dtype=torch.bool)) | ((at - left >= n) if left >= 0 else False)
+        some = some or bool(dead.any())
+        assert bool((want[2][b, dead] == 0).all())
+        q2[b, dead] = value
+        do2[b, dead] = -value
+    assert some
+    for a, b in zip(want, _call(q2, k, v, do2, **kw)):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("Lq,Lk,left", [(1, 700, 100), (3, 1000, 300), (130, 900, 65), (300, 700, 17), (128, 4097, 500)])
 def test_garbage_in_keys_in_front_of_every_window(Lq, Lk, left, D):
