@@ -171,8 +171,9 @@ class _LayerNormFn(torch.autograd.Function):
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
         want_w, want_b = ctx.needs_input_grad[1], ctx.needs_input_grad[2]
-        dx, dw, db = B.layer_norm_backward(_as_rows(dy), _as_rows(x), weight, mean, rstd, want_weight=want_w, want_bias=want_b)
-        return *_once("layer_norm", (dx.view(x.shape), dw, db if db is None else db.to(ctx.bias_dtype)), dy, x, weight), None
+        dx, dw, db = B.layer_norm_backward(_as_rows(dy), _as_rows(x), weight, mean, rstd, want_weight=want_w, want_bias=want_b,
+                                           bias_dtype=ctx.bias_dtype)
+        return *_once("layer_norm", (dx.view(x.shape), dw, db), dy, x, weight), None
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:

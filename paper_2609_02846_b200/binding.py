@@ -123,12 +123,16 @@ def _check(status: int, where: str) -> None:
         raise Ue5m3Error(status, where)
 
 
-def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
+def _dtype_code_of(dtype: torch.dtype) -> int:
+    if dtype == torch.float32:
         return F32
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return BF16
-    raise TypeError(f"unsupported dtype {t.dtype}: the library takes float32 or bfloat16")
+    raise TypeError(f"unsupported dtype {dtype}: the library takes float32 or bfloat16")
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    return _dtype_code_of(t.dtype)
 
 
 def _dev_ptr(t: Optional[torch.Tensor]):
@@ -507,9 +511,10 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
-                        want_weight: bool = True, want_bias: bool = True, out: Optional[torch.Tensor] = None) -> tuple:
+                        want_weight: bool = True, want_bias: bool = True, out: Optional[torch.Tensor] = None,
+                        bias_dtype: Optional[torch.dtype] = None) -> tuple:
     """ue5m3_layer_norm_backward: (dx, dweight, dbias).  dweight is None without a weight or when not wanted, dbias when not
-    wanted; both have the weight's type (x's without a weight)."""
+    wanted; both have the weight's type.  Without a weight dbias has the type `bias_dtype` (x's by default)."""
     rows, cols, ldx = _rows(x)
     lddy = _rows(dy, x)[2]
     _vector(weight, cols, x)
@@ -519,15 +524,18 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
         out, lddx = x.new_empty((rows, cols)), cols
     else:
         lddx = _rows(out, x)[2]
-    param = weight if weight is not None else x
+    param = weight.dtype if weight is not None else x.dtype if bias_dtype is None else bias_dtype
+    if bias_dtype is not None and bias_dtype != param:
+        raise ValueError(f"weight and bias have one type: {param} and {bias_dtype}")
+    param_code = _dtype_code_of(param)
     lib = _load()
-    dw = x.new_empty(cols, dtype=param.dtype) if want_weight and weight is not None else None
-    db = x.new_empty(cols, dtype=param.dtype) if want_bias else None
+    dw = x.new_empty(cols, dtype=param) if want_weight and weight is not None else None
+    db = x.new_empty(cols, dtype=param) if want_bias else None
     ws = None
     if dw is not None or db is not None:
         ws = x.new_empty(lib.ue5m3_layer_norm_backward_workspace_bytes(rows, cols), dtype=torch.uint8)
     _call(lib.ue5m3_layer_norm_backward, "ue5m3_layer_norm_backward", x, dy.data_ptr(), lddy, x.data_ptr(), _dtype_code(x), rows, cols, ldx,
-          _ptr(weight), _dtype_code(param), mean.data_ptr(), rstd.data_ptr(), out.data_ptr(), lddx, _ptr(dw), _ptr(db), _ptr(ws))
+          _ptr(weight), param_code, mean.data_ptr(), rstd.data_ptr(), out.data_ptr(), lddx, _ptr(dw), _ptr(db), _ptr(ws))
     return out, dw, db
 
 

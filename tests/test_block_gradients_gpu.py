@@ -1,0 +1,35 @@
+"""Gradients of the differentiable wrappers where types and shapes of their inputs differ."""
+import pytest
+import torch
+
+import paper_2609_02846_b200 as lib
+from paper_2609_02846_b200 import autograd as A
+from block_reference import assert_within, layer_norm_backward
+from test_layer_norm_gpu import make
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, F = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("dt,bdt", [(BF, F), (F, BF), (BF, BF), (F, F)])
+@pytest.mark.parametrize("cols", [256, 333])
+def test_gradient_of_a_bias_without_a_weight_has_the_bias_type(cols, dt, bdt):
+    """Held to the bound of the bias's own type: a binary32 sum is not rounded to the activations' BF16 on its way."""
+    x, _, b, dy = make(500, cols, dt, bdt, seed=cols)
+    _, mean, rstd = lib.layer_norm(x, None, b)
+    want = layer_norm_backward(dy, x, None, mean, rstd)
+    dx, dw, db = lib.layer_norm_backward(dy, x, None, mean, rstd, bias_dtype=bdt)
+    assert dw is None and db.dtype == bdt
+    assert_within(db, *want[2], "db")
+    assert_within(dx, *want[0], "dx")
+    xx, bb = x.clone().requires_grad_(), b.clone().requires_grad_()
+    A.layer_norm(xx, None, bb).backward(dy)
+    assert bb.grad.dtype == bdt and torch.equal(bb.grad, db) and torch.equal(xx.grad, dx)
+    assert lib.layer_norm_backward(dy, x, None, mean, rstd)[2].dtype == dt           # nothing asked for: x's type
+    w = torch.ones(cols, dtype=bdt, device=DEV)
+    assert lib.layer_norm_backward(dy, x, w, mean, rstd, bias_dtype=bdt)[2].dtype == bdt
+    with pytest.raises(ValueError):
+        lib.layer_norm_backward(dy, x, w, mean, rstd, bias_dtype=F if bdt == BF else BF)       # two types of parameters
+    with pytest.raises(TypeError):
+        lib.layer_norm_backward(dy, x, None, mean, rstd, bias_dtype=torch.float16)
