@@ -198,14 +198,14 @@ class LayerNorm(torch.nn.Module):
 class _DropoutAddFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, p, seed):
-        ctx.p, ctx.seed = p, seed
+        ctx.p, ctx.seed, ctx.residual_shape = p, seed, None if residual is None else residual.shape
         y = B.dropout_add(_as_rows(x), p, seed, None if residual is None else _as_rows(residual))
         return y.view(x.shape)
 
     @staticmethod
     def backward(ctx, dy):
         dx = dropout_add(dy, ctx.p, ctx.seed) if ctx.needs_input_grad[0] else None         # the same linear map, differentiable again
-        return dx, dy if ctx.needs_input_grad[1] else None, None, None
+        return dx, dy.reshape(ctx.residual_shape) if ctx.needs_input_grad[1] else None, None, None
 
 
 def dropout_add(x: torch.Tensor, p: float, seed: int, residual: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -103,3 +103,11 @@ def test_dropout_has_a_second_derivative(calls):
     u = torch.randn(4, 8, requires_grad=True)
     g, = torch.autograd.grad(A.dropout_add(x, 0.2, 1), x, u, create_graph=True)
     assert torch.equal(torch.autograd.grad(g.sum(), u)[0], keep)
+
+
+def test_residual_of_another_shape_gets_a_gradient_of_its_own(calls):
+    """The call adds rows to rows, so a residual may come flattened: its gradient has its shape."""
+    x, r = torch.randn(2, 3, 8, requires_grad=True), torch.randn(6, 8, requires_grad=True)
+    dy = torch.randn(2, 3, 8)
+    A.dropout_add(x, 0.2, 1, r).backward(dy)
+    assert torch.equal(r.grad, dy.view(6, 8)) and torch.equal(x.grad, dy * _keep(48).view(2, 3, 8))
