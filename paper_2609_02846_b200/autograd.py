@@ -146,7 +146,7 @@ class Ue5m3Linear(torch.nn.Module):
 # Between the linears
 def _as_rows(t: torch.Tensor) -> torch.Tensor:
     """[.., cols] as a matrix with contiguous rows (a copy only where the strides leave no other way, e.g. an expanded gradient)."""
-    t = t.reshape(-1, t.shape[-1])
+    t = t.reshape(t.shape[:-1].numel(), t.shape[-1])
     ok = (t.stride(1) == 1 or t.shape[1] == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])
     return t if ok else t.contiguous()
 

@@ -111,3 +111,13 @@ def test_residual_of_another_shape_gets_a_gradient_of_its_own(calls):
     dy = torch.randn(2, 3, 8)
     A.dropout_add(x, 0.2, 1, r).backward(dy)
     assert torch.equal(r.grad, dy.view(6, 8)) and torch.equal(x.grad, dy * _keep(48).view(2, 3, 8))
+
+
+@pytest.mark.parametrize("shape", [(3, 0), (2, 3, 0), (0, 8), (0, 3, 8), (2, 0, 8)])
+def test_empty_tensors(calls, shape):
+    """No rows and rows of no columns are matrices like any other."""
+    x, r = torch.randn(shape, requires_grad=True), torch.randn(shape, requires_grad=True)
+    y = A.dropout_add(x, 0.2, 1, r)
+    assert y.shape == shape
+    y.sum().backward()
+    assert x.grad.shape == r.grad.shape == shape
