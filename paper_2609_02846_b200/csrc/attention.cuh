@@ -281,13 +281,13 @@ struct AttentionParams {
         return n < 0 ? 0 : (n > k_len ? k_len : n);
     }
     // keys [lo, hi) that query i sees (empty when hi <= lo)
-    __device__ __forceinline__ int key_lo(int i) const { return left >= 0 ? max(0, i + (k_len - q_len) - left) : 0; }
-    __device__ __forceinline__ int key_hi(int i, int keys) const { return causal ? min(keys, i + (k_len - q_len) + 1) : keys; }
+    __host__ __device__ __forceinline__ int key_lo(int i) const { return left >= 0 ? max(0, i + (k_len - q_len) - left) : 0; }
+    __host__ __device__ __forceinline__ int key_hi(int i, int keys) const { return causal ? min(keys, i + (k_len - q_len) + 1) : keys; }
     // queries from this one on see no key: their windows begin behind the sequence's end
-    __device__ __forceinline__ int queries_end(int keys) const { return left >= 0 ? min(q_len, keys - k_len + q_len + left) : q_len; }
+    __host__ __device__ __forceinline__ int queries_end(int keys) const { return left >= 0 ? min(q_len, keys - k_len + q_len + left) : q_len; }
     // queries [lo, hi) that see key j, given that j < keys
-    __device__ __forceinline__ int query_lo(int j) const { return causal ? max(0, j - (k_len - q_len)) : 0; }
-    __device__ __forceinline__ int query_hi(int j) const { return left >= 0 ? min(q_len, j - (k_len - q_len) + left + 1) : q_len; }
+    __host__ __device__ __forceinline__ int query_lo(int j) const { return causal ? max(0, j - (k_len - q_len)) : 0; }
+    __host__ __device__ __forceinline__ int query_hi(int j) const { return left >= 0 ? min(q_len, j - (k_len - q_len) + left + 1) : q_len; }
 };
 
 // ----------------------------------------------------------------------------- host side
@@ -310,8 +310,9 @@ inline AttentionParams attention_params(const ue5m3_attention_shape& s) {
     AttentionParams p{};
     p.q_len = (int)s.q_len; p.k_len = (int)s.k_len; p.heads = (int)s.heads; p.group = (int)(s.heads / s.kv_heads);
     p.kv_heads = (int)s.kv_heads; p.causal = s.causal; p.batch = (int)s.batch; p.k_lens = s.k_lens;
-    const int64_t all = s.q_len + s.k_len;                  // a window as long as this hides nothing
-    p.left = s.window_left < 0 ? -1 : (int)(s.window_left < all ? s.window_left : all);
+    // no query stands behind the last key, so a window that reaches from there to the first one hides nothing; a shorter one keeps
+    // every sum of positions below within 32 bits (lengths end at 2^30)
+    p.left = s.window_left < s.k_len - 1 ? (int)s.window_left : -1;
     p.scale = s.scale;
     p.scale_log2 = s.scale * 1.4426950408889634f;
     p.q_pad = (int)attention_padded_q(s.q_len);
