@@ -401,9 +401,8 @@ UE5M3_API int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const
 
 /*
  * Failure-detection self-test of the attention and layer norm kernels, as ue5m3_gemm_stall_selftest: a small problem with the
- * copies switched off (layer norm: those of the second half of its rows) and every wait bounded by wait_limit_cycles.  All threads
- * give up, drain, release tensor memory and return; ue5m3_last_device_status() then returns UE5M3_ERR_TIMEOUT once, and the context
- * stays usable.
+ * copies switched off and every wait bounded by wait_limit_cycles.  All threads give up, drain, release tensor memory and return;
+ * ue5m3_last_device_status() then returns UE5M3_ERR_TIMEOUT once, and the context stays usable.
  *   which    0 = attention, 1 = attention with few queries (keys shared out; the joining kernel runs behind it), 2 = attention backward,
  *            3 = layer norm, 4 = layer norm backward (these go through all their rows and write values of no meaning).
  *   buffer   device, 16-byte aligned, at least UE5M3_BLOCK_SELFTEST_BYTES: the problem's tensors, o first.  o is not written by 0.

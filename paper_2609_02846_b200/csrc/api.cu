@@ -380,7 +380,7 @@ int ue5m3_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64
     if (rows == 0) return UE5M3_OK;
     LayerNormArgs a{};
     a.x = x; a.ldx = ldx; a.weight = weight; a.bias = bias; a.y = y; a.ldy = ldy; a.mean = mean; a.rstd = rstd;
-    a.rows = a.copy_rows = rows; a.cols = cols; a.eps = eps;
+    a.rows = rows; a.cols = cols; a.eps = eps;
     return launch_layer_norm(a, dtype, weight_dtype, sms, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
@@ -411,7 +411,7 @@ int ue5m3_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int d
     a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.weight = weight; a.y = dx; a.ldy = lddx;
     a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
     a.dweight = dweight; a.dbias = dbias; a.partial = sums ? static_cast<float*>(workspace) : nullptr;
-    a.rows = a.copy_rows = rows; a.cols = cols;
+    a.rows = rows; a.cols = cols;
     return launch_layer_norm_backward(a, dtype, weight_dtype, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
@@ -614,14 +614,12 @@ int ue5m3_block_stall_selftest(int which, void* buffer, size_t bytes, int64_t wa
         a.mean = static_cast<float*>(take(rows * sizeof(float)));
         a.rstd = static_cast<float*>(take(rows * sizeof(float)));
         a.rows = rows;
-        a.copy_rows = rows / 2;                           // the second row that a row group takes arrives or does not, its third does not
-        a.wait_limit = wait_limit_cycles;
-        if (which == 3) return launch_layer_norm(a, UE5M3_BF16, UE5M3_F32, sms, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+        if (which == 3) return launch_layer_norm(a, UE5M3_BF16, UE5M3_F32, sms, (cudaStream_t)stream, stall) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
         a.dy = take(matrix);
         a.dweight = take(cols * sizeof(float));
         a.dbias = take(cols * sizeof(float));
         a.partial = static_cast<float*>(take(ue5m3_layer_norm_backward_workspace_bytes(rows, cols)));
-        return launch_layer_norm_backward(a, UE5M3_BF16, UE5M3_F32, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+        return launch_layer_norm_backward(a, UE5M3_BF16, UE5M3_F32, (cudaStream_t)stream, stall) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
     }
     ue5m3_attention_shape s{};
     s.batch = s.kv_heads = 1;

@@ -20,7 +20,7 @@ inline cudaError_t allow_smem(Kernel* kernel, int bytes, std::atomic<int> (&gran
     return e;
 }
 
-// Failure-detection self-test of the attention kernels: the bound of every device-side wait in SM clocks, with the copies switched off (0: a normal launch).
+// Failure-detection self-test: the bound of every device-side wait in SM clocks, with the copies switched off (0: a normal launch).
 struct StallTest { long long wait_limit = 0; };
 
 struct LayerNormArgs {
@@ -33,13 +33,11 @@ struct LayerNormArgs {
     float* partial;                       // backward only: [groups][2][cols]
     int64_t rows, cols;
     float eps;
-    int64_t copy_rows;                    // rows that the rings copy: all of them, or fewer in the self-test
-    long long wait_limit;                 // of a ring's waits, SM clocks; 0: the default
 };
 // CTAs of the backward kernel = rows of column sums it leaves in the workspace
 int layer_norm_backward_groups(int64_t rows);
-cudaError_t launch_layer_norm(const LayerNormArgs& a, int dtype, int weight_dtype, int num_sms, cudaStream_t st);
-cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, int dtype, int weight_dtype, cudaStream_t st);
+cudaError_t launch_layer_norm(const LayerNormArgs& a, int dtype, int weight_dtype, int num_sms, cudaStream_t st, const StallTest& stall = {});
+cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, int dtype, int weight_dtype, cudaStream_t st, const StallTest& stall = {});
 
 struct DropoutArgs {
     const void* x; const void* residual; void* y;

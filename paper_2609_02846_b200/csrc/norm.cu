@@ -127,38 +127,44 @@ __device__ __forceinline__ void zero_scratch(float* scratch, int floats) {
 // Thread 0 of the group issues the copies; an entry is refilled once the whole group has read it into registers (behind the
 // barrier of the row's first sum).  Waits are bounded.  One that gives up sets the status word and the CTA's flag, and the threads, which
 // still have to meet at the barriers, go through the rows that are left with what is there: no wait is tried a second time, nothing
-// more is copied (an entry is refilled only by a thread that has seen its copy end), and the copies in flight are seen out at the end.
-struct RingHead {                      // at the front of the shared memory
+// more is copied (an entry is refilled only by a thread that has seen its copy end), and the copies in flight are seen out.
+struct RingHead {                                  // at the front of the CTA's dynamic shared memory
     int gave_up;
-    struct { int64_t from, to; } lost[15];         // per row group: rows that were being copied when its thread 0 gave up
+    int slots;
+    long long limit;                               // of a wait, SM clocks
+    int64_t step, rows;
 };
-constexpr int kRingHead = 256;
-static_assert(sizeof(RingHead) <= kRingHead, "RingHead");
-constexpr int64_t kNoMore = (int64_t)1 << 61;      // the next row to be copied, of a thread 0 that gave up (rows end at 2^60)
+constexpr int kRingHead = 32;
+static_assert(sizeof(RingHead) == kRingHead, "RingHead");
+extern __shared__ __align__(16) uint8_t ring_raw[];
+constexpr int64_t kNoMore = (int64_t)1 << 61;      // the next row to be copied, where no more are (rows end at 2^60)
+// A wait that did not end at once: true when it was given up.  Thread 0 then waits, bounded too, for its copies in flight (if there are):
+// those of this row and of the slots - 1 that it takes after it.  A function of its own, with what it needs in shared memory: in line it
+// cost the backward kernel 4 % (16384 x 4096 BF16 71.7 -> 74.8 us), and with more arguments 20 % by spilling (16384 x 1000 29.0 -> 34.7).
+__device__ __noinline__ bool ring_wait_slow(uint32_t bars, int slot, uint32_t phase, int64_t row, bool in_flight) {
+    RingHead* head = reinterpret_cast<RingHead*>(ring_raw);
+    volatile int* gave_up = &head->gave_up;
+    const long long limit = head->limit;
+    if (!*gave_up && mbar_wait_slow(bars + 8u * (uint32_t)slot, phase, gave_up, &g_norm_status, limit)) return false;
+    if (threadIdx.x == 0 && in_flight)
+        for (int i = 0; i < head->slots && row < head->rows; ++i, row += head->step) {
+            mbar_wait_drain(bars + 8u * (uint32_t)slot, phase, &g_norm_status, limit);
+            if (++slot == head->slots) { slot = 0; phase ^= 1; }
+        }
+    return true;
+}
+__device__ __forceinline__ void init_ring_head(int slots, long long limit, int64_t step, int64_t rows) {
+    if (threadIdx.x == 0 && threadIdx.y == 0) *reinterpret_cast<RingHead*>(ring_raw) = RingHead{0, slots, limit > 0 ? limit : WAIT_LIMIT_CYCLES, step, rows};
+}
 struct RowRing {
     uint32_t base, bars, entry_bytes;
     int slots;
     int slot = 0;                      // entry of the current row, and its phase
     uint32_t phase = 0;
-    static __device__ __forceinline__ long long bound(const LayerNormArgs& a) { return a.wait_limit > 0 ? a.wait_limit : WAIT_LIMIT_CYCLES; }
     __device__ __forceinline__ uint32_t entry() const { return base + (uint32_t)slot * entry_bytes; }
     __device__ __forceinline__ uint32_t bar() const { return bars + 8u * (uint32_t)slot; }
-    __device__ __forceinline__ void wait(const LayerNormArgs& a, RingHead* head, int64_t row, int64_t& next) const {
-        if (mbar_try_wait(bar(), phase)) return;
-        volatile int* gave_up = &head->gave_up;
-        if (!*gave_up && mbar_wait_slow(bar(), phase, gave_up, &g_norm_status, bound(a))) return;
-        if (threadIdx.x == 0 && next < kNoMore) {
-            head->lost[threadIdx.y] = {row, min(next, a.copy_rows)};
-            next = kNoMore;
-        }
-    }
-    // Thread 0 of a group, behind its last row: if it gave up, waits, bounded, for the copies in flight.
-    __device__ __forceinline__ void drain(const LayerNormArgs& a, const RingHead* head, int64_t first, int64_t step, int64_t next) const {
-        if (next < kNoMore) return;
-        for (int64_t row = head->lost[threadIdx.y].from; row < head->lost[threadIdx.y].to; row += step) {
-            const int64_t i = (row - first) / step;
-            mbar_wait_drain(bars + 8u * (uint32_t)(i % slots), (uint32_t)(i / slots) & 1u, &g_norm_status, bound(a));
-        }
+    __device__ __forceinline__ void wait(int64_t row, int64_t& next) const {          // next: the thread's next row to be copied
+        if (!mbar_try_wait(bar(), phase) && ring_wait_slow(bars, slot, phase, row, next < kNoMore)) next = kNoMore;
     }
     __device__ __forceinline__ void advance() {
         if (++slot == slots) { slot = 0; phase ^= 1; }
@@ -197,10 +203,8 @@ __device__ __forceinline__ float f2_total(f32x2 v) {
 // nothing is conditional (a fifth of the instructions of a row go).
 template <typename TX, typename TW, int NV, bool FULL>
 __global__ void __launch_bounds__(512)
-layer_norm_ring_kernel(const LayerNormArgs a, const int slots) {
+layer_norm_ring_kernel(const LayerNormArgs a, const int slots, const long long wait_limit) {
     constexpr int VEC = 16 / sizeof(TX), PAIRS = VEC / 2;
-    extern __shared__ __align__(16) uint8_t ring_raw[];
-    RingHead* head = reinterpret_cast<RingHead*>(ring_raw);
     uint8_t* ring_smem = ring_raw + kRingHead;
     const int T = blockDim.x, R = blockDim.y, bar_id = 1 + threadIdx.y;
     const uint32_t row_bytes = (uint32_t)a.cols * sizeof(TX), smem = smem_u32(ring_smem);
@@ -212,9 +216,9 @@ layer_norm_ring_kernel(const LayerNormArgs a, const int slots) {
     const int64_t step = (int64_t)gridDim.x * R, first = (int64_t)blockIdx.x * R + threadIdx.y;
     const TX* x = static_cast<const TX*>(a.x);
     const TX* src = x + first * a.ldx;                     // the next row to be copied
-    int64_t next = first;
+    int64_t next = wait_limit > 0 ? kNoMore : first;      // the self-test copies nothing
     auto fill = [&](uint32_t entry, uint32_t bar) {
-        if (next < a.copy_rows) {
+        if (next < a.rows) {
             mbar_expect_tx(bar, row_bytes);
             bulk_load(entry, src, row_bytes, bar);
         }
@@ -241,14 +245,14 @@ layer_norm_ring_kernel(const LayerNormArgs a, const int slots) {
         for (int j = 0; j < PAIRS; ++j) { w[k][j] = f2_pack(t[2 * j], t[2 * j + 1]); b[k][j] = f2_pack(u[2 * j], u[2 * j + 1]); }
     }
     zero_scratch(reinterpret_cast<float*>(ring_smem), R * 64);
-    if (threadIdx.x == 0 && threadIdx.y == 0) head->gave_up = 0;
-    __syncthreads();                                       // the barriers, the scratch and the flag exist
+    init_ring_head(slots, wait_limit, step, a.rows);
+    __syncthreads();                                       // the barriers, the scratch and the head exist
     const float inv_n = 1.0f / (float)a.cols;
     int turn = 0;
     TX* dst = static_cast<TX*>(a.y) + first * a.ldy + threadIdx.x * VEC;
     for (int64_t row = first; row < a.rows; row += step, dst += step * a.ldy) {
         f32x2 f[NV][PAIRS], acc = 0;
-        ring.wait(a, head, row, next);
+        ring.wait(row, next);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             if constexpr (!FULL) {
@@ -292,7 +296,6 @@ layer_norm_ring_kernel(const LayerNormArgs a, const int slots) {
             if (a.rstd) a.rstd[row] = rstd;
         }
     }
-    if (threadIdx.x == 0) ring.drain(a, head, first, step, next);
 }
 
 // Rows without 16-byte alignment: NV single columns per thread, prefetched one row ahead; otherwise as above.
@@ -451,10 +454,8 @@ __device__ __forceinline__ void leave_columns(const LayerNormArgs& a, float* sum
 // are 80 registers already.  16384 x 4096 BF16 with the adding kernel: 72 us, 5.6 TB/s (0.86 of the measured copy).
 template <typename TX, typename TW, int NV, bool FULL>
 __global__ void __launch_bounds__(512)
-layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
+layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots, const long long wait_limit) {
     constexpr int VEC = 16 / sizeof(TX), PAIRS = VEC / 2;
-    extern __shared__ __align__(16) uint8_t ring_raw[];
-    RingHead* head = reinterpret_cast<RingHead*>(ring_raw);
     float* smem = reinterpret_cast<float*>(ring_raw + kRingHead);
     asm volatile("griddepcontrol.launch_dependents;");    // the adding kernel may take its place; it waits for this grid's end
     const int T = blockDim.x, R = blockDim.y, bar_id = 1 + threadIdx.y;
@@ -467,9 +468,9 @@ layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
     const TX* x = static_cast<const TX*>(a.x);
     const TX* src_x = x + first * a.ldx;                  // the next row to be copied
     const TX* src_dy = static_cast<const TX*>(a.dy) + first * a.lddy;
-    int64_t next = first;
+    int64_t next = wait_limit > 0 ? kNoMore : first;      // the self-test copies nothing
     auto fill = [&](uint32_t entry, uint32_t bar) {
-        if (next < a.copy_rows) {
+        if (next < a.rows) {
             mbar_expect_tx(bar, 2 * row_bytes);
             bulk_load(entry, src_x, row_bytes, bar);
             bulk_load(entry + row_bytes, src_dy, row_bytes, bar);
@@ -496,8 +497,8 @@ layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
         for (int j = 0; j < PAIRS; ++j) { w[k][j] = f2_pack(t[2 * j], t[2 * j + 1]); dw[k][j] = 0; db[k][j] = 0; }
     }
     zero_scratch(smem, R * 128);
-    if (threadIdx.x == 0 && threadIdx.y == 0) head->gave_up = 0;
-    __syncthreads();                                       // the barriers, the scratch and the flag exist
+    init_ring_head(slots, wait_limit, step, a.rows);
+    __syncthreads();                                       // the barriers, the scratch and the head exist
     const float inv_n = 1.0f / (float)a.cols;
     float next_mean = 0.0f, next_rstd = 0.0f;
     if (first < a.rows) { next_mean = __ldg(a.mean + first); next_rstd = __ldg(a.rstd + first); }
@@ -508,7 +509,7 @@ layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
         if (row + step < a.rows) { next_mean = __ldg(a.mean + row + step); next_rstd = __ldg(a.rstd + row + step); }
         const f32x2 minus = f2_pack(-mean, -mean), rr = f2_pack(rstd, rstd);
         f32x2 xh[NV][PAIRS], g[NV][PAIRS], sg = 0, sgx = 0;
-        ring.wait(a, head, row, next);
+        ring.wait(row, next);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (mine(k)) {
@@ -541,7 +542,6 @@ layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots) {
                 stg_pairs(dst + (int64_t)k * T * VEC, o);
             }
     }
-    if (threadIdx.x == 0) ring.drain(a, head, first, step, next);
     if (!a.partial) return;
     // every copy has been waited for: the rings' memory is free once all groups are here
     leave_columns<VEC, NV>(a, smem + R * 128, nvec, [&](int which, int k, int j) {
@@ -727,7 +727,7 @@ int ring_slots(int groups, int64_t entry_bytes) {
 constexpr int kRingSmem = 200 * 1024;                    // dynamic shared memory asked for; the largest use is 2 x 64 KB + scratch
 
 template <typename TX, typename TW, int PER, bool FULL>
-cudaError_t run_forward_ring(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
+cudaError_t run_forward_ring(const LayerNormArgs& a, long long wait_limit, int num_sms, cudaStream_t st) {
     constexpr int NV = PER * sizeof(TX) / 16;
     RowShape s = row_shape(a.cols, PER, 512);
     const int64_t spread = (a.rows + num_sms - 1) / num_sms;             // few rows: one group per SM rather than full CTAs
@@ -739,7 +739,7 @@ cudaError_t run_forward_ring(const LayerNormArgs& a, int num_sms, cudaStream_t s
     const cudaError_t e = allow_smem(layer_norm_ring_kernel<TX, TW, NV, FULL>, kRingSmem, granted);
     if (e != cudaSuccess) return e;
     const int64_t need = (a.rows + s.groups - 1) / s.groups;
-    layer_norm_ring_kernel<TX, TW, NV, FULL><<<(unsigned)(need < num_sms ? need : num_sms), dim3(s.threads, s.groups), smem, st>>>(a, slots);
+    layer_norm_ring_kernel<TX, TW, NV, FULL><<<(unsigned)(need < num_sms ? need : num_sms), dim3(s.threads, s.groups), smem, st>>>(a, slots, wait_limit);
     return cudaGetLastError();
 }
 
@@ -761,7 +761,7 @@ cudaError_t run_forward(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
 }
 
 template <typename TX, typename TW>
-cudaError_t forward_of(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
+cudaError_t forward_of(const LayerNormArgs& a, long long wait_limit, int num_sms, cudaStream_t st) {
     constexpr int V = 16 / sizeof(TX);
     const bool vec = a.cols % V == 0 && (a.ldx * (int64_t)sizeof(TX)) % 16 == 0 && (a.ldy * (int64_t)sizeof(TX)) % 16 == 0 &&
                      aligned(a.x, 16) && aligned(a.y, 16) && aligned(a.weight, 16) && aligned(a.bias, 16);
@@ -771,8 +771,8 @@ cudaError_t forward_of(const LayerNormArgs& a, int num_sms, cudaStream_t st) {
         else layer_norm_long_kernel<TX, TW, 1><<<grid, kMaxRowThreads, 0, st>>>(a);
         return cudaGetLastError();
     }
-    if (vec && a.cols >= 2048) return a.cols % 1024 == 0 ? run_forward_ring<TX, TW, 32, true>(a, num_sms, st) : run_forward_ring<TX, TW, 32, false>(a, num_sms, st);
-    if (vec) return a.cols % 512 == 0 ? run_forward_ring<TX, TW, 16, true>(a, num_sms, st) : run_forward_ring<TX, TW, 16, false>(a, num_sms, st);
+    if (vec && a.cols >= 2048) return a.cols % 1024 == 0 ? run_forward_ring<TX, TW, 32, true>(a, wait_limit, num_sms, st) : run_forward_ring<TX, TW, 32, false>(a, wait_limit, num_sms, st);
+    if (vec) return a.cols % 512 == 0 ? run_forward_ring<TX, TW, 16, true>(a, wait_limit, num_sms, st) : run_forward_ring<TX, TW, 16, false>(a, wait_limit, num_sms, st);
     if (a.cols > kPerThread * 512) return run_forward<TX, TW, kPerThread, kMaxRowThreads>(a, num_sms, st);
     return a.cols <= 4 * 256 ? run_forward<TX, TW, 4, 256>(a, num_sms, st) : run_forward<TX, TW, kPerThread, 512>(a, num_sms, st);
 }
@@ -792,7 +792,7 @@ cudaError_t add_columns(const LayerNormArgs& a, int groups, cudaStream_t st) {
 }
 
 template <typename TX, typename TW, bool RING, bool FULL, int PER, int CTA>
-cudaError_t run_backward(const LayerNormArgs& a, cudaStream_t st) {
+cudaError_t run_backward(const LayerNormArgs& a, long long wait_limit, cudaStream_t st) {
     RowShape s = row_shape(a.cols, PER, CTA);
     const int64_t spread = (a.rows + kBwdGroups - 1) / kBwdGroups;
     if (s.groups > spread) s.groups = spread < 1 ? 1 : (int)spread;
@@ -808,7 +808,7 @@ cudaError_t run_backward(const LayerNormArgs& a, cudaStream_t st) {
     if constexpr (RING) {
         constexpr int NV = PER * sizeof(TX) / 16;
         e = allow_smem(layer_norm_backward_ring_kernel<TX, TW, NV, FULL>, kRingSmem, granted);
-        if (e == cudaSuccess && grid > 0) layer_norm_backward_ring_kernel<TX, TW, NV, FULL><<<grid, dim3(s.threads, s.groups), smem, st>>>(a, slots);
+        if (e == cudaSuccess && grid > 0) layer_norm_backward_ring_kernel<TX, TW, NV, FULL><<<grid, dim3(s.threads, s.groups), smem, st>>>(a, slots, wait_limit);
     } else {
         e = allow_smem(layer_norm_backward_kernel<TX, TW, PER, CTA>, kRingSmem, granted);
         if (e == cudaSuccess && grid > 0) layer_norm_backward_kernel<TX, TW, PER, CTA><<<grid, dim3(s.threads, s.groups), smem, st>>>(a);
@@ -818,7 +818,7 @@ cudaError_t run_backward(const LayerNormArgs& a, cudaStream_t st) {
 }
 
 template <typename TX, typename TW>
-cudaError_t backward_of(const LayerNormArgs& a, cudaStream_t st) {
+cudaError_t backward_of(const LayerNormArgs& a, long long wait_limit, cudaStream_t st) {
     constexpr int V = 16 / sizeof(TX);
     const bool vec = a.cols % V == 0 && (a.ldx * (int64_t)sizeof(TX)) % 16 == 0 && (a.ldy * (int64_t)sizeof(TX)) % 16 == 0 &&
                      (a.lddy * (int64_t)sizeof(TX)) % 16 == 0 && aligned(a.x, 16) && aligned(a.y, 16) && aligned(a.dy, 16) && aligned(a.weight, 16);
@@ -839,25 +839,27 @@ cudaError_t backward_of(const LayerNormArgs& a, cudaStream_t st) {
         if (e == cudaSuccess) e = cudaGetLastError();
         return e != cudaSuccess || !a.partial ? e : add_columns<TW>(a, grid, st);
     }
-    if (!vec && a.cols <= 1024) return run_backward<TX, TW, false, false, 4, 768>(a, st);
-    if (!vec && a.cols <= 6 * 768) return run_backward<TX, TW, false, false, 6, 768>(a, st);
-    if (!vec) return run_backward<TX, TW, false, false, kPerThread, 512>(a, st);
-    return a.cols % (kPerThread * 32) == 0 ? run_backward<TX, TW, true, true, kPerThread, 512>(a, st) : run_backward<TX, TW, true, false, kPerThread, 512>(a, st);
+    if (!vec && a.cols <= 1024) return run_backward<TX, TW, false, false, 4, 768>(a, wait_limit, st);
+    if (!vec && a.cols <= 6 * 768) return run_backward<TX, TW, false, false, 6, 768>(a, wait_limit, st);
+    if (!vec) return run_backward<TX, TW, false, false, kPerThread, 512>(a, wait_limit, st);
+    return a.cols % (kPerThread * 32) == 0 ? run_backward<TX, TW, true, true, kPerThread, 512>(a, wait_limit, st) : run_backward<TX, TW, true, false, kPerThread, 512>(a, wait_limit, st);
 }
 
 }  // namespace
 
 int layer_norm_backward_groups(int64_t rows) { return (int)(rows < kBwdGroups ? (rows < 1 ? 1 : rows) : kBwdGroups); }
 
-cudaError_t launch_layer_norm(const LayerNormArgs& a, int dtype, int weight_dtype, int num_sms, cudaStream_t st) {
+cudaError_t launch_layer_norm(const LayerNormArgs& a, int dtype, int weight_dtype, int num_sms, cudaStream_t st, const StallTest& stall) {
+    const long long limit = stall.wait_limit;
     if (dtype == UE5M3_BF16)
-        return weight_dtype == UE5M3_BF16 ? forward_of<__nv_bfloat16, __nv_bfloat16>(a, num_sms, st) : forward_of<__nv_bfloat16, float>(a, num_sms, st);
-    return weight_dtype == UE5M3_BF16 ? forward_of<float, __nv_bfloat16>(a, num_sms, st) : forward_of<float, float>(a, num_sms, st);
+        return weight_dtype == UE5M3_BF16 ? forward_of<__nv_bfloat16, __nv_bfloat16>(a, limit, num_sms, st) : forward_of<__nv_bfloat16, float>(a, limit, num_sms, st);
+    return weight_dtype == UE5M3_BF16 ? forward_of<float, __nv_bfloat16>(a, limit, num_sms, st) : forward_of<float, float>(a, limit, num_sms, st);
 }
-cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, int dtype, int weight_dtype, cudaStream_t st) {
+cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, int dtype, int weight_dtype, cudaStream_t st, const StallTest& stall) {
+    const long long limit = stall.wait_limit;
     if (dtype == UE5M3_BF16)
-        return weight_dtype == UE5M3_BF16 ? backward_of<__nv_bfloat16, __nv_bfloat16>(a, st) : backward_of<__nv_bfloat16, float>(a, st);
-    return weight_dtype == UE5M3_BF16 ? backward_of<float, __nv_bfloat16>(a, st) : backward_of<float, float>(a, st);
+        return weight_dtype == UE5M3_BF16 ? backward_of<__nv_bfloat16, __nv_bfloat16>(a, limit, st) : backward_of<__nv_bfloat16, float>(a, limit, st);
+    return weight_dtype == UE5M3_BF16 ? backward_of<float, __nv_bfloat16>(a, limit, st) : backward_of<float, float>(a, limit, st);
 }
 
 int read_and_clear_norm_status() {
