@@ -305,7 +305,8 @@ UE5M3_API int ue5m3_gemm_stall_selftest(int which, int64_t Mo, int64_t No, int64
  *   weight, bias   device, [cols] contiguous; each may be null (1 and 0).
  *   mean, rstd     device, [rows] binary32 outputs, each may be null; ue5m3_layer_norm_backward takes them.
  *   ldx, ldy >= cols.  Pointers are aligned to their element; rows that are 16-byte aligned throughout (pointers, leading
- *   dimensions and cols * element size) are read with 16-byte loads, others element by element.
+ *   dimensions and cols * element size) are read with 16-byte loads, others element by element.  y may be x (same pointer and
+ *   leading dimension) and else has no element in common with it.
  *   eps >= 0 and finite.
  */
 UE5M3_API int ue5m3_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx,
@@ -318,7 +319,7 @@ UE5M3_API int ue5m3_layer_norm(const void* x, int dtype, int64_t rows, int64_t c
  *     dweight = sum_r dy * xh,   dbias = sum_r dy
  * One pass over x and dy; the column sums are kept in binary32 per CTA, written to `workspace` and added in a fixed order
  * by a second kernel, so that the result does not change from call to call.
- *   dx             device, [rows, cols], leading dimension lddx, type dtype.
+ *   dx             device, [rows, cols], leading dimension lddx, type dtype; may be dy or x (same pointer and leading dimension).
  *   dweight, dbias device, [cols], type weight_dtype; each may be null.  weight may be null (1).
  *   workspace      device, ue5m3_layer_norm_backward_workspace_bytes(rows, cols) bytes, 16-byte aligned; may be null when
  *                  dweight and dbias both are.

@@ -35,8 +35,9 @@ template <typename T> struct Raw;
 template <> struct Raw<__nv_bfloat16> { unsigned short v; };
 template <> struct Raw<float> { float v; };
 
-__device__ __forceinline__ void load_raw(Raw<__nv_bfloat16>& r, const __nv_bfloat16* p) { r.v = __ldg(reinterpret_cast<const unsigned short*>(p)); }
-__device__ __forceinline__ void load_raw(Raw<float>& r, const float* p) { r.v = __ldg(p); }
+// (plain loads: y may be x, and a load through the read-only path promises that the kernel writes nothing there)
+__device__ __forceinline__ void load_raw(Raw<__nv_bfloat16>& r, const __nv_bfloat16* p) { r.v = *reinterpret_cast<const unsigned short*>(p); }
+__device__ __forceinline__ void load_raw(Raw<float>& r, const float* p) { r.v = *p; }
 __device__ __forceinline__ float unpack(const Raw<__nv_bfloat16>& r) { return __uint_as_float((uint32_t)r.v << 16); }
 __device__ __forceinline__ float unpack(const Raw<float>& r) { return r.v; }
 

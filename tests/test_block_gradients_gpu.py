@@ -33,3 +33,18 @@ def test_gradient_of_a_bias_without_a_weight_has_the_bias_type(cols, dt, bdt):
         lib.layer_norm_backward(dy, x, w, mean, rstd, bias_dtype=F if bdt == BF else BF)       # two types of parameters
     with pytest.raises(TypeError):
         lib.layer_norm_backward(dy, x, None, mean, rstd, bias_dtype=torch.float16)
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("rows,cols", [(700, 33), (3000, 1023), (300, 1537), (900, 4607), (300, 8191), (40, 12001), (30, 16385), (3000, 1024), (60, 16384)])
+def test_layer_norm_in_place(rows, cols, dt):
+    """y over x, dx over dy and dx over x: aligned rows and rows at every offset from 16 bytes, all kernels."""
+    x, w, b, dy = make(rows, cols, dt, F, seed=cols)
+    y, mean, rstd = lib.layer_norm(x, w, b)
+    want = lib.layer_norm_backward(dy, x, w, mean, rstd)
+    z = x.clone()
+    assert all(torch.equal(a, c) for a, c in zip(lib.layer_norm(z, w, b, out=z), (y, mean, rstd)))
+    z = dy.clone()
+    assert all(torch.equal(a, c) for a, c in zip(lib.layer_norm_backward(z, x, w, mean, rstd, out=z), want))
+    z = x.clone()
+    assert all(torch.equal(a, c) for a, c in zip(lib.layer_norm_backward(dy, z, w, mean, rstd, out=z), want))
