@@ -214,9 +214,10 @@ def dropout_add(x: torch.Tensor, p: float, seed: int, residual: Optional[torch.T
 
 
 class DropoutAdd(torch.nn.Module):
-    """residual + dropout(x) with a draw stream of its own per layer, rank and step (call `advance()` once per optimizer step, as for
-    Ue5m3Linear: within a step the same mask is drawn every time, so a recomputed forward pass meets the same one).  In
-    evaluation mode nothing is dropped."""
+    """residual + dropout(x) with a draw stream of its own per layer, rank and step.  Call `advance()` once per batch that a gradient is
+    taken of: per optimizer step and, where gradients are accumulated, per micro-batch.  In between the same mask is drawn every time, so
+    a recomputed forward pass meets the same one; a module that stands twice in a model therefore draws one mask for both places.
+    In evaluation mode nothing is dropped."""
 
     def __init__(self, p: float, seed: Optional[int] = None, group=None):
         super().__init__()

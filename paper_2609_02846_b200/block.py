@@ -18,7 +18,8 @@ from .autograd import DropoutAdd, LayerNorm, Ue5m3Linear, attention
 
 class TransformerBlock(torch.nn.Module):
     """One pre-norm block over x [batch, tokens, hidden] (bfloat16), grouped-query attention.  `linear(in, out)` builds the four
-    linears (Ue5m3Linear by default: tokens and widths must then be multiples of 128).  Call `advance()` once per optimizer step."""
+    linears (Ue5m3Linear by default: tokens and widths must then be multiples of 128).  Call `advance()` once per optimizer step and, where
+    gradients are accumulated, `next_micro_batch()` between the micro-batches of a step."""
 
     def __init__(self, hidden: int, heads: int, kv_heads: int, ffn: int, p: float = 0.1, window_left: int = -1,
                  linear: Optional[Callable] = None):
@@ -37,6 +38,11 @@ class TransformerBlock(torch.nn.Module):
         for m in self.children():
             if hasattr(m, "advance"):
                 m.advance()
+
+    def next_micro_batch(self) -> None:
+        """New dropout masks; the linears stay at their step."""
+        self.drop1.advance()
+        self.drop2.advance()
 
     def forward(self, x: torch.Tensor, k_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
         B, L, hidden = x.shape

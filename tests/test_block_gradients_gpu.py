@@ -4,6 +4,7 @@ import torch
 
 import paper_2609_02846_b200 as lib
 from paper_2609_02846_b200 import autograd as A
+from paper_2609_02846_b200.block import TransformerBlock
 from block_reference import assert_within, layer_norm_backward
 from test_layer_norm_gpu import make
 
@@ -48,3 +49,24 @@ def test_layer_norm_in_place(rows, cols, dt):
     assert all(torch.equal(a, c) for a, c in zip(lib.layer_norm_backward(z, x, w, mean, rstd, out=z), want))
     z = x.clone()
     assert all(torch.equal(a, c) for a, c in zip(lib.layer_norm_backward(dy, z, w, mean, rstd, out=z), want))
+
+
+def test_micro_batches_of_a_step_draw_masks_of_their_own():
+    """Accumulated gradients: next_micro_batch() moves the dropout layers alone, so the linears keep the step (and with it the schedule of
+    their tensor references), and a micro-batch that is computed again before it meets its own masks again."""
+    block = TransformerBlock(256, 4, 2, 512, 0.5)
+    x = torch.randn(1, 128, 256, device=DEV, dtype=BF)
+    zeros = lambda drop: drop(torch.ones(64, 256, device=DEV)) == 0
+    seen = []
+    for micro in range(3):
+        masks = [zeros(block.drop1), zeros(block.drop2)]
+        assert torch.equal(masks[0], zeros(block.drop1))
+        y = block(x)
+        assert torch.equal(y, block(x))
+        for mask in masks:
+            assert all(abs(float((mask == other).float().mean()) - 0.5) < 0.05 for other in seen)
+            seen.append(mask)
+        block.next_micro_batch()
+    assert block.qkv.step == block.down.step == 0
+    block.advance()
+    assert block.qkv.step == 1 and block.drop1.step == block.drop2.step == 4
