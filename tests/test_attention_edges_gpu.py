@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2609_02846_b200 as lib
+from block_reference import allowed, attention, attention_backward
 from test_attention_gpu import make
 
 pytestmark = pytest.mark.gpu
@@ -102,3 +103,48 @@ def test_garbage_in_keys_in_front_of_every_window(Lq, Lk, left, D):
         v2[:, :first:3] = float("nan")
         for a, b in zip(want, _call(q, k2, v2, do, **kw)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("Lq,Lk,H,Hk,D,causal,left,lens", [
+    (150, 150, 2, 1, 64, True, -1, None), (200, 200, 4, 2, 128, True, 40, None), (130, 300, 2, 2, 72, False, -1, [250]), (1, 260, 8, 2, 128, True, -1, None)])
+def test_gradients_against_differences_along_them(Lq, Lk, H, Hk, D, causal, left, lens):
+    """Along u = g / |g| for the gradient g that the formulas give in 64 bits, the difference quotient of sum(o * dout) is |g|, and the
+    kernel's gradient projected on u lies within the roundings, element by element: P and dS in BF16 (the reference's bound), o in BF16
+    inside dout . o, the gradient's own.  They are below half of |g| here, so that zero, the negated gradient and its double all fail."""
+    q, k, v, do = make(1, Lq, Lk, H, Hk, D, seed=Lq + Lk)
+    kl = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+    kw = dict(causal=causal, window_left=left, k_lens=kl)
+    o, lse = lib.attention(q, k, v, **kw)
+    grads = lib.attention_backward(do, q, k, v, o, lse, **kw)
+    for want, tol, got, *others in along_the_gradient(q, k, v, do, o, lse, grads, causal, left, lens):
+        assert tol < 0.5 * want
+        assert abs(got - want) <= tol
+        assert all(abs(x - want) > tol for x in others)
+
+
+def along_the_gradient(q, k, v, do, o, lse, grads, causal, left, lens):
+    """(difference quotient, tolerance, projection of the gradient, projections of wrong ones) for q, k and v."""
+    ins = [t.double() for t in (q, k, v)]
+    exact_o, exact_lse, off_o, _ = attention(*ins, causal, left, lens)
+    formulas = attention_backward(do, *ins, exact_o, exact_lse, causal, left, lens)
+    f = lambda *t: float((attention(*t, causal, left, lens)[0] * do.double()).sum())
+    # what the rounding of o changes in D = dout . o, and that in dq and dk (dv does not depend on o)
+    off_d = (do.double().abs() * (off_o + 2.0 ** -8 * exact_o.abs())).sum(-1)                                # [1, Lq, H]
+    group = q.shape[2] // k.shape[2]
+    extra = [torch.zeros_like(t) for t in ins]
+    n = k.shape[1] if lens is None else lens[0]
+    ok = allowed(q.shape[1], k.shape[1], causal, left, n, q.device)
+    for h in range(q.shape[2]):
+        qq, kk = ins[0][0, :, h], ins[1][0, :, h // group]
+        s = (qq @ kk.T * q.shape[3] ** -0.5).masked_fill(~ok, float("-inf"))
+        p = torch.softmax(s, 1) * off_d[0, :, h, None] * q.shape[3] ** -0.5
+        extra[0][0, :, h] = p @ kk.abs()
+        extra[1][0, :, h // group] += p.T @ qq.abs()
+    for i in range(3):
+        g, bound = formulas[i]
+        u, e = g / g.norm(), 1e-3
+        at = lambda s: f(*(t + s * e * u if j == i else t for j, t in enumerate(ins)))
+        want = (at(1) - at(-1)) / (2 * e)
+        tol = float(((bound + extra[i] + 2.0 ** -8 * g.abs()) * u.abs()).sum()) + 1e-4 * want
+        got = float((grads[i].double() * u).sum())
+        yield want, tol, got, 0.0, -got, 2 * got
