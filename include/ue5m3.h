@@ -317,8 +317,8 @@ UE5M3_API int ue5m3_layer_norm(const void* x, int dtype, int64_t rows, int64_t c
  * Backward pass of ue5m3_layer_norm.  With xh = (x - mean) * rstd and g = dy * weight:
  *     dx = rstd * (g - sum_c g / cols - xh * sum_c (g * xh) / cols)
  *     dweight = sum_r dy * xh,   dbias = sum_r dy
- * One pass over x and dy; the column sums are kept in binary32 per CTA, written to `workspace` and added in a fixed order
- * by a second kernel, so that the result does not change from call to call.
+ * One pass over x and dy (two for cols > 8192); the column sums are kept in binary32 per CTA, written to `workspace` and
+ * added in a fixed order by a second kernel, so that the result does not change from call to call.
  *   dx             device, [rows, cols], leading dimension lddx, type dtype; may be dy or x (same pointer and leading dimension).
  *   dweight, dbias device, [cols], type weight_dtype; each may be null.  weight may be null (1).
  *   workspace      device, ue5m3_layer_norm_backward_workspace_bytes(rows, cols) bytes, 16-byte aligned; may be null when
@@ -364,7 +364,9 @@ typedef struct {
 /*
  * Attention.  Query i of a sequence stands at key position i + k_len - q_len; it sees the keys j with j < k_lens[b],
  * j <= position (causal) and j >= position - window_left (window_left >= 0).  Query head h uses key/value head
- * h / (heads / kv_heads).
+ * h / (heads / kv_heads).  Positions count from the common k_len, not from k_lens[b], as right-padded sequences have them; on caches of
+ * different lengths a sequence with k_lens[b] <= position - window_left has no key in its window, and causal hides none of the keys of
+ * a sequence that ends in front of the first query. 
  *     S_ij = scale * q_i . k_j,   lse_i = log sum_j exp S_ij,   o_i = sum_j exp(S_ij - lse_i) v_j      over the keys it sees
  * A query that sees no key gets o = 0 and lse = -inf.  Keys and values at positions >= k_lens[b], and those in front of every
  * query's window, are never used, whatever they hold (NaN included).  Products of BF16 values are accumulated in binary32; the probabilities are rounded to BF16

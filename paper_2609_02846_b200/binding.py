@@ -580,8 +580,9 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
               k_lens: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> tuple:
     """ue5m3_attention: (o, lse) for q [batch, tokens, heads, head_dim] and k, v [batch, keys, kv_heads, head_dim], bfloat16.  Any
     strides with a contiguous last dimension (views of a fused projection); `window_left` = keys a query sees before its own
-    position (-1: all), `k_lens` int32 [batch] = valid keys of each sequence, `scale` defaults to head_dim ** -0.5.  `out` may be q;
-    any other overlap with an input is refused."""
+    position (-1: all), `k_lens` int32 [batch] = valid keys of each sequence, `scale` defaults to head_dim ** -0.5.  Query i stands at
+    position i + keys - tokens of every sequence, whatever its k_lens (right-padded batches).  `out` may be q; any other overlap with
+    an input is refused."""
     shape = _attention_shape(q, k, causal, window_left, k_lens, scale)
     if out is None:
         out = q.new_empty(q.shape)

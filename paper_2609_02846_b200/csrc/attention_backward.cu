@@ -12,9 +12,15 @@
 // and add binary32 parts in order).  The three overlap: the keys kernel sets itself up under the rows kernel, the queries kernel fills
 // the tail of the keys kernel.
 //
-// 2 x 4096 tokens, 32 / 8 heads of 128, causal: rows 25 us (5.4 TB/s), keys 403, queries 371 (ncu), together 757 us: 908 TFLOP/s of
-// the 5 products that the gradients need, 1271 of the 7 that are computed, 0.92 of what a BF16 product sustains under the power
-// cap that both reach.  A step of the keys kernel takes 2620 cycles (products 2048), of the queries kernel about 2200 (1536).
+// 2 x 4096 tokens, 32 / 8 heads of 128, causal: rows 25 us (5.4 TB/s), keys 403, queries 371 (ncu), together 757 to 780 us in short
+// bursts: about 890 TFLOP/s of the 5 products that the gradients need, 1250 of the 7 that are computed, 0.76 of the measured burst rate
+// of a BF16 product.  One call after the other, under the power cap, 878 to 888 us: 1090 TFLOP/s of the 7, 0.79 of the sustained
+// rate.  A step of the keys kernel takes 2620 cycles (products 2048), of the queries kernel about 2200 (1536): what bounds both is the
+// chain of a step, S - P - dP - dS - product, with two tiles in tensor memory to overlap it.
+//
+// P and dS are rounded to BF16 for the products that add them up, since the other operand (dO, Q, K) is BF16 and a product has one type:
+// 2^-8 of each value at most, in binary32 before and after.  Against 64 bits the gradients are off by a relative 0.0024 of their norm (up
+// to 0.0032 where a few pairs carry it), of which their own rounding makes 0.0017.
 //
 // P and dS never touch shared memory: the softmax warps read S and dP from tensor memory and write P and dS (BF16) over them,
 // from where the tensor core takes them as the A operand.  Both kernels have the same roles:

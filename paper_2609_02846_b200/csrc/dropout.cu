@@ -5,7 +5,8 @@
 // One call of the generator serves a group of eight consecutive elements: 16 bytes of BF16, 32 bytes of FP32.  A thread takes one
 // group, its loads first; the generator's ~70 instructions hide behind the memory latency of the other warps.
 // Bound by memory: 6 bytes per BF16 element with a residual, 4 without; without one the generator begins to show.  16384 x 4096 BF16
-// with a residual: 57.5 us, 7.0 TB/s (two groups per thread 57.8, a persistent grid 66.8); without 45.4 us, 5.9 TB/s (48.6, 56.2).
+// with a residual: 57.5 us, 7.0 TB/s (two groups per thread 57.8, a persistent grid 66.8), calls from Python in a row 61.5; without
+// 45.4 us, 5.9 TB/s (48.6, 56.2).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>

@@ -4,13 +4,15 @@
 //   backward  xh = (x - mean) rstd, g = dy w:  dx = rstd (g - sum g / n - xh sum(g xh) / n),  dw = sum_r dy xh, db = sum_r dy
 //
 // Both are bound by memory (2 and 3 elements moved per element, 8 and 14 operations).  The kernels are persistent: a group of
-// T threads owns a row at a time, every thread the same 16 columns of each of its rows, so the weights are read once per CTA
-// into registers, the column sums of dw and db stay in registers until the CTA ends, and the row itself stays in registers
+// T threads owns a row at a time, every thread the same columns of each of its rows (aligned rows: 32 forward from 2048 columns on, else
+// 16; others: 16, or 4 and 6 where that was faster, see there), so the weights are read once per CTA into registers, the column sums of dw and db stay in registers until the CTA ends, and the row itself stays in registers
 // between the reductions (the variance is that of the centred values: no cancellation for a large mean).
 // Rows that are 16-byte aligned come through a ring in shared memory, filled by bulk copies several rows ahead: about 100 KB are
 // in flight per SM, which a prefetch in registers cannot hold.  Other rows are prefetched element by element, one row ahead.
 // Column sums leave as one binary32 row per CTA and are added by a second small kernel in a fixed order: no atomics.
-// Rows longer than 16 * 1024 columns take a kernel that re-reads the row instead.
+// Rows of more than 16384 columns (backward: 8192) take kernels that re-read the row instead.
+// Times below are GPU time, calls back to back in a graph; calls from Python in a row take up to 8 % longer where the GPU is what
+// takes the time (forward 8192 x 4096 26.6 us, backward 16384 x 4096 77.4) and the host's 14 to 21 us where it is not.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -200,7 +202,7 @@ __device__ __forceinline__ float f2_total(f32x2 v) {
 // ------------------------------------------------------------------------------------------------ forward
 // blockDim = (T, R): R groups of T threads, a row each, NV 16-byte vectors per thread: 32 columns from 2048 columns on, 16 below.
 // What a row costs besides its columns (two sums through shuffles and a barrier, ~150 instructions per warp) made 16 columns per
-// thread issue-bound: 30.6 us at 8192 x 4096 BF16 against 24.7 us with 32.  FULL: the columns fill the group's threads exactly, so
+// thread issue-bound: 30.6 us at 8192 x 4096 BF16 against 24.4 us with 32 (24.4 to 27 by box; 5.5 TB/s, 0.84 of the measured copy; FP32 48.9 us, 0.84).  FULL: the columns fill the group's threads exactly, so
 // nothing is conditional (a fifth of the instructions of a row go).
 template <typename TX, typename TW, int NV, bool FULL>
 __global__ void __launch_bounds__(512)
@@ -299,7 +301,8 @@ layer_norm_ring_kernel(const LayerNormArgs a, const int slots, const long long w
     }
 }
 
-// Rows without 16-byte alignment: NV single columns per thread, prefetched one row ahead; otherwise as above.
+// Rows without 16-byte alignment: NV single columns per thread, prefetched one row ahead; otherwise as above.  8000 x 1537 FP32 27.1 us
+// (3.6 TB/s, 0.55 of the measured copy), 8192 x 1537 BF16 29.9 (1.7 TB/s): bound by the number of loads, one per element.
 template <typename TX, typename TW, int NV, int MAXT>
 __global__ void __launch_bounds__(MAXT)
 layer_norm_kernel(const LayerNormArgs a) {
@@ -452,7 +455,7 @@ __device__ __forceinline__ void leave_columns(const LayerNormArgs& a, float* sum
 
 // Rows of x and dy come through the ring (an entry holds both).  Dynamic shared memory: the head, [R][128] reduction scratch, [R][slots]
 // barriers, [R][slots][2] rows; at the end the column sums over them.  16 columns per thread: weights, both column sums and both rows
-// are 80 registers already.  16384 x 4096 BF16 with the adding kernel: 72 us, 5.6 TB/s (0.86 of the measured copy).
+// are 80 registers already.  16384 x 4096 BF16 with the adding kernel: 71.5 us, 5.6 TB/s (0.86 of the measured copy).
 template <typename TX, typename TW, int NV, bool FULL>
 __global__ void __launch_bounds__(512)
 layer_norm_backward_ring_kernel(const LayerNormArgs a, const int slots, const long long wait_limit) {
@@ -622,7 +625,7 @@ layer_norm_backward_kernel(const LayerNormArgs a) {
 // Rows of any length (over 8192 columns), one row per CTA at a time: x and dy are read twice, the second time from the caches.
 // The column sums stay in shared memory up to 24576 columns, beyond that in this CTA's row of the workspace; a thread always
 // has the same columns, so they need no order between threads.  VEC columns per access (1 where rows are not 16-byte aligned).
-// 4096 x 16384 BF16: 191 us, 2.1 TB/s: a row at a time per SM waits for its own loads; such rows are rare enough to leave it there.
+// 4096 x 16384 BF16: 191 us, 2.1 TB/s (0.32 of the measured copy): a row at a time per SM waits for its own loads.
 template <typename TX, typename TW, int VEC>
 __global__ void __launch_bounds__(kMaxRowThreads) layer_norm_backward_long_kernel(const LayerNormArgs a, const int sums_in_smem) {
     extern __shared__ __align__(16) float smem[];          // [128] reduction scratch, [2][cols] sums
