@@ -5,7 +5,7 @@
  * are stored as packed E2M1 payloads (4 bits) with one unsigned E5M3 block scale per 16 values
  * and one FP32 tensor reference per operand, and the three GEMMs of a linear layer are computed
  * on those operands.  Beside them stand the operators between the linears of a transformer block: layer norm, dropout
- * added to the residual and attention, each with its backward pass.
+ * added to the residual, norms and rotary positions of queries and keys, and attention, each with its backward pass; and the AdamW step.
  *
  * General rules for every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller.  Nothing is allocated, nothing
@@ -401,6 +401,106 @@ UE5M3_API int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const
                               const ue5m3_heads* k, const ue5m3_heads* v, const ue5m3_heads* o, const float* lse,
                               const ue5m3_heads* dq, const ue5m3_heads* dk, const ue5m3_heads* dv, void* workspace,
                               void* stream);
+
+/*
+ * Rotary positions of queries and keys.  A head's row of head_dim values has rotary_dim / 2 pairs; pair i of a token at position p is
+ * turned by the angle p * frequencies[i] and multiplied by `amplitude`:
+ *     a' = amplitude (a cos t - b sin t),   b' = amplitude (a sin t + b cos t),   t = p * frequencies[i]
+ * The pairs are (i, i + rotary_dim / 2), or neighbours (2 i, 2 i + 1) with `interleaved`; the values from rotary_dim on stay as they are.
+ * Angles are products in binary64 (radians per position), reduced there; what follows is binary32, rounded once to the output's type.
+ * `inverse` = 1 negates the angles: with the same amplitude that is the transposed map, and so the backward pass.
+ *   q, q_out [batch, tokens, heads, head_dim], k, k_out [batch, tokens, kv_heads, head_dim], the last dimension contiguous, strides in
+ *   elements, positive where the dimension is larger than 1; pointers aligned to their element.  kv_heads = 0: no k (its pointers may be null).
+ *   An output may be its own input (same pointer and strides) and else has no element in common with an input or the other output
+ *   (UE5M3_ERR_INVALID_ARG where that is found out, as for all views of one buffer).
+ *   Rows whose pairs can be read by 16 (8, 4) bytes throughout are: pointers, strides, head_dim / 2 and, without `interleaved`, rotary_dim / 2.
+ */
+typedef struct {
+    int64_t batch, tokens, heads, kv_heads;
+    int64_t head_dim;             /* even, at most 256 */
+    int64_t rotary_dim;           /* even, 2 .. head_dim */
+    const double* frequencies;    /* device, [rotary_dim / 2] */
+    const void* positions;        /* device, int32 or int64; null: first_position + index of the token */
+    int64_t position_stride;      /* elements from one sequence's positions to the next (0: all sequences have the same); tokens are contiguous */
+    int64_t first_position;       /* without `positions` */
+    int position_bytes;           /* 4 or 8, with `positions` */
+    int interleaved;              /* 0 or 1 */
+    float amplitude;              /* finite */
+    int dtype;                    /* UE5M3_F32 or UE5M3_BF16, of q, k and the outputs */
+} ue5m3_rotary_shape;
+
+UE5M3_API int ue5m3_rotary(const ue5m3_rotary_shape* shape, int inverse, const ue5m3_heads* q, const ue5m3_heads* k,
+                           const ue5m3_heads* q_out, const ue5m3_heads* k_out, void* stream);
+
+/*
+ * Norms of queries and keys for each head, with the rotary positions in the same pass:
+ *     r = 1 / sqrt(sum_d x_d^2 / head_dim + eps),   y = rotate(x * r * weight)
+ * with q_weight and k_weight [head_dim] (type weight_dtype; null: 1).  Everything in binary32 (the angles as above), rounded once.
+ * Other arguments as in ue5m3_rotary.  eps >= 0 and finite.
+ */
+UE5M3_API int ue5m3_qk_norm_rotary(const ue5m3_rotary_shape* shape, const ue5m3_heads* q, const ue5m3_heads* k, const void* q_weight,
+                                   const void* k_weight, int weight_dtype, float eps, const ue5m3_heads* q_out, const ue5m3_heads* k_out,
+                                   void* stream);
+
+/*
+ * Backward pass of ue5m3_qk_norm_rotary from its inputs (nothing else is kept; r is computed again).  With u = dy turned back, g = u * weight, xh = x * r:
+ *     dx = r * (g - xh * sum_d (g * xh) / head_dim),   dweight = sum over batch, tokens and heads of u * xh
+ *   dq_out may be dq or q, dk_out may be dk or k (same pointer and strides), otherwise as above.
+ *   dq_weight, dk_weight  device, [head_dim], type weight_dtype; each may be null.  Summed in binary32 in a fixed order, by way of `workspace`:
+ *   device, ue5m3_qk_norm_rotary_backward_workspace_bytes(shape) bytes, 16-byte aligned; may be null when both are.
+ */
+UE5M3_API size_t ue5m3_qk_norm_rotary_backward_workspace_bytes(const ue5m3_rotary_shape* shape);
+UE5M3_API int ue5m3_qk_norm_rotary_backward(const ue5m3_rotary_shape* shape, const ue5m3_heads* dq, const ue5m3_heads* dk, const ue5m3_heads* q,
+                                   const ue5m3_heads* k, const void* q_weight, const void* k_weight, int weight_dtype, float eps,
+                                   const ue5m3_heads* dq_out, const ue5m3_heads* dk_out, void* dq_weight, void* dk_weight, void* workspace,
+                                   void* stream);
+
+/*
+ * One AdamW step over many tensors, in place (launches of up to 400 tensors each):
+ *     g = grad * grad_scale,   m = beta1 m + (1 - beta1) g,   v = beta2 v + ((1 - beta2) g) g         (binary32, every operation rounded)
+ *     w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * w is `master` (binary32) where there is one, and param then is its rounded copy; else it is param, read and rounded to nearest in its type (in
+ * BF16 updates below 2^-9 of a weight are lost: keep a master).
+ * state_bits = 32: m and v are binary32 [n].  state_bits = 8: m and v are bytes [n] with binary32 scales m_scale and v_scale, one for
+ * every 256 elements ([ceil(n / 256)]); element = code's value * scale.  m's code is a sign bit and E4M3 (bias 7, largest value 448), v's is UE5M3.  All zero bytes
+ * and scales are the state before the first step.  With a = the block's largest magnitude, F = 448 or 61440, e = -6 or -14 (binary32, every operation rounded):
+ *     scale = a * (1 / F),   t = (|x| * ((1 / a) * F)) * 2^(-126 - e),   code = min((bits(t) + 16 draw + 8) >> 20, code of F)
+ * which rounds up with the probability of |x|'s place between two codes, to 16 bits.  A positive v has a code of at least 1.  Blocks with
+ * a < 2^-110 are stored as zeros; blocks in which a value is not finite get the scale NaN.  The draws come from Philox4x32 with 7 rounds, key = (seed low, seed high) and
+ * counter = (low32(i >> 3), stream, 2, low32(step)) for element i: lane j = i & 7 uses half (j & 1) of output word j >> 1 for v, and the same 16 bits with their two bytes exchanged for m.
+ *   tensors       host array of `count` descriptors; all memory they point to is on the device, contiguous, aligned to its element and has nothing in common
+ *                 with that of another.  Tensors whose pointers are 16-byte aligned are read with 16-byte loads.  n = 0 is left out.
+ *   step          host struct, read during the call.
+ *   grad_scale    device, 1 float, may be null (1): for instance a clipping factor.  Where it is not finite the step is left out: nothing is written.
+ *   clock         device, UE5M3_ADAMW_CLOCK_BYTES, 8-byte aligned, zero before the first step; may be null.  With it the number of the step is
+ *                 counted in its first int64, which every call raises by one before it uses it (unless the step is left out), and `step` is ignored: a call that was captured into a
+ *                 graph then takes a new step with every replay.  (lr and the other numbers stay those of the capture.)
+ */
+typedef struct {
+    void* param;
+    const void* grad;
+    float* master;                /* null: none */
+    void* m;
+    void* v;
+    float* m_scale;               /* state_bits = 8 only */
+    float* v_scale;
+    int64_t n;                    /* at most 2^35 */
+    uint32_t stream;              /* of the draws: another one for every tensor */
+    uint8_t param_dtype, grad_dtype;      /* UE5M3_F32 or UE5M3_BF16 */
+    uint16_t reserved;
+} ue5m3_adamw_tensor;
+
+typedef struct {
+    int64_t step;                 /* 1 for the first */
+    double lr, beta1, beta2, eps, weight_decay;       /* lr, eps, weight_decay >= 0 and finite (eps > 0 with 8 bits), 0 <= beta < 1 */
+    const float* grad_scale;
+    void* clock;
+    uint64_t seed;
+    int state_bits;               /* 8 or 32 */
+} ue5m3_adamw_step;
+
+#define UE5M3_ADAMW_CLOCK_BYTES 32
+UE5M3_API int ue5m3_adamw(const ue5m3_adamw_tensor* tensors, int64_t count, const ue5m3_adamw_step* step, void* stream);
 
 /*
  * Failure-detection self-test of the attention and layer norm kernels, as ue5m3_gemm_stall_selftest: a small problem with the

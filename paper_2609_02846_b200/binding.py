@@ -7,7 +7,9 @@ here.  The library is required: a missing or unloadable ``libue5m3.so`` raises a
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
+from array import array
 from dataclasses import dataclass
 from typing import Optional
 
@@ -25,7 +27,8 @@ SYMBOLS = ("ue5m3_sample_amax", "ue5m3_quantize", "ue5m3_quantize_dual", "ue5m3_
            "ue5m3_gemm_probe_matched", "ue5m3_gemm_stall_selftest", "ue5m3_scales_bytes", "ue5m3_unswizzle_scales",
            "ue5m3_last_device_status", "ue5m3_status_string", "ue5m3_layer_norm", "ue5m3_layer_norm_backward_workspace_bytes",
            "ue5m3_layer_norm_backward", "ue5m3_dropout_add", "ue5m3_attention_workspace_bytes", "ue5m3_attention",
-           "ue5m3_attention_backward_workspace_bytes", "ue5m3_attention_backward", "ue5m3_block_stall_selftest")
+           "ue5m3_attention_backward_workspace_bytes", "ue5m3_attention_backward", "ue5m3_block_stall_selftest", "ue5m3_rotary",
+           "ue5m3_qk_norm_rotary", "ue5m3_qk_norm_rotary_backward_workspace_bytes", "ue5m3_qk_norm_rotary_backward", "ue5m3_adamw")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libue5m3.so")
@@ -40,6 +43,19 @@ class _AttentionShape(C.Structure):         # ue5m3_attention_shape
     _fields_ = [("batch", C.c_int64), ("q_len", C.c_int64), ("k_len", C.c_int64), ("heads", C.c_int64), ("kv_heads", C.c_int64),
                 ("head_dim", C.c_int64), ("window_left", C.c_int64), ("k_lens", C.c_void_p), ("scale", C.c_float), ("dtype", C.c_int),
                 ("causal", C.c_int)]
+
+
+class _RotaryShape(C.Structure):            # ue5m3_rotary_shape
+    _fields_ = [("batch", C.c_int64), ("tokens", C.c_int64), ("heads", C.c_int64), ("kv_heads", C.c_int64), ("head_dim", C.c_int64),
+                ("rotary_dim", C.c_int64), ("frequencies", C.c_void_p), ("positions", C.c_void_p), ("position_stride", C.c_int64),
+                ("first_position", C.c_int64), ("position_bytes", C.c_int), ("interleaved", C.c_int), ("amplitude", C.c_float),
+                ("dtype", C.c_int)]
+
+
+class _AdamwStep(C.Structure):              # ue5m3_adamw_step
+    _fields_ = [("step", C.c_int64), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("grad_scale", C.c_void_p), ("clock", C.c_void_p), ("seed", C.c_uint64),
+                ("state_bits", C.c_int)]
 
 
 class Ue5m3Error(RuntimeError):
@@ -106,6 +122,17 @@ def _load() -> C.CDLL:
         L.ue5m3_attention_backward_workspace_bytes.argtypes = [shape]
         L.ue5m3_attention_backward.restype = ci
         L.ue5m3_attention_backward.argtypes = [shape, heads, heads, heads, heads, heads, vp, heads, heads, heads, vp, vp]
+        turn = C.POINTER(_RotaryShape)
+        L.ue5m3_rotary.restype = ci
+        L.ue5m3_rotary.argtypes = [turn, ci, heads, heads, heads, heads, vp]
+        L.ue5m3_qk_norm_rotary.restype = ci
+        L.ue5m3_qk_norm_rotary.argtypes = [turn, heads, heads, vp, vp, ci, f32, heads, heads, vp]
+        L.ue5m3_qk_norm_rotary_backward_workspace_bytes.restype = C.c_size_t
+        L.ue5m3_qk_norm_rotary_backward_workspace_bytes.argtypes = [turn]
+        L.ue5m3_qk_norm_rotary_backward.restype = ci
+        L.ue5m3_qk_norm_rotary_backward.argtypes = [turn, heads, heads, heads, heads, vp, vp, ci, f32, heads, heads, vp, vp, vp, vp]
+        L.ue5m3_adamw.restype = ci
+        L.ue5m3_adamw.argtypes = [vp, i64, C.POINTER(_AdamwStep), vp]
         L.ue5m3_block_stall_selftest.restype = ci
         L.ue5m3_block_stall_selftest.argtypes = [ci, vp, C.c_size_t, i64, vp]
         L.ue5m3_status_string.restype = C.c_char_p
@@ -611,6 +638,180 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     _call(lib.ue5m3_attention_backward, "ue5m3_attention_backward", q, shape, _heads(dout, qs, q), _heads(q, qs, q), _heads(k, ks, q),
           _heads(v, ks, q), _heads(o, qs, q), lse.data_ptr(), _heads(dq, qs, q), _heads(dk, ks, q), _heads(dv, ks, q), ws.data_ptr())
     return dq, dk, dv
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                       trained_length: Optional[int] = None, fast: float = 32.0, slow: float = 1.0, device="cuda") -> tuple:
+    """(frequencies, amplitude) for the rotary calls: base^(-2 i / rotary_dim) radians per position, a float64 tensor [rotary_dim / 2], and
+    1.0.  For contexts `factor` times longer than the trained one, `scaling`:
+      "linear"  every frequency divided by the factor (positions shrunk);
+      "base"    a larger base, by which the slowest pair turns `factor` times slower and the fastest as before;
+      "parts"   pairs that turn at most `slow` times within `trained_length` positions are divided by the factor, those that turn `fast`
+                times or more stay, a linear ramp in between; the amplitude is 0.1 ln(factor) + 1."""
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError(f"rotary_dim = {rotary_dim}: a positive even number is wanted")
+    if not base > 0 or not factor >= 1:
+        raise ValueError(f"base {base} has to be positive and factor {factor} at least 1")
+    if scaling not in (None, "linear", "base", "parts"):
+        raise ValueError(f"unknown scaling {scaling!r}: None, 'linear', 'base' or 'parts'")
+    if scaling == "base" and rotary_dim > 2:
+        base = base * factor ** (rotary_dim / (rotary_dim - 2))
+    f = torch.tensor([base ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)], dtype=torch.float64)
+    amplitude = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "parts":
+        if not trained_length or not fast > slow:
+            raise ValueError("scaling 'parts' wants the trained_length and fast > slow")
+        keep = ((trained_length * f / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+        f = f * keep + f / factor * (1 - keep)
+        amplitude = 0.1 * math.log(factor) + 1.0
+    return f.to(device), amplitude
+
+
+def _rotary_shape(q, k, frequencies, positions, interleaved, amplitude) -> _RotaryShape:
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError("expected tensors [batch, tokens, heads, head_dim]")
+    B, L, H, D = q.shape
+    Hk = 0
+    if k is not None:
+        Bk, Lk, Hk, Dk = k.shape
+        if Bk != B or Lk != L or Dk != D:
+            raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} differ in more than the heads")
+    if frequencies.dim() != 1 or frequencies.dtype != torch.float64 or not frequencies.is_contiguous() or frequencies.get_device() != q.get_device():
+        raise ValueError("frequencies must be a contiguous float64 vector on the queries' device (see rotary_frequencies)")
+    first, stride, size, at = 0, 0, 0, None
+    if isinstance(positions, int):
+        first = positions
+    elif positions is not None:
+        if positions.dtype not in (torch.int32, torch.int64) or positions.get_device() != q.get_device() or positions.dim() not in (1, 2) or \
+                positions.shape[-1] != L or (L > 1 and positions.stride(-1) != 1) or (positions.dim() == 2 and positions.shape[0] not in (1, B)):
+            raise ValueError(f"positions must be an int32 or int64 tensor [{L}] or [{B}, {L}] with contiguous tokens on the queries' device")
+        at, size = positions.data_ptr(), positions.element_size()
+        stride = positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else 0
+    return _RotaryShape(B, L, H, Hk, D, 2 * frequencies.shape[0], frequencies.data_ptr(), at, stride, first, size, 1 if interleaved else 0,
+                        amplitude, _dtype_code(q))
+
+
+def _pair(t: tuple, q: torch.Tensor, k: Optional[torch.Tensor]) -> tuple:
+    """C descriptions of two tensors like q and k."""
+    return _heads(t[0], q.shape, q), None if k is None else _heads(t[1], k.shape, q)
+
+
+def _new_pair(q: torch.Tensor, k: Optional[torch.Tensor], out: Optional[tuple]) -> tuple:
+    return (q.new_empty(q.shape), None if k is None else k.new_empty(k.shape)) if out is None else out
+
+
+def rotary(q: torch.Tensor, k: Optional[torch.Tensor], frequencies: torch.Tensor, positions=None, interleaved: bool = False,
+           amplitude: float = 1.0, inverse: bool = False, out: Optional[tuple] = None) -> tuple:
+    """ue5m3_rotary: (q, k) with the first 2 * len(frequencies) values of every head's row turned by position * frequency.  q [batch, tokens,
+    heads, head_dim], k [batch, tokens, kv_heads, head_dim] or None, float32 or bfloat16, any strides with a contiguous last dimension;
+    `frequencies` float64 (see rotary_frequencies).  `positions`: None (the tokens' indices), the first token's position, or an int32 / int64
+    tensor [tokens] or [batch, tokens].  `inverse` turns back, which is the gradient.  `out` may be (q, k)."""
+    shape = _rotary_shape(q, k, frequencies, positions, interleaved, amplitude)
+    out = _new_pair(q, k, out)
+    _call(_load().ue5m3_rotary, "ue5m3_rotary", q, shape, 1 if inverse else 0, *_pair((q, k), q, k), *_pair(out, q, k))
+    return out
+
+
+def _norm_weights(q, q_weight, k_weight):
+    """The weights' type code."""
+    one = q_weight if q_weight is not None else k_weight
+    dtype = None if one is None else one.dtype
+    for w in (q_weight, k_weight):
+        _vector(w, q.shape[-1], q, dtype)
+    return F32 if one is None else _dtype_code_of(dtype)
+
+
+def qk_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                   frequencies: torch.Tensor, positions=None, interleaved: bool = False, amplitude: float = 1.0, eps: float = 1e-6,
+                   out: Optional[tuple] = None) -> tuple:
+    """ue5m3_qk_norm_rotary: (q, k) with every head's row divided by its root mean square, times the weight [head_dim] (float32 or bfloat16,
+    None: 1), and turned as by `rotary`, whose other arguments these are."""
+    shape = _rotary_shape(q, k, frequencies, positions, interleaved, amplitude)
+    code = _norm_weights(q, q_weight, k_weight)
+    out = _new_pair(q, k, out)
+    _call(_load().ue5m3_qk_norm_rotary, "ue5m3_qk_norm_rotary", q, shape, *_pair((q, k), q, k), _ptr(q_weight), _ptr(k_weight), code, eps,
+          *_pair(out, q, k))
+    return out
+
+
+def qk_norm_rotary_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: torch.Tensor, k: Optional[torch.Tensor],
+                            q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor], frequencies: torch.Tensor, positions=None,
+                            interleaved: bool = False, amplitude: float = 1.0, eps: float = 1e-6, want_weights: bool = True,
+                            out: Optional[tuple] = None) -> tuple:
+    """ue5m3_qk_norm_rotary_backward: (dq, dk, dq_weight, dk_weight) from the gradients of what `qk_norm_rotary` returned and its arguments.
+    A weight's gradient has the weight's type; it is None without the weight or when not wanted.  `out`: where dq and dk go (may be the
+    upstream gradients)."""
+    shape = _rotary_shape(q, k, frequencies, positions, interleaved, amplitude)
+    code = _norm_weights(q, q_weight, k_weight)
+    out = _new_pair(q, k, out)
+    dqw = q_weight.new_empty(q_weight.shape) if want_weights and q_weight is not None else None
+    dkw = k_weight.new_empty(k_weight.shape) if want_weights and k_weight is not None else None
+    lib = _load()
+    ws = None
+    if dqw is not None or dkw is not None:
+        ws = q.new_empty(lib.ue5m3_qk_norm_rotary_backward_workspace_bytes(shape), dtype=torch.uint8)
+    _call(lib.ue5m3_qk_norm_rotary_backward, "ue5m3_qk_norm_rotary_backward", q, shape, *_pair((dq, dk), q, k), *_pair((q, k), q, k),
+          _ptr(q_weight), _ptr(k_weight), code, eps, *_pair(out, q, k), _ptr(dqw), _ptr(dkw), _ptr(ws))
+    return *out, dqw, dkw
+
+
+ADAMW_BLOCK = 256           # elements that share a scale of 8-bit moments
+ADAMW_CLOCK_BYTES = 32
+
+
+def adamw(params, grads, m, v, step: int = 1, lr: float = 1e-3, betas: tuple = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+          master=None, m_scale=None, v_scale=None, grad_scale: Optional[torch.Tensor] = None, seed: int = 0,
+          clock: Optional[torch.Tensor] = None, streams=None) -> None:
+    """ue5m3_adamw: one AdamW step over lists of contiguous tensors on one device, in place.  params and grads float32 or bfloat16; `master`: float32
+    copies of the params (a list, entries may be None) that take the step instead and are rounded into them.  Moments m and v: float32, or uint8
+    with `m_scale` and `v_scale` (float32, one for every ADAMW_BLOCK elements; all zeros before the first step), rounded by draws of (seed, stream, step,
+    element), where `streams` (default: the places in the lists) tell the tensors apart.  `step` counts from 1; `clock` (ADAMW_CLOCK_BYTES zero bytes, uint8 or int64)
+    counts on the device instead, for steps captured into a graph.  `grad_scale`: float32 tensor of one value that the gradients are multiplied by; where it
+    is not finite nothing is written."""
+    count = len(params)
+    eight = m_scale is not None
+    if not (len(grads) == len(m) == len(v) == count) or any(x is not None and len(x) != count for x in (master, m_scale, v_scale, streams)) or \
+            eight != (v_scale is not None):
+        raise ValueError("params, grads and their states are lists of the same length (m_scale and v_scale both or neither)")
+    if count == 0:
+        return
+    device = params[0].get_device()
+    state = torch.uint8 if eight else torch.float32
+
+    def at(t, n, dtype, what, i):
+        if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+            raise ValueError(f"{what}[{i}]: expected a contiguous tensor of {n} {dtype} on {params[0].device}, got [{tuple(t.shape)}, {t.dtype}, {t.device}]")
+        return t.data_ptr()
+
+    flat, seen = array("q"), set()
+    for i in range(count):
+        p, g = params[i], grads[i]
+        n = p.numel()
+        code = _dtype_code_of(p.dtype)
+        if g.shape != p.shape:
+            raise ValueError(f"grads[{i}] has shape {tuple(g.shape)}, params[{i}] {tuple(p.shape)}")
+        first = at(p, n, p.dtype, "params", i)
+        if n:
+            if first in seen:
+                raise ValueError(f"params[{i}] stands in the list twice")
+            seen.add(first)
+        copy = None if master is None else master[i]
+        blocks = -(-n // ADAMW_BLOCK)
+        flat.extend((first, at(g, n, g.dtype, "grads", i), 0 if copy is None else at(copy, n, torch.float32, "master", i),
+                     at(m[i], n, state, "m", i), at(v[i], n, state, "v", i),
+                     at(m_scale[i], blocks, torch.float32, "m_scale", i) if eight else 0, at(v_scale[i], blocks, torch.float32, "v_scale", i) if eight else 0,
+                     n, ((i if streams is None else streams[i]) & 0xFFFFFFFF) | code << 32 | _dtype_code(g) << 40))
+    for t, what in ((grad_scale, "grad_scale"), (clock, "clock")):
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{what} is on {t.device}, the params on {params[0].device}")
+    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+        raise ValueError("grad_scale must be a float32 tensor of one value")
+    if clock is not None and (clock.numel() * clock.element_size() < ADAMW_CLOCK_BYTES or not clock.is_contiguous()):
+        raise ValueError(f"clock must hold {ADAMW_CLOCK_BYTES} bytes")
+    how = _AdamwStep(step, lr, betas[0], betas[1], eps, weight_decay, _ptr(grad_scale), _ptr(clock), int(seed) & (2 ** 64 - 1), 8 if eight else 32)
+    _call(_load().ue5m3_adamw, "ue5m3_adamw", params[0], flat.buffer_info()[0], count, how)
 
 
 def block_stall_selftest(which: int, buffer: torch.Tensor, wait_limit_cycles: int = 2_000_000) -> None:

@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <mutex>
 #include "../../include/ue5m3.h"
@@ -589,6 +590,161 @@ int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_hea
     int sms = 0;
     if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
     return launch_attention_backward(s, *dout, *q, *k, *v, *o, lse, *dq, *dk, *dv, static_cast<float*>(workspace), (cudaStream_t)stream);
+}
+
+// ----------------------------------------------------------------------------- rotary positions, norms of queries and keys
+static int check_rotary_shape(const ue5m3_rotary_shape* s) {
+    if (!s || s->batch < 0 || s->tokens < 0 || s->heads <= 0 || s->kv_heads < 0 || s->head_dim <= 0 || s->rotary_dim <= 0) return UE5M3_ERR_INVALID_ARG;
+    if (!known_dtype(s->dtype) || (s->interleaved != 0 && s->interleaved != 1) || !(std::fabs(s->amplitude) <= 3.0e38f)) return UE5M3_ERR_INVALID_ARG;
+    if (!s->frequencies || (s->positions && s->position_bytes != 4 && s->position_bytes != 8)) return UE5M3_ERR_INVALID_ARG;
+    if (s->rotary_dim > s->head_dim || s->rotary_dim % 2 || s->head_dim % 2) return UE5M3_ERR_SHAPE;
+    const int64_t most = (int64_t)1 << 30;
+    if (s->head_dim > 256 || s->batch > most || s->tokens > most || s->heads > 65536 || s->kv_heads > 65536 || s->batch * s->tokens > most) return UE5M3_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(s->frequencies) % 8 || (s->positions && reinterpret_cast<uintptr_t>(s->positions) % (uintptr_t)s->position_bytes)) return UE5M3_ERR_ALIGN;
+    return UE5M3_OK;
+}
+// A tensor [batch, tokens, heads, head_dim] of any alignment.
+static int check_rows(const ue5m3_heads* t, const ue5m3_rotary_shape& s, int64_t heads) {
+    if (heads == 0) return UE5M3_OK;
+    if (!t) return UE5M3_ERR_INVALID_ARG;
+    if (s.batch * s.tokens == 0) return UE5M3_OK;
+    if (!t->data) return UE5M3_ERR_INVALID_ARG;
+    if (!aligned_to(t->data, s.dtype)) return UE5M3_ERR_ALIGN;
+    const int64_t sizes[3] = {s.batch, s.tokens, heads}, strides[3] = {t->batch_stride, t->token_stride, t->head_stride};
+    for (int i = 0; i < 3; ++i) {
+        if (sizes[i] <= 1) continue;
+        if (strides[i] <= 0) return UE5M3_ERR_ALIGN;
+        if (sizes[i] > ((int64_t)1 << 58) / strides[i]) return UE5M3_ERR_UNSUPPORTED;       // no such memory
+    }
+    return UE5M3_OK;
+}
+// Where its elements lie, in units of elements.
+static Extent extent_of_rows(const ue5m3_heads& t, const ue5m3_rotary_shape& s, int64_t heads) {
+    Extent e{(int64_t)(reinterpret_cast<uintptr_t>(t.data) / (s.dtype == UE5M3_BF16 ? 2 : 4)), {s.batch, s.tokens, heads, s.head_dim},
+             {t.batch_stride, t.token_stride, t.head_stride, 1}, 0};
+    for (int i = 0; i < 4; ++i) e.last += (e.sizes[i] - 1) * (e.sizes[i] > 1 ? e.strides[i] : 0);
+    return e;
+}
+// Checks what the three calls have in common and launches.  `in`, `up`, `out`: queries and keys; up is null but for the backward pass.
+static int rotary_call(RotaryArgs& a, const ue5m3_rotary_shape* shape, const ue5m3_heads* const (&in)[2], const ue5m3_heads* const (&up)[2],
+                       const ue5m3_heads* const (&out)[2], void* stream) {
+    int bad = check_rotary_shape(shape);
+    if (bad != UE5M3_OK) return bad;
+    const ue5m3_rotary_shape& s = *shape;
+    const bool backward = a.op == RotaryArgs::kBackward;
+    if (a.op != RotaryArgs::kRotary) {
+        if (!known_dtype(a.weight_dtype) || !(a.eps >= 0.0f) || a.eps > 3.0e38f) return UE5M3_ERR_INVALID_ARG;
+        for (int k = 0; k < 2; ++k)
+            if (!aligned_to(a.weight[k], a.weight_dtype) || !aligned_to(a.dweight[k], a.weight_dtype)) return UE5M3_ERR_ALIGN;
+    }
+    const int64_t heads[2] = {s.heads, s.kv_heads};
+    for (int k = 0; k < 2; ++k) {
+        if ((bad = check_rows(in[k], s, heads[k])) != UE5M3_OK || (bad = check_rows(out[k], s, heads[k])) != UE5M3_OK) return bad;
+        if (backward && (bad = check_rows(up[k], s, heads[k])) != UE5M3_OK) return bad;
+    }
+    const bool wants = backward && (a.dweight[0] || (a.dweight[1] && s.kv_heads > 0));
+    if (wants && !a.partial) return UE5M3_ERR_INVALID_ARG;
+    if (!aligned16(a.partial)) return UE5M3_ERR_ALIGN;
+    if (s.batch * s.tokens > 0) {
+        Extent o[2];
+        for (int k = 0; k < 2; ++k) {
+            if (heads[k] == 0) continue;
+            o[k] = extent_of_rows(*out[k], s, heads[k]);
+            for (int j = 0; j < 2; ++j) {
+                if (heads[j] == 0) continue;
+                for (const ue5m3_heads* t : {in[j], backward ? up[j] : in[j]}) {
+                    const Extent e = extent_of_rows(*t, s, heads[j]);
+                    // in place: the threads that write a row are the only ones that read it, and have read it
+                    if (!(j == k && same_layout(o[k], e)) && overlap(o[k], e)) return UE5M3_ERR_INVALID_ARG;
+                }
+            }
+        }
+        if (s.kv_heads > 0 && overlap(o[0], o[1])) return UE5M3_ERR_INVALID_ARG;
+    }
+    int sms = 0;
+    if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
+    const size_t size = a.weight_dtype == UE5M3_BF16 ? 2 : 4;
+    if (s.batch * s.tokens == 0 || (s.kv_heads == 0 && a.dweight[1])) {
+        // nothing to add up: zeros
+        for (int k = 0; k < 2; ++k)
+            if (a.dweight[k] && (k == 1 || s.batch * s.tokens == 0) &&
+                cudaMemsetAsync(a.dweight[k], 0, (size_t)s.head_dim * size, (cudaStream_t)stream) != cudaSuccess) return UE5M3_ERR_CUDA;
+        if (s.batch * s.tokens == 0) return UE5M3_OK;
+        a.dweight[1] = nullptr;
+    }
+    if (!wants) a.partial = nullptr;
+    a.s = s;
+    for (int k = 0; k < 2; ++k)
+        if (heads[k] > 0) a.side[k] = RotaryArgs::Tensors{*in[k], backward ? *up[k] : ue5m3_heads{}, *out[k]};
+    return launch_rotary(a, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+}
+
+int ue5m3_rotary(const ue5m3_rotary_shape* shape, int inverse, const ue5m3_heads* q, const ue5m3_heads* k, const ue5m3_heads* q_out,
+                 const ue5m3_heads* k_out, void* stream) {
+    const ApiRange range_("ue5m3_rotary");
+    if (inverse != 0 && inverse != 1) return UE5M3_ERR_INVALID_ARG;
+    RotaryArgs a{};
+    a.op = RotaryArgs::kRotary;
+    a.inverse = inverse;
+    return rotary_call(a, shape, {q, k}, {nullptr, nullptr}, {q_out, k_out}, stream);
+}
+
+int ue5m3_qk_norm_rotary(const ue5m3_rotary_shape* shape, const ue5m3_heads* q, const ue5m3_heads* k, const void* q_weight, const void* k_weight,
+                         int weight_dtype, float eps, const ue5m3_heads* q_out, const ue5m3_heads* k_out, void* stream) {
+    const ApiRange range_("ue5m3_qk_norm_rotary");
+    RotaryArgs a{};
+    a.op = RotaryArgs::kNorm;
+    a.weight[0] = q_weight; a.weight[1] = k_weight;
+    a.weight_dtype = weight_dtype;
+    a.eps = eps;
+    return rotary_call(a, shape, {q, k}, {nullptr, nullptr}, {q_out, k_out}, stream);
+}
+
+size_t ue5m3_qk_norm_rotary_backward_workspace_bytes(const ue5m3_rotary_shape* shape) {
+    if (check_rotary_shape(shape) != UE5M3_OK) return 0;
+    return (size_t)rotary_backward_ctas() * 2 * (size_t)shape->head_dim * sizeof(float);
+}
+
+int ue5m3_qk_norm_rotary_backward(const ue5m3_rotary_shape* shape, const ue5m3_heads* dq, const ue5m3_heads* dk, const ue5m3_heads* q,
+                                  const ue5m3_heads* k, const void* q_weight, const void* k_weight, int weight_dtype, float eps,
+                                  const ue5m3_heads* dq_out, const ue5m3_heads* dk_out, void* dq_weight, void* dk_weight, void* workspace,
+                                  void* stream) {
+    const ApiRange range_("ue5m3_qk_norm_rotary_backward");
+    RotaryArgs a{};
+    a.op = RotaryArgs::kBackward;
+    a.inverse = 1;
+    a.weight[0] = q_weight; a.weight[1] = k_weight;
+    a.dweight[0] = dq_weight; a.dweight[1] = dk_weight;
+    a.weight_dtype = weight_dtype;
+    a.eps = eps;
+    a.partial = static_cast<float*>(workspace);
+    return rotary_call(a, shape, {q, k}, {dq, dk}, {dq_out, dk_out}, stream);
+}
+
+// ----------------------------------------------------------------------------- AdamW
+int ue5m3_adamw(const ue5m3_adamw_tensor* tensors, int64_t count, const ue5m3_adamw_step* step, void* stream) {
+    const ApiRange range_("ue5m3_adamw");
+    if (!step || count < 0 || (count > 0 && !tensors)) return UE5M3_ERR_INVALID_ARG;
+    const ue5m3_adamw_step& s = *step;
+    auto number = [](double x) { return x >= 0.0 && x <= 3.0e38; };
+    if (!number(s.lr) || !number(s.eps) || !number(s.weight_decay) || !(s.beta1 >= 0.0 && s.beta1 < 1.0) || !(s.beta2 >= 0.0 && s.beta2 < 1.0)) return UE5M3_ERR_INVALID_ARG;
+    if ((s.state_bits != 8 && s.state_bits != 32) || (!s.clock && s.step < 1)) return UE5M3_ERR_INVALID_ARG;
+    if (s.state_bits == 8 && (float)s.eps == 0.0f) return UE5M3_ERR_INVALID_ARG;
+    if (!aligned_to(s.grad_scale, UE5M3_F32) || reinterpret_cast<uintptr_t>(s.clock) % 8) return UE5M3_ERR_ALIGN;
+    for (int64_t i = 0; i < count; ++i) {
+        const ue5m3_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || !known_dtype(t.param_dtype) || !known_dtype(t.grad_dtype)) return UE5M3_ERR_INVALID_ARG;
+        if (t.n == 0) continue;
+        if (t.n > ((int64_t)1 << 35)) return UE5M3_ERR_UNSUPPORTED;
+        if (!t.param || !t.grad || !t.m || !t.v || (s.state_bits == 8 && (!t.m_scale || !t.v_scale))) return UE5M3_ERR_INVALID_ARG;
+        if (!aligned_to(t.param, t.param_dtype) || !aligned_to(t.grad, t.grad_dtype) || !aligned_to(t.master, UE5M3_F32)) return UE5M3_ERR_ALIGN;
+        if (s.state_bits == 8 ? !aligned_to(t.m_scale, UE5M3_F32) || !aligned_to(t.v_scale, UE5M3_F32) : !aligned_to(t.m, UE5M3_F32) || !aligned_to(t.v, UE5M3_F32))
+            return UE5M3_ERR_ALIGN;
+    }
+    int sms = 0;
+    const int bad = device_ready(sms);
+    if (bad != UE5M3_OK) return bad;
+    return launch_adamw(tensors, count, s, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
 // Self-test problems: 4500 rows of 64 columns in BF16, three to each of the 148 x 15 row groups; one sequence, heads of 64 that share one key/value head, 300 queries of two heads on 300 keys or one query of

@@ -1,4 +1,4 @@
-// Host-side launch interface of the operators between the quantized linears (layer norm, dropout, attention).
+// Host-side launch interface of the operators between the quantized linears (layer norm, dropout, rotary positions, attention) and of the AdamW step.
 #pragma once
 #include <cuda_runtime.h>
 #include <atomic>
@@ -48,6 +48,21 @@ struct DropoutArgs {
     uint64_t seed;
 };
 cudaError_t launch_dropout_add(const DropoutArgs& a, int dtype, cudaStream_t st);
+
+struct RotaryArgs {
+    enum Op { kRotary, kNorm, kBackward } op;
+    ue5m3_rotary_shape s;
+    struct Tensors { ue5m3_heads x, dy, y; } side[2];      // queries, keys; y: the output (backward: dx)
+    int inverse;
+    const void* weight[2];
+    int weight_dtype;
+    float eps;
+    void* dweight[2];
+    float* partial;                       // backward: [CTAs][2][head_dim]; null: no gradients of the weights
+};
+int rotary_backward_ctas();               // most CTAs of the backward kernel
+cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t st);
+cudaError_t launch_adamw(const ue5m3_adamw_tensor* tensors, int64_t count, const ue5m3_adamw_step& s, cudaStream_t st);
 
 // returns a UE5M3_* status
 int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
