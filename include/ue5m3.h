@@ -403,6 +403,20 @@ UE5M3_API int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const
                               void* stream);
 
 /*
+ * Attention with sinks: ue5m3_attention and its backward pass where the first `sinks` keys (0 .. 128) of a sequence stay visible behind a
+ * query's window: it sees the keys j < k_lens[b], j <= position (causal), with j >= position - window_left or j < sinks.  Without a window
+ * (window_left = -1), and with sinks = 0, these are the calls above.  Never used, whatever they hold, are keys and values behind a sequence's
+ * end and those in front of every window that are no sinks.  Other arguments and errors as above (sinks > 128: UE5M3_ERR_UNSUPPORTED); the forward
+ * pass's workspace is ue5m3_attention_workspace_bytes, the backward pass's its own.
+ */
+UE5M3_API int ue5m3_attention_sinks(const ue5m3_attention_shape* shape, int64_t sinks, const ue5m3_heads* q, const ue5m3_heads* k,
+                              const ue5m3_heads* v, const ue5m3_heads* o, float* lse, void* workspace, void* stream);
+UE5M3_API size_t ue5m3_attention_sinks_backward_workspace_bytes(const ue5m3_attention_shape* shape, int64_t sinks);
+UE5M3_API int ue5m3_attention_sinks_backward(const ue5m3_attention_shape* shape, int64_t sinks, const ue5m3_heads* dout,
+                              const ue5m3_heads* q, const ue5m3_heads* k, const ue5m3_heads* v, const ue5m3_heads* o, const float* lse,
+                              const ue5m3_heads* dq, const ue5m3_heads* dk, const ue5m3_heads* dv, void* workspace, void* stream);
+
+/*
  * Rotary positions of queries and keys.  A head's row of head_dim values has rotary_dim / 2 pairs; pair i of a token at position p is
  * turned by the angle p * frequencies[i] and multiplied by `amplitude`:
  *     a' = amplitude (a cos t - b sin t),   b' = amplitude (a sin t + b cos t),   t = p * frequencies[i]

@@ -28,7 +28,8 @@ SYMBOLS = ("ue5m3_sample_amax", "ue5m3_quantize", "ue5m3_quantize_dual", "ue5m3_
            "ue5m3_last_device_status", "ue5m3_status_string", "ue5m3_layer_norm", "ue5m3_layer_norm_backward_workspace_bytes",
            "ue5m3_layer_norm_backward", "ue5m3_dropout_add", "ue5m3_attention_workspace_bytes", "ue5m3_attention",
            "ue5m3_attention_backward_workspace_bytes", "ue5m3_attention_backward", "ue5m3_block_stall_selftest", "ue5m3_rotary",
-           "ue5m3_qk_norm_rotary", "ue5m3_qk_norm_rotary_backward_workspace_bytes", "ue5m3_qk_norm_rotary_backward", "ue5m3_adamw")
+           "ue5m3_qk_norm_rotary", "ue5m3_qk_norm_rotary_backward_workspace_bytes", "ue5m3_qk_norm_rotary_backward", "ue5m3_adamw",
+           "ue5m3_attention_sinks", "ue5m3_attention_sinks_backward_workspace_bytes", "ue5m3_attention_sinks_backward")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libue5m3.so")
@@ -122,6 +123,12 @@ def _load() -> C.CDLL:
         L.ue5m3_attention_backward_workspace_bytes.argtypes = [shape]
         L.ue5m3_attention_backward.restype = ci
         L.ue5m3_attention_backward.argtypes = [shape, heads, heads, heads, heads, heads, vp, heads, heads, heads, vp, vp]
+        L.ue5m3_attention_sinks.restype = ci
+        L.ue5m3_attention_sinks.argtypes = [shape, i64, heads, heads, heads, heads, vp, vp, vp]
+        L.ue5m3_attention_sinks_backward_workspace_bytes.restype = C.c_size_t
+        L.ue5m3_attention_sinks_backward_workspace_bytes.argtypes = [shape, i64]
+        L.ue5m3_attention_sinks_backward.restype = ci
+        L.ue5m3_attention_sinks_backward.argtypes = [shape, i64, heads, heads, heads, heads, heads, vp, heads, heads, heads, vp, vp]
         turn = C.POINTER(_RotaryShape)
         L.ue5m3_rotary.restype = ci
         L.ue5m3_rotary.argtypes = [turn, ci, heads, heads, heads, heads, vp]
@@ -604,8 +611,8 @@ def _attention_shape(q, k, causal, window_left, k_lens, scale) -> _AttentionShap
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, window_left: int = -1,
-              k_lens: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> tuple:
-    """ue5m3_attention: (o, lse) for q [batch, tokens, heads, head_dim] and k, v [batch, keys, kv_heads, head_dim], bfloat16.  Any
+              k_lens: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None, sinks: int = 0) -> tuple:
+    """ue5m3_attention (ue5m3_attention_sinks with `sinks`: the first keys, up to 128, that stay visible behind the window): (o, lse) for q [batch, tokens, heads, head_dim] and k, v [batch, keys, kv_heads, head_dim], bfloat16.  Any
     strides with a contiguous last dimension (views of a fused projection); `window_left` = keys a query sees before its own
     position (-1: all), `k_lens` int32 [batch] = valid keys of each sequence, `scale` defaults to head_dim ** -0.5.  Query i stands at
     position i + keys - tokens of every sequence, whatever its k_lens (right-padded batches).  `out` may be q; any other overlap with
@@ -617,15 +624,18 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     lib = _load()
     need = lib.ue5m3_attention_workspace_bytes(shape)
     ws = q.new_empty(need, dtype=torch.uint8) if need else None
-    _call(lib.ue5m3_attention, "ue5m3_attention", q, shape, _heads(q, q.shape, q), _heads(k, k.shape, q), _heads(v, k.shape, q),
-          _heads(out, q.shape, q), lse.data_ptr(), _ptr(ws))
+    args = _heads(q, q.shape, q), _heads(k, k.shape, q), _heads(v, k.shape, q), _heads(out, q.shape, q), lse.data_ptr(), _ptr(ws)
+    if sinks:
+        _call(lib.ue5m3_attention_sinks, "ue5m3_attention_sinks", q, shape, sinks, *args)
+    else:
+        _call(lib.ue5m3_attention, "ue5m3_attention", q, shape, *args)
     return out, lse
 
 
 def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
                        causal: bool = False, window_left: int = -1, k_lens: Optional[torch.Tensor] = None,
-                       scale: Optional[float] = None, out: Optional[tuple] = None) -> tuple:
-    """ue5m3_attention_backward: (dq, dk, dv) from what `attention` returned (o, lse) and the gradient of o; the other arguments as
+                       scale: Optional[float] = None, out: Optional[tuple] = None, sinks: int = 0) -> tuple:
+    """ue5m3_attention_backward (ue5m3_attention_sinks_backward with `sinks`): (dq, dk, dv) from what `attention` returned (o, lse) and the gradient of o; the other arguments as
     in that call.  `out`: three tensors to write to (any strides with a contiguous last dimension, e.g. views of one fused
     gradient) that overlap neither one another nor dout, q, k, v."""
     shape = _attention_shape(q, k, causal, window_left, k_lens, scale)
@@ -634,9 +644,14 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
         raise ValueError("lse must be the contiguous float32 [batch, heads, tokens] tensor that attention returned")
     dq, dk, dv = (q.new_empty(qs), k.new_empty(ks), k.new_empty(ks)) if out is None else out
     lib = _load()
-    ws = q.new_empty(lib.ue5m3_attention_backward_workspace_bytes(shape), dtype=torch.uint8)
-    _call(lib.ue5m3_attention_backward, "ue5m3_attention_backward", q, shape, _heads(dout, qs, q), _heads(q, qs, q), _heads(k, ks, q),
-          _heads(v, ks, q), _heads(o, qs, q), lse.data_ptr(), _heads(dq, qs, q), _heads(dk, ks, q), _heads(dv, ks, q), ws.data_ptr())
+    need = lib.ue5m3_attention_sinks_backward_workspace_bytes(shape, sinks) if sinks else lib.ue5m3_attention_backward_workspace_bytes(shape)
+    ws = q.new_empty(need, dtype=torch.uint8)
+    args = _heads(dout, qs, q), _heads(q, qs, q), _heads(k, ks, q), _heads(v, ks, q), _heads(o, qs, q), lse.data_ptr(), _heads(dq, qs, q), \
+        _heads(dk, ks, q), _heads(dv, ks, q), ws.data_ptr()
+    if sinks:
+        _call(lib.ue5m3_attention_sinks_backward, "ue5m3_attention_sinks_backward", q, shape, sinks, *args)
+    else:
+        _call(lib.ue5m3_attention_backward, "ue5m3_attention_backward", q, shape, *args)
     return dq, dk, dv
 
 

@@ -521,11 +521,12 @@ size_t ue5m3_attention_workspace_bytes(const ue5m3_attention_shape* shape) {
     return (size_t)parts * (size_t)shape->batch * (size_t)shape->heads * (size_t)shape->q_len * (size_t)(shape->head_dim + 4) * sizeof(float);
 }
 
-int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, const ue5m3_heads* k, const ue5m3_heads* v,
-                    const ue5m3_heads* o, float* lse, void* workspace, void* stream) {
-    const ApiRange range_("ue5m3_attention");
+static int check_sinks(int64_t sinks) { return sinks < 0 ? UE5M3_ERR_INVALID_ARG : sinks > 128 ? UE5M3_ERR_UNSUPPORTED : UE5M3_OK; }
+
+static int attention_call(const ue5m3_attention_shape* shape, int64_t sinks, const ue5m3_heads* q, const ue5m3_heads* k, const ue5m3_heads* v,
+                          const ue5m3_heads* o, float* lse, void* workspace, void* stream) {
     int bad = check_attention_shape(shape);
-    if (bad != UE5M3_OK) return bad;
+    if (bad != UE5M3_OK || (bad = check_sinks(sinks)) != UE5M3_OK) return bad;
     const ue5m3_attention_shape& s = *shape;
     for (const ue5m3_heads* t : {q, o})
         if ((bad = check_heads(t, s.batch, s.q_len, s.heads)) != UE5M3_OK) return bad;
@@ -544,24 +545,37 @@ int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, co
     if (!aligned_to(lse, UE5M3_F32) || !aligned16(workspace)) return UE5M3_ERR_ALIGN;
     int sms = 0;
     if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
-    return launch_attention(s, *q, *k, *v, *o, lse, static_cast<float*>(workspace), sms, (cudaStream_t)stream);
+    return launch_attention(s, sinks, *q, *k, *v, *o, lse, static_cast<float*>(workspace), sms, (cudaStream_t)stream);
+}
+int ue5m3_attention(const ue5m3_attention_shape* shape, const ue5m3_heads* q, const ue5m3_heads* k, const ue5m3_heads* v,
+                    const ue5m3_heads* o, float* lse, void* workspace, void* stream) {
+    const ApiRange range_("ue5m3_attention");
+    return attention_call(shape, 0, q, k, v, o, lse, workspace, stream);
+}
+int ue5m3_attention_sinks(const ue5m3_attention_shape* shape, int64_t sinks, const ue5m3_heads* q, const ue5m3_heads* k, const ue5m3_heads* v,
+                          const ue5m3_heads* o, float* lse, void* workspace, void* stream) {
+    const ApiRange range_("ue5m3_attention_sinks");
+    return attention_call(shape, sinks, q, k, v, o, lse, workspace, stream);
 }
 
-size_t ue5m3_attention_backward_workspace_bytes(const ue5m3_attention_shape* shape) {
-    if (check_attention_shape(shape) != UE5M3_OK) return 0;
+size_t ue5m3_attention_sinks_backward_workspace_bytes(const ue5m3_attention_shape* shape, int64_t sinks) {
+    if (check_attention_shape(shape) != UE5M3_OK || check_sinks(sinks) != UE5M3_OK) return 0;
+    const int shares = attention_sink_parts(*shape, sinks);
     const int parts = attention_backward_splits(*shape);
     const size_t heads = (size_t)shape->batch * (size_t)shape->heads;
     // two numbers per query, padded to whole tiles; binary32 dq of every part
     return (heads * (size_t)attention_padded_q(shape->q_len) * 2 +
-            (parts > 1 ? (size_t)parts * heads * (size_t)shape->q_len * (size_t)shape->head_dim : 0)) * sizeof(float);
+            (parts > 1 ? (size_t)parts * heads * (size_t)shape->q_len * (size_t)shape->head_dim : 0) +
+            // binary32 dk and dv of every part of the first key tile
+            (shares > 1 ? (size_t)shares * (size_t)shape->batch * (size_t)shape->kv_heads * 2 * 128 * (size_t)shape->head_dim : 0)) * sizeof(float);
 }
+size_t ue5m3_attention_backward_workspace_bytes(const ue5m3_attention_shape* shape) { return ue5m3_attention_sinks_backward_workspace_bytes(shape, 0); }
 
-int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_heads* dout, const ue5m3_heads* q, const ue5m3_heads* k,
-                             const ue5m3_heads* v, const ue5m3_heads* o, const float* lse, const ue5m3_heads* dq, const ue5m3_heads* dk,
-                             const ue5m3_heads* dv, void* workspace, void* stream) {
-    const ApiRange range_("ue5m3_attention_backward");
+static int attention_backward_call(const ue5m3_attention_shape* shape, int64_t sinks, const ue5m3_heads* dout, const ue5m3_heads* q,
+                                   const ue5m3_heads* k, const ue5m3_heads* v, const ue5m3_heads* o, const float* lse, const ue5m3_heads* dq,
+                                   const ue5m3_heads* dk, const ue5m3_heads* dv, void* workspace, void* stream) {
     int bad = check_attention_shape(shape);
-    if (bad != UE5M3_OK) return bad;
+    if (bad != UE5M3_OK || (bad = check_sinks(sinks)) != UE5M3_OK) return bad;
     const ue5m3_attention_shape& s = *shape;
     for (const ue5m3_heads* t : {dout, q, o, dq})
         if ((bad = check_heads(t, s.batch, s.q_len, s.heads)) != UE5M3_OK) return bad;
@@ -589,7 +603,19 @@ int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_hea
     if (!aligned_to(lse, UE5M3_F32) || !aligned16(workspace)) return UE5M3_ERR_ALIGN;
     int sms = 0;
     if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
-    return launch_attention_backward(s, *dout, *q, *k, *v, *o, lse, *dq, *dk, *dv, static_cast<float*>(workspace), (cudaStream_t)stream);
+    return launch_attention_backward(s, sinks, *dout, *q, *k, *v, *o, lse, *dq, *dk, *dv, static_cast<float*>(workspace), (cudaStream_t)stream);
+}
+int ue5m3_attention_backward(const ue5m3_attention_shape* shape, const ue5m3_heads* dout, const ue5m3_heads* q, const ue5m3_heads* k,
+                             const ue5m3_heads* v, const ue5m3_heads* o, const float* lse, const ue5m3_heads* dq, const ue5m3_heads* dk,
+                             const ue5m3_heads* dv, void* workspace, void* stream) {
+    const ApiRange range_("ue5m3_attention_backward");
+    return attention_backward_call(shape, 0, dout, q, k, v, o, lse, dq, dk, dv, workspace, stream);
+}
+int ue5m3_attention_sinks_backward(const ue5m3_attention_shape* shape, int64_t sinks, const ue5m3_heads* dout, const ue5m3_heads* q,
+                                   const ue5m3_heads* k, const ue5m3_heads* v, const ue5m3_heads* o, const float* lse, const ue5m3_heads* dq,
+                                   const ue5m3_heads* dk, const ue5m3_heads* dv, void* workspace, void* stream) {
+    const ApiRange range_("ue5m3_attention_sinks_backward");
+    return attention_backward_call(shape, sinks, dout, q, k, v, o, lse, dq, dk, dv, workspace, stream);
 }
 
 // ----------------------------------------------------------------------------- rotary positions, norms of queries and keys
@@ -793,11 +819,11 @@ int ue5m3_block_stall_selftest(int which, void* buffer, size_t bytes, int64_t wa
     float* lse = static_cast<float*>(take((size_t)(s.heads * s.q_len) * sizeof(float)));
     if (which < 2) {
         float* ws = static_cast<float*>(take(ue5m3_attention_workspace_bytes(&s)));
-        return launch_attention(s, q, k, v, o, lse, ws, sms, (cudaStream_t)stream, stall);
+        return launch_attention(s, 0, q, k, v, o, lse, ws, sms, (cudaStream_t)stream, stall);
     }
     const ue5m3_heads dout = tensor(s.q_len, s.heads), dq = tensor(s.q_len, s.heads), dk = tensor(s.k_len, 1), dv = tensor(s.k_len, 1);
     float* ws = static_cast<float*>(take(ue5m3_attention_backward_workspace_bytes(&s)));
-    return launch_attention_backward(s, dout, q, k, v, o, lse, dq, dk, dv, ws, (cudaStream_t)stream, stall);
+    return launch_attention_backward(s, 0, dout, q, k, v, o, lse, dq, dk, dv, ws, (cudaStream_t)stream, stall);
 }
 
 int ue5m3_last_device_status(void) {

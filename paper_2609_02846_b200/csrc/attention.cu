@@ -28,6 +28,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 #include "../../include/ue5m3.h"
 #include "attention.cuh"
 #include "block_ops.h"
@@ -70,10 +71,14 @@ struct Item {
     int b, h, h_end, kvh, part, q0, keys;                 // h_end: heads of the group of h end there (PACK)
     int lo[2], hi[2];                                     // key tiles of the two query tiles
     int first, last;                                      // ... and of both together
+    int skip;                                             // SINKS: key tiles left out between tile 0 and the windows'; lo .. last count the others
     __device__ __forceinline__ bool on(int t) const { return hi[t] > lo[t]; }
+    template <bool SINKS> __device__ __forceinline__ int key_tile(int j) const { return SINKS && j > 0 ? j + skip : j; }
 };
 // Heads fastest (heads that share keys run side by side), long query tiles first.
-template <bool PARTS, bool PACK>
+// SINKS: key tile 0 stands in front of the windows' tiles of both query tiles, of which the second then begins with the first's (one
+// tile of hidden scores at most).
+template <bool PARTS, bool PACK, bool SINKS>
 __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int q_tiles) {
     Item w;
     w.part = PARTS ? index % p.parts : 0;
@@ -104,6 +109,21 @@ __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int
             w.hi[t] = max(min(w.hi[t], (int)((int64_t)n * (w.part + 1) / p.parts)), w.lo[t]);
         }
     }
+    w.skip = 0;
+    if (SINKS && w.part == 0) {                           // (the first part has tile 0)
+        int base = 0x7FFFFFFF;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            if (w.on(t)) base = min(base, w.lo[t]);
+        w.skip = base == 0x7FFFFFFF || base == 0 ? 0 : base - 1;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int r0 = PACK ? 0 : w.q0 + t * BQ, r1 = min(r0 + BQ, p.q_len) - 1;
+            const bool sees = (PACK ? w.h + t * p.pack < w.h_end : r0 < p.q_len) && p.key_hi(r1, w.keys) > 0;
+            w.hi[t] = sees ? (w.on(t) ? w.hi[t] - w.skip : 1) : 0;
+            w.lo[t] = 0;
+        }
+    }
     w.first = w.on(0) ? (w.on(1) ? min(w.lo[0], w.lo[1]) : w.lo[0]) : w.lo[1];
     w.last = w.on(0) ? (w.on(1) ? max(w.hi[0], w.hi[1]) : w.hi[0]) : (w.on(1) ? w.hi[1] : w.first);
     return w;
@@ -113,7 +133,7 @@ __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int
 // by itself: the next item's Q and keys are copied and its first S computed while the softmax warps still write this one's output.
 // 233 us at 2 x 4096 tokens against 240 with a CTA per item.
 // PARTS: binary32 results for attention_join_kernel.
-template <int DP, bool PARTS, bool PACK>
+template <int DP, bool PARTS, bool PACK, bool SINKS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                  const __grid_constant__ CUtensorMap map_v, const AttentionParams p, const OutputParams out, const int q_tiles, const int items) {
@@ -169,13 +189,13 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             int n = 0, q_uses[2] = {0, 0};
             bool go = !p.stall;
             for (int turn = 0, index; go && (index = item_at(turn)) < items; ++turn) {
-                const Item w = item_of<PARTS, PACK>(p, index, q_tiles);
+                const Item w = item_of<PARTS, PACK, SINKS>(p, index, q_tiles);
                 const int pairs = w.last > w.first ? w.last - w.first + 1 : 0;
                 auto load = [&](int tile_n, const CUtensorMap* m, uint32_t bar, int tile) {
                     mbar_expect_tx(bar, T::TILE);
 #pragma unroll
                     for (int c = 0; c < T::PANELS; ++c)
-                        tma_load_4d(ring + (tile_n % T::RING) * T::TILE + c * T::PANEL, m, bar, c * 64, tile * BK, w.kvh, w.b);
+                        tma_load_4d(ring + (tile_n % T::RING) * T::TILE + c * T::PANEL, m, bar, c * 64, w.key_tile<SINKS>(tile) * BK, w.kvh, w.b);
                 };
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -226,8 +246,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             wait_all(kv_full + 8 * slot, phase);
             if (++slot == T::PAIRS) { slot = 0; phase ^= 1; }
             // values behind the sequence's end and in front of every window may hold anything: they become zeros
-            const int from = p.first_key - j * BK, valid = w.keys - j * BK;
-            if (j >= w.first && ((p.k_lens && valid < BK) || from > 0)) keep_rows<DP>(smem_gen + (2 + v_tile) * T::TILE, from, valid, lane);
+            const int at = w.key_tile<SINKS>(j) * BK, from = p.first_key - at, valid = w.keys - at;
+            if (j >= w.first && ((p.k_lens && valid < BK) || from > 0)) {
+                if constexpr (SINKS) keep_rows_sinks<DP>(smem_gen + (2 + v_tile) * T::TILE, from, valid, at == 0 ? p.sinks : 0, lane);
+                else keep_rows<DP>(smem_gen + (2 + v_tile) * T::TILE, from, valid, lane);
+            }
             const uint32_t v = v_tile;
             v_tile = v + 2 >= T::RING ? v + 2 - T::RING : v + 2;
             return v;
@@ -265,7 +288,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (++done == T::PAIRS) done = 0;
         };
         for (int turn = 0, index; ok && (index = item_at(turn)) < items; ++turn) {
-            const Item w = item_of<PARTS, PACK>(p, index, q_tiles);
+            const Item w = item_of<PARTS, PACK, SINKS>(p, index, q_tiles);
             if (w.last <= w.first) continue;
             const uint32_t k0 = k_tile(next_pair(w, w.first - 1));
 #pragma unroll
@@ -317,7 +340,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         uint32_t n = 0, uses = 0;                          // S tiles and items of this query tile so far
         bool ok = true;
         for (int turn = 0, index; ok && (index = item_at(turn)) < items; ++turn) {
-        const Item w = item_of<PARTS, PACK>(p, index, q_tiles);
+        const Item w = item_of<PARTS, PACK, SINKS>(p, index, q_tiles);
         const int r0 = PACK ? 0 : w.q0 + t * BQ, r_last = PACK ? p.q_len - 1 : r0 + BQ - 1;
         const int h = PACK ? w.h + t * p.pack + r_head : w.h, row = r0 + r_query;
         const bool exists = PACK ? r_head < p.pack && h < w.h_end : row < p.q_len;
@@ -360,9 +383,15 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, s + c * 32);
             tmem_ld_wait();
-            const bool masked = j < plain_lo || j >= plain_hi;
-            const int from = key_lo - j * BK, to = key_hi - j * BK;    // columns of this tile that the row sees
-            if (masked) hide_scores<128>(s, from, to, p.left >= 0);
+            const int tile = w.key_tile<SINKS>(j);
+            const bool masked = tile < plain_lo || tile >= plain_hi;
+            const int from = key_lo - tile * BK, to = key_hi - tile * BK;      // columns of this tile that the row sees
+            auto hide = [&](auto cols, uint32_t* x) {
+                constexpr int N = decltype(cols)::value;
+                if (SINKS && tile == 0) hide_scores_sinks<N>(x, from, to, p.sinks);
+                else hide_scores<N>(x, from, to, p.left >= 0);
+            };
+            if (masked) hide(std::integral_constant<int, 128>(), s);
             uint32_t pk[32];
             float base = m == -INFINITY ? 0.0f : m;
             // The first half's exponentials are taken against the maximum so far, while this tile's is being found: it raises the
@@ -387,7 +416,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 tmem_ld32(ts, again);
                 tmem_ld32(ts + 32, again + 32);
                 tmem_ld_wait();
-                if (masked) hide_scores<64>(again, from, to, p.left >= 0);
+                if (masked) hide(std::integral_constant<int, 64>(), again);
                 exp_scores<32>(again, pk, sum, c2, f2_pack(-base, -base));
             }
             publish(0, pk);
@@ -523,16 +552,21 @@ int64_t query_pairs(const ue5m3_attention_shape& s) {
     return pack ? s.batch * s.kv_heads * ((group + 2 * pack - 1) / (2 * pack)) : (s.q_len + 2 * BQ - 1) / (2 * BQ) * s.batch * s.heads;
 }
 
-template <int DP, bool PARTS, bool PACK>
+template <int DP, bool PARTS, bool PACK, bool SINKS>
 int run(const ue5m3_attention_shape& s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
         const OutputParams& o, int num_sms, cudaStream_t st) {
     using T = Tiles<DP>;
     const int64_t q_tiles = (s.q_len + 2 * BQ - 1) / (2 * BQ), items = query_pairs(s) * p.parts;
     if (items > 0x7FFFFFFF - 2 * num_sms) return UE5M3_ERR_UNSUPPORTED;
     static std::atomic<int> granted[64];
-    if (allow_smem(attention_kernel<DP, PARTS, PACK>, T::SMEM, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-    attention_kernel<DP, PARTS, PACK><<<(unsigned)(items < num_sms ? items : num_sms), kThreads, T::SMEM, st>>>(q, k, v, p, o, (int)q_tiles, (int)items);
+    if (allow_smem(attention_kernel<DP, PARTS, PACK, SINKS>, T::SMEM, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
+    attention_kernel<DP, PARTS, PACK, SINKS><<<(unsigned)(items < num_sms ? items : num_sms), kThreads, T::SMEM, st>>>(q, k, v, p, o, (int)q_tiles, (int)items);
     return cudaGetLastError() == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
+}
+template <int DP, bool PARTS, bool PACK>
+int run(const ue5m3_attention_shape& s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
+        const OutputParams& o, int num_sms, cudaStream_t st) {
+    return p.sinks > 0 ? run<DP, PARTS, PACK, true>(s, q, k, v, p, o, num_sms, st) : run<DP, PARTS, PACK, false>(s, q, k, v, p, o, num_sms, st);
 }
 template <bool PARTS>
 int run(const ue5m3_attention_shape& s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const AttentionParams& p,
@@ -557,7 +591,7 @@ int attention_splits(const ue5m3_attention_shape& s) {
     return n > 1 && (double)tiles / n + 2 + n * part < 0.75 * (double)tiles ? (int)n : 1;
 }
 
-int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
+int launch_attention(const ue5m3_attention_shape& s, int64_t sinks, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
                      const ue5m3_heads& o, float* lse, float* workspace, int num_sms, cudaStream_t st, const StallTest& stall) {
     if (s.batch == 0 || s.q_len == 0) return UE5M3_OK;
     CUtensorMap mq, mk, mv;
@@ -566,7 +600,7 @@ int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const
     if (s.k_len == 0) mk = mv = mq;                        // no key tile is ever read
     else if (!make_heads_map(&mk, k, s.batch, s.k_len, s.kv_heads, s.head_dim, BK) || !make_heads_map(&mv, v, s.batch, s.k_len, s.kv_heads, s.head_dim, BK))
         return UE5M3_ERR_CUDA;
-    AttentionParams p = attention_params(s);
+    AttentionParams p = attention_params(s, sinks);
     p.lse = lse;
     p.parts = attention_splits(s);
     p.pack = pack;

@@ -115,6 +115,12 @@ __device__ __forceinline__ void hide_scores(uint32_t* s, int from, int to, bool 
         for (int c = 0; c < N; ++c) s[c] = c < to ? s[c] : 0xFF800000u;
     }
 }
+// The same in the key tile that holds the first keys of all: columns below `sinks` stay too.
+template <int N>
+__device__ __forceinline__ void hide_scores_sinks(uint32_t* s, int from, int to, int sinks) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) s[c] = (c >= from || c < sinks) && c < to ? s[c] : 0xFF800000u;
+}
 __device__ __forceinline__ f32x2 ex2_pair(f32x2 x) {
     float a, b;
     f2_unpack(x, a, b);
@@ -162,6 +168,16 @@ __device__ __forceinline__ void hide_pairs(f32x2* p, int from, int to, bool lowe
             f2_unpack(p[i], a, b);
             p[i] = f2_pack(2 * i >= from ? a : 0.0f, 2 * i + 1 >= from ? b : 0.0f);
         }
+    }
+}
+// The same in the key tile that holds the first keys of all: columns below `sinks` stay too.
+template <int N>
+__device__ __forceinline__ void hide_pairs_sinks(f32x2* p, int from, int to, int sinks) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float a, b;
+        f2_unpack(p[i], a, b);
+        p[i] = f2_pack((2 * i >= from || 2 * i < sinks) && 2 * i < to ? a : 0.0f, (2 * i + 1 >= from || 2 * i + 1 < sinks) && 2 * i + 1 < to ? b : 0.0f);
     }
 }
 // x where p is not zero (0 * NaN would be NaN where a pair does not exist)
@@ -256,6 +272,17 @@ __device__ __forceinline__ void keep_rows(uint8_t* tile, int from, int to, int l
     __syncwarp();
 }
 
+// The same with rows below `sinks` kept too.
+template <int DP>
+__device__ __forceinline__ void keep_rows_sinks(uint8_t* tile, int from, int to, int sinks, int lane) {
+    for (int i = lane; i < 128 * (DP / 8); i += 32) {
+        const int r = i / (DP / 8), c = i % (DP / 8);
+        if ((r < from && r >= sinks) || r >= to) *reinterpret_cast<uint4*>(tile + (c / 8) * (128 * 128) + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
+    }
+    fence_proxy_async();
+    __syncwarp();
+}
+
 // ----------------------------------------------------------------------------- which pairs exist
 struct AttentionParams {
     int q_len, k_len, heads, group;      // group = heads per key/value head
@@ -274,6 +301,9 @@ struct AttentionParams {
     float* part_o; float* part_lse;      // parts > 1: o (backward: dq) [parts][batch][heads][q_len][dim]; forward: lse [..][q_len]
     long long wait_limit;
     int stall;                           // self-test: no copy is issued, so every wait for one runs out
+    int sinks;                           // first keys that a window does not hide (0 without a window), at most one key tile
+    int sink_parts;                      // backward: CTAs that share the queries of key tile 0 ...
+    float* part_kv;                      // ... and then leave binary32 sums here: [sink_parts][batch][kv_heads][dv, dk][128][dim]
 
     __device__ __forceinline__ int keys_of(int b) const {
         if (!k_lens) return k_len;
@@ -288,6 +318,9 @@ struct AttentionParams {
     // queries [lo, hi) that see key j, given that j < keys
     __host__ __device__ __forceinline__ int query_lo(int j) const { return causal ? max(0, j - (k_len - q_len)) : 0; }
     __host__ __device__ __forceinline__ int query_hi(int j) const { return left >= 0 ? min(q_len, j - (k_len - q_len) + left + 1) : q_len; }
+    // With sinks (SINKS): every query from query_lo on sees the first keys, and with them every query sees some key if there are any.
+    template <bool SINKS> __host__ __device__ __forceinline__ int queries_end_of(int keys) const { return SINKS ? q_len : queries_end(keys); }
+    template <bool SINKS> __host__ __device__ __forceinline__ int query_hi_of(int j) const { return SINKS && j < sinks ? q_len : query_hi(j); }
 };
 
 // ----------------------------------------------------------------------------- host side
@@ -306,7 +339,7 @@ inline bool make_heads_map(CUtensorMap* m, const ue5m3_heads& t, int64_t batch, 
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-inline AttentionParams attention_params(const ue5m3_attention_shape& s) {
+inline AttentionParams attention_params(const ue5m3_attention_shape& s, int64_t sinks) {
     AttentionParams p{};
     p.q_len = (int)s.q_len; p.k_len = (int)s.k_len; p.heads = (int)s.heads; p.group = (int)(s.heads / s.kv_heads);
     p.kv_heads = (int)s.kv_heads; p.causal = s.causal; p.batch = (int)s.batch; p.k_lens = s.k_lens;
@@ -321,6 +354,8 @@ inline AttentionParams attention_params(const ue5m3_attention_shape& s) {
     p.first_key = p.left >= 0 ? (int)std::max<int64_t>(0, s.k_len - s.q_len - p.left) : 0;
     p.dim = (int)s.head_dim;
     p.parts = 1;
+    p.sinks = p.left >= 0 ? (int)sinks : 0;
+    p.sink_parts = 1;
     return p;
 }
 

@@ -155,7 +155,9 @@ template <int DP> struct KeySmem {
 
 // IDLE: queries that see no key may exist.  Looking for their tiles takes the issuing warp 1 to 2 % of the kernel's time (2501 tokens,
 // window 511: 66.9 us against 65.8 of the whole backward pass), so calls without such queries do not.
-template <int DP, bool IDLE>
+// SINKS: key tile 0 holds keys that all queries see, many times the work of another tile, so its queries are shared out among the first
+// `sink_parts` CTAs of a head, whose binary32 sums attention_sinks_kernel adds.
+template <int DP, bool IDLE, bool SINKS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
                       const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -175,14 +177,21 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 
     // key tiles of one head side by side, those that most queries see (causal: the first) at the front
     const int bh_count = p.batch * kv_heads;
-    const int bh = blockIdx.x % bh_count, j0 = (int)(blockIdx.x / bh_count) * B128;
+    const int bh = blockIdx.x % bh_count, turn = (int)(blockIdx.x / bh_count);
+    const int j0 = SINKS ? max(turn - p.sink_parts + 1, 0) * B128 : turn * B128;
+    const bool shared = SINKS && p.sink_parts > 1 && j0 == 0;         // this CTA has a part of tile 0
     const int b = bh / kv_heads, kvh = bh - b * kv_heads;
     const int keys = p.keys_of(b);
     const int j1 = min(j0 + B128, keys) - 1;                          // last key of the tile
     int lo = 0, hi = 0;                                               // query tiles
     if (j0 < keys) {
-        const int a = p.query_lo(j0), z = p.query_hi(j1);
+        const int a = p.query_lo(j0), z = SINKS ? max(p.query_hi_of<SINKS>(j0), p.query_hi(j1)) : p.query_hi(j1);
         if (z > a) { lo = a / B128; hi = (z + B128 - 1) / B128; }
+    }
+    if (shared) {
+        const int first = lo, n = hi - lo;
+        lo = first + (int)((int64_t)n * turn / p.sink_parts);
+        hi = first + (int)((int64_t)n * (turn + 1) / p.sink_parts);
     }
     const int per_head = hi - lo, steps = per_head * p.group;
 
@@ -258,7 +267,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         // S(0) dP(0) | dV(0) S(1) dK(0) dP(1) | dV(1) S(2) dK(1) dP(2) | ...   S is in order behind dV, which reads P out of its columns
         const bool elected = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-        const int n = uniform(steps), q_end = uniform(p.queries_end(keys)), i_first = uniform(lo) * B128, i_end = uniform(hi) * B128;
+        const int n = uniform(steps), q_end = uniform(p.queries_end_of<SINKS>(keys)), i_first = uniform(lo) * B128, i_end = uniform(hi) * B128;
         bool ok = true;
         auto pass = [&](uint32_t bar, uint32_t parity) {   // the phase is complete, or `ok` is false in the whole warp
             if (!__all_sync(0xFFFFFFFFu, try_wait_cta(bar, parity))) ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
@@ -327,10 +336,10 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         const int key = j0 + q * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
         const uint32_t ts = lane_base + COL_S + g * 64, td = lane_base + COL_DP + g * 64;
-        const int q_lo = key < keys ? p.query_lo(key) : 0, q_hi = key < keys ? p.query_hi(key) : 0;
+        const int q_lo = key < keys ? p.query_lo(key) : 0, q_hi = key < keys ? p.query_hi_of<SINKS>(key) : 0;
         // query tiles [plain_lo, plain_hi) see every key of this tile
         const int plain_lo = j0 + B128 <= keys ? (p.query_lo(j0 + B128 - 1) + B128 - 1) / B128 : hi;
-        const int plain_hi = p.left >= 0 ? max(p.query_hi(j0), 0) / B128 : p.q_len / B128 + 1;
+        const int plain_hi = p.left >= 0 ? max(p.query_hi_of<SINKS>(SINKS && j0 == 0 ? min(p.sinks, B128 - 1) : j0), 0) / B128 : p.q_len / B128 + 1;
         const bool upper = p.left >= 0 || j0 + B128 > keys;
         // Some keys of the tile take no part (behind the sequence's end, in front of every window): what they hold may be NaN, and so then
         // is their dP.
@@ -399,6 +408,24 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             ok = warp_wait(acc_full, 0, abort_flag, p.wait_limit);
             tc_fence_after();
         }
+        if (shared) {
+            if (ok) {                                                 // the accumulators as they are, a thread its row
+                float* dst = p.part_kv + ((((int64_t)turn * bh_count + bh) * 2 + g) * B128 + q * 32 + lane) * p.dim;
+#pragma unroll 1
+                for (int c = 0; c < DP; c += 32) {
+                    uint32_t o[32];
+#pragma unroll
+                    for (int v = 0; v < 32; ++v) o[v] = 0u;
+                    if (steps > 0) {
+                        tmem_ld32(lane_base + (g == 0 ? COL_ACC0 : COL_ACC1) + c, o);
+                        tmem_ld_wait();
+                    }
+#pragma unroll
+                    for (int v = 0; v < 32; v += 4)
+                        if (c + v < p.dim) *reinterpret_cast<uint4*>(dst + c + v) = make_uint4(o[v], o[v + 1], o[v + 2], o[v + 3]);
+                }
+            }
+        } else
         // group 0 writes dV over V's tile, group 1 dK over K's: no MMA reads them any more (or they were never loaded)
         if (ok && j0 + q * 32 < p.k_len) {
             if (g == 0) store_accumulator<DP>(lane_base + COL_ACC0, smem_gen, smem, T::TILE, q, lane, &map_dv, 1.0f, steps == 0, j0 + q * 32, kvh, b);
@@ -422,8 +449,9 @@ template <int DP> struct QuerySmem {
 };
 constexpr uint32_t COL_Q = 384, COL_DO = 448;                         // in place of the second accumulator
 
-// PARTS: a CTA takes a share of the keys and leaves a binary32 sum for attention_sum_kernel.
-template <int DP, bool PARTS>
+// PARTS: a CTA takes a share of the keys and leaves a binary32 sum for attention_sum_kernel.  SINKS: key tile 0 comes in front of the
+// window's where that does not begin with it.
+template <int DP, bool PARTS, bool SINKS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
                          const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -454,8 +482,11 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             lo = max(lo, (int)((int64_t)n * part / p.parts));
             hi = max(min(hi, (int)((int64_t)n * (part + 1) / p.parts)), lo);
         }
+        if (SINKS && part == 0 && z > 0 && hi == lo) { lo = 0; hi = 1; }       // no key in any window: tile 0 alone
     }
-    const int steps = hi - lo;
+    const int front = SINKS && part == 0 && lo > 0 && hi > lo;
+    const int steps = hi - lo + front;
+    auto key_tile = [&](int it) { return SINKS ? (front && it == 0 ? 0 : lo + it - front) : lo + it; };
 
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -487,7 +518,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 if (!wait(empty + 8 * s, ((it / M::STAGES) & 1) ^ 1, abort_flag, p.wait_limit)) break;
                 mbar_expect_tx(full + 8 * s, T::TILE);
                 if (it < 2) tile(smem + s * T::TILE, it ? &map_do : &map_q, full + 8 * s, i0, h);
-                else tile(smem + s * T::TILE, (it & 1) ? &map_v : &map_k, full + 8 * s, (lo + (it >> 1) - 1) * B128, kvh);
+                else tile(smem + s * T::TILE, (it & 1) ? &map_v : &map_k, full + 8 * s, key_tile((it >> 1) - 1) * B128, kvh);
             }
             for (int back = 0; back < M::STAGES && back < it; ++back) {
                 const int j = it - 1 - back;
@@ -500,7 +531,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         // order behind the product that reads dS out of its columns
         const bool elected = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-        const int n = uniform(steps), n_keys = uniform(keys), first = uniform(lo);
+        const int n = uniform(steps), n_keys = uniform(keys), first = uniform(lo), lead = SINKS ? uniform(front) : 0;
         bool ok = true;
         auto pass = [&](uint32_t bar, uint32_t parity) {   // the phase is complete, or `ok` is false in the whole warp
             if (!__all_sync(0xFFFFFFFFu, try_wait_cta(bar, parity))) ok = ok && __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, p.wait_limit));
@@ -517,8 +548,11 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         };
         auto clean_k = [&](int it, uint32_t s) {
             // keys behind the sequence's end and in front of every window may hold anything (dS is zero there): they become zeros
-            const int from = p.first_key - (first + it) * B128, valid = n_keys - (first + it) * B128;
-            if ((p.k_lens && valid < B128) || from > 0) keep_rows<DP>(smem_gen + s * T::TILE, from, valid, lane);
+            const int at = (SINKS && lead && it == 0 ? 0 : first + it - lead) * B128, from = p.first_key - at, valid = n_keys - at;
+            if ((p.k_lens && valid < B128) || from > 0) {
+                if constexpr (SINKS) keep_rows_sinks<DP>(smem_gen + s * T::TILE, from, valid, at == 0 ? p.sinks : 0, lane);
+                else keep_rows<DP>(smem_gen + s * T::TILE, from, valid, lane);
+            }
         };
         uint32_t k0 = 0, k1 = 0, k2 = 0;                   // slots of K(it), K(it + 1), K(it + 2)
         auto issue_s = [&](int it) {
@@ -565,7 +599,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         const int k_lo = p.key_lo(row), k_hi = p.key_hi(row, keys);
         const int plain_lo = p.left >= 0 ? (p.key_lo(i0 + B128 - 1) + B128 - 1) / B128 : 0;
         const int plain_hi = max(p.key_hi(i0, keys), 0) / B128;
-        const bool idle_queries = i0 < p.first_query || i1 >= p.queries_end(keys);
+        const bool idle_queries = i0 < p.first_query || i1 >= p.queries_end_of<SINKS>(keys);
         const int64_t at = ((int64_t)b * p.heads + h) * p.q_pad + row;
         const float nl = load_device(p.lse2 + at), nd = load_device(p.delta + at);         // visible: see launch_dependents in the keys kernel
         const f32x2 c2 = f2_pack(p.scale_log2, p.scale_log2), nl2 = f2_pack(nl, nl), nd2 = f2_pack(nd, nd);
@@ -589,7 +623,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             }
         }
         for (int it = 0; ok && it < steps; ++it) {
-            const int kt = lo + it;
+            const int kt = key_tile(it);
             const bool plain = kt >= plain_lo && kt < plain_hi;
             const int base = kt * B128 + g * 64 - k_lo, width = k_hi - k_lo;
             const uint32_t ts = lane_base + COL_S + g * 64, td = lane_base + COL_DP + g * 64;
@@ -605,7 +639,10 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             f32x2 pr[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) pr[i] = ex2_pair(f2_fma(pair_of(s + 2 * i), c2, nl2));
-            if (!plain) hide_pairs<32>(pr, -base, width - base, p.left >= 0, true);
+            if (!plain) {
+                if (SINKS && kt == 0) hide_pairs_sinks<32>(pr, -base, width - base, p.sinks - g * 64);
+                else hide_pairs<32>(pr, -base, width - base, p.left >= 0, true);
+            }
             // values, and dO of queries, that take no part may be NaN, and so then is dP
             const bool idle = (p.k_lens && (kt + 1) * B128 > keys) || kt * B128 < p.first_key || idle_queries;
             if (!(ok = warp_wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
@@ -678,6 +715,27 @@ __global__ void __launch_bounds__(256) attention_sum_kernel(const AttentionParam
         make_uint2(pack_bf16x2(s.x * p.scale, s.y * p.scale), pack_bf16x2(s.z * p.scale, s.w * p.scale));
 }
 
+// dk and dv of key tile 0 from the parts its queries were shared out into, added in order: four values per thread.
+struct SinkOutputs { __nv_bfloat16* out[2]; int64_t stride[2][3]; };       // dv, dk: batch, token, head
+__global__ void __launch_bounds__(256) attention_sinks_kernel(const AttentionParams p, const SinkOutputs o) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int per_row = p.dim / 4;
+    const int64_t all = (int64_t)p.batch * p.kv_heads * 2 * B128 * per_row, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= all) return;
+    const int64_t row = at / per_row;
+    const int c = (int)(at - row * per_row) * 4, key = (int)(row % B128), which = (int)(row / B128 % 2);
+    if (key >= p.k_len) return;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int k = 0; k < p.sink_parts; ++k) {
+        const float4 v = reinterpret_cast<const float4*>(p.part_kv)[k * all + at];
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const float f = which ? p.scale : 1.0f;
+    const int64_t bh = row / (2 * B128), b = bh / p.kv_heads, h = bh - b * p.kv_heads;
+    *reinterpret_cast<uint2*>(o.out[which] + b * o.stride[which][0] + key * o.stride[which][1] + h * o.stride[which][2] + c) =
+        make_uint2(pack_bf16x2(s.x * f, s.y * f), pack_bf16x2(s.z * f, s.w * f));
+}
+
 struct Maps { CUtensorMap q, dout, k, v, dq, dk, dv; };
 
 // A launch that may begin before the one in front of it has ended (`early`): the kernel says itself what it waits for.
@@ -697,37 +755,44 @@ int launch(void (*kernel)(Args...), int64_t grid, int threads, int smem, bool ea
     return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
-template <int DP, bool PARTS>
+template <int DP, bool PARTS, bool SINKS>
 int run_queries(const Maps& m, const AttentionParams& p, int64_t grid, int q_tiles, bool early, cudaStream_t st) {
     static std::atomic<int> granted[64];
-    if (allow_smem(attention_queries_kernel<DP, PARTS>, QuerySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-    return launch(attention_queries_kernel<DP, PARTS>, grid, kThreads, QuerySmem<DP>::SIZE, early, st, m.q, m.dout, m.k, m.v, m.dq, p, q_tiles);
+    if (allow_smem(attention_queries_kernel<DP, PARTS, SINKS>, QuerySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
+    return launch(attention_queries_kernel<DP, PARTS, SINKS>, grid, kThreads, QuerySmem<DP>::SIZE, early, st, m.q, m.dout, m.k, m.v, m.dq, p, q_tiles);
 }
 
-template <int DP, bool IDLE>
+template <int DP, bool IDLE, bool SINKS>
 int run_keys(const Maps& m, const AttentionParams& p, int64_t grid, int kv_heads, bool early, cudaStream_t st) {
     static std::atomic<int> granted[64];
-    if (allow_smem(attention_keys_kernel<DP, IDLE>, KeySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
-    return launch(attention_keys_kernel<DP, IDLE>, grid, kThreads, KeySmem<DP>::SIZE, early, st, m.q, m.dout, m.k, m.v, m.dk, m.dv, p, kv_heads);
+    if (allow_smem(attention_keys_kernel<DP, IDLE, SINKS>, KeySmem<DP>::SIZE, granted) != cudaSuccess) return UE5M3_ERR_CUDA;
+    return launch(attention_keys_kernel<DP, IDLE, SINKS>, grid, kThreads, KeySmem<DP>::SIZE, early, st, m.q, m.dout, m.k, m.v, m.dk, m.dv, p, kv_heads);
 }
 
-template <int DP>
-int run(const ue5m3_attention_shape& s, const ue5m3_heads& dq, const Maps& m, const AttentionParams& p, cudaStream_t st) {
+template <int DP, bool SINKS>
+int run(const ue5m3_attention_shape& s, const ue5m3_heads& dq, const ue5m3_heads& dk, const ue5m3_heads& dv, const Maps& m, const AttentionParams& p,
+        cudaStream_t st) {
     const int64_t k_tiles = (s.k_len + 127) / 128, q_tiles = (s.q_len + 127) / 128;
-    const int64_t ck = k_tiles * s.batch * s.kv_heads, cq = q_tiles * s.batch * s.heads * p.parts;
+    const int64_t ck = k_tiles > 0 ? (k_tiles + p.sink_parts - 1) * s.batch * s.kv_heads : 0, cq = q_tiles * s.batch * s.heads * p.parts;
     if (ck > 0) {
         // queries in front of every key, or with a window that begins behind the end of their sequence
-        const bool idle = p.first_query > 0 || (p.left >= 0 && p.k_lens);
-        const int r = idle ? run_keys<DP, true>(m, p, ck, (int)s.kv_heads, cq > 0, st) : run_keys<DP, false>(m, p, ck, (int)s.kv_heads, cq > 0, st);
+        const bool idle = p.first_query > 0 || (!SINKS && p.left >= 0 && p.k_lens);
+        const int r = idle ? run_keys<DP, true, SINKS>(m, p, ck, (int)s.kv_heads, cq > 0, st) : run_keys<DP, false, SINKS>(m, p, ck, (int)s.kv_heads, cq > 0, st);
         if (r != UE5M3_OK) return r;
     }
     if (cq == 0) return UE5M3_OK;
-    if (p.parts == 1) return run_queries<DP, false>(m, p, cq, (int)q_tiles, ck > 0, st);
-    const int r = run_queries<DP, true>(m, p, cq, (int)q_tiles, ck > 0, st);
+    const int r = p.parts == 1 ? run_queries<DP, false, SINKS>(m, p, cq, (int)q_tiles, ck > 0, st) : run_queries<DP, true, SINKS>(m, p, cq, (int)q_tiles, ck > 0, st);
     if (r != UE5M3_OK) return r;
-    const int64_t rows = s.batch * s.heads * s.q_len;
-    return launch(attention_sum_kernel, (rows * (s.head_dim / 4) + 255) / 256, 256, 0, true, st, p, static_cast<__nv_bfloat16*>(dq.data),
-                  dq.batch_stride, dq.token_stride, dq.head_stride);
+    if (p.parts > 1) {
+        const int64_t rows = s.batch * s.heads * s.q_len;
+        const int e = launch(attention_sum_kernel, (rows * (s.head_dim / 4) + 255) / 256, 256, 0, true, st, p, static_cast<__nv_bfloat16*>(dq.data),
+                             dq.batch_stride, dq.token_stride, dq.head_stride);
+        if (e != UE5M3_OK) return e;
+    }
+    if (p.sink_parts == 1) return UE5M3_OK;
+    const SinkOutputs o{{static_cast<__nv_bfloat16*>(dv.data), static_cast<__nv_bfloat16*>(dk.data)},
+                        {{dv.batch_stride, dv.token_stride, dv.head_stride}, {dk.batch_stride, dk.token_stride, dk.head_stride}}};
+    return launch(attention_sinks_kernel, (s.batch * s.kv_heads * 2 * B128 * (s.head_dim / 4) + 255) / 256, 256, 0, true, st, p, o);
 }
 
 }  // namespace
@@ -744,7 +809,18 @@ int attention_backward_splits(const ue5m3_attention_shape& s) {
     return n < 1 ? 1 : (int)n;
 }
 
-int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q, const ue5m3_heads& k,
+// Parts into which the queries of key tile 0 are shared out: as many as leave none longer than another tile's window, or than half of what
+// every SM has to do in all (these parts start first).
+int attention_sink_parts(const ue5m3_attention_shape& s, int64_t sinks) {
+    const AttentionParams p = attention_params(s, sinks);
+    if (p.sinks == 0 || s.q_len == 0 || s.k_len == 0 || s.batch == 0) return 1;
+    const int64_t q_tiles = (s.q_len + 127) / 128 - p.query_lo(0) / 128, k_tiles = (s.k_len + 127) / 128;
+    const int64_t window = std::min<int64_t>(q_tiles, (p.left + 127) / 128 + 1);
+    const int64_t most = std::max<int64_t>(window, k_tiles * s.batch * s.kv_heads * window / (2 * 148));
+    return (int)std::max<int64_t>(1, (q_tiles + most - 1) / most);
+}
+
+int launch_attention_backward(const ue5m3_attention_shape& s, int64_t sinks, const ue5m3_heads& dout, const ue5m3_heads& q, const ue5m3_heads& k,
                               const ue5m3_heads& v, const ue5m3_heads& o, const float* lse, const ue5m3_heads& dq,
                               const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace, cudaStream_t st, const StallTest& stall) {
     if (s.batch == 0 || (s.q_len == 0 && s.k_len == 0)) return UE5M3_OK;
@@ -758,7 +834,7 @@ int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads&
         return UE5M3_ERR_CUDA;
     if (s.q_len == 0) m.q = m.dout = m.k;                  // an empty side is never read
     if (s.k_len == 0) m.k = m.v = m.q;
-    AttentionParams p = attention_params(s);
+    AttentionParams p = attention_params(s, sinks);
     if (stall.wait_limit > 0) { p.wait_limit = stall.wait_limit; p.stall = 1; }
     if (s.q_len > 0) {
         RowParams r{};
@@ -772,12 +848,15 @@ int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads&
         p.lse2 = r.lse2; p.delta = r.delta;
         p.parts = attention_backward_splits(s);
         p.part_o = workspace + 2 * r.rows;
+        p.sink_parts = attention_sink_parts(s, sinks);
+        p.part_kv = p.part_o + (p.parts > 1 ? p.parts * B * s.heads * s.q_len * D : 0);
         const int64_t grid = (r.rows * 8 + 255) / 256;
         if (grid > 0x7FFFFFFF) return UE5M3_ERR_UNSUPPORTED;
         attention_rows_kernel<<<(unsigned)grid, 256, 0, st>>>(r);
         if (cudaGetLastError() != cudaSuccess) return UE5M3_ERR_CUDA;
     }
-    return D <= 64 ? run<64>(s, dq, m, p, st) : run<128>(s, dq, m, p, st);
+    if (p.sinks > 0) return D <= 64 ? run<64, true>(s, dq, dk, dv, m, p, st) : run<128, true>(s, dq, dk, dv, m, p, st);
+    return D <= 64 ? run<64, false>(s, dq, dk, dv, m, p, st) : run<128, false>(s, dq, dk, dv, m, p, st);
 }
 
 int read_and_clear_attention_backward_status() {

@@ -65,14 +65,15 @@ cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t st);
 cudaError_t launch_adamw(const ue5m3_adamw_tensor* tensors, int64_t count, const ue5m3_adamw_step& s, cudaStream_t st);
 
 // returns a UE5M3_* status
-int launch_attention(const ue5m3_attention_shape& s, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
+int launch_attention(const ue5m3_attention_shape& s, int64_t sinks, const ue5m3_heads& q, const ue5m3_heads& k, const ue5m3_heads& v,
                      const ue5m3_heads& o, float* lse, float* workspace, int num_sms, cudaStream_t st, const StallTest& stall = {});
 int attention_splits(const ue5m3_attention_shape& s);      // parts into which the keys are shared out (1: none)
-int launch_attention_backward(const ue5m3_attention_shape& s, const ue5m3_heads& dout, const ue5m3_heads& q,
+int launch_attention_backward(const ue5m3_attention_shape& s, int64_t sinks, const ue5m3_heads& dout, const ue5m3_heads& q,
                               const ue5m3_heads& k, const ue5m3_heads& v, const ue5m3_heads& o, const float* lse,
                               const ue5m3_heads& dq, const ue5m3_heads& dk, const ue5m3_heads& dv, float* workspace,
                               cudaStream_t st, const StallTest& stall = {});
 int attention_backward_splits(const ue5m3_attention_shape& s);        // the same for the queries' gradient
+int attention_sink_parts(const ue5m3_attention_shape& s, int64_t sinks);      // parts into which the queries of the first key tile are
 int read_and_clear_norm_status();                 // these three synchronise the device
 int read_and_clear_attention_status();
 int read_and_clear_attention_backward_status();
