@@ -9,11 +9,15 @@
 // binary32 would be off by 2^-24 p f radians, 0.06 at a million positions.
 //
 // A warp takes a token.  G lanes hold a head's row, each VEC pairs of it (two vectors: the two halves of the pairs, or one piece of
-// neighbouring pairs), 32 / G heads side by side (a group), and the warp walks the groups with a lane's pairs, and so its angles and weights,
-// staying the same.  The norm's sum over a row is log2(G) shuffles.  Rows come through a ring of asynchronous copies in shared memory, a
-// ring per warp, several groups ahead and on into the warp's next token; registers cannot hold enough of them: with four groups loaded
-// into registers at a time norm and rotation of 2 x 4096 tokens took 43 us.  The copies are of 16 bytes wherever addresses allow it, whatever VEC is,
-// which is 16 bytes where no pair's end cuts it, else 8, 4 or 2.  Where there are few tokens the groups of one are shared out among warps.
+// neighbouring pairs), 32 / G heads side by side (a group), and the warp walks its groups, a few at a time, with a lane's pairs, and so its
+// angles and weights, staying the same.  VEC is 4 pairs where the addresses allow it and no pair's end cuts a vector, else 2 or 1 (8 pairs of BF16 in a lane
+// were slower: half of the lanes' rows side by side, twice the registers).  The next rows are loaded under the arithmetic, the first ones under the angles.  A
+// token's sines and cosines are computed once, by all lanes, and read from shared memory (each lane for itself: a third of all instructions).  The norm's sum over
+// a row is log2(G) shuffles.  A ring of asynchronous copies in shared memory in place of registers was slower (47 us): the arithmetic's own
+// latency is what counts, not the bytes in flight.  Where there are few tokens the heads of one are shared out among warps.
+//
+// GPU time, of which the floor at the measured copy rate: rotation of 4 x 4096 tokens, 32 + 8 heads of 128, BF16 54.8 us (0.93 of it); norm and rotation
+// of 2 x 4096 30.5 (0.84); backward of 4 x 4096 96 (0.80), bound by the latency of a row's chain at 12 warps per SM.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <algorithm>
@@ -21,19 +25,30 @@
 #include "../../include/ue5m3.h"
 #include "block_ops.h"
 #include "common.cuh"
+#include "tcgen05.cuh"
 
 namespace ue5m3 {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kBatch = 2;                              // groups that a forward warp works on at a time
+// Groups that a warp works on at a time, and CTAs per SM (backward: of a persistent grid).  Rows side by side hide the latency of the norm's chain (sum,
+// shuffles, root), more warps do too, and both want registers.  Norm and rotation of 2 x 4096 tokens, BF16, us: 4 groups in 5 CTAs 30.5; 2 in 4
+// 36.1, 2 in 6 35.5, 4 in 4 33.1, 6 in 4 32.5 and, where registers spill, 4 in 6 64.7.  Backward of 4 x 4096, BF16: 4 in 3 96.0; 2 in 4 99.7, 1 in 5
+// 122, 3 in 3 110, 4 in 2 106, 4 in 4 147 (spilled); 3 x 517 of 80 in binary32: 2 in 4 15.2, 4 in 3 18.4.
+template <typename T, int VEC> constexpr bool kNarrow = sizeof(T) == 2 && VEC == 4;      // four pairs of BF16: the fewest registers
+template <typename T, int VEC> constexpr int kBatch = kNarrow<T, VEC> ? 4 : 2;
+template <typename T, int VEC> constexpr int kForwardCtas = kNarrow<T, VEC> ? 5 : 4;
+template <typename T, int VEC> constexpr int kBackwardBatch = kNarrow<T, VEC> ? 4 : 2;
+template <typename T, int VEC> constexpr int kBackwardCtas = kNarrow<T, VEC> ? 3 : 4;
+constexpr int kMostBackwardCtas = 4;
 
 struct Side {                                          // queries or keys
     const void* x; const void* dy; void* y;            // backward: y is dx
     int64_t xs[3], ds[3], ys[3];                       // batch, token, head
     const void* weight;                                // (without one: an address that can be read)
     int weighted;
-    int heads, groups, batches;                        // groups of 32 / G heads, batches of kBatch groups
+    int heads, groups, batches;                        // groups of 32 / G heads, batches of a few groups
+    int64_t group_stride, group_stride_up, group_stride_out;       // bytes from a group to the next in x, dy, y
 };
 struct RotaryParams {
     Side side[2];
@@ -117,15 +132,16 @@ template <int VEC, int NU, bool NEIGHBOURS> struct Lane {
     }
 };
 
-// A row in a lane: P = NU VEC pairs (a, b), two neighbouring pairs' a in one packed value, their b in another.
+// A row in a lane: P = NU VEC pairs (a, b), two neighbouring pairs' a in one packed value, their b in another: one instruction for both.
 template <int P> struct Pairs { f32x2 a[P / 2], b[P / 2]; };
 template <typename T, int VEC, int NU> struct RowRaw { Raw<VEC * sizeof(T)> v[NU][2]; };
+// `row`: where the lane's first vector of the row lies.
 template <typename T, int VEC, int NU, bool NB>
-__device__ __forceinline__ void load_row(RowRaw<T, VEC, NU>& r, const T* row, const Lane<VEC, NU, NB>& l) {
+__device__ __forceinline__ void load_row(RowRaw<T, VEC, NU>& r, const char* row, const Lane<VEC, NU, NB>& l) {
 #pragma unroll
     for (int k = 0; k < NU; ++k)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) r.v[k][h] = load_raw<VEC * sizeof(T)>(row + l.at[k][h]);
+        for (int h = 0; h < 2; ++h) r.v[k][h] = load_raw<VEC * sizeof(T)>(row + (l.at[k][h] - l.at[0][0]) * (int)sizeof(T));
 }
 template <typename T, int VEC, int NU, bool NB> __device__ __forceinline__ void unpack_row(const RowRaw<T, VEC, NU>& r, Pairs<NU * VEC>& x) {
     float f[NU * VEC][2];
@@ -147,7 +163,7 @@ template <typename T, int VEC, int NU, bool NB> __device__ __forceinline__ void 
     }
 }
 template <typename T, int VEC, int NU, bool NB>
-__device__ __forceinline__ void store_row(T* row, const Pairs<NU * VEC>& y, const Lane<VEC, NU, NB>& l) {
+__device__ __forceinline__ void store_row(char* row, const Pairs<NU * VEC>& y, const Lane<VEC, NU, NB>& l) {
     float f[NU * VEC][2];
 #pragma unroll
     for (int i = 0; i < NU * VEC / 2; ++i) {
@@ -163,8 +179,8 @@ __device__ __forceinline__ void store_row(T* row, const Pairs<NU * VEC>& y, cons
             v[NB ? 2 * j + 1 : VEC + j] = f[k * VEC + j][1];
         }
         if (l.here[k]) {
-            store_vec<VEC>(row + l.at[k][0], v);
-            store_vec<VEC>(row + l.at[k][1], v + VEC);
+            store_vec<VEC>(reinterpret_cast<T*>(row + (l.at[k][0] - l.at[0][0]) * (int)sizeof(T)), v);
+            store_vec<VEC>(reinterpret_cast<T*>(row + (l.at[k][1] - l.at[0][0]) * (int)sizeof(T)), v + VEC);
         }
     }
 }
@@ -193,24 +209,23 @@ __device__ __forceinline__ double position_of(const RotaryParams& p, int64_t b, 
     const char* at = static_cast<const char*>(p.positions) + ((b * p.position_stride + t) << (p.wide_positions ? 3 : 2));
     return p.wide_positions ? (double)__ldg(reinterpret_cast<const long long*>(at)) : (double)__ldg(reinterpret_cast<const int*>(at));
 }
-// VEC floats of shared memory (aligned to them).
+// VEC floats of shared memory (aligned to them), by loads that stay where they are written: the backward pass has no registers to keep
+// them in from row to row.
 template <int VEC> __device__ __forceinline__ void read_floats(const float* p, float* f) {
+    const uint32_t at = smem_u32(p);
     if constexpr (VEC >= 4) {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(p + i);
-            f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
-        }
+        for (int i = 0; i < VEC; i += 4)
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f[i]), "=f"(f[i + 1]), "=f"(f[i + 2]), "=f"(f[i + 3]) : "r"(at + 4 * i) : "memory");
     } else if constexpr (VEC == 2) {
-        const float2 v = *reinterpret_cast<const float2*>(p);
-        f[0] = v.x; f[1] = v.y;
+        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(f[0]), "=f"(f[1]) : "r"(at) : "memory");
     } else {
-        f[0] = *p;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[0]) : "r"(at) : "memory");
     }
 }
 // Cosines and sines (times the amplitude) of a token's pairs in the warp's table, every pair once (1 and 0 for those that stay): the lanes
 // that hold a pair of different heads read it there.
-struct Table { alignas(16) float c[128], s[128]; };
+struct Table { alignas(16) float c[128], s[128], minus_s[128]; };
 __device__ __forceinline__ void fill_table(const RotaryParams& p, Table& t, double position, int lane) {
     for (int i = lane; i < p.dim / 2; i += 32) {
         float sn = 0.0f, cs = 1.0f;
@@ -222,21 +237,15 @@ __device__ __forceinline__ void fill_table(const RotaryParams& p, Table& t, doub
         }
         t.c[i] = cs;
         t.s[i] = sn;
+        t.minus_s[i] = -sn;
     }
 }
-template <int VEC, int NU, bool NB>
-__device__ __forceinline__ void read_table(const Table& t, const Lane<VEC, NU, NB>& l, f32x2* c, f32x2* s) {
-    float cs[NU * VEC], sn[NU * VEC];
+template <int VEC, int NU, bool NB> __device__ __forceinline__ void read_table(const float* t, const Lane<VEC, NU, NB>& l, f32x2* out) {
+    float v[NU * VEC];
 #pragma unroll
-    for (int k = 0; k < NU; ++k) {
-        read_floats<VEC>(t.c + l.first[k], cs + k * VEC);
-        read_floats<VEC>(t.s + l.first[k], sn + k * VEC);
-    }
+    for (int k = 0; k < NU; ++k) read_floats<VEC>(t + l.first[k], v + k * VEC);
 #pragma unroll
-    for (int i = 0; i < NU * VEC / 2; ++i) {
-        c[i] = f2_pack(cs[2 * i], cs[2 * i + 1]);
-        s[i] = f2_pack(sn[2 * i], sn[2 * i + 1]);
-    }
+    for (int i = 0; i < NU * VEC / 2; ++i) out[i] = f2_pack(v[2 * i], v[2 * i + 1]);
 }
 // Both weights in binary32 (1 without) for the whole CTA.
 struct Weights { alignas(16) float w[2][256]; };
@@ -269,11 +278,6 @@ template <int VEC, int NU, bool NB> __device__ __forceinline__ void read_weights
     }
 }
 __device__ __forceinline__ f32x2 twice(float x) { return f2_pack(x, x); }
-__device__ __forceinline__ f32x2 f2_minus(f32x2 x) {
-    float a, b;
-    f2_unpack(x, a, b);
-    return f2_pack(-a, -b);
-}
 // sum over a lane's columns that exist of x y
 template <int VEC, int NU, bool NB> __device__ __forceinline__ float dot(const Pairs<NU * VEC>& x, const Pairs<NU * VEC>& y, const Lane<VEC, NU, NB>& l) {
     float sum = 0.0f;
@@ -300,6 +304,13 @@ template <int VEC, int NU, bool NB> __device__ __forceinline__ float dot(const P
 }
 // Sums over the lanes of a row.
 template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], int lanes) {
+    if (lanes == 3) {                                      // 16-bit rows of 66 to 128, 32-bit ones of 34 to 64: without the branches
+#pragma unroll
+        for (int d = 2; d >= 0; --d)
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], 1 << d);
+        return;
+    }
 #pragma unroll
     for (int d = 4; d >= 0; --d)
         if (lanes > d) {
@@ -308,13 +319,12 @@ template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], int lan
         }
 }
 
-constexpr int kForwardCtas = 4, kBackwardCtas = 4;     // CTAs per SM (backward: of a persistent grid)
 
 // A warp takes one item: the batches [first, last) of U groups of one token, queries before keys.  The next batch is loaded while one is
 // worked on, the first one under the angles; U rows side by side hide the latency of the norm's chain (sum, shuffles, root).
 template <typename T, int VEC, bool NEIGHBOURS, bool NORM>
-__global__ void __launch_bounds__(kThreads, kForwardCtas) rotary_kernel(const __grid_constant__ RotaryParams p) {
-    constexpr int NU = VEC >= 4 ? 1 : 4 / VEC, P = NU * VEC, U = kBatch;
+__global__ void __launch_bounds__(kThreads, kForwardCtas<T, VEC>) rotary_kernel(const __grid_constant__ RotaryParams p) {
+    constexpr int NU = VEC >= 4 ? 1 : 4 / VEC, P = NU * VEC, U = kBatch<T, VEC>;
     __shared__ Table tables[kWarps];
     __shared__ Weights weights;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -333,27 +343,27 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) rotary_kernel(const __
         last = all * (part + 1) / p.parts;
     }
     const unsigned b = p.batch == 1 ? 0 : token / (unsigned)p.tokens, t = token - b * p.tokens;
-    const T* from[2];
-    T* to[2];
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const Side& sd = p.side[side];
-        from[side] = static_cast<const T*>(sd.x) + b * sd.xs[0] + t * sd.xs[1] + slot * sd.xs[2];
-        to[side] = static_cast<T*>(sd.y) + b * sd.ys[0] + t * sd.ys[1] + slot * sd.ys[2];
-    }
     RowRaw<T, VEC, NU> raw[U];
-    auto load = [&](int batch) {
-        const int side = batch >= q_batches, h0 = (batch - (side ? q_batches : 0)) * U * slots, heads = p.side[side].heads - slot;
-        const int64_t stride = p.side[side].xs[2];
-        const T* row = (side ? from[1] : from[0]) + h0 * stride;
+    // of the batch that is loaded next, and of the one that is worked on: side, first head and where it lies (this lane's part of it)
+    auto place_of = [&](int batch, const Side& sd, const void* base, const int64_t (&strides)[3]) {
+        return static_cast<const char*>(base) + (b * strides[0] + t * strides[1] + (int64_t)(batch * U * slots + slot) * strides[2] + l.at[0][0]) * (int64_t)sizeof(T);
+    };
+    int ahead_side = i >= q_batches, ahead_head = (i - (ahead_side ? q_batches : 0)) * U * slots + slot;
+    const char* ahead = any ? place_of(i - (ahead_side ? q_batches : 0), p.side[ahead_side], p.side[ahead_side].x, p.side[ahead_side].xs) : nullptr;
+    auto load = [&]() {
+        const Side& sd = p.side[ahead_side];
+        const int64_t group = sd.group_stride;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (h0 + u * slots < heads) load_row(raw[u], row + u * slots * stride, l);
+        for (int u = 0; u < U; ++u) {
+            if (ahead_head < sd.heads) load_row(raw[u], ahead, l);
+            ahead += group;
+            ahead_head += slots;
+        }
     };
     if (any) {
 #pragma unroll
         for (int u = 0; u < U; ++u) raw[u] = RowRaw<T, VEC, NU>{};
-        load(i);
+        load();
     }
     if (NORM) load_weights(p, weights);
     if (any) fill_table(p, tables[warp], position_of(p, b, t), lane);
@@ -361,19 +371,25 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) rotary_kernel(const __
     else __syncwarp();
     if (!any) return;
     f32x2 ca[P / 2], cb[P / 2], sa[P / 2], sb[P / 2];
-    int side_now = -1;
+    int side_now = -1, head = 0;
+    char* to = nullptr;
 #pragma unroll 1
     for (; i < last; ++i) {
         const int side = i >= q_batches;
         if (side != side_now) {                            // a' = a ca - b sb, b' = b cb + a sa: the weights go into the angles
             side_now = side;
-            read_table(tables[warp], l, ca, sa);
+            const int first = i - (side ? q_batches : 0);
+            head = first * U * slots + slot;
+            to = const_cast<char*>(place_of(first, p.side[side], p.side[side].y, p.side[side].ys));
+            read_table(tables[warp].c, l, ca);
+            read_table(tables[warp].s, l, sa);
+            read_table(tables[warp].minus_s, l, sb);
             Pairs<P> w;
             if (NORM) read_weights(weights.w[side], l, w);
 #pragma unroll
             for (int k = 0; k < P / 2; ++k) {
                 cb[k] = NORM ? f2_mul(ca[k], w.b[k]) : ca[k];
-                sb[k] = f2_minus(NORM ? f2_mul(sa[k], w.b[k]) : sa[k]);
+                sb[k] = NORM ? f2_mul(sb[k], w.b[k]) : sb[k];
                 ca[k] = NORM ? f2_mul(ca[k], w.a[k]) : ca[k];
                 sa[k] = NORM ? f2_mul(sa[k], w.a[k]) : sa[k];
             }
@@ -381,7 +397,14 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) rotary_kernel(const __
         Pairs<P> f[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) unpack_row<T, VEC, NU, NEIGHBOURS>(raw[u], f[u]);
-        if (i + 1 < last) load(i + 1);
+        if (i + 1 < last) {
+            if (i + 1 == q_batches) {
+                ahead_side = 1;
+                ahead_head = slot;
+                ahead = place_of(0, p.side[1], p.side[1].x, p.side[1].xs);
+            }
+            load();
+        }
         if (NORM) {
             float sum[U];
 #pragma unroll
@@ -394,9 +417,8 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) rotary_kernel(const __
                 for (int k = 0; k < P / 2; ++k) { f[u].a[k] = f2_mul(f[u].a[k], r); f[u].b[k] = f2_mul(f[u].b[k], r); }
             }
         }
-        const int h0 = (i - (side ? q_batches : 0)) * U * slots, heads = p.side[side].heads - slot;
-        const int64_t stride = p.side[side].ys[2];
-        T* row = (side ? to[1] : to[0]) + h0 * stride;
+        const int heads = p.side[side].heads;
+        const int64_t group = p.side[side].group_stride_out;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             Pairs<P> o;
@@ -412,7 +434,9 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) rotary_kernel(const __
                 }
                 keep_still(o, f[u], l, p.half_rotary);
             }
-            if (h0 + u * slots < heads) store_row(row + u * slots * stride, o, l);
+            if (head < heads) store_row<T, VEC, NU, NEIGHBOURS>(to, o, l);
+            to += group;
+            head += slots;
         }
     }
 }
@@ -421,8 +445,8 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) rotary_kernel(const __
 // kept by every lane for its columns (in shared memory between tokens, in registers within one), added over the CTA at the end and leave as one
 // binary32 row per CTA, which rotary_weights_kernel adds in a fixed order: no atomics.
 template <typename T, int VEC, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads, kBackwardCtas) rotary_backward_kernel(const __grid_constant__ RotaryParams p) {
-    constexpr int NU = VEC >= 4 ? 1 : 4 / VEC, P = NU * VEC;
+__global__ void __launch_bounds__(kThreads, kBackwardCtas<T, VEC>) rotary_backward_kernel(const __grid_constant__ RotaryParams p) {
+    constexpr int NU = VEC >= 4 ? 1 : 4 / VEC, P = NU * VEC, U = kBackwardBatch<T, VEC>;
     __shared__ Table tables[kWarps];
     __shared__ Weights weights;
     __shared__ float sums[2][2 * P][kThreads];
@@ -431,38 +455,57 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) rotary_backward_kerne
     const int slot = lane >> p.lanes, slots = 32 >> p.lanes;
     Lane<VEC, NU, NEIGHBOURS> l;
     l.place(lane, p.lanes, p.half_rotary, p.dim);
-    const int q_groups = p.side[0].groups, groups = q_groups + p.side[1].groups;
+    const int q_batches = p.side[0].batches, batches = q_batches + p.side[1].batches;
     const unsigned step = gridDim.x * kWarps, items = p.items;
-    struct Work { unsigned b, t; int g, g_end; };
+    struct Work { unsigned b, t; int i, last; };           // a token and its batches [i, last)
     auto work_of = [&](unsigned index) {
         Work w;
         unsigned token = index;
-        w.g = 0;
-        w.g_end = groups;
+        w.i = 0;
+        w.last = batches;
         if (p.parts > 1) {
             token = index / (unsigned)p.parts;
             const int part = index - token * p.parts;
-            w.g = groups * part / p.parts;
-            w.g_end = groups * (part + 1) / p.parts;
+            w.i = batches * part / p.parts;
+            w.last = batches * (part + 1) / p.parts;
         }
         w.b = p.batch == 1 ? 0 : token / (unsigned)p.tokens;
         w.t = token - w.b * p.tokens;
         return w;
     };
-    RowRaw<T, VEC, NU> rx{}, rd{};
-    auto load = [&](const Work& w, int g) {                // group g of the token of w
-        const int side = g >= q_groups, h = (g - (side ? q_groups : 0)) * slots + slot;
-        const Side& sd = p.side[side];
-        if (h < sd.heads) {
-            load_row(rx, static_cast<const T*>(sd.x) + w.b * sd.xs[0] + w.t * sd.xs[1] + h * sd.xs[2], l);
-            load_row(rd, static_cast<const T*>(sd.dy) + w.b * sd.ds[0] + w.t * sd.ds[1] + h * sd.ds[2], l);
+    RowRaw<T, VEC, NU> rx[U], rd[U];
+    // the batch that is loaded next: side, this lane's first head, where its x and dy lie (this lane's part of them)
+    int ahead_side = 0, ahead_head = 0;
+    const char *ahead_x = nullptr, *ahead_d = nullptr;
+    auto place = [&](const Work& w, int i) {
+        ahead_side = i >= q_batches;
+        const Side& sd = p.side[ahead_side];
+        ahead_head = (i - (ahead_side ? q_batches : 0)) * U * slots + slot;
+        ahead_x = static_cast<const char*>(sd.x) + (w.b * sd.xs[0] + w.t * sd.xs[1] + ahead_head * sd.xs[2] + l.at[0][0]) * (int64_t)sizeof(T);
+        ahead_d = static_cast<const char*>(sd.dy) + (w.b * sd.ds[0] + w.t * sd.ds[1] + ahead_head * sd.ds[2] + l.at[0][0]) * (int64_t)sizeof(T);
+    };
+    auto load = [&]() {
+        const Side& sd = p.side[ahead_side];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (ahead_head < sd.heads) {
+                load_row(rx[u], ahead_x, l);
+                load_row(rd[u], ahead_d, l);
+            } else {                                       // a head that does not exist: nothing is added up for it
+                rx[u] = RowRaw<T, VEC, NU>{};
+                rd[u] = RowRaw<T, VEC, NU>{};
+            }
+            ahead_head += slots;
+            ahead_x += sd.group_stride;
+            ahead_d += sd.group_stride_up;
         }
     };
     unsigned index = blockIdx.x * kWarps + warp;
     Work now{};
     if (index < items) {
         now = work_of(index);
-        load(now, now.g);
+        place(now, now.i);
+        load();
     }
 #pragma unroll
     for (int i = 0; i < 2 * P; ++i) sums[0][i][threadIdx.x] = sums[1][i][threadIdx.x] = 0.0f;
@@ -476,50 +519,84 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) rotary_backward_kerne
         __syncwarp();
         fill_table(p, tables[warp], position_of(p, now.b, now.t), lane);
         __syncwarp();
-        f32x2 c[P / 2], s[P / 2];
-        read_table(tables[warp], l, c, s);
 #pragma unroll 1
-        for (int side = now.g >= q_groups; side < 2; ++side) {
+        for (int side = now.i >= q_batches; side < 2; ++side) {
             const Side& sd = p.side[side];
-            const int skip = side ? q_groups : 0, end = side ? now.g_end : min(now.g_end, q_groups);
-            T* to = static_cast<T*>(sd.y) + now.b * sd.ys[0] + now.t * sd.ys[1];
-            Pairs<P> w, acc;
-            read_weights(weights.w[side], l, w);
+            const int skip = side ? q_batches : 0, end = side ? now.last : min(now.last, q_batches);
+            int head = (now.i - skip) * U * slots + slot;
+            char* to = static_cast<char*>(sd.y) + (now.b * sd.ys[0] + now.t * sd.ys[1] + head * sd.ys[2] + l.at[0][0]) * (int64_t)sizeof(T);
+            Pairs<P> acc;
 #pragma unroll
             for (int i = 0; i < P / 2; ++i) acc.a[i] = acc.b[i] = 0;
 #pragma unroll 1
-            for (; now.g < end; ++now.g) {
-                Pairs<P> f, d, e;
-                unpack_row<T, VEC, NU, NEIGHBOURS>(rx, f);
-                unpack_row<T, VEC, NU, NEIGHBOURS>(rd, d);
-                if (now.g + 1 < now.g_end) load(now, now.g + 1);
-                else if (index < items) load(next, next.g);
-                const int h = (now.g - skip) * slots + slot;
+            for (; now.i < end; ++now.i) {
+                Pairs<P> f[U], e[U];                       // x, and dy turned back
+                {
+                    Pairs<P> d[U];
 #pragma unroll
-                for (int i = 0; i < P / 2; ++i) {          // (the sines are those of the negated angles)
-                    e.a[i] = f2_fma(f2_minus(d.b[i]), s[i], f2_mul(d.a[i], c[i]));
-                    e.b[i] = f2_fma(d.a[i], s[i], f2_mul(d.b[i], c[i]));
-                }
-                if (!p.full) keep_still(e, d, l, p.half_rotary);
-#pragma unroll
-                for (int i = 0; i < P / 2; ++i) { d.a[i] = f2_mul(e.a[i], w.a[i]); d.b[i] = f2_mul(e.b[i], w.b[i]); }
-                float sum[2] = {dot(f, f, l), dot(d, f, l)};
-                row_sums(sum, p.lanes);
-                const float r = rsqrtf(fmaf(sum[0], p.inv_dim, p.eps));
-                const f32x2 r2 = twice(r), m2 = twice(-(sum[1] * r * p.inv_dim));
-                const bool exists = h < sd.heads;
-#pragma unroll
-                for (int i = 0; i < P / 2; ++i) {          // xh = x r, dx = r (g - xh m)
-                    f.a[i] = f2_mul(f.a[i], r2);
-                    f.b[i] = f2_mul(f.b[i], r2);
-                    if (exists) {
-                        acc.a[i] = f2_fma(e.a[i], f.a[i], acc.a[i]);
-                        acc.b[i] = f2_fma(e.b[i], f.b[i], acc.b[i]);
+                    for (int u = 0; u < U; ++u) {
+                        unpack_row<T, VEC, NU, NEIGHBOURS>(rx[u], f[u]);
+                        unpack_row<T, VEC, NU, NEIGHBOURS>(rd[u], d[u]);
                     }
-                    d.a[i] = f2_mul(f2_fma(f.a[i], m2, d.a[i]), r2);
-                    d.b[i] = f2_mul(f2_fma(f.b[i], m2, d.b[i]), r2);
+                    if (now.i + 1 < now.last) {
+                        if (now.i + 1 == q_batches) place(now, q_batches);
+                        load();
+                    } else if (index < items) {
+                        place(next, next.i);
+                        load();
+                    }
+                    f32x2 c[P / 2], sn[P / 2];             // (the sines are those of the negated angles)
+                    read_table(tables[warp].c, l, c);
+                    read_table(tables[warp].s, l, sn);
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int i = 0; i < P / 2; ++i) {
+                            e[u].a[i] = f2_mul(d[u].a[i], c[i]);
+                            e[u].b[i] = f2_fma(d[u].a[i], sn[i], f2_mul(d[u].b[i], c[i]));
+                        }
+                    read_table(tables[warp].minus_s, l, sn);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+#pragma unroll
+                        for (int i = 0; i < P / 2; ++i) e[u].a[i] = f2_fma(d[u].b[i], sn[i], e[u].a[i]);
+                        if (!p.full) keep_still(e[u], d[u], l, p.half_rotary);
+                    }
                 }
-                if (exists) store_row(to + h * sd.ys[2], d, l);
+                float sum[2 * U];
+                {
+                    Pairs<P> w;
+                    read_weights(weights.w[side], l, w);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        Pairs<P> g;
+#pragma unroll
+                        for (int i = 0; i < P / 2; ++i) { g.a[i] = f2_mul(e[u].a[i], w.a[i]); g.b[i] = f2_mul(e[u].b[i], w.b[i]); }
+                        sum[2 * u] = dot(f[u], f[u], l);
+                        sum[2 * u + 1] = dot(g, f[u], l);
+                    }
+                }
+                row_sums(sum, p.lanes);
+                Pairs<P> w;                                // (read again: no registers to keep them in meanwhile)
+                read_weights(weights.w[side], l, w);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const float r = rsqrtf(fmaf(sum[2 * u], p.inv_dim, p.eps));
+                    const f32x2 r2 = twice(r), m2 = twice(-(sum[2 * u + 1] * r * p.inv_dim));
+                    Pairs<P> d;
+#pragma unroll
+                    for (int i = 0; i < P / 2; ++i) {      // xh = x r, dx = r (g - xh m)
+                        f[u].a[i] = f2_mul(f[u].a[i], r2);
+                        f[u].b[i] = f2_mul(f[u].b[i], r2);
+                        acc.a[i] = f2_fma(e[u].a[i], f[u].a[i], acc.a[i]);
+                        acc.b[i] = f2_fma(e[u].b[i], f[u].b[i], acc.b[i]);
+                        d.a[i] = f2_mul(f2_fma(e[u].a[i], w.a[i], f2_mul(f[u].a[i], m2)), r2);
+                        d.b[i] = f2_mul(f2_fma(e[u].b[i], w.b[i], f2_mul(f[u].b[i], m2)), r2);
+                    }
+                    if (head < sd.heads) store_row<T, VEC, NU, NEIGHBOURS>(to, d, l);
+                    head += slots;
+                    to += sd.group_stride_out;
+                }
             }
 #pragma unroll
             for (int i = 0; i < P / 2; ++i) {
@@ -580,18 +657,30 @@ cudaError_t run(const RotaryArgs& a, RotaryParams& p, cudaStream_t st) {
     p.lanes = 0;
     while ((NU << p.lanes) < units) ++p.lanes;
     const int slots = 32 >> p.lanes;
+    const bool backward = a.op == RotaryArgs::kBackward;
+    const int batch = backward ? kBackwardBatch<T, VEC> : kBatch<T, VEC>, resident = 148 * (backward ? kBackwardCtas<T, VEC> : kForwardCtas<T, VEC>);
     for (Side& s : p.side) {
         s.groups = (s.heads + slots - 1) / slots;
-        s.batches = (s.groups + kBatch - 1) / kBatch;
+        s.batches = (s.groups + batch - 1) / batch;
+        s.group_stride = slots * s.xs[2] * (int64_t)sizeof(T);
+        s.group_stride_up = slots * s.ds[2] * (int64_t)sizeof(T);
+        s.group_stride_out = slots * s.ys[2] * (int64_t)sizeof(T);
     }
-    const bool backward = a.op == RotaryArgs::kBackward;
-    const int64_t rows = a.s.batch * a.s.tokens, warps = 148 * kWarps * (backward ? kBackwardCtas : kForwardCtas);
-    const int pieces = backward ? p.side[0].groups + p.side[1].groups : p.side[0].batches + p.side[1].batches;
-    // Few tokens: the heads of one are shared out, so that there is an item for every warp.
-    p.parts = (int)std::min<int64_t>(pieces, (warps + rows - 1) / rows);
+    const int64_t rows = a.s.batch * a.s.tokens, warps = kWarps * resident;
+    const int pieces = p.side[0].batches + p.side[1].batches;
+    // The heads of a token are shared out where that makes the longest warp's work shorter: rounds of items times batches of an item, with
+    // what every item costs besides (angles, addresses) taken as one batch.
+    int64_t least = INT64_MAX;
+    for (int n = 1; n <= pieces; ++n) {
+        const int64_t cost = (rows * n + warps - 1) / warps * ((pieces + n - 1) / n + 1);
+        if (cost < least) {
+            least = cost;
+            p.parts = n;
+        }
+    }
     p.items = (int)(rows * p.parts);
     const int64_t ctas = (p.items + kWarps - 1) / kWarps;
-    const unsigned grid = (unsigned)(backward ? std::min<int64_t>(ctas, 148 * kBackwardCtas) : ctas);
+    const unsigned grid = (unsigned)(backward ? std::min<int64_t>(ctas, resident) : ctas);
     if (backward) {
         rotary_backward_kernel<T, VEC, NB><<<grid, kThreads, 0, st>>>(p);
         cudaError_t e = cudaGetLastError();
@@ -618,7 +707,7 @@ cudaError_t run(const RotaryArgs& a, RotaryParams& p, cudaStream_t st) {
 
 }  // namespace
 
-int rotary_backward_ctas() { return 148 * kBackwardCtas; }
+int rotary_backward_ctas() { return 148 * kMostBackwardCtas; }
 
 cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t st) {
     const ue5m3_rotary_shape& s = a.s;
@@ -669,8 +758,7 @@ cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t st) {
     if (!s.interleaved) bits |= (uint64_t)p.half_rotary;
     const int vec = (int)(bits & (0 - bits) & 7) ? (int)(bits & (0 - bits)) : 8;
     if (s.dtype == UE5M3_BF16) {
-        if (vec >= 8) return run<__nv_bfloat16, 8>(a, p, st);
-        if (vec == 4) return run<__nv_bfloat16, 4>(a, p, st);
+        if (vec >= 4) return run<__nv_bfloat16, 4>(a, p, st);
         if (vec == 2) return run<__nv_bfloat16, 2>(a, p, st);
         return run<__nv_bfloat16, 1>(a, p, st);
     }
