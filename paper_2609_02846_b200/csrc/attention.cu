@@ -41,6 +41,7 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr int BQ = 128, BK = 128;
+constexpr int kFewSinks = 32;
 constexpr float kRaise = 8.0f;                            // log2 of the growth of a row's maximum that is tolerated
 
 template <int DP> struct Tiles {                          // DP: head dimension padded to 64 or 128
@@ -71,13 +72,18 @@ struct Item {
     int b, h, h_end, kvh, part, q0, keys;                 // h_end: heads of the group of h end there (PACK)
     int lo[2], hi[2];                                     // key tiles of the two query tiles
     int first, last;                                      // ... and of both together
-    int skip;                                             // SINKS: key tiles left out between tile 0 and the windows'; lo .. last count the others
+    // SINKS: tiles are counted from `base`, the windows' first one, and behind the windows' last comes tile 0 as number `sinks_at` (-1: it does not), for
+    // the query tiles that do not see it in their window.  lo .. hi[t] has the tiles lo .. window[t] and that one.
+    int base, sinks_at, window[2];
     __device__ __forceinline__ bool on(int t) const { return hi[t] > lo[t]; }
-    template <bool SINKS> __device__ __forceinline__ int key_tile(int j) const { return SINKS && j > 0 ? j + skip : j; }
+    template <bool SINKS> __device__ __forceinline__ int key_tile(int j) const { return !SINKS ? j : j == sinks_at ? 0 : base + j; }
+    template <bool SINKS> __device__ __forceinline__ bool takes(int t, int j) const { return j >= lo[t] && j < hi[t] && (!SINKS || j < window[t] || j == sinks_at); }
+    // Tile 0 for its sinks, and those are few: the products and exponentials of 32 keys will do.
+    template <bool SINKS> __device__ __forceinline__ bool few(int j, int sinks) const { return SINKS && j == sinks_at && sinks <= kFewSinks; }
 };
 // Heads fastest (heads that share keys run side by side), long query tiles first.
-// SINKS: key tile 0 stands in front of the windows' tiles of both query tiles, of which the second then begins with the first's (one
-// tile of hidden scores at most).
+// SINKS: key tile 0 comes behind the tiles of the windows.  2 x 4096 tokens with a window of 1023: 183 us (in front of them, or in front of the last one, the
+// same; all 128 of its keys in place of 32 186), without sinks 157: a step of its own, of which there are nine, and 6 % for the tiles' numbers.
 template <bool PARTS, bool PACK, bool SINKS>
 __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int q_tiles) {
     Item w;
@@ -109,19 +115,28 @@ __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int
             w.hi[t] = max(min(w.hi[t], (int)((int64_t)n * (w.part + 1) / p.parts)), w.lo[t]);
         }
     }
-    w.skip = 0;
-    if (SINKS && w.part == 0) {                           // (the first part has tile 0)
-        int base = 0x7FFFFFFF;
+    w.base = 0;
+    w.sinks_at = -1;
+    w.window[0] = w.window[1] = 0;
+    if (SINKS) {
+        int first = 0x7FFFFFFF, end = 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-            if (w.on(t)) base = min(base, w.lo[t]);
-        w.skip = base == 0x7FFFFFFF || base == 0 ? 0 : base - 1;
+            if (w.on(t)) {
+                first = min(first, w.lo[t]);
+                end = max(end, w.hi[t]);
+            }
+        w.base = end > 0 ? first : 0;
+        const int last = end - w.base;                    // tiles of both windows
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int r0 = PACK ? 0 : w.q0 + t * BQ, r1 = min(r0 + BQ, p.q_len) - 1;
-            const bool sees = (PACK ? w.h + t * p.pack < w.h_end : r0 < p.q_len) && p.key_hi(r1, w.keys) > 0;
-            w.hi[t] = sees ? (w.on(t) ? w.hi[t] - w.skip : 1) : 0;
-            w.lo[t] = 0;
+            const bool sees = (PACK ? w.h + t * p.pack < w.h_end : r0 < p.q_len) && p.key_hi(r1, w.keys) > 0, any = w.on(t);
+            const bool apart = w.part == 0 && sees && !(any && w.lo[t] == 0);           // (the first part has tile 0)
+            w.window[t] = any ? w.hi[t] - w.base : 0;
+            w.lo[t] = any ? w.lo[t] - w.base : last;
+            w.hi[t] = apart ? last + 1 : any ? w.window[t] : w.lo[t];
+            if (apart) w.sinks_at = last;
         }
     }
     w.first = w.on(0) ? (w.on(1) ? min(w.lo[0], w.lo[1]) : w.lo[0]) : w.lo[1];
@@ -257,27 +272,29 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         };
         auto k_tile = [&](uint32_t v) { return v + 1 == T::RING ? 0 : v + 1; };
         const uint64_t qd = umma_smem_desc(smem), kd0 = umma_smem_desc(ring), vd0 = umma_mn_desc(ring, T::PANEL);
-        auto issue_s = [&](int t, uint32_t tile) {         // S_t = Q_t K^T
+        auto issue_s = [&](int t, uint32_t tile, bool few) {         // S_t = Q_t K^T
             if (elected) {
                 const uint64_t kd = kd0 + tile * (T::TILE >> 4);
+                const uint32_t id = SINKS && few ? umma_idesc(kFewSinks, false) : id_s;
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k) {
                     const uint32_t off = (k / 4) * (T::PANEL >> 4) + (k % 4) * 2;
-                    umma1_ss(tm + t * BK, qd + t * (T::TILE >> 4) + off, kd + off, id_s, k != 0);
+                    umma1_ss(tm + t * BK, qd + t * (T::TILE >> 4) + off, kd + off, id, k != 0);
                 }
                 umma1_commit(s_full + 8 * t);
             }
             __syncwarp();
         };
         uint32_t np[2] = {0, 0}, uses[2] = {0, 0};         // probability tiles consumed and items begun, per query tile
-        auto issue_o = [&](int t, uint32_t tile, int half, bool begin, bool end) {     // O_t (+)= P_t V, 64 keys
+        auto issue_o = [&](int t, uint32_t tile, int half, bool begin, bool end, bool few) {     // O_t (+)= P_t V, 64 keys
             if (!wait_all(p_full + 16 * t + 8 * half, np[t] & 1)) return;
             tc_fence_after();
             if (elected) {
                 const uint64_t vd = vd0 + tile * (T::TILE >> 4);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    umma1_ts(tm + 2 * BK + t * 128, tm + t * BK + half * 32 + k * 8, vd + (half * 4 + k) * (2048 >> 4), id_o, !begin || half != 0 || k != 0);
+                    if (!SINKS || !few || half * 4 + k < kFewSinks / 16)
+                        umma1_ts(tm + 2 * BK + t * 128, tm + t * BK + half * 32 + k * 8, vd + (half * 4 + k) * (2048 >> 4), id_o, !begin || half != 0 || k != 0);
                 if (end) umma1_commit(o_full + 8 * t);
             }
             __syncwarp();
@@ -297,7 +314,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     wait_all(q_full + 8 * t, uses[t] & 1);
                     ++uses[t];
                     if (ok && w.lo[t] == w.first) {
-                        issue_s(t, k0);
+                        issue_s(t, k0, w.few<SINKS>(w.first, p.sinks));
                         if (w.hi[t] == w.first + 1 && elected) umma1_commit(q_empty + 8 * t);
                     }
                 }
@@ -306,17 +323,18 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const uint32_t v = next_pair(w, j), k = k_tile(v);
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const bool here = j >= w.lo[t] && j < w.hi[t], more = j + 1 < w.hi[t] && j + 1 >= w.lo[t];
+                    const bool here = w.takes<SINKS>(t, j), more = w.takes<SINKS>(t, j + 1);
                     if (here && ok) {
                         const bool begin = j == w.lo[t];
                         // the item before has read its O_t out
                         if (begin && !wait_all(o_empty + 8 * t, uses[t] & 1)) break;
-                        issue_o(t, v, 0, begin, false);
-                        if (ok) issue_o(t, v, 1, false, !more);
+                        const bool few = w.few<SINKS>(j, p.sinks);
+                        issue_o(t, v, 0, begin, false, few);
+                        if (ok) issue_o(t, v, 1, false, SINKS ? j + 1 == w.hi[t] : !more, few);
                         ++np[t];
                     }
                     if (more && ok) {
-                        issue_s(t, k);
+                        issue_s(t, k, w.few<SINKS>(j + 1, p.sinks));
                         if (j + 2 == w.hi[t] && elected) umma1_commit(q_empty + 8 * t);       // the last S of this tile: Q is free behind it
                     }
                 }
@@ -376,9 +394,34 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             __syncwarp();
             if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * half);
         };
-        for (int j = n0; j < n1; ++j, ++n) {
+        const int window = t == 0 ? w.window[0] : w.window[1];
+        for (int j = n0; j < n1; ++j) {
+            if (SINKS && j >= window && j != w.sinks_at) continue;
             if (!(ok = warp_wait(s_full + 8 * t, n & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
+            if (SINKS && w.few<SINKS>(j, p.sinks)) {
+                uint32_t s[kFewSinks], pk[kFewSinks / 2];
+                tmem_ld32(ts, s);
+                tmem_ld_wait();
+                hide_scores_sinks<kFewSinks>(s, key_lo, key_hi, p.sinks);
+                float top = __uint_as_float(s[0]);
+#pragma unroll
+                for (int c = 1; c < kFewSinks; ++c) top = fmaxf(top, __uint_as_float(s[c]));
+                top = PACK && !exists ? -INFINITY : top * p.scale_log2;
+                if (__any_sync(0xFFFFFFFFu, top > m + kRaise)) raise(top, j == n0);
+                const float base = m == -INFINITY ? 0.0f : m;
+                exp_scores<kFewSinks / 2>(s, pk, l2, c2, f2_pack(-base, -base));
+                tmem_st16(ts, pk);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(p_full + 16 * t);
+                    mbar_arrive(p_full + 16 * t + 8);
+                }
+                ++n;
+                continue;
+            }
             uint32_t s[128];
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, s + c * 32);
@@ -423,6 +466,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             exp_scores<32>(s + 64, pk, sum, c2, f2_pack(-base, -base));
             publish(1, pk);
             l2 = f2_add(l2, sum);
+            ++n;
         }
         if (!ok) break;
         float l;
