@@ -1,5 +1,6 @@
 """The library's calls as torch.autograd.Functions and modules: the linear layer whose three GEMMs run in UE5M3-FP4, and what
-stands between such linears in a transformer block (layer norm, attention, dropout added to the residual).
+stands between such linears in a transformer block (layer norm, norms and rotary positions of queries and keys, attention, dropout added
+to the residual).
 
 Nothing is computed here: forward and backward only call `quantize`, `gemm` and `sample_amax` of the C ABI in
 the order the recipe prescribes (X and W rounded to nearest even, the upstream gradient rounded stochastically
@@ -239,21 +240,89 @@ class DropoutAdd(torch.nn.Module):
 
 class _AttentionFn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, causal, window_left, k_lens, scale):
-        o, lse = B.attention(_as_heads(q), _as_heads(k), _as_heads(v), causal, window_left, k_lens, scale)
+    def forward(ctx, q, k, v, causal, window_left, k_lens, scale, sinks):
+        o, lse = B.attention(_as_heads(q), _as_heads(k), _as_heads(v), causal, window_left, k_lens, scale, None, sinks)
         ctx.save_for_backward(q, k, v, o, lse, k_lens)
-        ctx.args = causal, window_left, scale
+        ctx.args = causal, window_left, scale, sinks
         return o
 
     @staticmethod
     def backward(ctx, do):
         q, k, v, o, lse, k_lens = ctx.saved_tensors
-        causal, window_left, scale = ctx.args
-        grads = B.attention_backward(*(_as_heads(t) for t in (do, q, k, v)), o, lse, causal, window_left, k_lens, scale)
-        return *_once("attention", grads, do, q, k, v), None, None, None, None
+        causal, window_left, scale, sinks = ctx.args
+        grads = B.attention_backward(*(_as_heads(t) for t in (do, q, k, v)), o, lse, causal, window_left, k_lens, scale, None, sinks)
+        return *_once("attention", grads, do, q, k, v), None, None, None, None, None
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, window_left: int = -1,
-              k_lens: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
-    """Differentiable ue5m3_attention: o [batch, tokens, heads, head_dim] (arguments as in the binding's `attention`)."""
-    return _AttentionFn.apply(q, k, v, causal, window_left, k_lens, scale)
+              k_lens: Optional[torch.Tensor] = None, scale: Optional[float] = None, sinks: int = 0) -> torch.Tensor:
+    """Differentiable ue5m3_attention and ue5m3_attention_sinks: o [batch, tokens, heads, head_dim] (arguments as in the binding's
+    `attention`)."""
+    return _AttentionFn.apply(q, k, v, causal, window_left, k_lens, scale, sinks)
+
+
+def _as_turnable(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """[batch, tokens, heads, dim] in a form that the rotary calls take (a copy only where the strides leave no other way)."""
+    if t is None:
+        return None
+    ok = (t.stride(3) == 1 or t.shape[3] == 1) and all(t.shape[i] <= 1 or t.stride(i) > 0 for i in range(3))
+    return t if ok else t.clone(memory_format=torch.contiguous_format)
+
+
+class _RotaryFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, frequencies, positions, interleaved, amplitude, inverse):
+        ctx.args = frequencies, positions, interleaved, amplitude, not inverse
+        return B.rotary(_as_turnable(q), _as_turnable(k), frequencies, positions, interleaved, amplitude, inverse)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        return *_RotaryFn.apply(dq, dk, *ctx.args), None, None, None, None, None         # the transposed linear map, differentiable again
+
+
+def rotary(q: torch.Tensor, k: Optional[torch.Tensor], frequencies: torch.Tensor, positions=None, interleaved: bool = False,
+           amplitude: float = 1.0) -> tuple:
+    """Differentiable ue5m3_rotary (arguments as in the binding's `rotary`).  Positions are read again in the backward pass: leave a tensor of
+    them as it is until then."""
+    return _RotaryFn.apply(q, k, frequencies, positions, interleaved, amplitude, False)
+
+
+class _QKNormRotaryFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, frequencies, positions, interleaved, amplitude, eps):
+        ctx.save_for_backward(q, k, q_weight, k_weight)
+        ctx.args = frequencies, positions, interleaved, amplitude, eps
+        return B.qk_norm_rotary(_as_turnable(q), _as_turnable(k), q_weight, k_weight, *ctx.args)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        q, k, q_weight, k_weight = ctx.saved_tensors
+        grads = B.qk_norm_rotary_backward(_as_turnable(dq), _as_turnable(dk), _as_turnable(q), _as_turnable(k), q_weight, k_weight, *ctx.args,
+                                          want_weights=any(ctx.needs_input_grad[2:4]))
+        return *_once("qk_norm_rotary", grads, dq, dk, q, k, q_weight, k_weight), None, None, None, None, None
+
+
+def qk_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                   frequencies: torch.Tensor, positions=None, interleaved: bool = False, amplitude: float = 1.0, eps: float = 1e-6) -> tuple:
+    """Differentiable ue5m3_qk_norm_rotary (arguments as in the binding's `qk_norm_rotary`; positions as in `rotary`)."""
+    return _QKNormRotaryFn.apply(q, k, q_weight, k_weight, frequencies, positions, interleaved, amplitude, eps)
+
+
+class QKNormRotary(torch.nn.Module):
+    """Rotary positions of q and k, with learned norms of every head's row in front of them (`norm`).  `rotary_dim` (default: the whole head)
+    and the arguments of `rotary_frequencies` say which pairs turn how fast."""
+
+    def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, norm: bool = True, eps: float = 1e-6, interleaved: bool = False,
+                 device="cuda", dtype=torch.float32, **frequencies):
+        super().__init__()
+        self.q_weight, self.k_weight = (torch.nn.Parameter(torch.ones(head_dim, device=device, dtype=dtype)) if norm else None for _ in range(2))
+        self.norm, self.eps, self.interleaved = bool(norm), float(eps), bool(interleaved)
+        # not a buffer: a module that is cast to another type must keep its frequencies in 64 bits
+        self.frequencies, self.amplitude = B.rotary_frequencies(head_dim if rotary_dim is None else rotary_dim, device=device, **frequencies)
+
+    def forward(self, q: torch.Tensor, k: torch.Tensor, positions=None) -> tuple:
+        if self.frequencies.device != q.device:
+            self.frequencies = self.frequencies.to(q.device)
+        if not self.norm:
+            return rotary(q, k, self.frequencies, positions, self.interleaved, self.amplitude)
+        return qk_norm_rotary(q, k, self.q_weight, self.k_weight, self.frequencies, positions, self.interleaved, self.amplitude, self.eps)

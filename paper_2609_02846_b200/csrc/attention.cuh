@@ -339,7 +339,7 @@ inline bool make_heads_map(CUtensorMap* m, const ue5m3_heads& t, int64_t batch, 
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-inline AttentionParams attention_params(const ue5m3_attention_shape& s, int64_t sinks) {
+inline AttentionParams attention_params(const ue5m3_attention_shape& s, int64_t sinks = 0) {
     AttentionParams p{};
     p.q_len = (int)s.q_len; p.k_len = (int)s.k_len; p.heads = (int)s.heads; p.group = (int)(s.heads / s.kv_heads);
     p.kv_heads = (int)s.kv_heads; p.causal = s.causal; p.batch = (int)s.batch; p.k_lens = s.k_lens;

@@ -1,0 +1,137 @@
+"""AdamW as a torch optimizer: one launch per group and step over all its tensors (ue5m3_adamw), moments in 32 or in 8 bits, float32 master
+copies of bfloat16 weights.
+
+Nothing is computed here; states are made, handed over and kept.  Data-parallel replicas that start alike stay alike: the draws that 8-bit
+moments are rounded by depend on the seed, the parameter's place, the step and the element only, not on the rank."""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import binding as B
+
+
+class AdamW(torch.optim.Optimizer):
+    """w = w (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) for contiguous float32 and bfloat16 parameters.
+
+    `state_bits` 32 or 8 (m as E4M3, v as UE5M3, a float32 scale per 256 elements, rounded stochastically: 2 bytes per weight in place of 8).
+    `master_weights`: keep float32 copies of bfloat16 parameters (by default yes: bfloat16 alone loses updates below 2^-9 of a weight).  The copies are
+    made at a parameter's first step; call `take_over_weights()` when parameters were changed from outside after that.
+    `capturable`: the step is counted on the device, so that a captured `step()` goes on counting when it is replayed; take one step before the
+    capture, which makes the states.  Every parameter that has a gradient is then counted as having had one in every step, and lr and the other numbers stay
+    those of the capture."""
+
+    def __init__(self, params, lr: float = 1e-3, betas: tuple = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+                 state_bits: int = 32, master_weights: bool = True, capturable: bool = False, seed: int = 0):
+        if state_bits not in (8, 32):
+            raise ValueError(f"state_bits = {state_bits}: 8 or 32")
+        if not lr >= 0 or not weight_decay >= 0 or not (eps > 0 or (eps == 0 and state_bits == 32)) or not all(0 <= b < 1 for b in betas):
+            raise ValueError(f"lr {lr}, betas {betas}, eps {eps}, weight_decay {weight_decay}: out of range")
+        super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay, state_bits=state_bits,
+                                      master_weights=bool(master_weights), capturable=bool(capturable), seed=int(seed)))
+
+    def _begin(self, p: torch.Tensor, group: dict) -> dict:
+        """The state of a parameter before its first step."""
+        if p.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("take a step before the capture: a graph that makes the optimizer's states would make them anew at every replay")
+        if not p.is_contiguous():
+            raise ValueError("parameters have to be contiguous")
+        state = self.state[p]
+        if group["state_bits"] == 32:
+            state["m"], state["v"] = (torch.zeros(p.shape, dtype=torch.float32, device=p.device) for _ in range(2))
+        else:
+            blocks = -(-p.numel() // B.ADAMW_BLOCK)
+            state["m"], state["v"] = (torch.zeros(p.shape, dtype=torch.uint8, device=p.device) for _ in range(2))
+            state["m_scale"], state["v_scale"] = (torch.zeros(blocks, dtype=torch.float32, device=p.device) for _ in range(2))
+        if group["master_weights"] and p.dtype != torch.float32:
+            state["master"] = p.detach().float()
+        state["step"] = 0
+        return state
+
+    @torch.no_grad()
+    def step(self, closure=None, grad_scale: Optional[torch.Tensor] = None):
+        """One step.  `grad_scale`: float32 tensor of one value that the gradients are multiplied by (a clipping factor, the inverse of a loss
+        scale); where it is not finite the step changes nothing (without `capturable` it is counted all the same)."""
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        place = 0                                   # of a parameter among all: the stream of its draws
+        for group in self.param_groups:
+            todo = {}                               # (device, step): parameters
+            for p in group["params"]:
+                place += 1
+                if p.grad is None:
+                    continue
+                if p.grad.is_sparse:
+                    raise RuntimeError("sparse gradients are not supported")
+                state = self.state[p] or self._begin(p, group)
+                state["step"] += 1
+                todo.setdefault((p.device, 0 if group["capturable"] else state["step"]), []).append((p, state, place - 1))
+            for (device, step), some in todo.items():
+                ps, states, places = zip(*some)
+                clock = None
+                if group["capturable"]:
+                    clocks = group.setdefault("clocks", {})
+                    if device not in clocks:
+                        clocks[device] = torch.tensor([states[0]["step"] - 1, 0, 0, 0], dtype=torch.int64, device=device)
+                    clock = clocks[device]
+                elif device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("a captured step wants capturable=True: this one would repeat its own number at every replay")
+                col = lambda key: [s.get(key) for s in states]
+                eight = group["state_bits"] == 8
+                master = col("master")
+                B.adamw(ps, [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in ps], col("m"), col("v"), step, lr=group["lr"],
+                        betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
+                        master=master if any(x is not None for x in master) else None, m_scale=col("m_scale") if eight else None,
+                        v_scale=col("v_scale") if eight else None, grad_scale=grad_scale, seed=group["seed"], clock=clock, streams=places)
+                torch.autograd.graph.increment_version(ps)        # a backward pass that still wants the old weights says so
+        return loss
+
+    @torch.no_grad()
+    def take_over_weights(self) -> None:
+        """The master copies become what the parameters are now (weights that were loaded after the first step)."""
+        for p, state in self.state.items():
+            if "master" in state:
+                state["master"].copy_(p)
+
+    def state_dict(self) -> dict:
+        """As torch's; the number of the step on the device (capturable) comes out as each parameter's."""
+        for group in self.param_groups:
+            clocks = group.get("clocks") or {}
+            for p in group["params"]:
+                if p.device in clocks and self.state.get(p):
+                    self.state[p]["step"] = int(clocks[p.device][0])
+        d = super().state_dict()
+        d["state"] = {i: dict(state) for i, state in d["state"].items()}        # (tensors are the optimizer's own, as in torch)
+        for group in d["param_groups"]:
+            group.pop("clocks", None)
+        return d
+
+    def load_state_dict(self, state_dict: dict) -> None:
+        """States keep their own types (torch's way casts them to the parameter's), and tensors that are there are written in place, so that
+        captured graphs go on with what was loaded."""
+        clocks = [group.get("clocks") for group in self.param_groups]
+        old = {p: self.state[p] for group in self.param_groups for p in group["params"] if self.state.get(p)}
+        super().load_state_dict({**state_dict, "state": {}})
+        saved = [i for group in state_dict["param_groups"] for i in group["params"]]
+        for i, p in zip(saved, [p for group in self.param_groups for p in group["params"]]):
+            if i not in state_dict["state"]:
+                continue
+            new = {}
+            for key, value in state_dict["state"][i].items():
+                if torch.is_tensor(value):
+                    there = old.get(p, {}).get(key)
+                    if there is not None and there.shape == value.shape and there.dtype == value.dtype:
+                        there.copy_(value)
+                        value = there
+                    else:
+                        value = value.detach().to(p.device, copy=True)
+                new[key] = value
+            self.state[p] = new
+        for group, there in zip(self.param_groups, clocks):
+            if there:
+                group["clocks"] = there
+                for device, clock in there.items():
+                    clock[0] = max((self.state[p]["step"] for p in group["params"] if p.device == device and self.state.get(p)), default=0)
