@@ -589,7 +589,7 @@ def dropout_add(x: torch.Tensor, p: float, seed: int, residual: Optional[torch.T
 
 
 def _heads(t: torch.Tensor, shape, like: torch.Tensor) -> _Heads:
-    if _differs(t, shape, like):
+    if t is not like and _differs(t, shape, like):
         raise _unlike(t, shape, like)
     batch, token, head, one = t.stride()
     if one != 1 and shape[3] > 1:
@@ -713,8 +713,18 @@ def _pair(t: tuple, q: torch.Tensor, k: Optional[torch.Tensor]) -> tuple:
     return _heads(t[0], q.shape, q), None if k is None else _heads(t[1], k.shape, q)
 
 
-def _new_pair(q: torch.Tensor, k: Optional[torch.Tensor], out: Optional[tuple]) -> tuple:
-    return (q.new_empty(q.shape), None if k is None else k.new_empty(k.shape)) if out is None else out
+def _out_pair(q: torch.Tensor, k: Optional[torch.Tensor], out: Optional[tuple]) -> tuple:
+    """((q's, k's output), their C descriptions): new contiguous tensors unless given."""
+    if out is not None:
+        return out, _pair(out, q, k)
+    shape = q.shape
+    _, L, H, D = shape
+    a = q.new_empty(shape)
+    if k is None:
+        return (a, None), (_Heads(a.data_ptr(), L * H * D, H * D, D), None)
+    shape = k.shape
+    b, n = k.new_empty(shape), shape[2] * D
+    return (a, b), (_Heads(a.data_ptr(), L * H * D, H * D, D), _Heads(b.data_ptr(), L * n, n, D))
 
 
 def rotary(q: torch.Tensor, k: Optional[torch.Tensor], frequencies: torch.Tensor, positions=None, interleaved: bool = False,
@@ -724,8 +734,8 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], frequencies: torch.Tensor
     `frequencies` float64 (see rotary_frequencies).  `positions`: None (the tokens' indices), the first token's position, or an int32 / int64
     tensor [tokens] or [batch, tokens].  `inverse` turns back, which is the gradient.  `out` may be (q, k)."""
     shape = _rotary_shape(q, k, frequencies, positions, interleaved, amplitude)
-    out = _new_pair(q, k, out)
-    _call(_load().ue5m3_rotary, "ue5m3_rotary", q, shape, 1 if inverse else 0, *_pair((q, k), q, k), *_pair(out, q, k))
+    out, to = _out_pair(q, k, out)
+    _call(_load().ue5m3_rotary, "ue5m3_rotary", q, shape, 1 if inverse else 0, *_pair((q, k), q, k), *to)
     return out
 
 
@@ -745,9 +755,8 @@ def qk_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optiona
     None: 1), and turned as by `rotary`, whose other arguments these are."""
     shape = _rotary_shape(q, k, frequencies, positions, interleaved, amplitude)
     code = _norm_weights(q, q_weight, k_weight)
-    out = _new_pair(q, k, out)
-    _call(_load().ue5m3_qk_norm_rotary, "ue5m3_qk_norm_rotary", q, shape, *_pair((q, k), q, k), _ptr(q_weight), _ptr(k_weight), code, eps,
-          *_pair(out, q, k))
+    out, to = _out_pair(q, k, out)
+    _call(_load().ue5m3_qk_norm_rotary, "ue5m3_qk_norm_rotary", q, shape, *_pair((q, k), q, k), _ptr(q_weight), _ptr(k_weight), code, eps, *to)
     return out
 
 
@@ -760,7 +769,7 @@ def qk_norm_rotary_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: tor
     upstream gradients)."""
     shape = _rotary_shape(q, k, frequencies, positions, interleaved, amplitude)
     code = _norm_weights(q, q_weight, k_weight)
-    out = _new_pair(q, k, out)
+    out, to = _out_pair(q, k, out)
     dqw = q_weight.new_empty(q_weight.shape) if want_weights and q_weight is not None else None
     dkw = k_weight.new_empty(k_weight.shape) if want_weights and k_weight is not None else None
     lib = _load()
@@ -768,7 +777,7 @@ def qk_norm_rotary_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: tor
     if dqw is not None or dkw is not None:
         ws = q.new_empty(lib.ue5m3_qk_norm_rotary_backward_workspace_bytes(shape), dtype=torch.uint8)
     _call(lib.ue5m3_qk_norm_rotary_backward, "ue5m3_qk_norm_rotary_backward", q, shape, *_pair((dq, dk), q, k), *_pair((q, k), q, k),
-          _ptr(q_weight), _ptr(k_weight), code, eps, *_pair(out, q, k), _ptr(dqw), _ptr(dkw), _ptr(ws))
+          _ptr(q_weight), _ptr(k_weight), code, eps, *to, _ptr(dqw), _ptr(dkw), _ptr(ws))
     return *out, dqw, dkw
 
 
@@ -795,29 +804,32 @@ def adamw(params, grads, m, v, step: int = 1, lr: float = 1e-3, betas: tuple = (
     device = params[0].get_device()
     state = torch.uint8 if eight else torch.float32
 
-    def at(t, n, dtype, what, i):
-        if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
-            raise ValueError(f"{what}[{i}]: expected a contiguous tensor of {n} {dtype} on {params[0].device}, got [{tuple(t.shape)}, {t.dtype}, {t.device}]")
-        return t.data_ptr()
+    def column(ts, sizes, dtype, what) -> list:
+        """Addresses of a list of tensors (None: 0), each contiguous, of its size and type, on the first one's device."""
+        at = []
+        for t, n in zip(ts, sizes):
+            if t is None:
+                at.append(0)
+            elif (dtype is None or t.dtype is dtype) and t.numel() == n and t.is_contiguous() and t.get_device() == device:
+                at.append(t.data_ptr())
+            else:
+                raise ValueError(f"{what}[{len(at)}]: expected a contiguous tensor of {n} {dtype or 'values'} on {params[0].device}, got [{tuple(t.shape)}, {t.dtype}, {t.device}]")
+        return at
 
-    flat, seen = array("q"), set()
-    for i in range(count):
-        p, g = params[i], grads[i]
-        n = p.numel()
-        code = _dtype_code_of(p.dtype)
+    sizes = [p.numel() for p in params]
+    first = column(params, sizes, None, "params")
+    if len(set(first)) != count and len({x for x, n in zip(first, sizes) if n}) != sum(n > 0 for n in sizes):
+        raise ValueError("a tensor stands in params twice")
+    for i, (p, g) in enumerate(zip(params, grads)):
         if g.shape != p.shape:
             raise ValueError(f"grads[{i}] has shape {tuple(g.shape)}, params[{i}] {tuple(p.shape)}")
-        first = at(p, n, p.dtype, "params", i)
-        if n:
-            if first in seen:
-                raise ValueError(f"params[{i}] stands in the list twice")
-            seen.add(first)
-        copy = None if master is None else master[i]
-        blocks = -(-n // ADAMW_BLOCK)
-        flat.extend((first, at(g, n, g.dtype, "grads", i), 0 if copy is None else at(copy, n, torch.float32, "master", i),
-                     at(m[i], n, state, "m", i), at(v[i], n, state, "v", i),
-                     at(m_scale[i], blocks, torch.float32, "m_scale", i) if eight else 0, at(v_scale[i], blocks, torch.float32, "v_scale", i) if eight else 0,
-                     n, ((i if streams is None else streams[i]) & 0xFFFFFFFF) | code << 32 | _dtype_code(g) << 40))
+    none = [0] * count
+    blocks = [-(-n // ADAMW_BLOCK) for n in sizes] if eight else none
+    rows = zip(first, column(grads, sizes, None, "grads"), none if master is None else column(master, sizes, torch.float32, "master"),
+               column(m, sizes, state, "m"), column(v, sizes, state, "v"), column(m_scale, blocks, torch.float32, "m_scale") if eight else none,
+               column(v_scale, blocks, torch.float32, "v_scale") if eight else none, sizes,
+               [(x & 0xFFFFFFFF) | _dtype_code(p) << 32 | _dtype_code(g) << 40 for x, p, g in zip(range(count) if streams is None else streams, params, grads)])
+    flat = array("q", [x for row in rows for x in row])
     for t, what in ((grad_scale, "grad_scale"), (clock, "clock")):
         if t is not None and t.get_device() != device:
             raise ValueError(f"{what} is on {t.device}, the params on {params[0].device}")

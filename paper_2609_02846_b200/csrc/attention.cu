@@ -28,7 +28,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <type_traits>
 #include "../../include/ue5m3.h"
 #include "attention.cuh"
 #include "block_ops.h"
@@ -73,7 +72,7 @@ struct Item {
     int lo[2], hi[2];                                     // key tiles of the two query tiles
     int first, last;                                      // ... and of both together
     // SINKS: tiles are counted from `base`, the windows' first one, and behind the windows' last comes tile 0 as number `sinks_at` (-1: it does not), for
-    // the query tiles that do not see it in their window.  lo .. hi[t] has the tiles lo .. window[t] and that one.
+    // the sinks that lie in front of a row's window.  lo .. hi[t] has the tiles lo .. window[t] and that one.
     int base, sinks_at, window[2];
     __device__ __forceinline__ bool on(int t) const { return hi[t] > lo[t]; }
     template <bool SINKS> __device__ __forceinline__ int key_tile(int j) const { return !SINKS ? j : j == sinks_at ? 0 : base + j; }
@@ -132,7 +131,7 @@ __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int
         for (int t = 0; t < 2; ++t) {
             const int r0 = PACK ? 0 : w.q0 + t * BQ, r1 = min(r0 + BQ, p.q_len) - 1;
             const bool sees = (PACK ? w.h + t * p.pack < w.h_end : r0 < p.q_len) && p.key_hi(r1, w.keys) > 0, any = w.on(t);
-            const bool apart = w.part == 0 && sees && !(any && w.lo[t] == 0);           // (the first part has tile 0)
+            const bool apart = w.part == 0 && sees && p.key_lo(r1) > 0;                 // (the first part has tile 0)
             w.window[t] = any ? w.hi[t] - w.base : 0;
             w.lo[t] = any ? w.lo[t] - w.base : last;
             w.hi[t] = apart ? last + 1 : any ? w.window[t] : w.lo[t];
@@ -262,10 +261,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (++slot == T::PAIRS) { slot = 0; phase ^= 1; }
             // values behind the sequence's end and in front of every window may hold anything: they become zeros
             const int at = w.key_tile<SINKS>(j) * BK, from = p.first_key - at, valid = w.keys - at;
-            if (j >= w.first && ((p.k_lens && valid < BK) || from > 0)) {
-                if constexpr (SINKS) keep_rows_sinks<DP>(smem_gen + (2 + v_tile) * T::TILE, from, valid, at == 0 ? p.sinks : 0, lane);
-                else keep_rows<DP>(smem_gen + (2 + v_tile) * T::TILE, from, valid, lane);
-            }
+            const bool sinks = SINKS && j == w.sinks_at;
+            if (j >= w.first && ((p.k_lens && valid < BK) || from > 0))
+                keep_rows<DP>(smem_gen + (2 + v_tile) * T::TILE, sinks ? 0 : from, sinks ? min(valid, p.sinks) : valid, lane);
             const uint32_t v = v_tile;
             v_tile = v + 2 >= T::RING ? v + 2 - T::RING : v + 2;
             return v;
@@ -362,7 +360,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const int r0 = PACK ? 0 : w.q0 + t * BQ, r_last = PACK ? p.q_len - 1 : r0 + BQ - 1;
         const int h = PACK ? w.h + t * p.pack + r_head : w.h, row = r0 + r_query;
         const bool exists = PACK ? r_head < p.pack && h < w.h_end : row < p.q_len;
-        const int key_lo = p.key_lo(row), key_hi = p.key_hi(row, w.keys);
+        const int key_lo = p.key_lo(row), key_hi = p.key_hi(row, w.keys), sinks_hi = SINKS ? p.sinks_hi(row, w.keys) : 0;
         const int n0 = t == 0 ? w.lo[0] : w.lo[1], n1 = t == 0 ? w.hi[0] : w.hi[1];
         // key tiles [plain_lo, plain_hi) are seen whole by every row of the tile
         const int plain_lo = p.left >= 0 ? (p.key_lo(r_last) + BK - 1) / BK : 0;
@@ -403,7 +401,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 uint32_t s[kFewSinks], pk[kFewSinks / 2];
                 tmem_ld32(ts, s);
                 tmem_ld_wait();
-                hide_scores_sinks<kFewSinks>(s, key_lo, key_hi, p.sinks);
+                hide_scores<kFewSinks>(s, 0, sinks_hi, false);
                 float top = __uint_as_float(s[0]);
 #pragma unroll
                 for (int c = 1; c < kFewSinks; ++c) top = fmaxf(top, __uint_as_float(s[c]));
@@ -427,14 +425,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, s + c * 32);
             tmem_ld_wait();
             const int tile = w.key_tile<SINKS>(j);
-            const bool masked = tile < plain_lo || tile >= plain_hi;
-            const int from = key_lo - tile * BK, to = key_hi - tile * BK;      // columns of this tile that the row sees
-            auto hide = [&](auto cols, uint32_t* x) {
-                constexpr int N = decltype(cols)::value;
-                if (SINKS && tile == 0) hide_scores_sinks<N>(x, from, to, p.sinks);
-                else hide_scores<N>(x, from, to, p.left >= 0);
-            };
-            if (masked) hide(std::integral_constant<int, 128>(), s);
+            const bool sinks = SINKS && j == w.sinks_at, masked = sinks || tile < plain_lo || tile >= plain_hi;
+            const int from = sinks ? 0 : key_lo - tile * BK, to = sinks ? sinks_hi : key_hi - tile * BK;       // columns of this tile that the row sees
+            if (masked) hide_scores<128>(s, from, to, p.left >= 0);
             uint32_t pk[32];
             float base = m == -INFINITY ? 0.0f : m;
             // The first half's exponentials are taken against the maximum so far, while this tile's is being found: it raises the
@@ -459,7 +452,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 tmem_ld32(ts, again);
                 tmem_ld32(ts + 32, again + 32);
                 tmem_ld_wait();
-                if (masked) hide(std::integral_constant<int, 64>(), again);
+                if (masked) hide_scores<64>(again, from, to, p.left >= 0);
                 exp_scores<32>(again, pk, sum, c2, f2_pack(-base, -base));
             }
             publish(0, pk);

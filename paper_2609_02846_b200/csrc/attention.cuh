@@ -115,12 +115,6 @@ __device__ __forceinline__ void hide_scores(uint32_t* s, int from, int to, bool 
         for (int c = 0; c < N; ++c) s[c] = c < to ? s[c] : 0xFF800000u;
     }
 }
-// The same in the key tile that holds the first keys of all: columns below `sinks` stay too.
-template <int N>
-__device__ __forceinline__ void hide_scores_sinks(uint32_t* s, int from, int to, int sinks) {
-#pragma unroll
-    for (int c = 0; c < N; ++c) s[c] = (c >= from || c < sinks) && c < to ? s[c] : 0xFF800000u;
-}
 __device__ __forceinline__ f32x2 ex2_pair(f32x2 x) {
     float a, b;
     f2_unpack(x, a, b);
@@ -168,16 +162,6 @@ __device__ __forceinline__ void hide_pairs(f32x2* p, int from, int to, bool lowe
             f2_unpack(p[i], a, b);
             p[i] = f2_pack(2 * i >= from ? a : 0.0f, 2 * i + 1 >= from ? b : 0.0f);
         }
-    }
-}
-// The same in the key tile that holds the first keys of all: columns below `sinks` stay too.
-template <int N>
-__device__ __forceinline__ void hide_pairs_sinks(f32x2* p, int from, int to, int sinks) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float a, b;
-        f2_unpack(p[i], a, b);
-        p[i] = f2_pack((2 * i >= from || 2 * i < sinks) && 2 * i < to ? a : 0.0f, (2 * i + 1 >= from || 2 * i + 1 < sinks) && 2 * i + 1 < to ? b : 0.0f);
     }
 }
 // x where p is not zero (0 * NaN would be NaN where a pair does not exist)
@@ -272,17 +256,6 @@ __device__ __forceinline__ void keep_rows(uint8_t* tile, int from, int to, int l
     __syncwarp();
 }
 
-// The same with rows below `sinks` kept too.
-template <int DP>
-__device__ __forceinline__ void keep_rows_sinks(uint8_t* tile, int from, int to, int sinks, int lane) {
-    for (int i = lane; i < 128 * (DP / 8); i += 32) {
-        const int r = i / (DP / 8), c = i % (DP / 8);
-        if ((r < from && r >= sinks) || r >= to) *reinterpret_cast<uint4*>(tile + (c / 8) * (128 * 128) + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
-    }
-    fence_proxy_async();
-    __syncwarp();
-}
-
 // ----------------------------------------------------------------------------- which pairs exist
 struct AttentionParams {
     int q_len, k_len, heads, group;      // group = heads per key/value head
@@ -321,6 +294,8 @@ struct AttentionParams {
     // With sinks (SINKS): every query from query_lo on sees the first keys, and with them every query sees some key if there are any.
     template <bool SINKS> __host__ __device__ __forceinline__ int queries_end_of(int keys) const { return SINKS ? q_len : queries_end(keys); }
     template <bool SINKS> __host__ __device__ __forceinline__ int query_hi_of(int j) const { return SINKS && j < sinks ? q_len : query_hi(j); }
+    // Where keys are walked, a query sees its window, and apart from that the keys from 0 up to here: sinks in front of the window.
+    __host__ __device__ __forceinline__ int sinks_hi(int i, int keys) const { return min(min(sinks, key_lo(i)), key_hi(i, keys)); }
 };
 
 // ----------------------------------------------------------------------------- host side

@@ -449,8 +449,8 @@ template <int DP> struct QuerySmem {
 };
 constexpr uint32_t COL_Q = 384, COL_DO = 448;                         // in place of the second accumulator
 
-// PARTS: a CTA takes a share of the keys and leaves a binary32 sum for attention_sum_kernel.  SINKS: key tile 0 comes in front of the
-// window's where that does not begin with it.
+// PARTS: a CTA takes a share of the keys and leaves a binary32 sum for attention_sum_kernel.  SINKS: key tile 0 comes in front of
+// the window's.
 template <int DP, bool PARTS, bool SINKS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
@@ -482,9 +482,9 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             lo = max(lo, (int)((int64_t)n * part / p.parts));
             hi = max(min(hi, (int)((int64_t)n * (part + 1) / p.parts)), lo);
         }
-        if (SINKS && part == 0 && z > 0 && hi == lo) { lo = 0; hi = 1; }       // no key in any window: tile 0 alone
     }
-    const int front = SINKS && part == 0 && lo > 0 && hi > lo;
+    // SINKS: tile 0 comes first, for the sinks that lie in front of a row's window (and again where that begins in it)
+    const int front = SINKS && part == 0 && p.key_hi(i1, keys) > 0 && p.key_lo(i1) > 0;
     const int steps = hi - lo + front;
     auto key_tile = [&](int it) { return SINKS ? (front && it == 0 ? 0 : lo + it - front) : lo + it; };
 
@@ -548,11 +548,9 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         };
         auto clean_k = [&](int it, uint32_t s) {
             // keys behind the sequence's end and in front of every window may hold anything (dS is zero there): they become zeros
-            const int at = (SINKS && lead && it == 0 ? 0 : first + it - lead) * B128, from = p.first_key - at, valid = n_keys - at;
-            if ((p.k_lens && valid < B128) || from > 0) {
-                if constexpr (SINKS) keep_rows_sinks<DP>(smem_gen + s * T::TILE, from, valid, at == 0 ? p.sinks : 0, lane);
-                else keep_rows<DP>(smem_gen + s * T::TILE, from, valid, lane);
-            }
+            const bool sinks = SINKS && lead && it == 0;
+            const int at = (sinks ? 0 : first + it - lead) * B128, from = p.first_key - at, valid = n_keys - at;
+            if ((p.k_lens && valid < B128) || from > 0) keep_rows<DP>(smem_gen + s * T::TILE, sinks ? 0 : from, sinks ? min(valid, p.sinks) : valid, lane);
         };
         uint32_t k0 = 0, k1 = 0, k2 = 0;                   // slots of K(it), K(it + 1), K(it + 2)
         auto issue_s = [&](int it) {
@@ -596,7 +594,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         const int g = (warp - 4) >> 2, q = warp & 3;
         const int row = i0 + q * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
-        const int k_lo = p.key_lo(row), k_hi = p.key_hi(row, keys);
+        const int k_lo = p.key_lo(row), k_hi = p.key_hi(row, keys), sinks_hi = SINKS ? p.sinks_hi(row, keys) : 0;
         const int plain_lo = p.left >= 0 ? (p.key_lo(i0 + B128 - 1) + B128 - 1) / B128 : 0;
         const int plain_hi = max(p.key_hi(i0, keys), 0) / B128;
         const bool idle_queries = i0 < p.first_query || i1 >= p.queries_end_of<SINKS>(keys);
@@ -624,8 +622,9 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         }
         for (int it = 0; ok && it < steps; ++it) {
             const int kt = key_tile(it);
-            const bool plain = kt >= plain_lo && kt < plain_hi;
-            const int base = kt * B128 + g * 64 - k_lo, width = k_hi - k_lo;
+            const bool sinks = SINKS && front && it == 0, plain = !sinks && kt >= plain_lo && kt < plain_hi;
+            // columns from <= column < to are seen
+            const int from = sinks ? 0 : k_lo - kt * B128 - g * 64, to = (sinks ? sinks_hi : k_hi - kt * B128) - g * 64;
             const uint32_t ts = lane_base + COL_S + g * 64, td = lane_base + COL_DP + g * 64;
             if (!(ok = warp_wait(s_full, it & 1, abort_flag, p.wait_limit))) break;
             tc_fence_after();
@@ -639,10 +638,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             f32x2 pr[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) pr[i] = ex2_pair(f2_fma(pair_of(s + 2 * i), c2, nl2));
-            if (!plain) {
-                if (SINKS && kt == 0) hide_pairs_sinks<32>(pr, -base, width - base, p.sinks - g * 64);
-                else hide_pairs<32>(pr, -base, width - base, p.left >= 0, true);
-            }
+            if (!plain) hide_pairs<32>(pr, from, to, p.left >= 0, true);
             // values, and dO of queries, that take no part may be NaN, and so then is dP
             const bool idle = (p.k_lens && (kt + 1) * B128 > keys) || kt * B128 < p.first_key || idle_queries;
             if (!(ok = warp_wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
