@@ -425,9 +425,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, s + c * 32);
             tmem_ld_wait();
             const int tile = w.key_tile<SINKS>(j);
-            const bool sinks = SINKS && j == w.sinks_at, masked = sinks || tile < plain_lo || tile >= plain_hi;
+            const bool sinks = SINKS && j == w.sinks_at, lower = !sinks && tile < plain_lo, upper = sinks || tile >= plain_hi;
             const int from = sinks ? 0 : key_lo - tile * BK, to = sinks ? sinks_hi : key_hi - tile * BK;       // columns of this tile that the row sees
-            if (masked) hide_scores<128>(s, from, to, p.left >= 0);
+            if constexpr (SINKS) hide_scores_by<128>(s, from, to, lower, upper);
+            else if (lower || upper) hide_scores<128>(s, from, to, p.left >= 0);
             uint32_t pk[32];
             float base = m == -INFINITY ? 0.0f : m;
             // The first half's exponentials are taken against the maximum so far, while this tile's is being found: it raises the
@@ -452,7 +453,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 tmem_ld32(ts, again);
                 tmem_ld32(ts + 32, again + 32);
                 tmem_ld_wait();
-                if (masked) hide_scores<64>(again, from, to, p.left >= 0);
+                if constexpr (SINKS) hide_scores_by<64>(again, from, to, lower, upper);
+                else if (lower || upper) hide_scores<64>(again, from, to, p.left >= 0);
                 exp_scores<32>(again, pk, sum, c2, f2_pack(-base, -base));
             }
             publish(0, pk);

@@ -349,7 +349,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         for (int it = 0; it < steps; ++it) {
             const int qt = lo + it % per_head;
             const float* rows = reinterpret_cast<const float*>(smem_gen + M::ROWS + (it % M::STAGES) * 1024) + g * 64;
-            const bool plain = qt >= plain_lo && qt < plain_hi;
+            const bool cut_lo = p.causal && qt < plain_lo, cut_hi = upper && (qt >= plain_hi || j0 + B128 > keys);
             const int base = qt * B128 + g * 64 - q_lo, width = q_hi - q_lo;
             if (!(ok = warp_wait(s_full, it & 1, abort_flag, p.wait_limit))) break;
             // this query tile's rows of lse2 and delta came with Q, whose barrier S waited for; seen by every thread
@@ -368,7 +368,7 @@ attention_keys_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     pr[c / 2] = ex2_pair(f2_fma(pair_of(s + c), c2, e.x));
                     pr[c / 2 + 1] = ex2_pair(f2_fma(pair_of(s + c + 2), c2, e.y));
                 }
-                if (!plain) hide_pairs<16>(pr + half * 16, -base - half * 32, width - base - half * 32, p.causal, upper);
+                if (cut_lo || cut_hi) hide_pairs<16>(pr + half * 16, -base - half * 32, width - base - half * 32, cut_lo, cut_hi);
                 uint32_t pk[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) pk[i] = pack_pair(pr[half * 16 + i]);
@@ -622,7 +622,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         }
         for (int it = 0; ok && it < steps; ++it) {
             const int kt = key_tile(it);
-            const bool sinks = SINKS && front && it == 0, plain = !sinks && kt >= plain_lo && kt < plain_hi;
+            const bool sinks = SINKS && front && it == 0, lower = !sinks && kt < plain_lo, upper = sinks || kt >= plain_hi;
             // columns from <= column < to are seen
             const int from = sinks ? 0 : k_lo - kt * B128 - g * 64, to = (sinks ? sinks_hi : k_hi - kt * B128) - g * 64;
             const uint32_t ts = lane_base + COL_S + g * 64, td = lane_base + COL_DP + g * 64;
@@ -638,7 +638,7 @@ attention_queries_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             f32x2 pr[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) pr[i] = ex2_pair(f2_fma(pair_of(s + 2 * i), c2, nl2));
-            if (!plain) hide_pairs<32>(pr, from, to, p.left >= 0, true);
+            if (lower || upper) hide_pairs<32>(pr, from, to, lower, upper);
             // values, and dO of queries, that take no part may be NaN, and so then is dP
             const bool idle = (p.k_lens && (kt + 1) * B128 > keys) || kt * B128 < p.first_key || idle_queries;
             if (!(ok = warp_wait(dp_full, it & 1, abort_flag, p.wait_limit))) break;
