@@ -427,7 +427,8 @@ UE5M3_API int ue5m3_attention_sinks_backward(const ue5m3_attention_shape* shape,
  *   elements, positive where the dimension is larger than 1; pointers aligned to their element.  kv_heads = 0: no k (its pointers may be null).
  *   An output may be its own input (same pointer and strides) and else has no element in common with an input or the other output
  *   (UE5M3_ERR_INVALID_ARG where that is found out, as for all views of one buffer).
- *   Rows whose pairs can be read by 16 (8, 4) bytes throughout are: pointers, strides, head_dim / 2 and, without `interleaved`, rotary_dim / 2.
+ *   Rows are read four pairs at a time (two vectors of 8 bytes in BF16, of 16 in binary32) where pointers, strides, head_dim / 2 and, without
+ *   `interleaved`, rotary_dim / 2 are multiples of 4 elements; else two pairs or one.
  */
 typedef struct {
     int64_t batch, tokens, heads, kv_heads;

@@ -581,7 +581,8 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas<T, VEC>) rotary_backwa
                 read_weights(weights.w[side], l, w);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const float r = rsqrtf(fmaf(sum[2 * u], p.inv_dim, p.eps));
+                    const bool exists = head < sd.heads;   // (else a row of zeros, whose root is 0 with an eps of 0)
+                    const float r = exists ? rsqrtf(fmaf(sum[2 * u], p.inv_dim, p.eps)) : 0.0f;
                     const f32x2 r2 = twice(r), m2 = twice(-(sum[2 * u + 1] * r * p.inv_dim));
                     Pairs<P> d;
 #pragma unroll
@@ -593,7 +594,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas<T, VEC>) rotary_backwa
                         d.a[i] = f2_mul(f2_fma(e[u].a[i], w.a[i], f2_mul(f[u].a[i], m2)), r2);
                         d.b[i] = f2_mul(f2_fma(e[u].b[i], w.b[i], f2_mul(f[u].b[i], m2)), r2);
                     }
-                    if (head < sd.heads) store_row<T, VEC, NU, NEIGHBOURS>(to, d, l);
+                    if (exists) store_row<T, VEC, NU, NEIGHBOURS>(to, d, l);
                     head += slots;
                     to += sd.group_stride_out;
                 }
@@ -671,7 +672,7 @@ cudaError_t run(const RotaryArgs& a, RotaryParams& p, cudaStream_t st) {
     // The heads of a token are shared out where that makes the longest warp's work shorter: rounds of items times batches of an item, with
     // what every item costs besides (angles, addresses) taken as one batch.
     int64_t least = INT64_MAX;
-    for (int n = 1; n <= pieces; ++n) {
+    for (int n = 1; n <= pieces; n = n < 32 ? n + 1 : n < pieces && 2 * n > pieces ? pieces : 2 * n) {
         const int64_t cost = (rows * n + warps - 1) / warps * ((pieces + n - 1) / n + 1);
         if (cost < least) {
             least = cost;

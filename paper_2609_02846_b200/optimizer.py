@@ -75,6 +75,8 @@ class AdamW(torch.optim.Optimizer):
                 if group["capturable"]:
                     clocks = group.setdefault("clocks", {})
                     if device not in clocks:
+                        if device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+                            raise RuntimeError("take a step before the capture: it makes the counter on the device")
                         clocks[device] = torch.tensor([states[0]["step"] - 1, 0, 0, 0], dtype=torch.int64, device=device)
                     clock = clocks[device]
                 elif device.type == "cuda" and torch.cuda.is_current_stream_capturing():

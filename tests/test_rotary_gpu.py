@@ -179,6 +179,22 @@ def test_no_tokens_and_rows_of_zeros():
     assert bool(out[0].isfinite().all()) and not out[2].any()
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_an_eps_of_zero_with_heads_left_over(dtype):
+    """Places in a warp that no head takes hold zeros: their root is zero, and nothing of them reaches the weights' gradients."""
+    B, L, H, Hk, D = 2, 9, 5, 3, 64
+    q, k = _inputs(B, L, H, Hk, D, dtype)
+    dq, dk = _inputs(B, L, H, Hk, D, dtype, seed=5)
+    w = 1 + 0.3 * torch.randn(D, generator=_gen(2), device=DEV)
+    f, _ = lib.rotary_frequencies(D)
+    pos = torch.arange(L, device=DEV)[None].expand(B, L)
+    out = lib.qk_norm_rotary_backward(dq, dk, q, k, w, w, f, eps=0.0)
+    for i, (x, dy, heads) in enumerate(((q, dq, H), (k, dk, Hk))):
+        (dx, bound), (dw, bound_dw) = ref.qk_norm_rotary_backward(dy, x, w, f, pos, False, 1.0, 0.0, _chain(B, L, heads))
+        assert_within(out[i], dx, bound)
+        assert_within(out[2 + i], dw, bound_dw)
+
+
 @pytest.mark.parametrize("neighbours", [False, True])
 @pytest.mark.parametrize("R", [64, 40])
 def test_what_is_not_turned_is_kept_as_it_is(neighbours, R):
@@ -206,6 +222,15 @@ def test_gradients_against_differences():
     for slope, want in (((loss(q + h * along_q, w) - loss(q - h * along_q, w)) / (2 * h), (dq.double() * along_q.double()).sum()),
                         ((loss(q, w + h * along_w) - loss(q, w - h * along_w)) / (2 * h), (dw.double() * along_w.double()).sum())):
         assert abs(float(slope / want) - 1) < 1e-2
+
+
+def test_very_many_heads():
+    """More of them than fit any batch, shared out among warps."""
+    q, k = _inputs(1, 2, 700, 1, 32, BF, fused=False)
+    f, _ = lib.rotary_frequencies(32)
+    pos = torch.arange(2, device=DEV)[None]
+    for got, x in zip(lib.rotary(q, k, f), (q, k)):
+        assert_within(got, *ref.rotary(x, f, pos))
 
 
 def test_graphs_and_other_streams():
