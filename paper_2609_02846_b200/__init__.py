@@ -1,5 +1,5 @@
 """UE5M3-FP4 quantize-and-multiply hot path for NVIDIA B200 (sm_100a), and the operators that stand between such linears in a
-transformer block (layer norm, dropout on the residual, attention).
+transformer block (layer norm, dropout on the residual, norms and rotary positions of queries and keys, attention) and the AdamW step.
 
 The work is done by hand-written CUDA kernels behind the C ABI declared in ``include/ue5m3.h``
 (``libue5m3.so``).  This package only marshals arguments: torch supplies device memory and streams.
