@@ -782,6 +782,7 @@ def qk_norm_rotary_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: tor
 
 
 ADAMW_BLOCK = 256           # elements that share a scale of 8-bit moments
+_NUMBERS = {torch.float32: F32, torch.bfloat16: BF16}
 ADAMW_CLOCK_BYTES = 32
 
 
@@ -804,31 +805,42 @@ def adamw(params, grads, m, v, step: int = 1, lr: float = 1e-3, betas: tuple = (
     device = params[0].get_device()
     state = torch.uint8 if eight else torch.float32
 
-    def column(ts, sizes, dtype, what) -> list:
-        """Addresses of a list of tensors (None: 0), each contiguous, of its size and type, on the first one's device."""
-        at = []
-        for t, n in zip(ts, sizes):
-            if t is None:
-                at.append(0)
-            elif (dtype is None or t.dtype is dtype) and t.numel() == n and t.is_contiguous() and t.get_device() == device:
-                at.append(t.data_ptr())
-            else:
-                raise ValueError(f"{what}[{len(at)}]: expected a contiguous tensor of {n} {dtype or 'values'} on {params[0].device}, got [{tuple(t.shape)}, {t.dtype}, {t.device}]")
+    def column(ts, sizes, types, what) -> list:
+        """Addresses of a list of tensors, each contiguous, of its size and one of the types, on the first one's device."""
+        at = [t.data_ptr() for t, n in zip(ts, sizes) if t.dtype in types and t.numel() == n and t.is_contiguous() and t.get_device() == device]
+        if len(at) != count:
+            for i, (t, n) in enumerate(zip(ts, sizes)):
+                if len(types) > 1:
+                    _dtype_code(t)
+                if t.dtype not in types or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+                    raise ValueError(f"{what}[{i}]: expected a contiguous tensor of {n} values of {types} on {params[0].device}, got [{tuple(t.shape)}, {t.dtype}, {t.device}]")
         return at
 
-    sizes = [p.numel() for p in params]
-    first = column(params, sizes, None, "params")
+    sizes, none = [p.numel() for p in params], [0] * count
+    first = column(params, sizes, _NUMBERS, "params")
     if len(set(first)) != count and len({x for x, n in zip(first, sizes) if n}) != sum(n > 0 for n in sizes):
         raise ValueError("a tensor stands in params twice")
-    for i, (p, g) in enumerate(zip(params, grads)):
-        if g.shape != p.shape:
-            raise ValueError(f"grads[{i}] has shape {tuple(g.shape)}, params[{i}] {tuple(p.shape)}")
-    none = [0] * count
-    blocks = [-(-n // ADAMW_BLOCK) for n in sizes] if eight else none
-    rows = zip(first, column(grads, sizes, None, "grads"), none if master is None else column(master, sizes, torch.float32, "master"),
-               column(m, sizes, state, "m"), column(v, sizes, state, "v"), column(m_scale, blocks, torch.float32, "m_scale") if eight else none,
-               column(v_scale, blocks, torch.float32, "v_scale") if eight else none, sizes,
-               [(x & 0xFFFFFFFF) | _dtype_code(p) << 32 | _dtype_code(g) << 40 for x, p, g in zip(range(count) if streams is None else streams, params, grads)])
+    at_grads = column(grads, sizes, _NUMBERS, "grads")
+    if [g.shape for g in grads] != [p.shape for p in params]:
+        raise ValueError("params and grads have different shapes")
+    copies = none
+    if master is not None:
+        some = [i for i, t in enumerate(master) if t is not None]
+        if len(some) == count:
+            copies = column(master, sizes, (torch.float32,), "master")
+        else:
+            copies = list(none)
+            for i in some:
+                t = master[i]
+                if t.dtype is not torch.float32 or t.numel() != sizes[i] or not t.is_contiguous() or t.get_device() != device:
+                    raise ValueError(f"master[{i}]: expected a contiguous tensor of {sizes[i]} float32 on {params[0].device}, got [{tuple(t.shape)}, {t.dtype}, {t.device}]")
+                copies[i] = t.data_ptr()
+    scales = none, none
+    if eight:
+        blocks = [-(-n // ADAMW_BLOCK) for n in sizes]
+        scales = column(m_scale, blocks, (torch.float32,), "m_scale"), column(v_scale, blocks, (torch.float32,), "v_scale")
+    kinds = [(x & 0xFFFFFFFF) | _NUMBERS[p.dtype] << 32 | _NUMBERS[g.dtype] << 40 for x, p, g in zip(range(count) if streams is None else streams, params, grads)]
+    rows = zip(first, at_grads, copies, column(m, sizes, (state,), "m"), column(v, sizes, (state,), "v"), *scales, sizes, kinds)
     flat = array("q", [x for row in rows for x in row])
     for t, what in ((grad_scale, "grad_scale"), (clock, "clock")):
         if t is not None and t.get_device() != device:
