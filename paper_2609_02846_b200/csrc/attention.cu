@@ -82,7 +82,7 @@ struct Item {
 };
 // Heads fastest (heads that share keys run side by side), long query tiles first.
 // SINKS: key tile 0 comes behind the tiles of the windows.  2 x 4096 tokens with a window of 1023: 183 us (in front of them, or in front of the last one, the
-// same; all 128 of its keys in place of 32 186), without sinks 157: a step of its own, of which there are nine, and 6 % for the tiles' numbers.
+// same; all 128 of its keys in place of 32 186), without sinks 164: a step of its own, of which there are nine.
 template <bool PARTS, bool PACK, bool SINKS>
 __device__ __forceinline__ Item item_of(const AttentionParams& p, int index, int q_tiles) {
     Item w;
