@@ -589,7 +589,7 @@ def dropout_add(x: torch.Tensor, p: float, seed: int, residual: Optional[torch.T
 
 
 def _heads(t: torch.Tensor, shape, like: torch.Tensor) -> _Heads:
-    if t is not like and _differs(t, shape, like):
+    if t.shape != shape or (t is not like and _differs(t, shape, like)):       # (`like` itself may stand where another shape is wanted)
         raise _unlike(t, shape, like)
     batch, token, head, one = t.stride()
     if one != 1 and shape[3] > 1:
