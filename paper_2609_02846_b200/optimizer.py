@@ -67,8 +67,7 @@ class AdamW(torch.optim.Optimizer):
                 if p.grad.is_sparse:
                     raise RuntimeError("sparse gradients are not supported")
                 state = self.state[p] or self._begin(p, group)
-                state["step"] += 1
-                todo.setdefault((p.device, 0 if group["capturable"] else state["step"]), []).append((p, state, place - 1))
+                todo.setdefault((p.device, 0 if group["capturable"] else state["step"] + 1), []).append((p, state, place - 1))
             for (device, step), some in todo.items():
                 ps, states, places = zip(*some)
                 clock = None
@@ -77,7 +76,7 @@ class AdamW(torch.optim.Optimizer):
                     if device not in clocks:
                         if device.type == "cuda" and torch.cuda.is_current_stream_capturing():
                             raise RuntimeError("take a step before the capture: it makes the counter on the device")
-                        clocks[device] = torch.tensor([states[0]["step"] - 1, 0, 0, 0], dtype=torch.int64, device=device)
+                        clocks[device] = torch.tensor([states[0]["step"], 0, 0, 0], dtype=torch.int64, device=device)
                     clock = clocks[device]
                 elif device.type == "cuda" and torch.cuda.is_current_stream_capturing():
                     raise RuntimeError("a captured step wants capturable=True: this one would repeat its own number at every replay")
@@ -89,6 +88,8 @@ class AdamW(torch.optim.Optimizer):
                         master=master if any(x is not None for x in master) else None, m_scale=col("m_scale") if eight else None,
                         v_scale=col("v_scale") if eight else None, grad_scale=grad_scale, seed=group["seed"], clock=clock, streams=places)
                 torch.autograd.graph.increment_version(ps)        # a backward pass that still wants the old weights says so
+                for state in states:                              # (a call that was refused is no step)
+                    state["step"] += 1
         return loss
 
     @torch.no_grad()
