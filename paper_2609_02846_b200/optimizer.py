@@ -49,6 +49,31 @@ class AdamW(torch.optim.Optimizer):
         state["step"] = 0
         return state
 
+    # A capturable group counts on the device: group["clocks"] has a counter per device, of which captured graphs know the address, so it is
+    # kept for good.  While group["clocks_behind"] is set the parameters' own numbers are the ones that hold, else the counters are.
+    def _read_clocks(self, group: dict) -> None:
+        """The parameters' numbers become the counters'."""
+        if group.get("clocks_behind"):
+            return
+        numbers = {device: int(clock[0]) for device, clock in group.get("clocks", {}).items()}
+        for p in group["params"]:
+            if p.device in numbers and self.state.get(p):
+                self.state[p]["step"] = numbers[p.device]
+
+    def _clock(self, group: dict, device: torch.device) -> torch.Tensor:
+        """The counter of a capturable group on a device, at the most that one of its parameters has counted."""
+        clocks = group.setdefault("clocks", {})
+        if device not in clocks or group.get("clocks_behind"):
+            if device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("take a step before the capture: it sets the counter on the device")
+            if device not in clocks:
+                clocks[device] = torch.zeros(B.ADAMW_CLOCK_BYTES // 8, dtype=torch.int64, device=device)
+            for other, clock in clocks.items():
+                if other == device or group.get("clocks_behind"):
+                    clock[0] = max((self.state[p]["step"] for p in group["params"] if p.device == other and self.state.get(p)), default=0)
+            group["clocks_behind"] = False
+        return clocks[device]
+
     @torch.no_grad()
     def step(self, closure=None, grad_scale: Optional[torch.Tensor] = None):
         """One step.  `grad_scale`: float32 tensor of one value that the gradients are multiplied by (a clipping factor, the inverse of a loss
@@ -59,6 +84,12 @@ class AdamW(torch.optim.Optimizer):
                 loss = closure()
         place = 0                                   # of a parameter among all: the stream of its draws
         for group in self.param_groups:
+            if not group["capturable"]:
+                if any(p.is_cuda and p.grad is not None for p in group["params"]) and torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("a captured step wants capturable=True: this one would repeat its own number at every replay")
+                if group.get("clocks") and not group.get("clocks_behind"):
+                    self._read_clocks(group)        # the count goes on on the host
+                    group["clocks_behind"] = True
             todo = {}                               # (device, step): parameters
             for p in group["params"]:
                 place += 1
@@ -70,16 +101,7 @@ class AdamW(torch.optim.Optimizer):
                 todo.setdefault((p.device, 0 if group["capturable"] else state["step"] + 1), []).append((p, state, place - 1))
             for (device, step), some in todo.items():
                 ps, states, places = zip(*some)
-                clock = None
-                if group["capturable"]:
-                    clocks = group.setdefault("clocks", {})
-                    if device not in clocks:
-                        if device.type == "cuda" and torch.cuda.is_current_stream_capturing():
-                            raise RuntimeError("take a step before the capture: it makes the counter on the device")
-                        clocks[device] = torch.tensor([states[0]["step"], 0, 0, 0], dtype=torch.int64, device=device)
-                    clock = clocks[device]
-                elif device.type == "cuda" and torch.cuda.is_current_stream_capturing():
-                    raise RuntimeError("a captured step wants capturable=True: this one would repeat its own number at every replay")
+                clock = self._clock(group, device) if group["capturable"] else None
                 col = lambda key: [s.get(key) for s in states]
                 eight = group["state_bits"] == 8
                 master = col("master")
@@ -102,19 +124,17 @@ class AdamW(torch.optim.Optimizer):
     def state_dict(self) -> dict:
         """As torch's; the number of the step on the device (capturable) comes out as each parameter's."""
         for group in self.param_groups:
-            clocks = group.get("clocks") or {}
-            for p in group["params"]:
-                if p.device in clocks and self.state.get(p):
-                    self.state[p]["step"] = int(clocks[p.device][0])
+            self._read_clocks(group)
         d = super().state_dict()
         d["state"] = {i: dict(state) for i, state in d["state"].items()}        # (tensors are the optimizer's own, as in torch)
         for group in d["param_groups"]:
-            group.pop("clocks", None)
+            for key in ("clocks", "clocks_behind"):
+                group.pop(key, None)
         return d
 
     def load_state_dict(self, state_dict: dict) -> None:
         """States keep their own types (torch's way casts them to the parameter's), and tensors that are there are written in place, so that
-        captured graphs go on with what was loaded."""
+        captured graphs go on with what was loaded.  `capturable` becomes what was saved, like every number of a group."""
         clocks = [group.get("clocks") for group in self.param_groups]
         old = {p: self.state[p] for group in self.param_groups for p in group["params"] if self.state.get(p)}
         super().load_state_dict({**state_dict, "state": {}})
@@ -135,6 +155,7 @@ class AdamW(torch.optim.Optimizer):
             self.state[p] = new
         for group, there in zip(self.param_groups, clocks):
             if there:
-                group["clocks"] = there
-                for device, clock in there.items():
-                    clock[0] = max((self.state[p]["step"] for p in group["params"] if p.device == device and self.state.get(p)), default=0)
+                group["clocks"], group["clocks_behind"] = there, True
+                if group["capturable"]:
+                    for device in there:
+                        self._clock(group, device)

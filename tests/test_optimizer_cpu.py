@@ -49,3 +49,62 @@ def test_a_step_that_is_refused_is_not_counted(steps, capturable):
     refused.grad = None
     opt.step()
     assert steps == [1, 1, 2, 3, 2, 4, 3]
+
+
+def _numbers(opt):
+    return [s["step"] for s in opt.state_dict()["state"].values()]
+
+
+def _taken(n, **kw):
+    opt = O.AdamW(_params(), **kw)
+    for _ in range(n):
+        opt.step()
+    return opt
+
+
+def test_a_count_on_the_device_that_is_no_longer_kept(steps):
+    """A capturable optimizer that loads a state which is not: what it counts on the host from there on stays."""
+    opt, other = _taken(2, capturable=True), _taken(5)
+    opt.load_state_dict(copy.deepcopy(other.state_dict()))
+    assert not opt.param_groups[0]["capturable"]
+    del steps[:]
+    for number in (6, 7):
+        opt.step()
+        assert _numbers(opt) == [number] * 2
+    opt.param_groups[0]["capturable"] = True               # and on the device again
+    opt.step()
+    assert _numbers(opt) == [8] * 2
+    opt.param_groups[0]["capturable"] = False
+    assert _numbers(opt) == [8] * 2
+    opt.step()
+    assert steps == [6, 7, 8, 9] and _numbers(opt) == [9] * 2
+
+
+def test_replays_are_counted_when_the_count_moves_to_the_host(steps):
+    opt = _taken(2, capturable=True)
+    opt.param_groups[0]["clocks"][torch.device("cpu")][0] += 3          # what replays of a captured step do
+    opt.param_groups[0]["capturable"] = False
+    opt.step()
+    assert steps[-1] == 6 and _numbers(opt) == [6] * 2
+
+
+def test_what_is_saved_names_no_counter_of_the_device(steps):
+    opt = _taken(2, capturable=True)
+    saved = opt.state_dict()
+    assert all(not torch.is_tensor(x) and not isinstance(x, dict) for group in saved["param_groups"] for x in group.values())
+    new = O.AdamW(_params(), capturable=True)
+    new.load_state_dict(copy.deepcopy(saved))
+    new.step()
+    assert steps == [1, 2, 3] and _numbers(new) == [3] * 2
+
+
+def test_a_count_on_the_device_begins_at_the_most_that_a_parameter_has(steps):
+    a, b = _params()
+    opt = O.AdamW([a, b])
+    opt.step()
+    a.grad, g = None, a.grad
+    opt.step()
+    a.grad = g
+    opt.param_groups[0]["capturable"] = True
+    opt.step()
+    assert steps == [1, 2, 3] and _numbers(opt) == [3] * 2
