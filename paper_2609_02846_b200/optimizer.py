@@ -5,6 +5,7 @@ Nothing is computed here; states are made, handed over and kept.  Data-parallel 
 moments are rounded by depend on the seed, the parameter's place, the step and the element only, not on the rank."""
 from __future__ import annotations
 
+import math
 from typing import Optional
 
 import torch
@@ -74,14 +75,47 @@ class AdamW(torch.optim.Optimizer):
             group["clocks_behind"] = False
         return clocks[device]
 
+    _notes = ()                                     # steps whose gradient scale the host has not seen yet: (its copy, when that is there, states)
+
+    def _note(self, grad_scale: torch.Tensor) -> list:
+        """Notes a step with this gradient scale; returns the list of the states that it counts in."""
+        if grad_scale.is_cuda:
+            with torch.cuda.device(grad_scale.device):
+                value = torch.empty(1, dtype=torch.float32, pin_memory=True).copy_(grad_scale.view(1), non_blocking=True)
+                there = torch.cuda.Event()
+                there.record()
+        else:
+            value, there = grad_scale.clone(), None
+        states: list = []
+        self._notes = (*self._notes, (value, there, states))
+        return states
+
+    def _take_back(self) -> None:
+        """The noted steps that were left out are not counted."""
+        if self._notes and not (torch.cuda.is_available() and torch.cuda.is_current_stream_capturing()):
+            notes, self._notes = self._notes, ()
+            for value, there, states in notes:
+                if there is not None:
+                    there.synchronize()
+                if not math.isfinite(float(value)):
+                    for state in states:
+                        state["step"] -= 1
+
+    def __getstate__(self) -> dict:
+        self._take_back()
+        return super().__getstate__()
+
     @torch.no_grad()
     def step(self, closure=None, grad_scale: Optional[torch.Tensor] = None):
         """One step.  `grad_scale`: float32 tensor of one value that the gradients are multiplied by (a clipping factor, the inverse of a loss
-        scale); where it is not finite the step changes nothing (without `capturable` it is counted all the same)."""
+        scale); where it is not finite the step changes nothing and is not counted.  (Without `capturable` its value is copied to the host and looked at
+        when the next step begins, which waits for the copy.)"""
         loss = None
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        self._take_back()
+        note = None                                 # of what this step counts on the host, should it turn out to be left out
         place = 0                                   # of a parameter among all: the stream of its draws
         for group in self.param_groups:
             if not group["capturable"]:
@@ -112,6 +146,9 @@ class AdamW(torch.optim.Optimizer):
                 torch.autograd.graph.increment_version(ps)        # a backward pass that still wants the old weights says so
                 for state in states:                              # (a call that was refused is no step)
                     state["step"] += 1
+                if grad_scale is not None and clock is None:
+                    note = note or self._note(grad_scale)
+                    note.extend(states)
         return loss
 
     @torch.no_grad()
@@ -123,6 +160,7 @@ class AdamW(torch.optim.Optimizer):
 
     def state_dict(self) -> dict:
         """As torch's; the number of the step on the device (capturable) comes out as each parameter's."""
+        self._take_back()
         for group in self.param_groups:
             self._read_clocks(group)
         d = super().state_dict()
@@ -138,6 +176,7 @@ class AdamW(torch.optim.Optimizer):
         clocks = [group.get("clocks") for group in self.param_groups]
         old = {p: self.state[p] for group in self.param_groups for p in group["params"] if self.state.get(p)}
         super().load_state_dict({**state_dict, "state": {}})
+        self._notes = ()
         saved = [i for group in state_dict["param_groups"] for i in group["params"]]
         for i, p in zip(saved, [p for group in self.param_groups for p in group["params"]]):
             if i not in state_dict["state"]:

@@ -108,3 +108,31 @@ def test_a_count_on_the_device_begins_at_the_most_that_a_parameter_has(steps):
     opt.param_groups[0]["capturable"] = True
     opt.step()
     assert steps == [1, 2, 3] and _numbers(opt) == [3] * 2
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+def test_steps_that_are_left_out_are_not_counted(steps, capturable):
+    """In both modes: the bias corrections and the draws of 8-bit moments go by the steps that were taken."""
+    opt = O.AdamW(_params(), capturable=capturable)
+    for scale in (1.0, float("nan"), 0.5, float("inf"), -float("inf")):
+        opt.step(grad_scale=torch.tensor([scale]))
+    opt.step()
+    assert _numbers(opt) == [3] * 2
+    opt.step(grad_scale=torch.tensor([float("nan")]))
+    assert _numbers(opt) == [3] * 2                        # what is saved knows it already
+    assert _numbers(copy.deepcopy(opt)) == [3] * 2
+    assert steps == ([1, 2, 3] if capturable else [1, 2, 2, 3, 3, 3, 4])          # (the device leaves them out by itself)
+
+
+def test_a_step_that_is_left_out_is_taken_back_from_those_that_took_part(steps):
+    a, b = _params()
+    opt = O.AdamW([a, b])
+    opt.step()
+    b.grad, g = None, b.grad
+    opt.step(grad_scale=torch.tensor([float("inf")]))
+    b.grad = g
+    opt.step()
+    assert _numbers(opt) == [2, 2]
+    opt.step(grad_scale=torch.tensor([float("inf")]))
+    opt.load_state_dict(_taken(7).state_dict())            # states that know nothing of it
+    assert _numbers(opt) == [7, 7]
