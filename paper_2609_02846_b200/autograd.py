@@ -269,36 +269,49 @@ def _as_turnable(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
     return t if ok else t.clone(memory_format=torch.contiguous_format)
 
 
+def _save(ctx, positions, *tensors) -> None:
+    """Keeps positions (a tensor, a number or None) and what else the backward pass reads, where torch sees whether it was written to meanwhile."""
+    ctx.first = None if torch.is_tensor(positions) else positions
+    ctx.save_for_backward(positions if torch.is_tensor(positions) else None, *tensors)
+
+
+def _saved(ctx) -> tuple:
+    positions, *tensors = ctx.saved_tensors
+    return (ctx.first if positions is None else positions, *tensors)
+
+
 class _RotaryFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, frequencies, positions, interleaved, amplitude, inverse):
-        ctx.args = frequencies, positions, interleaved, amplitude, not inverse
+        _save(ctx, positions, frequencies)
+        ctx.args = interleaved, amplitude, not inverse
         return B.rotary(_as_turnable(q), _as_turnable(k), frequencies, positions, interleaved, amplitude, inverse)
 
     @staticmethod
     def backward(ctx, dq, dk):
-        return *_RotaryFn.apply(dq, dk, *ctx.args), None, None, None, None, None         # the transposed linear map, differentiable again
+        positions, frequencies = _saved(ctx)
+        return *_RotaryFn.apply(dq, dk, frequencies, positions, *ctx.args), None, None, None, None, None         # the transposed linear map, differentiable again
 
 
 def rotary(q: torch.Tensor, k: Optional[torch.Tensor], frequencies: torch.Tensor, positions=None, interleaved: bool = False,
            amplitude: float = 1.0) -> tuple:
-    """Differentiable ue5m3_rotary (arguments as in the binding's `rotary`).  Positions are read again in the backward pass: leave a tensor of
-    them as it is until then."""
+    """Differentiable ue5m3_rotary (arguments as in the binding's `rotary`).  Positions are read again in the backward pass, which refuses
+    a tensor of them that was written to meanwhile."""
     return _RotaryFn.apply(q, k, frequencies, positions, interleaved, amplitude, False)
 
 
 class _QKNormRotaryFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, frequencies, positions, interleaved, amplitude, eps):
-        ctx.save_for_backward(q, k, q_weight, k_weight)
-        ctx.args = frequencies, positions, interleaved, amplitude, eps
-        return B.qk_norm_rotary(_as_turnable(q), _as_turnable(k), q_weight, k_weight, *ctx.args)
+        _save(ctx, positions, frequencies, q, k, q_weight, k_weight)
+        ctx.args = interleaved, amplitude, eps
+        return B.qk_norm_rotary(_as_turnable(q), _as_turnable(k), q_weight, k_weight, frequencies, positions, *ctx.args)
 
     @staticmethod
     def backward(ctx, dq, dk):
-        q, k, q_weight, k_weight = ctx.saved_tensors
-        grads = B.qk_norm_rotary_backward(_as_turnable(dq), _as_turnable(dk), _as_turnable(q), _as_turnable(k), q_weight, k_weight, *ctx.args,
-                                          want_weights=any(ctx.needs_input_grad[2:4]))
+        positions, frequencies, q, k, q_weight, k_weight = _saved(ctx)
+        grads = B.qk_norm_rotary_backward(_as_turnable(dq), _as_turnable(dk), _as_turnable(q), _as_turnable(k), q_weight, k_weight, frequencies,
+                                          positions, *ctx.args, want_weights=any(ctx.needs_input_grad[2:4]))
         return *_once("qk_norm_rotary", grads, dq, dk, q, k, q_weight, k_weight), None, None, None, None, None
 
 
