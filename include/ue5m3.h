@@ -507,7 +507,8 @@ typedef struct {
 
 typedef struct {
     int64_t step;                 /* 1 for the first */
-    double lr, beta1, beta2, eps, weight_decay;       /* lr, eps, weight_decay >= 0 and finite (eps > 0 with 8 bits), 0 <= beta < 1 */
+    double lr, beta1, beta2, eps, weight_decay;       /* lr, weight_decay >= 0 and finite, 0 <= beta < 1; eps finite and at least 2^-126, or 0 (a v
+                                     of zero is then divided by); with 8 bits at least 2^-50 */
     const float* grad_scale;
     void* clock;
     uint64_t seed;

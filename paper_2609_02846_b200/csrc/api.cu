@@ -755,7 +755,9 @@ int ue5m3_adamw(const ue5m3_adamw_tensor* tensors, int64_t count, const ue5m3_ad
     auto number = [](double x) { return x >= 0.0 && x <= 3.0e38; };
     if (!number(s.lr) || !number(s.eps) || !number(s.weight_decay) || !(s.beta1 >= 0.0 && s.beta1 < 1.0) || !(s.beta2 >= 0.0 && s.beta2 < 1.0)) return UE5M3_ERR_INVALID_ARG;
     if ((s.state_bits != 8 && s.state_bits != 32) || (!s.clock && s.step < 1)) return UE5M3_ERR_INVALID_ARG;
-    if (s.state_bits == 8 && (float)s.eps == 0.0f) return UE5M3_ERR_INVALID_ARG;
+    // An eps that binary32 holds as a normal number, or none.  8 bits: second moments below 2^-110 may be stored as zeros beside a first moment of about their
+    // root, 2^-55, times the root of 1 / (1 - beta2), 2^5 for 0.999: with eps alone under it that is a step of lr, with less under it one without bounds.
+    if (s.eps < (s.state_bits == 8 ? 0x1p-50 : 0x1p-126) && !(s.eps == 0.0 && s.state_bits == 32)) return UE5M3_ERR_INVALID_ARG;
     if (!aligned_to(s.grad_scale, UE5M3_F32) || reinterpret_cast<uintptr_t>(s.clock) % 8) return UE5M3_ERR_ALIGN;
     for (int64_t i = 0; i < count; ++i) {
         const ue5m3_adamw_tensor& t = tensors[i];

@@ -16,7 +16,8 @@ from . import binding as B
 class AdamW(torch.optim.Optimizer):
     """w = w (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) for contiguous float32 and bfloat16 parameters.
 
-    `state_bits` 32 or 8 (m as E4M3, v as UE5M3, a float32 scale per 256 elements, rounded stochastically: 2 bytes per weight in place of 8).
+    `state_bits` 32 or 8 (m as E4M3, v as UE5M3, a float32 scale per 256 elements, rounded stochastically: 2 bytes per weight in place of 8).  `eps` is at
+    least 2^-126, or 0; with 8 bits at least 2^-50.
     `master_weights`: keep float32 copies of bfloat16 parameters (by default yes: bfloat16 alone loses updates below 2^-9 of a weight).  The copies are
     made at a parameter's first step; call `take_over_weights()` when parameters were changed from outside after that.
     `capturable`: the step is counted on the device, so that a captured `step()` goes on counting when it is replayed; take one step before the
@@ -27,7 +28,7 @@ class AdamW(torch.optim.Optimizer):
                  state_bits: int = 32, master_weights: bool = True, capturable: bool = False, seed: int = 0):
         if state_bits not in (8, 32):
             raise ValueError(f"state_bits = {state_bits}: 8 or 32")
-        if not lr >= 0 or not weight_decay >= 0 or not (eps > 0 or (eps == 0 and state_bits == 32)) or not all(0 <= b < 1 for b in betas):
+        if not lr >= 0 or not weight_decay >= 0 or not (eps >= (2.0 ** -50 if state_bits == 8 else 2.0 ** -126) or (eps == 0 and state_bits == 32)) or not all(0 <= b < 1 for b in betas):
             raise ValueError(f"lr {lr}, betas {betas}, eps {eps}, weight_decay {weight_decay}: out of range")
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay, state_bits=state_bits,
                                       master_weights=bool(master_weights), capturable=bool(capturable), seed=int(seed)))
