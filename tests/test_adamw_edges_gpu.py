@@ -6,6 +6,7 @@ import torch
 import paper_2609_02846_b200 as lib
 from block_reference import assert_within
 import adamw_reference as ref
+import test_adamw_gpu as small
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -41,3 +42,24 @@ def test_second_moments_below_the_normal_numbers(bits, eps):
     assert_within(p, torch.from_numpy(want), torch.from_numpy(bound))
     if eps == 0:
         assert abs(float(np.abs(before - want).mean()) / lr - 1) < 1e-3            # a step of lr, as for any gradient
+
+
+@pytest.mark.parametrize("pdtype,gdtype,master,offset", [(F, F, False, 0), (BF, BF, True, 0), (BF, F, True, 1), (F, BF, False, 1)])
+def test_8_bits_in_shares_of_several_chunks(pdtype, gdtype, master, offset):
+    """From 9.7 million elements on a CTA takes four chunks of 512 in a row, of which it loads each under the one before.  Lengths that leave its last
+    share one to four chunks, whole ones and ones that end inside a vector, a block and a chunk; addresses that allow vectors and that do not."""
+    ends = [1, 2, 3, 4]
+    sizes = [(3 * 2048 + 512 * c - d,) for c in ends for d in (0, 3, 256, 300, 511)] + [(1,), (9_700_003,), (2049,), (0,), (511,)]
+    assert sum(-(-s[0] // 512) for s in sizes) >= 148 * 16 * 2 * 4          # shares of several chunks
+    case = small.Case(sizes, pdtype, gdtype, master, 8, seed=11, offset=offset)
+    before = case.numpy()
+    case.call(step=3, seed=77)
+    small._check(case, before, 3, 77)
+
+
+def test_8_bits_in_shares_of_several_chunks_beside_small_launches():
+    """The rule looks at each launch of 400 tensors: the first takes shares of several chunks, the second does not."""
+    case = small.Case([(9_700_003,)] + [((53 * i) % 700 + 1,) for i in range(404)], F, F, False, 8, seed=12)
+    before = case.numpy()
+    case.call(step=9, seed=1)
+    small._check(case, before, 9, 1)
