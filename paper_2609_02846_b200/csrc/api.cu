@@ -4,7 +4,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <memory>
 #include <mutex>
+#include <new>
 #include "../../include/ue5m3.h"
 #include "block_ops.h"
 #include "launch.h"
@@ -748,6 +750,47 @@ int ue5m3_qk_norm_rotary_backward(const ue5m3_rotary_shape* shape, const ue5m3_h
 }
 
 // ----------------------------------------------------------------------------- AdamW
+// Does an array that the step writes have a byte in common with any other of its arrays?  (The CTAs of all tensors run side by side.)  The ranges
+// are walked in the order of their first bytes: one that is written may begin before no end so far, one that is only read before no end of a written one.
+// A call from Python with 8 tensors takes 25 us as without it, with 400 766 in place of 745.
+static int adamw_apart(const ue5m3_adamw_tensor* tensors, int64_t count, const ue5m3_adamw_step& s) {
+    struct Range { uintptr_t from, to; bool written; };
+    constexpr int kEach = 7, kFew = 16;
+    Range few[kEach * kFew + 2];
+    const std::unique_ptr<Range[]> heap(count > kFew ? new (std::nothrow) Range[kEach * (size_t)count + 2] : nullptr);
+    if (count > kFew && !heap) return UE5M3_ERR_UNSUPPORTED;
+    Range* const all = count > kFew ? heap.get() : few;
+    size_t n = 0;
+    auto add = [&](const void* p, int64_t bytes, bool written) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p) all[n++] = Range{at, at + (uintptr_t)bytes, written};
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        const ue5m3_adamw_tensor& t = tensors[i];
+        if (t.n == 0) continue;
+        const int64_t moment = t.n * (s.state_bits / 8), scales = (t.n + 255) / 256 * 4;
+        add(t.param, t.n * (t.param_dtype == UE5M3_BF16 ? 2 : 4), true);
+        add(t.grad, t.n * (t.grad_dtype == UE5M3_BF16 ? 2 : 4), false);
+        add(t.master, t.n * 4, true);
+        add(t.m, moment, true);
+        add(t.v, moment, true);
+        if (s.state_bits == 8) {
+            add(t.m_scale, scales, true);
+            add(t.v_scale, scales, true);
+        }
+    }
+    add(s.clock, UE5M3_ADAMW_CLOCK_BYTES, true);
+    add(s.grad_scale, 4, false);
+    std::sort(all, all + n, [](const Range& x, const Range& y) { return x.from < y.from; });
+    uintptr_t end = 0, written_end = 0;
+    for (size_t i = 0; i < n; ++i) {
+        if (all[i].from < (all[i].written ? end : written_end)) return UE5M3_ERR_INVALID_ARG;
+        end = std::max(end, all[i].to);
+        if (all[i].written) written_end = std::max(written_end, all[i].to);
+    }
+    return UE5M3_OK;
+}
+
 int ue5m3_adamw(const ue5m3_adamw_tensor* tensors, int64_t count, const ue5m3_adamw_step* step, void* stream) {
     const ApiRange range_("ue5m3_adamw");
     if (!step || count < 0 || (count > 0 && !tensors)) return UE5M3_ERR_INVALID_ARG;
@@ -769,9 +812,10 @@ int ue5m3_adamw(const ue5m3_adamw_tensor* tensors, int64_t count, const ue5m3_ad
         if (s.state_bits == 8 ? !aligned_to(t.m_scale, UE5M3_F32) || !aligned_to(t.v_scale, UE5M3_F32) : !aligned_to(t.m, UE5M3_F32) || !aligned_to(t.v, UE5M3_F32))
             return UE5M3_ERR_ALIGN;
     }
-    int sms = 0;
-    const int bad = device_ready(sms);
+    int bad = adamw_apart(tensors, count, s);
     if (bad != UE5M3_OK) return bad;
+    int sms = 0;
+    if ((bad = device_ready(sms)) != UE5M3_OK) return bad;
     return launch_adamw(tensors, count, s, (cudaStream_t)stream) == cudaSuccess ? UE5M3_OK : UE5M3_ERR_CUDA;
 }
 
