@@ -31,10 +31,11 @@ class TransformerBlock(torch.nn.Module):
         super().__init__()
         if hidden % heads or heads % kv_heads:
             raise ValueError(f"hidden {hidden}, heads {heads} and kv_heads {kv_heads} do not divide")
-        if qk_norm and not rotary:
+        turns = isinstance(rotary, dict) or bool(rotary)         # (a dict may have no arguments)
+        if qk_norm and not turns:
             raise ValueError("norms of q and k come with rotary positions (rotary=True)")
         self.heads, self.kv_heads, self.head_dim, self.window_left, self.sinks = heads, kv_heads, hidden // heads, window_left, sinks
-        self.turn = QKNormRotary(self.head_dim, norm=qk_norm, **(rotary if isinstance(rotary, dict) else {})) if rotary else None
+        self.turn = QKNormRotary(self.head_dim, norm=qk_norm, **(rotary if isinstance(rotary, dict) else {})) if turns else None
         linear = Ue5m3Linear if linear is None else linear
         self.norm1, self.norm2 = LayerNorm(hidden), LayerNorm(hidden)
         self.qkv = linear(hidden, (heads + 2 * kv_heads) * self.head_dim)
