@@ -3,8 +3,9 @@
 //   m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2,   w' = w (1 - lr wd) - lr / (1 - b1^t) m' / (sqrt(v' / (1 - b2^t)) + eps)
 //
 // m' and v' are made of single binary32 roundings in the order written (products, then the sum), so that the codes of 8-bit moments are
-// defined to the bit.  w' takes a fused product and approximate root and reciprocal: their error is 2^-22 of the update, which is itself
-// of the size lr.
+// defined to the bit.  w' takes a fused product and approximate root and reciprocal.  The update, itself of the size lr, is off by at most 2^-21 of it where
+// v' / (1 - b2^t) is a normal number: bias correction and its product, each halved by the root, 2^-24 together, root 2^-23, sum 2^-24, reciprocal 2^-23, its
+// product 2^-24, step size 2^-24 (a subnormal product adds its own rounding); the weight's factor and its product by 2^-24 each, and w' is rounded once more.
 //
 // 8-bit moments: blocks of 256 elements share a binary32 scale; m is a sign and E4M3, v unsigned E5M3 (the format of the FP4 block
 // scales: a moment that is never negative needs no sign, and v spans the square of m's range).  A block's largest magnitude gets the format's largest value.  Both are
@@ -14,8 +15,8 @@
 // A positive v' never gets the code 0: an m next to it would be divided by eps alone in the next step.
 //
 // Bound by memory: 28 bytes per element with binary32 moments (weight read and written, gradient, two moments; or BF16 weight, copy in binary32,
-// BF16 gradient): 176 M weights in 713 us, 6.9 TB/s.  16 bytes with 8-bit ones: 460 us, 6.15 TB/s (0.94 of the measured copy rate) at 73
-// instructions per element, two thirds of what the SMs issue.
+// BF16 gradient): 176 M weights in 713 us, 6.9 TB/s.  16 bytes with 8-bit ones: 462 us, 6.1 TB/s (0.93 of the measured copy rate) at 75
+// instructions per element, in 0.79 of the SMs' issue slots.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -136,10 +137,11 @@ __device__ __forceinline__ BlockScale block_scale_of(float most, float top) {
 template <bool HIGH> __device__ __forceinline__ uint32_t rounded(float x, float up, float low, uint32_t draw) {
     return dp2a_lo_u32(draw, HIGH ? 0x1000u : 0x0010u, __float_as_uint(__fmul_rn(__fmul_rn(fabsf(x), up), low)) + 8u);
 }
-// The codes of two elements in the upper bytes of two words.
+// The codes of two elements in the upper bytes of two words.  m and v share 16 bits of draws, the bytes exchanged for m: each is uniform, so each code is right on
+// average; together they are not independent (a draw's high byte is the other one's low byte: a correlation of 512 / 65537 = 0.008), which nothing asks for.
 __device__ __forceinline__ void encode_m(const float* x, float up, uint32_t draw, uint32_t* out) {
     const uint32_t most = (0x7Eu << 20) | 0xFFFFFu;
-    const uint32_t turned = __byte_perm(draw, 0, 0x2301);          // v's bits with the bytes of each half exchanged: as good as independent
+    const uint32_t turned = __byte_perm(draw, 0, 0x2301);          // v's bits with the bytes of each half exchanged
     out[0] = min(rounded<false>(x[0], up, kMinM, turned), most) << 4;
     out[1] = min(rounded<true>(x[1], up, kMinM, turned), most) << 4;
 #pragma unroll

@@ -17,7 +17,7 @@
 // latency is what counts, not the bytes in flight.  Where there are few tokens the heads of one are shared out among warps.
 //
 // GPU time, of which the floor at the measured copy rate: rotation of 4 x 4096 tokens, 32 + 8 heads of 128, BF16 54.8 us (0.93 of it); norm and rotation
-// of 2 x 4096 30.5 (0.84); backward of 4 x 4096 96 (0.80), bound by the latency of a row's chain at 12 warps per SM.
+// of 2 x 4096 30.5 (0.84); backward of 4 x 4096 97 (0.79), bound by the latency of a row's chain at 12 warps per SM.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <algorithm>
