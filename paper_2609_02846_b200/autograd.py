@@ -269,15 +269,18 @@ def _as_turnable(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
     return t if ok else t.clone(memory_format=torch.contiguous_format)
 
 
-def _save(ctx, positions, *tensors) -> None:
-    """Keeps positions (a tensor, a number or None) and what else the backward pass reads, where torch sees whether it was written to meanwhile."""
-    ctx.first = None if torch.is_tensor(positions) else positions
-    ctx.save_for_backward(positions if torch.is_tensor(positions) else None, *tensors)
+def _save(ctx, positions, frequencies, *tensors) -> None:
+    """Keeps what the backward pass reads again where torch sees whether it was written to meanwhile (positions may be a number or None; tensors of
+    inference mode have no version)."""
+    two = positions, frequencies
+    seen = [torch.is_tensor(t) and not t.is_inference() for t in two]
+    ctx.unseen = [None if s else t for s, t in zip(seen, two)]
+    ctx.save_for_backward(*(t if s else None for s, t in zip(seen, two)), *tensors)
 
 
 def _saved(ctx) -> tuple:
-    positions, *tensors = ctx.saved_tensors
-    return (ctx.first if positions is None else positions, *tensors)
+    positions, frequencies, *tensors = ctx.saved_tensors
+    return (ctx.unseen[0] if positions is None else positions, ctx.unseen[1] if frequencies is None else frequencies, *tensors)
 
 
 class _RotaryFn(torch.autograd.Function):

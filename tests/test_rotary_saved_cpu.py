@@ -37,3 +37,13 @@ def test_both_passes_get_the_same_arguments(call, at, stubs):
     assert torch.equal(back[0], f)
     assert back[1] == at if not torch.is_tensor(at) else torch.equal(back[1], at)
     assert there[2:4] == back[2:4] == (True, 1.5)
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_tensors_of_inference_mode(call, stubs):
+    """They have no version to check, as those that a module takes to another device in an evaluation have none: they are used as they are."""
+    with torch.inference_mode():
+        f, at = torch.ones(4, dtype=torch.float64), torch.arange(3)
+    q = torch.ones(1, 3, 2, 8, requires_grad=True)
+    call(q, f, at)[0].sum().backward()
+    assert stubs[1][0] is f and stubs[1][1] is at and q.grad is not None
