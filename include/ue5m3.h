@@ -484,7 +484,7 @@ UE5M3_API int ue5m3_qk_norm_rotary_backward(const ue5m3_rotary_shape* shape, con
  * a < 2^-110 are stored as zeros; blocks in which a value is not finite get the scale NaN.  The draws come from Philox4x32 with 7 rounds, key = (seed low, seed high) and
  * counter = (low32(i >> 3), stream, 2, low32(step)) for element i: lane j = i & 7 uses half (j & 1) of output word j >> 1 for v, and the same 16 bits with their two bytes exchanged for m.
  *   tensors       host array of `count` descriptors; all memory they point to is on the device, contiguous, aligned to its element.  What the step writes
- *                 has nothing in common with any other array of it (UE5M3_ERR_INVALID_ARG); gradients may be shared.  Tensors whose pointers are 16-byte aligned are read with 16-byte loads.  n = 0 is left out.
+ *                 has nothing in common with any other array of it (UE5M3_ERR_INVALID_ARG); gradients may be shared, and an F32 param may be its own master.  Tensors whose pointers are 16-byte aligned are read with 16-byte loads.  n = 0 is left out.
  *   step          host struct, read during the call.
  *   grad_scale    device, 1 float, may be null (1): for instance a clipping factor.  Where it is not finite the step is left out: nothing is written.
  *   clock         device, UE5M3_ADAMW_CLOCK_BYTES, 8-byte aligned, zero before the first step; may be null.  With it the number of the step is

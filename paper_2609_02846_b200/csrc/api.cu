@@ -771,7 +771,7 @@ static int adamw_apart(const ue5m3_adamw_tensor* tensors, int64_t count, const u
         const int64_t moment = t.n * (s.state_bits / 8), scales = (t.n + 255) / 256 * 4;
         add(t.param, t.n * (t.param_dtype == UE5M3_BF16 ? 2 : 4), true);
         add(t.grad, t.n * (t.grad_dtype == UE5M3_BF16 ? 2 : 4), false);
-        add(t.master, t.n * 4, true);
+        if (t.master != t.param || t.param_dtype != UE5M3_F32) add(t.master, t.n * 4, true);       // (a copy that is the param itself: the same values)
         add(t.m, moment, true);
         add(t.v, moment, true);
         if (s.state_bits == 8) {

@@ -63,3 +63,13 @@ def test_8_bits_in_shares_of_several_chunks_beside_small_launches():
     before = case.numpy()
     case.call(step=9, seed=1)
     small._check(case, before, 9, 1)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_a_float32_param_as_its_own_copy(bits, offset):
+    a, b = (small.Case([(700,), (2500,)], F, BF, False, bits, seed=13, offset=offset) for _ in range(2))
+    a.master = a.p
+    a.call(step=5, seed=3)
+    b.call(step=5, seed=3)
+    assert all(torch.equal(x, y) for x, y in zip(a.p + a.m + a.v, b.p + b.m + b.v))
